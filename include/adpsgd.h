@@ -455,6 +455,130 @@ int adpsgd_verify_plan(int32_t n, int64_t K, const int32_t* worker, const int32_
 int adpsgd_synth_gradient(uint64_t seed, uint64_t k, float std, int64_t d, float* out_device,
                           void* stream);
 
+/* ---- Operators of a worker's own training step -----------------------------------------------------------
+ * Products with their epilogue, log-probabilities and losses over a vocabulary, and AdamW, for gradient functions of
+ * ADPSGD_MODEL_EXTERNAL and programs around them.  No handle is needed (AdamW has one of its own).  All pointers are device
+ * memory unless "host" is stated; nothing is allocated, work is enqueued on `stream` and the calls return at once.  Elements are
+ * addressed with 64-bit offsets, and tensors need the alignment of their type only.  adpsgd_last_error(NULL) has the message of
+ * the calling thread's last failure. */
+enum { ADPSGD_TYPE_F32 = 0, ADPSGD_TYPE_BF16 = 1, ADPSGD_TYPE_F16 = 2 };
+enum { ADPSGD_ACT_NONE = 0, ADPSGD_ACT_RELU = 1, ADPSGD_ACT_GELU = 2, ADPSGD_ACT_SILU = 3 };
+
+/* Dense layer  y = act(x w^T + b) + r,  w given as out x in.  All tensors are of one type, BF16 or F16; products are added in 32
+ * bits, the epilogue is computed in 32 bits and y is rounded once.  gelu is z Phi(z) with the normal distribution's Phi, not an
+ * approximation of it. */
+typedef struct {
+    int32_t type;            /* ADPSGD_TYPE_BF16 or _F16                                                     */
+    int32_t activation;      /* ADPSGD_ACT_*                                                                 */
+    int64_t M, N, K;         /* rows, outputs, inputs;  M >= 0, N, K >= 1                                    */
+    const void* x;           /* M x K, row m at x + m ldx                                                    */
+    int64_t ldx;
+    const void* w;           /* w_transposed = 0: N x K, row n at w + n ldw;  1: K x N, row k at w + k ldw   */
+    int64_t ldw;
+    int32_t w_transposed;
+    int32_t reserved;
+    const void* b;           /* N, or NULL                                                                   */
+    const void* r;           /* M x N, row m at r + m ldr, or NULL                                           */
+    int64_t ldr;
+    void* workspace;         /* adpsgd_dense_workspace_bytes, 16-byte aligned; may be used again in stream order */
+    int64_t workspace_bytes;
+} adpsgd_dense_t;
+
+/* Host only: the workspace of a forward (backward = 0) or backward call of these sizes; -1 where an argument is refused. */
+int64_t adpsgd_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward);
+
+/* y: M x N, contiguous.  slope (or NULL): M x N 16-bit words, contiguous, receives act'(z) for the backward call (sign, 3 bits of
+ * exponent, 12 of fraction: within 2^-13 of its value from 2^-6 up, within 2^-19 below). */
+int adpsgd_dense_forward(const adpsgd_dense_t* o, void* y, uint16_t* slope, void* stream);
+
+/* Gradients for dy (M x N, row m at dy + m lddy): dx (M x K, contiguous), dw (as w is stored: N x K or K x N, contiguous) and db (N);
+ * each may be NULL.  slope: as the forward call wrote it; NULL with ADPSGD_ACT_NONE only.  dz = dy act'(z) is rounded to the type
+ * once for the two products; db adds it before that rounding.  b, r are not read (the residual's gradient is dy). */
+int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, int64_t lddy, const uint16_t* slope, void* dx, void* dw, void* db,
+                          void* stream);
+
+/* Logits of `rows` positions over a vocabulary: row i at z + i ld.  tokens: one of the vocabulary for each row; a negative one is a
+ * position that does not count (its row is not read: log-probability 0, gradient 0, no share in a loss), one beyond the vocabulary
+ * makes its results NaN.  Logits of -infinity are tokens that cannot be; where a row has nothing else its results are NaN. */
+typedef struct {
+    int32_t type;            /* ADPSGD_TYPE_*                                                                */
+    int32_t reserved;
+    int64_t rows, vocab;     /* rows >= 0, 1 <= vocab <= 2^30                                                */
+    const void* z;
+    int64_t ld;              /* >= vocab                                                                     */
+    const int64_t* tokens;   /* rows                                                                         */
+    void* workspace;         /* adpsgd_loss_workspace_bytes, 16-byte aligned; may be used again in stream order */
+    int64_t workspace_bytes;
+} adpsgd_logits_t;
+
+/* Host only: the workspace of each of the three calls below; -1 where an argument is refused. */
+int64_t adpsgd_loss_workspace_bytes(int64_t rows, int64_t vocab);
+
+/* log_probs[i] = z[i][tokens[i]] - log sum_v exp z[i][v]. */
+int adpsgd_token_log_probs(const adpsgd_logits_t* o, float* log_probs, void* stream);
+
+/* Clipped policy loss with a KL term.  With l_i the log-probability of row i's token, rho = exp(l - old), c the counted rows:
+ *   loss = 1/max(1, c) sum_i [ -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(ref - l) - (ref - l) - 1) ]
+ * dlogits (rows x vocab, contiguous, the type of z) receives its gradient, log_probs (rows) l, loss (1) the loss.  ref may be NULL
+ * where kl_coef is 0. */
+int adpsgd_policy_loss(const adpsgd_logits_t* o, const float* old_log_probs, const float* advantages, const float* ref_log_probs,
+                       float clip_low, float clip_high, float kl_coef, float* loss, void* dlogits, float* log_probs, void* stream);
+
+/* Preference loss of `pairs` pairs: sequence q is rows offsets[q] .. offsets[q + 1] (2 pairs + 1 entries, ascending from 0 to rows;
+ * else the loss is NaN), q < pairs the chosen answers and pairs + q their rejected ones.  s_q = sum of its log-probabilities,
+ *   margin_q = beta ((s_q - ref_q) - (s_{pairs+q} - ref_{pairs+q})),
+ *   loss = 1/pairs sum_q [ -(1 - label_smoothing) log sigma(margin_q) - label_smoothing log sigma(-margin_q) ]
+ * dlogits, loss as above; log_probs (2 pairs) receives s, margins (pairs) the margins. */
+int adpsgd_preference_loss(const adpsgd_logits_t* o, const int64_t* offsets, int64_t pairs, const float* ref_log_probs, float beta,
+                           float label_smoothing, float* loss, void* dlogits, float* log_probs, float* margins, void* stream);
+
+/* AdamW over many tensors at once.  With g' = f grad_scale g, f = min(1, max_norm / (|grad_scale g| + 1e-6)) over all tensors
+ * (1 where max_norm is 0), t the number of the step from 1:
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,  u = (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *   p = p - lr (u + weight_decay p)              p: the master where there is one, and the parameter is its rounding
+ * With `out` the direction u + weight_decay p goes there, and no parameter is written: what an event of the engine takes as gradient.
+ * The state of a tensor begins at a multiple of 256 elements.  state_bits 32: m, v fp32.  state_bits 8: blocks of 256 with an
+ * exponent each, m as e4m3 times 2^k and v as the square of an e4m3 number times 2^k, both rounded up with the probability that
+ * keeps the mean (of v, not of its root), by Philox4x32-10 with counter (element / 4, step) and key `seed`; v > 0 stays so.  The update
+ * itself uses m and v before they are rounded.  An element that is not finite is kept as NaN. */
+typedef struct adpsgd_adamw adpsgd_adamw_t;
+typedef struct {
+    int32_t tensors;
+    int32_t param_type, grad_type;   /* ADPSGD_TYPE_*                                                        */
+    int32_t state_bits;              /* 8 or 32                                                              */
+    const int64_t* sizes;            /* host: elements of each tensor                                        */
+    void* const* params;             /* host: contiguous tensors, borrowed for the life of the handle ...    */
+    const void* const* grads;        /* host                                                                 */
+    float* const* masters;           /* host, or NULL                                                        */
+    float* const* out;               /* host, or NULL                                                        */
+    const float* weight_decay;       /* host: of each tensor                                                 */
+    double beta1, beta2, eps;        /* 0 <= beta < 1, eps > 0                                               */
+    uint64_t seed;
+    void* m;                         /* state_bits 32: state_length floats, 8: state_length bytes; zero at the start ... */
+    void* v;
+    int8_t* exponents;               /* state_bits 8: 2 for each block of 256 (m's, v's), else NULL          */
+} adpsgd_adamw_opts_t;
+
+/* Host only: elements of the state of tensors of these sizes (each rounded up to a multiple of 256); -1 where one is negative. */
+int64_t adpsgd_adamw_state_length(const int64_t* sizes, int32_t tensors);
+
+int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts_t* opts);
+void adpsgd_adamw_destroy(adpsgd_adamw_t* h);
+
+/* One step on `stream`; norm (or NULL; with max_norm 0 it may be NULL only) receives |grad_scale g| before clipping.  The number
+ * of the step is the host's, so a stream that is being captured is refused (ADPSGD_ERR_STATE).  Calls on one handle follow each
+ * other in stream order. */
+int adpsgd_adamw_step(adpsgd_adamw_t* h, double lr, double max_norm, double grad_scale, float* norm, void* stream);
+
+/* Steps done, and to continue a stored run. */
+int adpsgd_adamw_get_steps(const adpsgd_adamw_t* h, int64_t* out);
+int adpsgd_adamw_set_steps(adpsgd_adamw_t* h, int64_t steps);
+
+/* state_bits 8: the values that the state stands for, state_length bf16 each (which hold them exactly), and the state from fp32
+ * values, each to the nearest (ADPSGD_ERR_STATE with 32). */
+int adpsgd_adamw_get_moments(adpsgd_adamw_t* h, uint16_t* m, uint16_t* v, void* stream);
+int adpsgd_adamw_set_moments(adpsgd_adamw_t* h, const float* m, const float* v, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

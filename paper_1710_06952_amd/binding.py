@@ -16,6 +16,8 @@ LIB_PATH = _HERE / "libadpsgd.so"
 OK, ERR_ARG, ERR_GRAPH, ERR_SCHEDULE, ERR_STATE, ERR_HIP, ERR_CALLBACK = 0, -1, -2, -3, -4, -5, -6
 MODEL_LSQ, MODEL_LOGREG, MODEL_SYNTH, MODEL_MLP, MODEL_EXTERNAL = 0, 1, 2, 3, 4
 ROUTE_AUTO, ROUTE_ROUNDS = 0, 1
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 FLAG_PROFILE, FLAG_DENSE_GRADIENT, FLAG_VERIFY_PLAN, FLAG_SYNC_IN_PLACE = 1, 2, 4, 8
 
 EXPORTS = [
@@ -25,6 +27,9 @@ EXPORTS = [
     "adpsgd_get_bf16_models", "adpsgd_classification_error", "adpsgd_get_momentum", "adpsgd_get_stats", "adpsgd_make_schedule", "adpsgd_plan_rounds",
     "adpsgd_synth_gradient", "adpsgd_run_sync_steps", "adpsgd_run_sync_steps_with", "adpsgd_metropolis_weights",
     "adpsgd_get_event_count", "adpsgd_set_event_count", "adpsgd_verify_plan", "adpsgd_objective", "adpsgd_objective_weighted", "adpsgd_count_nonfinite",
+    "adpsgd_dense_workspace_bytes", "adpsgd_dense_forward", "adpsgd_dense_backward", "adpsgd_loss_workspace_bytes", "adpsgd_token_log_probs",
+    "adpsgd_policy_loss", "adpsgd_preference_loss", "adpsgd_adamw_state_length", "adpsgd_adamw_create", "adpsgd_adamw_destroy", "adpsgd_adamw_step",
+    "adpsgd_adamw_get_steps", "adpsgd_adamw_set_steps", "adpsgd_adamw_get_moments", "adpsgd_adamw_set_moments",
 ]
 
 
@@ -77,6 +82,26 @@ class Stats(C.Structure):
     _fields_ = [("events", C.c_int64), ("rounds", C.c_int64), ("fused_launches", C.c_int64),
                 ("grad_launches", C.c_int64), ("max_round_pairs", C.c_int64), ("slots", C.c_int64),
                 ("fused_ms", C.c_double), ("grad_ms", C.c_double)]
+
+
+class Dense(C.Structure):
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("w_transposed", C.c_int32),
+                ("reserved", C.c_int32), ("b", C.c_void_p), ("r", C.c_void_p), ("ldr", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64)]
+
+
+class Logits(C.Structure):
+    _fields_ = [("type", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64), ("z", C.c_void_p),
+                ("ld", C.c_int64), ("tokens", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class AdamwOpts(C.Structure):
+    _fields_ = [("tensors", C.c_int32), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32),
+                ("sizes", C.POINTER(C.c_int64)), ("params", C.POINTER(C.c_void_p)), ("grads", C.POINTER(C.c_void_p)),
+                ("masters", C.POINTER(C.c_void_p)), ("out", C.POINTER(C.c_void_p)), ("weight_decay", C.POINTER(C.c_float)),
+                ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("seed", C.c_uint64), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("exponents", C.c_void_p)]
 
 
 _lib = None
@@ -142,6 +167,25 @@ def lib():
         L.adpsgd_get_event_count.argtypes = [vp, P(u64)]
         L.adpsgd_set_event_count.argtypes = [vp, u64]
         L.adpsgd_metropolis_weights.argtypes = [P(Graph), P(C.c_float), P(C.c_float)]
+        f32, f64 = C.c_float, C.c_double
+        L.adpsgd_dense_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.adpsgd_dense_forward.argtypes = [P(Dense), vp, vp, vp]
+        L.adpsgd_dense_backward.argtypes = [P(Dense), vp, i64, vp, vp, vp, vp, vp]
+        L.adpsgd_loss_workspace_bytes.argtypes = [i64, i64]
+        L.adpsgd_token_log_probs.argtypes = [P(Logits), vp, vp]
+        L.adpsgd_policy_loss.argtypes = [P(Logits), vp, vp, vp, f32, f32, f32, vp, vp, vp, vp]
+        L.adpsgd_preference_loss.argtypes = [P(Logits), vp, i64, vp, f32, f32, vp, vp, vp, vp, vp]
+        L.adpsgd_adamw_state_length.argtypes = [P(i64), i32]
+        L.adpsgd_adamw_create.argtypes = [P(vp), P(AdamwOpts)]
+        L.adpsgd_adamw_destroy.argtypes = [vp]
+        L.adpsgd_adamw_destroy.restype = None
+        L.adpsgd_adamw_step.argtypes = [vp, f64, f64, f64, vp, vp]
+        L.adpsgd_adamw_get_steps.argtypes = [vp, P(i64)]
+        L.adpsgd_adamw_set_steps.argtypes = [vp, i64]
+        L.adpsgd_adamw_get_moments.argtypes = [vp, vp, vp, vp]
+        L.adpsgd_adamw_set_moments.argtypes = [vp, vp, vp, vp]
+        for name in ("adpsgd_dense_workspace_bytes", "adpsgd_loss_workspace_bytes", "adpsgd_adamw_state_length"):
+            getattr(L, name).restype = i64
         _lib = L
     return _lib
 

@@ -1,0 +1,100 @@
+// Shared by the kernels of dense layers: their two types, the activations with their slopes, and the 16-bit form of a slope.
+#pragma once
+
+#include "device_common.hpp"
+#include "operators.hpp"
+
+namespace adpsgd_impl {
+
+typedef v4u v4u_any __attribute__((aligned(2)));        // 16 bytes at any multiple of an element
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint16_t v8h __attribute__((ext_vector_type(8)));
+
+struct Bf16 {
+    typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+    __device__ static float up(uint16_t h) { return bf16_to_float(h); }
+    __device__ static uint16_t down(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
+    __device__ static v4f mfma(v4u a, v4u b, v4f c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+};
+struct F16 {
+    typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+    __device__ static float up(uint16_t h) { return static_cast<float>(__builtin_bit_cast(_Float16, h)); }
+    __device__ static uint16_t down(float f) { return __builtin_bit_cast(uint16_t, static_cast<_Float16>(f)); }
+    __device__ static v4f mfma(v4u a, v4u b, v4f c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
+    }
+};
+
+// Eight values rounded.
+template <class T>
+__device__ __forceinline__ v4u pack8(const float* f) {
+    v4u v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = T::down(f[2 * i]) | static_cast<uint32_t>(T::down(f[2 * i + 1])) << 16;
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void unpack8(v4u v, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = T::up(static_cast<uint16_t>(v[i] & 0xFFFFu));
+        f[2 * i + 1] = T::up(static_cast<uint16_t>(v[i] >> 16));
+    }
+}
+
+// act(z) and its derivative.  gelu: the upper tail of the normal distribution is exp(-t^2 / 2) P(1 / (1 + 0.38 t)), P of degree 7
+// fitted to the least largest relative error over t >= 0, 2.6e-6: the tail keeps its relative accuracy, unlike 1 + erf.
+template <bool kSlope>
+__device__ __forceinline__ float activated(float z, int act, float& slope) {
+    if (act == ADPSGD_ACT_NONE) {
+        slope = 1.0f;
+        return z;
+    }
+    if (act == ADPSGD_ACT_RELU) {
+        slope = z > 0.0f ? 1.0f : 0.0f;
+        return z <= 0.0f ? 0.0f : z;                     // NaN stays
+    }
+    if (act == ADPSGD_ACT_GELU) {
+        const float t = fabsf(z), u = __builtin_amdgcn_rcpf(fmaf(0.38f, t, 1.0f));
+        const float e = __builtin_amdgcn_exp2f(t * t * -0.7213475204444817f);
+        float p = fmaf(u, 0.04894981298366624f, -0.16002513951519665f);
+        p = fmaf(p, u, 0.11438935044517826f);
+        p = fmaf(p, u, 0.05999139163590317f);
+        p = fmaf(p, u, 0.1337908999955492f);
+        p = fmaf(p, u, 0.15129931401177749f);
+        p = fmaf(p, u, 0.15160565325274758f);
+        const float tail = e * (p * u), phi = z < 0.0f ? tail : 1.0f - tail;
+        if (kSlope) slope = fmaf(z * 0.3989422804014327f, e, phi);
+        return z * phi;
+    }
+    const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+    if (kSlope) slope = sig * fmaf(z, 1.0f - sig, 1.0f);
+    return z * sig;
+}
+
+// A slope (under 2 in magnitude) in 16 bits: sign, 3 bits of exponent (2^-6 to 1, and steps of 2^-18 below), 12 of fraction.  As
+// a power of two takes the exponent there the fp32 form of |s| 2^-120 is that format, with bits to spare.  Four times as fine as
+// fp16 where slopes are: dz, which is rounded to the type once, is not visibly further off for it.  0x7FFF is NaN.
+__device__ __forceinline__ uint16_t slope_word(float s) {
+    const uint32_t bits = __float_as_uint(fabsf(s) * 0x1p-120f), rounded = (bits + 0x3FFu + (bits >> 11 & 1u)) >> 11;
+    return static_cast<uint16_t>((s == s ? rounded : 0x7FFFu) | (__float_as_uint(s) >> 16 & 0x8000u));
+}
+__device__ __forceinline__ float slope_of(uint16_t w) {
+    const uint32_t mag = w & 0x7FFFu;
+    const float s = __uint_as_float(mag << 11) * 0x1p120f;
+    return mag == 0x7FFFu ? NAN : __uint_as_float(__float_as_uint(s) | (w & 0x8000u) << 16);
+}
+
+// How a product is cut: tiles of side x side, `splits` parts of k whose sums are joined afterwards.
+struct DensePlan {
+    int side;
+    int splits;
+};
+DensePlan dense_plan(int64_t I, int64_t J, int64_t K);
+
+template <class T>
+void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
+
+}  // namespace adpsgd_impl

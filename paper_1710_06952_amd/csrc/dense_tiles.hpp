@@ -1,0 +1,319 @@
+// Tiled products D[i][j] = sum_k A(i, k) B(j, k) on the matrix cores, operands stored either way round, any sizes and strides.
+//
+// A block owns a tile of D and walks k in steps of 64: the next step's operands are on their way from memory into registers while
+// the present ones are multiplied out of LDS, then they go to the other half of the LDS; one barrier a step.
+//
+// Loads are 16 bytes wide at any multiple of two bytes, so odd leading dimensions take the same path.  Rows beyond the end of A
+// or B are the last row again (their results are not stored); what lies beyond the end of k is zero in both operands.  A vector
+// that the end cuts is read ending there and shifted, so nothing outside of a row is ever read.
+//
+// LDS.  An operand with k inner is kept [row][64 k]; its rows of 128 bytes hold their 16-byte pieces exchanged by bits of the row, so
+// that the 16 rows of a matrix operand come from different banks.  One with k outer is kept [k][row] and read by ds_read_b64_tr_b16,
+// which gives 16 lanes the transpose of 4 k times 16 rows; pieces are exchanged by bits of k.
+//
+// Operand layout of v_mfma_f32_16x16x32 (D = A B + C): lane l supplies A[l % 16][8 (l / 16) ..+7] and B[8 (l / 16) ..+7][l % 16], and
+// receives D[4 (l / 16) + v][l % 16].  Here B's rows j go in as the instruction's A, and the wavefront's 16 TJ values of j are dealt to its
+// TJ instructions so that a lane ends with 4 TJ neighbouring j of one row i: with TJ = 4 a row's 64 results are 128 bytes from 4 lanes.
+#pragma once
+
+#include "dense.hpp"
+
+namespace adpsgd_impl {
+namespace {
+
+constexpr int kBK = 64;
+
+// Elements start .. start + 7 of a row that ends at `end` (zero beyond it; start may lie beyond).
+__device__ __forceinline__ v4u load_cut(const uint16_t* row, int64_t start, int64_t end) {
+    if (end < 8) {
+        v8h h = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (start + i < end) h[i] = row[start + i];
+        return __builtin_bit_cast(v4u, h);
+    }
+    const int64_t at = start < end - 8 ? start : end - 8;
+    const v4u x = *reinterpret_cast<const v4u_any*>(row + at);
+    const int64_t by = start - at;                      // elements to drop
+    if (by == 0) return x;
+    if (by >= 8) return v4u{0, 0, 0, 0};
+    uint64_t lo = x.x | static_cast<uint64_t>(x.y) << 32, hi = x.z | static_cast<uint64_t>(x.w) << 32;
+    const int bits = static_cast<int>(by) * 16;
+    if (bits >= 64) {
+        lo = hi >> (bits - 64);
+        hi = 0;
+    } else {
+        lo = lo >> bits | hi << (64 - bits);
+        hi >>= bits;
+    }
+    return v4u{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+}
+
+// One operand: kRows rows (of i or j) by 64 k, loaded by kThreads threads; kStep: 4 TJ of the permuted operand, or 0.
+template <bool kOuter, int kRows, int kThreads, int kStep>
+struct Operand {
+    static constexpr int kVectors = kRows * kBK / 8 / kThreads;      // of a thread
+    static constexpr int kPieces = kRows / 8;                        // of a k where k is outer
+    static_assert(kRows * kBK / 8 % kThreads == 0, "");
+    const uint16_t* base;       // row 0 of the tile at k 0
+    int64_t ld, rows, depth;    // rows of the tile that are there
+    bool edge;
+    v4u x[kVectors];
+
+    __device__ void start(const void* p, int64_t stride, int64_t first, int64_t all, int64_t K) {
+        ld = stride;
+        rows = all - first < kRows ? all - first : kRows;
+        edge = rows < kRows;
+        depth = K;
+        base = static_cast<const uint16_t*>(p) + (kOuter ? first : first * stride);
+    }
+    __device__ static int piece_of(int k) {             // exchange of the 16-byte pieces of a k
+        if (kStep == 0) return ((k & 3) << 1 | ((k >> 3 & 1) << 3)) & (kPieces - 1);
+        if (kStep == 16) return ((k & 1) | (k >> 1 & 1) << 3 | (k >> 3 & 1) << 4) & (kPieces - 1);
+        return ((k & 3) << 2) & (kPieces - 1);
+    }
+    __device__ static int turn_of(int row) { return kStep == 0 ? row & 7 : (row & 3) | (row / (kStep ? kStep : 1) & 1) << 2; }
+
+    // k step `step`; `last`: it reaches the end of k
+    __device__ __forceinline__ void load(int64_t step, bool last) {
+#pragma unroll
+        for (int s = 0; s < kVectors; ++s) {
+            const int id = s * kThreads + static_cast<int>(threadIdx.x);
+            if (!kOuter) {
+                int row = id >> 3;
+                row = row < rows ? row : static_cast<int>(rows) - 1;
+                const int64_t k = step * kBK + (id & 7) * 8;
+                const uint16_t* p = base + static_cast<int64_t>(row) * ld;
+                x[s] = last ? load_cut(p, k, depth) : *reinterpret_cast<const v4u_any*>(p + k);
+            } else {
+                const int64_t k = step * kBK + id / kPieces;
+                const int at = id % kPieces * 8;
+                if (last && k >= depth) {
+                    x[s] = v4u{0, 0, 0, 0};
+                } else {
+                    const uint16_t* p = base + k * ld;
+                    x[s] = edge ? load_cut(p, at, rows) : *reinterpret_cast<const v4u_any*>(p + at);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t* lds) const {
+#pragma unroll
+        for (int s = 0; s < kVectors; ++s) {
+            const int id = s * kThreads + static_cast<int>(threadIdx.x);
+            int place;
+            if (!kOuter) {
+                const int row = id >> 3;
+                place = row * 8 + ((id & 7) ^ turn_of(row));
+            } else {
+                const int k = id / kPieces;
+                place = k * kPieces + ((id % kPieces) ^ piece_of(k));
+            }
+            *reinterpret_cast<v4u*>(lds + place * 8) = x[s];
+        }
+    }
+    // The matrix operand of 16 rows and 32 k (half `h` of the 64): rows row0 + l % 16, or with kStep the rows
+    // row0 + (l % 16 / 4) kStep + 4 t + l % 4.
+    __device__ static __forceinline__ v4u fragment(const uint16_t* lds, int row0, int t, int h) {
+        const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
+        if (!kOuter) {
+            const int row = kStep == 0 ? row0 + 16 * t + l : row0 + (l >> 2) * kStep + 4 * t + (l & 3);
+            return *reinterpret_cast<const v4u*>(lds + (row * 8 + ((4 * h + q) ^ turn_of(row))) * 8);
+        }
+        typedef short v4s __attribute__((ext_vector_type(4)));
+        const int row = kStep == 0 ? row0 + 16 * t + (l & 3) * 4 : row0 + (l & 3) * kStep + 4 * t;     // four from here on, at k + l / 4
+        v2u half[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int k = 32 * h + 8 * q + 4 * e + (l >> 2);
+            const uint16_t* p = lds + (k * kPieces + ((row >> 3) ^ piece_of(k))) * 8 + (row & 4);
+            half[e] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p)));
+        }
+        return v4u{half[0].x, half[0].y, half[1].x, half[1].y};
+    }
+};
+
+// bias, activation, slope, residual and rounding of n <= kN neighbouring results (kN a multiple of 4) of row i from column j on
+template <class T, int kN>
+__device__ __forceinline__ void finish(const DenseGemm& g, int64_t i, int64_t j, float* f) {
+    const int64_t at = i * g.J + j;
+    const bool whole = j + kN <= g.J;
+    uint16_t* out = static_cast<uint16_t*>(g.out) + at;
+    const uint16_t* res = g.res ? static_cast<const uint16_t*>(g.res) + i * g.ldres + j : nullptr;
+    const uint16_t* bias = g.bias ? static_cast<const uint16_t*>(g.bias) + j : nullptr;
+    uint16_t r[kN], b[kN], y[kN], w[kN];
+    if (whole) {
+        if (res) __builtin_memcpy(r, res, sizeof r);
+        if (bias) __builtin_memcpy(b, bias, sizeof b);
+    } else {
+#pragma unroll
+        for (int v = 0; v < kN; ++v) {
+            r[v] = res && j + v < g.J ? res[v] : 0;
+            b[v] = bias && j + v < g.J ? bias[v] : 0;
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < kN; ++v) {
+        float slope = 1.0f, z = f[v] + (bias ? T::up(b[v]) : 0.0f);
+        float a = g.slope ? activated<true>(z, g.act, slope) : activated<false>(z, g.act, slope);
+        if (g.slope) w[v] = slope_word(slope);
+        if (res) a += T::up(r[v]);
+        y[v] = T::down(a);
+    }
+    if (whole) {
+        __builtin_memcpy(out, y, sizeof y);
+        if (g.slope) __builtin_memcpy(g.slope + at, w, sizeof w);
+    } else {
+#pragma unroll
+        for (int v = 0; v < kN; ++v)
+            if (j + v < g.J) {
+                out[v] = y[v];
+                if (g.slope) g.slope[at + v] = w[v];
+            }
+    }
+}
+
+// Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of
+// neighbouring ones, and a run goes down 8 tiles of i before it moves on in j, so that the tiles at work on an XCD share rows of both.
+__device__ __forceinline__ void place_of(int64_t b, int64_t blocks, int64_t tiles_i, int64_t tiles_j, int64_t& ti, int64_t& tj, int64_t& split) {
+    const int64_t q = blocks / 8, r = blocks % 8, xcd = b % 8;
+    const int64_t id = xcd * q + (xcd < r ? xcd : r) + b / 8;
+    split = id / (tiles_i * tiles_j);
+    const int64_t t = id % (tiles_i * tiles_j), group = t / (8 * tiles_j), first = group * 8;
+    const int64_t size = tiles_i - first < 8 ? tiles_i - first : 8, in = t % (8 * tiles_j);
+    ti = first + in % size;
+    tj = in / size;
+}
+
+// kSide x kSide tiles, kWI x kWJ wavefronts
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
+__global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseGemm g, const int splits) {
+    constexpr int kThreads = kWI * kWJ * 64, kTI = kSide / kWI / 16, kTJ = kSide / kWJ / 16;
+    typedef Operand<kAOuter, kSide, kThreads, 0> OpA;
+    typedef Operand<kBOuter, kSide, kThreads, 4 * kTJ> OpB;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
+    constexpr int kHalf = kSide * kBK;                                   // elements of one operand's step
+    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSide - 1) / kSide;
+    int64_t ti, tj, split;
+    place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
+    const int64_t steps = (g.K + kBK - 1) / kBK, s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
+    OpA a;
+    OpB b;
+    a.start(g.a, g.lda, ti * kSide, g.I, g.K);
+    b.start(g.b, g.ldb, tj * kSide, g.J, g.K);
+    const int wave = threadIdx.x >> 6, wi = wave / kWJ * (kTI * 16), wj = wave % kWJ * (kTJ * 16);
+    v4f acc[kTI][kTJ];
+#pragma unroll
+    for (int m = 0; m < kTI; ++m)
+#pragma unroll
+        for (int n = 0; n < kTJ; ++n) acc[m][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    auto fetch = [&](int64_t step) {
+        const bool last = step == steps - 1;             // uniform
+        if (last) {
+            a.load(step, true);
+            b.load(step, true);
+        } else {
+            a.load(step, false);
+            b.load(step, false);
+        }
+    };
+    if (s0 < s1) {
+        fetch(s0);
+        a.store(lds);
+        b.store(lds + kHalf);
+        __syncthreads();
+    }
+    for (int64_t step = s0; step < s1; ++step) {
+        const uint16_t* now = lds + ((step - s0) & 1) * (2 * kHalf);
+        if (step + 1 < s1) fetch(step + 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v4u fa[kTI], fb[kTJ];
+#pragma unroll
+            for (int n = 0; n < kTJ; ++n) fb[n] = OpB::fragment(now + kHalf, wj, n, h);
+#pragma unroll
+            for (int m = 0; m < kTI; ++m) fa[m] = OpA::fragment(now, wi, m, h);
+#pragma unroll
+            for (int m = 0; m < kTI; ++m)
+#pragma unroll
+                for (int n = 0; n < kTJ; ++n) acc[m][n] = T::mfma(fb[n], fa[m], acc[m][n]);
+        }
+        if (step + 1 < s1) {
+            uint16_t* next = lds + ((step + 1 - s0) & 1) * (2 * kHalf);
+            a.store(next);
+            b.store(next + kHalf);
+        }
+        __syncthreads();
+    }
+
+    const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
+    const int64_t j = tj * kSide + wj + q * (4 * kTJ);
+#pragma unroll
+    for (int m = 0; m < kTI; ++m) {
+        const int64_t i = ti * kSide + wi + m * 16 + l;
+        if (i >= g.I || j >= g.J) continue;
+        float f[4 * kTJ];
+#pragma unroll
+        for (int n = 0; n < kTJ; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) f[4 * n + v] = acc[m][n][v];
+        if (splits > 1) {
+            float* out = g.partial + (split * g.I + i) * g.J + j;
+            if (j + 4 * kTJ <= g.J) {
+                __builtin_memcpy(out, f, sizeof f);
+            } else {
+#pragma unroll
+                for (int v = 0; v < 4 * kTJ; ++v)
+                    if (j + v < g.J) out[v] = f[v];
+            }
+        } else {
+            finish<T, 4 * kTJ>(g, i, j, f);
+        }
+    }
+}
+
+// The parts of k in their order, then the same end.  grid: ceil(I ceil(J / 4) / 256).
+template <class T>
+__global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, const int splits) {
+    const int64_t quads = (g.J + 3) / 4, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = id / quads, j = id % quads * 4;
+    if (i >= g.I) return;
+    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < splits; ++s) {
+        const float* p = g.partial + (s * g.I + i) * g.J + j;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (j + v < g.J) f[v] += p[v];
+    }
+    finish<T, 4>(g, i, j, f);
+}
+
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
+void launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
+    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
+    constexpr int kBytes = 4 * kSide * kBK * 2;
+    auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ>;
+    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    (void)allowed;                                       // a refusal shows at the launch
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * splits)), dim3(kWI * kWJ * 64), kBytes, s, g, splits);
+}
+template <class T, bool kAOuter, bool kBOuter>
+void launch_tiles_of(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
+    if (p.side == 256) launch_tile<T, kAOuter, kBOuter, 256, 2, 4>(g, p.splits, s);
+    else if (p.side == 128) launch_tile<T, kAOuter, kBOuter, 128, 2, 2>(g, p.splits, s);
+    else launch_tile<T, kAOuter, kBOuter, 64, 2, 2>(g, p.splits, s);
+}
+
+}  // namespace
+
+template <class T>
+void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
+    if (g.a_outer) launch_tiles_of<T, true, true>(g, p, s);
+    else if (g.b_outer) launch_tiles_of<T, false, true>(g, p, s);
+    else launch_tiles_of<T, false, false>(g, p, s);
+    if (p.splits > 1)
+        hipLaunchKernelGGL(dense_join_kernel<T>, dim3(static_cast<uint32_t>((g.I * ((g.J + 3) / 4) + 255) / 256)), dim3(256), 0, s, g, p.splits);
+}
+
+}  // namespace adpsgd_impl

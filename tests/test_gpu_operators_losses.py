@@ -1,0 +1,295 @@
+"""Log-probabilities and losses over a vocabulary against their formulas in 64 bits (GPU).
+
+Tolerances.  A sum of V exponentials in 32 bits: each is off by |d| 2^-23 + 2^-22 relative (difference, product, instruction), weighted with
+e^d |d| at most log V in the mean; additions of a thread's at most V / 64 + 64 terms: (V / 64 + 64) 2^-24.  l is off by that, and by the
+rounding of its difference and of the result.  Gradients: those of an exponential, the sum's, the coefficient's, one rounding to the type."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(1, 1), (1, 2), (3, 10), (5, 255), (64, 1000), (7, 4097), (33, 2048), (9, 16_385), (17, 50_001), (2, 131_072), (3, 140_001), (1, 300_000), (2100, 77)]
+TYPES = ["float32", "bfloat16", "float16"]
+
+
+def make(R, V, dtype, seed, pad=0, masked=0.25, unused=True):
+    """Logits (whose surroundings and masked rows are NaN), tokens."""
+    import torch
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(seed)
+    store = torch.full((R + 1, V + pad), math.nan, dtype=dtype, device="cuda:0")
+    z = 2 * torch.randn(R, V, generator=g, device="cuda:0")
+    tokens = torch.randint(0, V, (R,), generator=g, device="cuda:0")
+    z.scatter_add_(1, tokens[:, None], 5 + torch.randn(R, 1, generator=g, device="cuda:0"))
+    if unused and V > 50:
+        z[:, V - 3:] = -math.inf
+        tokens.clamp_(max=V - 4)
+    if V > 8 and dtype != torch.float16 and R > 2:
+        z[1, 1:5] = torch.finfo(torch.float32).min       # a mask of the type's lowest value
+        tokens[1] = 0
+    tokens[torch.rand(R, generator=g, device="cuda:0") < masked] = -1
+    z[tokens < 0] = math.nan
+    lowest = torch.finfo(dtype).min
+    z = torch.where(z < lowest, torch.where(torch.isinf(z), z, lowest), z)
+    store[:R, :V] = z.to(dtype)
+    return store[:R, :V], tokens, g
+
+
+def log_probs(z, tokens):
+    """l and softmax in 64 bits, and how far l may be off."""
+    import torch
+    V = z.shape[1]
+    z = z.double()
+    lse = torch.logsumexp(z, 1)
+    at = z.gather(1, tokens.clamp(min=0)[:, None])[:, 0]
+    l = torch.where(tokens >= 0, at - lse, 0.0)
+    off = (V / 64 + 64) * 2.0 ** -24 + math.log(V + 1) * 2.0 ** -22 + 2.0 ** -22
+    return l, lse, off + 2.0 ** -23 * torch.where(tokens >= 0, l.abs() + (at - z.amax(1)).abs(), 0.0)
+
+
+def gradient_close(dz, z, tokens, lse, coef, coef_off, loff):
+    """dz against coef (onehot - softmax)."""
+    import torch
+    live = tokens >= 0
+    assert not dz[~live].any()
+    z, dz, tokens, lse, coef, coef_off, loff = z[live].double(), dz[live], tokens[live], lse[live], coef[live], coef_off[live], loff[live]
+    if not len(z):
+        return
+    p = torch.exp(z - lse[:, None])
+    want = -coef[:, None] * p
+    gap = torch.where(torch.isinf(z), 0.0, (z - z.amax(1, keepdim=True)).abs())
+    rel = gap * 2.0 ** -23 + 2.0 ** -21 + loff[:, None]
+    bound = coef.abs()[:, None] * p * rel + coef_off[:, None] * p
+    want.scatter_add_(1, tokens[:, None], coef[:, None])
+    bound.scatter_add_(1, tokens[:, None], coef_off[:, None] + 2.0 ** -23 * coef.abs()[:, None])
+    info = torch.finfo(dz.dtype)
+    tiny = info.smallest_normal * info.eps / 2 if dz.dtype == torch.float16 else 1e-37
+    bound = 1.01 * bound + 1.01 * info.eps / 2 * want.abs() + tiny
+    worst = float(((dz.double() - want).abs() / bound).max())
+    assert torch.isfinite(dz).all() and worst <= 1.0, "gradient: %.3f of the bound" % worst
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", TYPES)
+def test_token_log_probs(size, dtype):
+    import torch
+    import paper_1710_06952_amd as P
+    for pad in (0, 7):
+        print(size, dtype, pad, flush=True)
+        z, tokens, _ = make(*size, getattr(torch, dtype), seed=sum(size) + pad, pad=pad)
+        got = P.token_log_probs(z, tokens)
+        l, _, off = log_probs(torch.where(tokens[:, None] >= 0, z, 0.0), tokens)
+        assert got.dtype == torch.float32 and not got[tokens < 0].any()
+        assert float(((got.double() - l).abs() / (off + 1e-9)).max()) <= 1.0
+        assert torch.equal(got, P.token_log_probs(z, tokens))
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kl", [0.0, 0.3])
+def test_policy_loss_and_gradient(size, dtype, kl):
+    import torch
+    import paper_1710_06952_amd as P
+    print(size, dtype, kl, flush=True)
+    R, V = size
+    z, tokens, g = make(R, V, getattr(torch, dtype), seed=R + V, pad=5 if kl else 0)
+    clean = torch.where(tokens[:, None] >= 0, z, 0.0)
+    l, lse, loff = log_probs(clean, tokens)
+    rand = lambda: torch.randn(R, generator=g, device="cuda:0")  # noqa: E731
+    old, ref, adv = (l + 0.3 * rand()).float(), (l + 0.5 * rand()).float(), rand()
+    adv[::5] = 0.0
+    lo, hi = 0.2, 0.3
+    rho = torch.exp(l - old.double())
+    for edge in (1 - lo, 1 + hi):                        # no ratio where rounding decides
+        old = torch.where((rho - edge).abs() < 1e-3, old + 0.01, old)
+    rho, A = torch.exp(l - old.double()), adv.double()
+    free, held = rho * A, rho.clamp(1 - lo, 1 + hi) * A
+    count = max(1, int((tokens >= 0).sum()))
+    term, slope = -torch.minimum(free, held), torch.where(free <= held, -free, 0.0)
+    term_off, slope_off = (A.abs() * rho) * (loff + 2.0 ** -23), (A.abs() * rho) * (loff + 2.0 ** -23)
+    if kl:
+        d = ref.double() - l
+        term, slope = term + kl * (torch.exp(d) - d - 1), slope + kl * (1 - torch.exp(d))
+        # the parameters are given in 32 bits
+        term_off, slope_off = term_off + kl * (1 + torch.exp(d)) * (loff + 2.0 ** -22), slope_off + kl * (1 + torch.exp(d)) * (loff + 2.0 ** -22)
+    live = tokens >= 0
+    r = P.policy_loss_and_gradient(z, tokens, old, adv, ref if kl else None, clip=(lo, hi), kl_coef=kl)
+    loss = float(term[live].sum()) / count
+    bound = float(term_off[live].sum()) / count + 2.0 ** -23 * (float(term[live].abs().sum()) / count + float(A.abs().sum()) / count) + 1e-12
+    assert r.loss.shape == () and abs(float(r.loss) - loss) <= bound
+    assert float(((r.log_probs.double() - l).abs() / (loff + 1e-9)).max()) <= 1.0
+    assert r.dlogits.dtype == z.dtype and r.dlogits.shape == z.shape
+    coef, coef_off = slope / count, slope_off / count + 2.0 ** -22 * slope.abs() / count + 1e-30
+    gradient_close(r.dlogits, clean, tokens, lse, coef, coef_off, loff)
+    again = P.policy_loss_and_gradient(z, tokens, old, adv, ref if kl else None, clip=(lo, hi), kl_coef=kl)
+    assert all(torch.equal(p, q) for p, q in zip(r, again))
+
+
+@pytest.mark.parametrize("vocab", [1, 10, 1000, 4097, 50_001, 131_072])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[1, 1], [3, 0, 2, 5], [0, 0], [40, 1, 7, 22, 300, 0, 13, 9]], ids=str)
+def test_preference_loss_and_gradient(vocab, dtype, lengths):
+    import torch
+    import paper_1710_06952_amd as P
+    R, pairs = sum(lengths), len(lengths) // 2
+    if R * vocab > 25_000_000:
+        lengths = [min(n, 20) for n in lengths]
+        R = sum(lengths)
+    print(vocab, dtype, lengths, flush=True)
+    for smoothing, beta in ((0.0, 0.1), (0.1, 0.5)):
+        z, tokens, g = make(R, vocab, getattr(torch, dtype), seed=vocab + R, pad=3)
+        offsets = torch.tensor([sum(lengths[:q]) for q in range(len(lengths) + 1)], device="cuda:0")
+        clean = torch.where(tokens[:, None] >= 0, z, 0.0)
+        l, lse, loff = log_probs(clean, tokens) if R else (torch.zeros(0, dtype=torch.float64, device="cuda:0"),) * 3
+        sums, offs = (torch.stack([p.sum() for p in t.split(lengths)]) for t in (l, torch.where(tokens >= 0, loff, 0.0) if R else loff))
+        ref = (sums + torch.randn(len(lengths), generator=g, device="cuda:0")).float()
+        b64 = float(torch.tensor(beta))                  # as the call takes it, in 32 bits
+        s64 = float(torch.tensor(smoothing))
+        over = sums - ref.double()
+        margin = b64 * (over[:pairs] - over[pairs:])
+        moff = b64 * (offs[:pairs] + offs[pairs:]) + 1e-12
+        loss = ((1 - s64) * torch.nn.functional.softplus(-margin) + s64 * torch.nn.functional.softplus(margin)).mean()
+        r = P.preference_loss_and_gradient(z, tokens, offsets, ref, beta=beta, label_smoothing=smoothing)
+        assert ((r.log_probs.double() - sums).abs() <= offs + 2.0 ** -23 * sums.abs() + 1e-12).all()
+        assert ((r.margins.double() - margin).abs() <= moff + 2.0 ** -23 * margin.abs()).all()
+        assert abs(float(r.loss) - float(loss)) <= float((moff + 2.0 ** -23 * margin.abs()).mean()) + 2.0 ** -23 * float(loss)
+        by = b64 / pairs * (torch.sigmoid(margin) - (1 - s64))
+        of = torch.repeat_interleave(torch.arange(len(lengths), device="cuda:0"), torch.tensor(lengths, device="cuda:0"))
+        coef = torch.cat([by, -by])[of]
+        coef_off = (torch.cat([moff, moff])[of] + 2.0 ** -22) * b64 / pairs
+        gradient_close(r.dlogits, clean, tokens, lse, coef, coef_off, loff)
+
+
+def test_gradients_against_differences():
+    import torch
+    import paper_1710_06952_amd as P
+    z, tokens, g = make(6, 12, torch.float32, seed=1, masked=0.2, unused=False)
+    z = torch.where(tokens[:, None] >= 0, z.clamp(-10, 10), 0.0).contiguous()
+    rand = lambda n: torch.randn(n, generator=g, device="cuda:0")  # noqa: E731
+    l = log_probs(z, tokens)[0]
+    old, adv, ref = (l + 0.1 * rand(6)).float(), rand(6), (l + 0.5 * rand(6)).float()
+    offsets = torch.tensor([0, 2, 3, 5, 6], device="cuda:0")
+    pref = rand(4)
+
+    def policy(z):
+        l = torch.where(tokens >= 0, z.gather(1, tokens.clamp(min=0)[:, None])[:, 0] - torch.logsumexp(z, 1), 0.0)
+        rho, d = torch.exp(l - old.double()), ref.double() - l
+        A = adv.double()
+        t = -torch.minimum(rho * A, rho.clamp(0.7, 1.3) * A) + 0.1 * (torch.exp(d) - d - 1)
+        return float(t[tokens >= 0].sum() / max(1, int((tokens >= 0).sum())))
+
+    def preference(z):
+        l = torch.where(tokens >= 0, z.gather(1, tokens.clamp(min=0)[:, None])[:, 0] - torch.logsumexp(z, 1), 0.0)
+        s = torch.stack([p.sum() for p in l.split([2, 1, 2, 1])]) - pref.double()
+        return float(torch.nn.functional.softplus(-0.2 * (s[:2] - s[2:])).mean())
+
+    got = (P.policy_loss_and_gradient(z, tokens, old, adv, ref, clip=(0.3, 0.3), kl_coef=0.1).dlogits,
+           P.preference_loss_and_gradient(z, tokens, offsets, pref, beta=0.2).dlogits)
+    for f, dz in zip((policy, preference), got):
+        for e in range(0, z.numel(), 5):
+            v = []
+            for sign in (1, -1):
+                moved = z.double()
+                moved.view(-1)[e] += sign * 1e-5
+                v.append(f(moved))
+            assert abs((v[0] - v[1]) / 2e-5 - float(dz.view(-1)[e])) <= 2e-6
+
+
+def test_rows_that_cannot_be_answered():
+    """A row of nothing but -infinity, a token that cannot be, one beyond the vocabulary, infinities and NaN: their own rows only."""
+    import torch
+    import paper_1710_06952_amd as P
+    for V in (40, 5000, 40_000):
+        for dtype in (torch.float32, torch.bfloat16):
+            print(V, dtype, flush=True)
+            z = torch.randn(8, V, device="cuda:0").to(dtype)
+            tokens = torch.arange(8, device="cuda:0")
+            good = P.token_log_probs(z, tokens)
+            z[1] = -math.inf
+            z[2, 2] = -math.inf
+            tokens[3] = V
+            z[4, 9] = math.nan
+            z[5, 9] = math.inf
+            got = P.token_log_probs(z, tokens)
+            assert torch.isnan(got[[1, 3, 4, 5]]).all() and got[2] == -math.inf and torch.equal(got[[0, 6, 7]], good[[0, 6, 7]])
+            one = torch.ones(8, device="cuda:0")
+            r = P.policy_loss_and_gradient(z, tokens, good, one)
+            assert torch.isnan(r.loss) and torch.isnan(r.dlogits[[1, 3, 4, 5]]).any(1).all()
+            assert torch.isfinite(r.dlogits[[0, 2, 6, 7]]).all() and torch.equal(r.log_probs[[0, 6, 7]], good[[0, 6, 7]])
+            tokens[[1, 3, 4, 5]] = -1                    # not counted: nothing of them is left
+            r = P.policy_loss_and_gradient(z, tokens, good, one)
+            assert torch.isfinite(r.loss) and torch.isfinite(r.dlogits).all() and not r.dlogits[[1, 3, 4, 5]].any()
+    # all logits at the type's lowest value: a uniform distribution
+    z = torch.full((2, 1024), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16, device="cuda:0")
+    got = P.token_log_probs(z, torch.tensor([0, 1023], device="cuda:0"))
+    assert torch.allclose(got, torch.full_like(got, -math.log(1024)), rtol=1e-6)
+
+
+def test_nothing_counted_and_no_rows():
+    import torch
+    import paper_1710_06952_amd as P
+    z = torch.full((5, 100), math.nan, device="cuda:0")
+    none = torch.full((5,), -1, device="cuda:0")
+    zero = torch.zeros(5, device="cuda:0")
+    r = P.policy_loss_and_gradient(z, none, zero, zero)
+    assert float(r.loss) == 0.0 and not r.dlogits.any() and not r.log_probs.any()
+    e = torch.empty(0, device="cuda:0")
+    r = P.policy_loss_and_gradient(z[:0], none[:0], e, e, e, kl_coef=0.1)
+    assert float(r.loss) == 0.0 and r.dlogits.shape == (0, 100) and P.token_log_probs(z[:0], none[:0]).shape == (0,)
+
+
+def test_offsets_that_do_not_fit_are_not_followed():
+    import torch
+    import paper_1710_06952_amd as P
+    z, tokens = torch.randn(6, 50, device="cuda:0"), torch.arange(6, device="cuda:0")
+    ref = torch.zeros(4, device="cuda:0")
+    for bad in ([0, 2, 4, 6, 7], [0, 4, 2, 5, 6], [1, 2, 3, 4, 6], [0, 2, 1 << 40, 4, 6], [0, -5, 3, 4, 6], [0, 2, 3, 4, 5]):
+        r = P.preference_loss_and_gradient(z, tokens, torch.tensor(bad, device="cuda:0"), ref)
+        assert torch.isnan(r.loss), bad
+
+
+def test_rows_beyond_32_bit_offsets():
+    import torch
+    import paper_1710_06952_amd as P
+    rows, V = 33_000, 70_000                             # 4.6 GB, 2.3 G elements
+    z = torch.zeros(rows, V, dtype=torch.bfloat16, device="cuda:0")
+    tokens = torch.full((rows,), -1, device="cuda:0")
+    tokens[0], tokens[-1] = 5, 7
+    z[-1, 7] = 3.0
+    got = P.token_log_probs(z, tokens)
+    want = [-math.log(V), 3.0 - math.log(V - 1 + math.exp(3.0))]
+    assert abs(float(got[0]) - want[0]) < 2e-4 and abs(float(got[-1]) - want[1]) < 2e-4 and not got[1:-1].any()
+    r = P.policy_loss_and_gradient(z, tokens, got, torch.ones(rows, device="cuda:0"))
+    assert abs(float(r.loss) + 1.0) < 1e-6 and abs(float(r.dlogits[-1, 7]) + 0.5 * (1 - math.exp(want[1]))) < 2e-3 and not r.dlogits[1:-1:1000].any()
+
+
+def test_capture_and_other_streams():
+    import torch
+    import paper_1710_06952_amd as P
+    for R, V, dtype in ((64, 1000, torch.float32), (3, 131_072, torch.bfloat16), (5, 140_001, torch.bfloat16)):
+        z, tokens, g = make(R, V, dtype, seed=2, unused=False)
+        z = torch.where(tokens[:, None] >= 0, z.float().clamp(-20, 20), 0.0).to(dtype).contiguous()
+        old, adv = torch.randn(R, device="cuda:0"), torch.randn(R, device="cuda:0")
+        offsets, ref = torch.tensor([0, 1, R], device="cuda:0"), torch.zeros(2, device="cuda:0")
+
+        def every():
+            return [P.token_log_probs(z, tokens), *P.policy_loss_and_gradient(z, tokens, old, adv, old, kl_coef=0.1),
+                    *P.preference_loss_and_gradient(z, tokens, offsets, ref)]
+        want = every()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = every()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = every()
+        for k in range(3):
+            z.mul_(0.7)
+            graph.replay()
+            torch.cuda.synchronize()
+            replayed = [t.clone() for t in got]
+            want = every()
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(replayed, want)), k
