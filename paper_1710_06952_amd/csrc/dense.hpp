@@ -17,6 +17,8 @@ struct Bf16 {
     __device__ static v4f mfma(v4u a, v4u b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
+    // c in accumulation registers, and in the same ones before and after; wait_mfma and settle_mfma before c is read
+    __device__ static void mfma_in_place(v4u a, v4u b, v4f& c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 struct F16 {
     typedef _Float16 V8 __attribute__((ext_vector_type(8)));
@@ -25,7 +27,13 @@ struct F16 {
     __device__ static v4f mfma(v4u a, v4u b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
+    __device__ static void mfma_in_place(v4u a, v4u b, v4f& c) { asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
+
+// An instruction that reads the result of a matrix instruction has to come some cycles later, which the compiler sees to for its
+// own only: 32 cycles cover every form.  One wait, then every result that it is for.
+__device__ __forceinline__ void wait_mfma() { asm volatile("s_nop 15\n\ts_nop 15"); }
+__device__ __forceinline__ void settle_mfma(v4f& c) { asm volatile("" : "+a"(c)); }
 
 // Eight values rounded.
 template <class T>
@@ -87,12 +95,17 @@ __device__ __forceinline__ float slope_of(uint16_t w) {
     return mag == 0x7FFFu ? NAN : __uint_as_float(__float_as_uint(s) | (w & 0x8000u) << 16);
 }
 
-// How a product is cut: tiles of side x side, `splits` parts of k whose sums are joined afterwards.
+// How a product is cut: tiles of side x side, `splits` parts of k whose sums are joined afterwards.  `aligned`: as rows of
+// 16-byte pieces (large_fits), which the tiles of 256 need.
 struct DensePlan {
     int side;
     int splits;
 };
-DensePlan dense_plan(int64_t I, int64_t J, int64_t K);
+DensePlan dense_plan(int64_t I, int64_t J, int64_t K, bool aligned);
+inline bool large_fits(const DenseGemm& g) {
+    auto rows = [](const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; };
+    return rows(g.a, g.lda, g.a_outer ? g.I : g.K) && rows(g.b, g.ldb, g.b_outer ? g.J : g.K) && g.K >= 1;
+}
 
 template <class T>
 void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);

@@ -1,0 +1,277 @@
+// Large tiled products D[i][j] = sum_k A(i, k) B(j, k): tiles of 256 x 256 by four wavefronts of 128 x 128, for operands whose rows
+// begin at multiples of 16 bytes.
+//
+// A wavefront alone on its SIMD has 512 registers: 256 hold its results, and both halves of a step of 64 k fit beside them, so the
+// loads of one half are under way while the other is multiplied.  128 x 128 results of a wavefront read 128 KB of a step's operands from LDS
+// a compute unit, 64 x 128 would read 192.
+//
+// Operands go from memory straight to LDS (buffer loads with the lds bit: 16 bytes a lane, a wavefront's 1024 bytes in a row), so
+// they cost no registers.  Two steps' operands are in LDS.  A turn of the loop:
+//     request half 1 of step s from LDS;  multiply half 0;
+//     wait for the loads of step s + 1 (requested a turn ago);  barrier: nobody reads step s any more, and step s + 1 is there for all;
+//     request step s + 2 from memory into the place of step s;  request half 0 of step s + 1 from LDS;  multiply half 1.
+// The pieces of 16 bytes are exchanged as in dense_tiles.hpp, here by the addresses that the lanes load from.
+//
+// What lies beyond the ends: rows of an operand with k inner are the last row again; pieces beyond the end of k, and rows of k beyond the
+// end where k is outer, are out of the buffer's range, for which the load delivers zeros.
+#pragma once
+
+#include "dense_tiles.hpp"
+
+namespace adpsgd_impl {
+namespace {
+
+typedef uint32_t v4su __attribute__((ext_vector_type(4)));
+
+// 16 bytes a lane from `rsrc` + offset to LDS at `lds` + 16 lane.  No register is written; the wait is `wait_loads`.
+__device__ __forceinline__ void load_to_lds(v4su rsrc, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(rsrc), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+constexpr uint32_t kOutOfRange = 0x80000000u;
+
+template <bool kOuter, int kStep>
+struct DirectOperand {
+    static constexpr int kSide = 256, kThreads = 256, kLoads = kSide * kBK / 8 / kThreads;
+    typedef Operand<kOuter, kSide, kThreads, kStep> Form;
+    uint64_t base, end;         // bytes
+    uint64_t advance;           // of a step
+    uint32_t offset[kLoads];
+    uint32_t beyond[2];         // k inner: out of range in the last step, for even and odd loads
+    v4su rsrc;                  // of the step that is being loaded ...
+    uint32_t to, cut, none;     // ... its place in LDS, all ones in the last step, and kOutOfRange behind it
+
+    __device__ void start(const void* p, int64_t ld, int64_t first, int64_t all, int64_t K) {
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        const uint32_t pitch = static_cast<uint32_t>(ld * 2);
+        if (!kOuter) {
+            base = at + static_cast<uint64_t>(first) * pitch;
+            end = at + static_cast<uint64_t>(all - 1) * pitch + 2 * K;
+            advance = 2 * kBK;
+            const int there = static_cast<int>((K - (K - 1) / kBK * kBK) / 8);       // pieces of the last step
+#pragma unroll
+            for (int s = 0; s < 2; ++s) beyond[s] = ((threadIdx.x & 7) ^ Form::turn_of(s * 32 + (threadIdx.x >> 3))) < there ? 0u : kOutOfRange;
+        } else {
+            base = at + 2 * first;
+            end = at + static_cast<uint64_t>(K - 1) * pitch + 2 * all;
+            advance = static_cast<uint64_t>(kBK) * pitch;
+        }
+        const int rows = static_cast<int>(all - first < kSide ? all - first : kSide);
+#pragma unroll
+        for (int s = 0; s < kLoads; ++s) {
+            const int id = s * kThreads + static_cast<int>(threadIdx.x);
+            if (!kOuter) {
+                const int row = id >> 3, piece = (id & 7) ^ Form::turn_of(row);
+                offset[s] = static_cast<uint32_t>(row < rows ? row : rows - 1) * pitch + piece * 16;
+            } else {
+                const int k = id / Form::kPieces, piece = (id % Form::kPieces) ^ Form::piece_of(k);
+                offset[s] = static_cast<uint32_t>(k) * pitch + piece * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void aim(int64_t step, int64_t steps, uint32_t lds) {
+        const uint64_t from = base + static_cast<uint64_t>(step) * advance;
+        const uint64_t left = end - from;
+        const uint32_t range = left < kOutOfRange - 1 ? static_cast<uint32_t>(left) : kOutOfRange - 1;
+        rsrc = v4su{static_cast<uint32_t>(from), static_cast<uint32_t>(from >> 32) & 0xFFFFu, range, 0x00020000u};
+        to = lds;
+        cut = step == steps - 1 ? 0xFFFFFFFFu : 0u;
+        none = step < steps ? 0u : kOutOfRange;
+    }
+    __device__ __forceinline__ void load(int s) const {
+        const uint32_t at = offset[s] | (kOuter ? none : (beyond[s & 1] & cut) | none);
+        load_to_lds(rsrc, at, to + s * kThreads * 16u);
+    }
+};
+
+// Where a lane reads its fragments of 16 rows and 32 k: what differs between fragments t and halves h by exchanged bits is a register,
+// the rest an immediate.  `flip` goes to the other step's operands.
+template <bool kOuter, int kStep>
+struct FragmentReader {
+    typedef Operand<kOuter, 256, 256, kStep> Form;
+    static constexpr int kPlaces = !kOuter ? 2 : kStep == 0 ? 8 : 4;
+    uint32_t at[kPlaces];
+
+    __device__ void start(uint32_t lds, int row0) {
+        const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
+#pragma unroll
+        for (int p = 0; p < kPlaces; ++p) {
+            if (!kOuter) {                               // the same exchange for all t
+                const int row = kStep == 0 ? row0 + l : row0 + (l >> 2) * kStep + (l & 3);
+                at[p] = lds + (row * 8 + ((4 * p + q) ^ Form::turn_of(row))) * 16;
+            } else {                                     // the same for both h and both fours of k
+                const int k = 8 * q + (l >> 2), row = kStep == 0 ? row0 + 16 * p + (l & 3) * 4 : row0 + (l & 3) * kStep + 8 * p;
+                at[p] = lds + (k * Form::kPieces + ((row >> 3) ^ Form::piece_of(k))) * 16 + (row & 4) * 2;
+            }
+        }
+    }
+    __device__ __forceinline__ void flip() {
+#pragma unroll
+        for (int p = 0; p < kPlaces; ++p) at[p] ^= 0x10000u;
+    }
+    __device__ __forceinline__ v4u read(int t, int h) const {
+        if (!kOuter) {
+            constexpr uint32_t kBytes = (kStep == 0 ? 16 : 4) * 128;
+            return *(const __attribute__((address_space(3))) v4u*)(static_cast<uintptr_t>(at[h] + t * kBytes));
+        }
+        typedef short v4s __attribute__((ext_vector_type(4)));
+        const uint32_t from = (kStep == 0 ? at[t] : at[t / 2] + t % 2 * 8) + h * (32 * 512);
+        v2u half[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            half[e] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(static_cast<uintptr_t>(from + e * (4 * 512)))));
+        return v4u{half[0].x, half[0].y, half[1].x, half[1].y};
+    }
+};
+
+template <class T, bool kAOuter, bool kBOuter>
+__global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) {
+    constexpr int kSide = 256, kTI = 8, kTJ = 8, kHalf = kSide * kBK;
+    typedef DirectOperand<kAOuter, 0> OpA;
+    typedef DirectOperand<kBOuter, 4 * kTJ> OpB;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
+    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSide - 1) / kSide;
+    int64_t ti, tj, split;
+    place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
+    const int64_t steps = (g.K + kBK - 1) / kBK;
+    OpA a;
+    OpB b;
+    a.start(g.a, g.lda, ti * kSide, g.I, g.K);
+    b.start(g.b, g.ldb, tj * kSide, g.J, g.K);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = (wave >> 1) * 128, wj = (wave & 1) * 128;
+    const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t*)lds)), place = at + wave * 1024;
+    FragmentReader<kAOuter, 0> read_a;
+    FragmentReader<kBOuter, 4 * kTJ> read_b;
+    read_a.start(at, wi);
+    read_b.start(at + 2 * kHalf, wj);
+    v4f acc[kTI][kTJ];
+#pragma unroll
+    for (int m = 0; m < kTI; ++m)
+#pragma unroll
+        for (int n = 0; n < kTJ; ++n) acc[m][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v4u fa[2][kTI], fb[2][kTJ];
+
+    auto aim = [&](int64_t step) {
+        const uint32_t to = place + static_cast<uint32_t>(step & 1) * (4 * kHalf);
+        a.aim(step, steps, to);
+        b.aim(step, steps, to + 2 * kHalf);
+    };
+    auto request = [&](int h, int n) {                   // fragment n of 16, from LDS: those of B first, all products need them
+        if (n < kTJ) fb[h][n] = read_b.read(n, h);
+        else fa[h][n - kTJ] = read_a.read(n - kTJ, h);
+    };
+    auto other_step = [&]() {
+        read_a.flip();
+        read_b.flip();
+    };
+    // The results take all 256 accumulation registers, so the products are written as instructions that leave a result where it is: the
+    // compiler's own form takes a new place for it, and with none left over moves results around (200 to 560 moves a step).
+    // Multiplies half h; between the products of one row of fragments and the next: three fragments of the other half, and four
+    // loads.  The order is the one written: a block of loads or reads in front of the products would hold them up.
+    auto multiply = [&](int h, bool loads) {
+#pragma unroll
+        for (int m = 0; m < kTI; ++m) {
+#pragma unroll
+            for (int n = 3 * m; n < 3 * m + 3; ++n)
+                if (n < kTI + kTJ) request(1 - h, n);
+            if (loads && m < 4) {
+#pragma unroll
+                for (int s = 2 * m; s < 2 * m + 2; ++s) {
+                    a.load(s);
+                    b.load(s);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kTJ; ++n) {
+                T::mfma_in_place(fb[h][n], fa[h][m], acc[m][n]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto all_loads = [&]() {
+#pragma unroll
+        for (int s = 0; s < OpA::kLoads; ++s) {
+            a.load(s);
+            b.load(s);
+        }
+    };
+    aim(0);
+    all_loads();
+    wait_loads();
+    __syncthreads();
+    aim(1);
+    all_loads();
+#pragma unroll
+    for (int n = 0; n < kTI + kTJ; ++n) request(0, n);
+    // Behind the last step nothing is loaded (out of range), and what is requested is not used: one loop without ends of its own.
+    for (int64_t step = 0; step < steps; ++step) {
+        multiply(0, false);
+        wait_loads();
+        __syncthreads();
+        aim(step + 2);
+        other_step();
+        multiply(1, true);
+    }
+    wait_loads();
+    wait_mfma();
+#pragma unroll
+    for (int m = 0; m < kTI; ++m)
+#pragma unroll
+        for (int n = 0; n < kTJ; ++n) settle_mfma(acc[m][n]);
+
+    // The results go through LDS, a wavefront's own 32 KB for 64 of its rows at a time: the end is a short loop over eight neighbouring
+    // results a lane instead of 256 copies of it, and rows are stored 256 bytes at a time.  Pieces of 16 bytes exchanged by the row.
+    __syncthreads();                                     // the operands in LDS have been read by all
+    float* own = reinterpret_cast<float*>(lds) + wave * (64 * 128);
+    const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
+    const Ending<T> end(g, tj * kSide + wj + 8 * l);
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < kTJ; ++n) {
+                const int row = m * 16 + l, piece = (q * kTJ + n) ^ (row & 31);
+                *reinterpret_cast<v4f*>(own + row * 128 + piece * 4) = acc[part * 4 + m][n];
+            }
+        wave_lds_sync();
+        // four turns at a time, the residual rows of the next four on their way
+        const int64_t i0 = ti * kSide + wi + part * 64 + q;
+        v4u next[4];
+        auto residual = [&](int first) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) next[u] = end.residual(i0 + (first + u) * 4);
+        };
+        residual(0);
+#pragma unroll 1
+        for (int first = 0; first < 16; first += 4) {
+            v4u r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) r[u] = next[u];
+            residual(first + 4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int row = (first + u) * 4 + q;
+                const v4f f0 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l) ^ (row & 31)) * 4);
+                const v4f f1 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l + 1) ^ (row & 31)) * 4);
+                float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+                end.finish(i0 + (first + u) * 4, f, r[u]);
+            }
+        }
+        wave_lds_sync();
+    }
+}
+
+template <class T, bool kAOuter, bool kBOuter>
+void launch_large(const DenseGemm& g, hipStream_t s) {
+    const int64_t tiles = (g.I + 255) / 256 * ((g.J + 255) / 256);
+    constexpr int kBytes = 4 * 256 * kBK * 2;
+    auto kernel = dense_large_kernel<T, kAOuter, kBOuter>;
+    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    (void)allowed;                                       // a refusal shows at the launch
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles)), dim3(256), kBytes, s, g);
+}
+
+}  // namespace
+}  // namespace adpsgd_impl

@@ -69,6 +69,7 @@ struct Operand {
     }
     __device__ static int piece_of(int k) {             // exchange of the 16-byte pieces of a k
         if (kStep == 0) return ((k & 3) << 1 | ((k >> 3 & 1) << 3)) & (kPieces - 1);
+        if (kStep == 32) return k & 3;
         if (kStep == 16) return ((k & 1) | (k >> 1 & 1) << 3 | (k >> 3 & 1) << 4) & (kPieces - 1);
         return ((k & 3) << 2) & (kPieces - 1);
     }
@@ -133,45 +134,82 @@ struct Operand {
     }
 };
 
-// bias, activation, slope, residual and rounding of n <= kN neighbouring results (kN a multiple of 4) of row i from column j on
-template <class T, int kN>
-__device__ __forceinline__ void finish(const DenseGemm& g, int64_t i, int64_t j, float* f) {
-    const int64_t at = i * g.J + j;
-    const bool whole = j + kN <= g.J;
-    uint16_t* out = static_cast<uint16_t*>(g.out) + at;
-    const uint16_t* res = g.res ? static_cast<const uint16_t*>(g.res) + i * g.ldres + j : nullptr;
-    const uint16_t* bias = g.bias ? static_cast<const uint16_t*>(g.bias) + j : nullptr;
-    uint16_t r[kN], b[kN], y[kN], w[kN];
-    if (whole) {
-        if (res) __builtin_memcpy(r, res, sizeof r);
-        if (bias) __builtin_memcpy(b, bias, sizeof b);
-    } else {
-#pragma unroll
-        for (int v = 0; v < kN; ++v) {
-            r[v] = res && j + v < g.J ? res[v] : 0;
-            b[v] = bias && j + v < g.J ? bias[v] : 0;
-        }
+// bias, activation, slope, residual and rounding of up to kN neighbouring results (4 or 8) of row i from column j on
+template <int kN>
+__device__ __forceinline__ void load_up_to(const uint16_t* p, int64_t n, uint16_t* h) {
+    if (n >= kN) {
+        __builtin_memcpy(h, p, 2 * kN);
+        return;
     }
 #pragma unroll
-    for (int v = 0; v < kN; ++v) {
-        float slope = 1.0f, z = f[v] + (bias ? T::up(b[v]) : 0.0f);
-        float a = g.slope ? activated<true>(z, g.act, slope) : activated<false>(z, g.act, slope);
-        if (g.slope) w[v] = slope_word(slope);
-        if (res) a += T::up(r[v]);
-        y[v] = T::down(a);
-    }
-    if (whole) {
-        __builtin_memcpy(out, y, sizeof y);
-        if (g.slope) __builtin_memcpy(g.slope + at, w, sizeof w);
-    } else {
-#pragma unroll
-        for (int v = 0; v < kN; ++v)
-            if (j + v < g.J) {
-                out[v] = y[v];
-                if (g.slope) g.slope[at + v] = w[v];
-            }
-    }
+    for (int v = 0; v < kN; ++v) h[v] = v < n ? p[v] : 0;
 }
+template <int kN>
+__device__ __forceinline__ void store_up_to(uint16_t* p, int64_t n, const uint16_t* h) {
+    if (n >= kN) {
+        __builtin_memcpy(p, h, 2 * kN);
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < kN; ++v)
+        if (v < n) p[v] = h[v];
+}
+// The end of eight neighbouring columns from j on: what all rows share is read once.
+template <class T>
+struct Ending {
+    const DenseGemm& g;
+    int64_t j;
+    int n;                      // columns that are there, up to 8
+    float bias[8];
+
+    __device__ __forceinline__ Ending(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
+        n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
+        uint16_t h[8];
+        if (g.bias && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.bias) + j, n, h);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) bias[v] = g.bias && v < n ? T::up(h[v]) : 0.0f;
+    }
+    __device__ __forceinline__ v4u residual(int64_t i) const {
+        uint16_t h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (g.res && i < g.I && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, n, h);
+        v4u r;
+        __builtin_memcpy(&r, h, 16);
+        return r;
+    }
+    __device__ __forceinline__ void finish(int64_t i, float* f, v4u r) const {
+        if (i >= g.I || n <= 0) return;
+        const int64_t at = i * g.J + j;
+        uint16_t h[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) f[v] += bias[v];
+        if (g.act != ADPSGD_ACT_NONE) {
+            if (g.slope) {
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    float slope;
+                    f[v] = activated<true>(f[v], g.act, slope);
+                    h[v] = slope_word(slope);
+                }
+                store_up_to<8>(g.slope + at, n, h);
+            } else {
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    float slope;
+                    f[v] = activated<false>(f[v], g.act, slope);
+                }
+            }
+        }
+        if (g.res) {
+            float add[8];
+            unpack8<T>(r, add);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) f[v] += add[v];
+        }
+#pragma unroll
+        for (int v = 0; v < 8; ++v) h[v] = T::down(f[v]);
+        store_up_to<8>(static_cast<uint16_t*>(g.out) + at, n, h);
+    }
+};
 
 // Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of
 // neighbouring ones, and a run goes down 8 tiles of i before it moves on in j, so that the tiles at work on an XCD share rows of both.
@@ -248,45 +286,66 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     }
 
     const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
-    const int64_t j = tj * kSide + wj + q * (4 * kTJ);
+    const int64_t j = tj * kSide + wj + q * (4 * kTJ), i0 = ti * kSide + wi + l;
+    if (j >= g.J) return;
+    if (splits > 1) {
 #pragma unroll
-    for (int m = 0; m < kTI; ++m) {
-        const int64_t i = ti * kSide + wi + m * 16 + l;
-        if (i >= g.I || j >= g.J) continue;
-        float f[4 * kTJ];
-#pragma unroll
-        for (int n = 0; n < kTJ; ++n)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) f[4 * n + v] = acc[m][n][v];
-        if (splits > 1) {
+        for (int m = 0; m < kTI; ++m) {
+            const int64_t i = i0 + m * 16;
+            if (i >= g.I) continue;
             float* out = g.partial + (split * g.I + i) * g.J + j;
-            if (j + 4 * kTJ <= g.J) {
-                __builtin_memcpy(out, f, sizeof f);
-            } else {
 #pragma unroll
-                for (int v = 0; v < 4 * kTJ; ++v)
-                    if (j + v < g.J) out[v] = f[v];
+            for (int n = 0; n < kTJ; ++n) {
+                if (j + 4 * n + 4 <= g.J) {
+                    __builtin_memcpy(out + 4 * n, &acc[m][n], 16);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (j + 4 * n + v < g.J) out[4 * n + v] = acc[m][n][v];
+                }
             }
-        } else {
-            finish<T, 4 * kTJ>(g, i, j, f);
+        }
+        return;
+    }
+#pragma unroll
+    for (int n = 0; n < kTJ; n += 2) {
+        const Ending<T> end(g, j + 4 * n);
+        v4u r[kTI];
+#pragma unroll
+        for (int m = 0; m < kTI; ++m) r[m] = end.residual(i0 + m * 16);
+#pragma unroll
+        for (int m = 0; m < kTI; ++m) {
+            float f[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) f[v] = acc[m][n + v / 4][v % 4];
+            end.finish(i0 + m * 16, f, r[m]);
         }
     }
 }
 
-// The parts of k in their order, then the same end.  grid: ceil(I ceil(J / 4) / 256).
+// The parts of k in their order, then the same end.  grid: ceil(I ceil(J / 8) / 256).
 template <class T>
 __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, const int splits) {
-    const int64_t quads = (g.J + 3) / 4, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t i = id / quads, j = id % quads * 4;
+    const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = id / eights, j = id % eights * 8;
     if (i >= g.I) return;
-    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const Ending<T> end(g, j);
+    const v4u r = end.residual(i);
+    float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) {
         const float* p = g.partial + (s * g.I + i) * g.J + j;
+        if (end.n == 8) {
+            float part[8];
+            __builtin_memcpy(part, p, sizeof part);
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (j + v < g.J) f[v] += p[v];
+            for (int v = 0; v < 8; ++v) f[v] += part[v];
+        } else {
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                if (v < end.n) f[v] += p[v];
+        }
     }
-    finish<T, 4>(g, i, j, f);
+    end.finish(i, f, r);
 }
 
 template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
@@ -298,22 +357,5 @@ void launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
     (void)allowed;                                       // a refusal shows at the launch
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * splits)), dim3(kWI * kWJ * 64), kBytes, s, g, splits);
 }
-template <class T, bool kAOuter, bool kBOuter>
-void launch_tiles_of(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
-    if (p.side == 256) launch_tile<T, kAOuter, kBOuter, 256, 2, 4>(g, p.splits, s);
-    else if (p.side == 128) launch_tile<T, kAOuter, kBOuter, 128, 2, 2>(g, p.splits, s);
-    else launch_tile<T, kAOuter, kBOuter, 64, 2, 2>(g, p.splits, s);
-}
-
 }  // namespace
-
-template <class T>
-void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
-    if (g.a_outer) launch_tiles_of<T, true, true>(g, p, s);
-    else if (g.b_outer) launch_tiles_of<T, false, true>(g, p, s);
-    else launch_tiles_of<T, false, false>(g, p, s);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(dense_join_kernel<T>, dim3(static_cast<uint32_t>((g.I * ((g.J + 3) / 4) + 255) / 256)), dim3(256), 0, s, g, p.splits);
-}
-
 }  // namespace adpsgd_impl

@@ -113,22 +113,22 @@ hipError_t launch_dense_dz(int32_t type, const void* dy, int64_t lddy, const uin
     return hipGetLastError();
 }
 
-DensePlan dense_plan(int64_t I, int64_t J, int64_t K) {
+DensePlan dense_plan(int64_t I, int64_t J, int64_t K, bool aligned) {
     auto tiles = [&](int64_t side) { return ((I + side - 1) / side) * ((J + side - 1) / side); };
-    if (tiles(256) >= 128) return DensePlan{256, 1};
+    if (aligned && tiles(256) >= 128) return DensePlan{256, 1};
     if (tiles(128) >= 128) return DensePlan{128, 1};
     const int64_t steps = (K + 63) / 64, n = tiles(64);
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(n, 1), steps / 4, 32}));
     return DensePlan{64, static_cast<int>(splits)};
 }
 int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
-    const DensePlan p = dense_plan(I, J, K);
+    const DensePlan p = dense_plan(I, J, K, false);       // aligned operands are cut into as many parts or none
     return p.splits > 1 ? p.splits * I * J * static_cast<int64_t>(sizeof(float)) : 0;
 }
 
 hipError_t launch_dense_gemm(int32_t type, const DenseGemm& g, hipStream_t s) {
     if (g.I == 0 || g.J == 0) return hipSuccess;
-    const DensePlan p = dense_plan(g.I, g.J, g.K);
+    const DensePlan p = dense_plan(g.I, g.J, g.K, large_fits(g));
     if (type == ADPSGD_TYPE_BF16) launch_dense_tiles<Bf16>(g, p, s);
     else launch_dense_tiles<F16>(g, p, s);
     return hipGetLastError();
