@@ -1,6 +1,8 @@
 // Shared by the kernels of dense layers: their two types, the activations with their slopes, and the 16-bit form of a slope.
 #pragma once
 
+#include <type_traits>
+
 #include "device_common.hpp"
 #include "operators.hpp"
 
@@ -54,45 +56,45 @@ __device__ __forceinline__ void unpack8(v4u v, float* f) {
 
 // act(z) and its derivative.  gelu: the upper tail of the normal distribution is exp(-t^2 / 2) P(1 / (1 + 0.38 t)), P of degree 7
 // fitted to the least largest relative error over t >= 0, 2.6e-6: the tail keeps its relative accuracy, unlike 1 + erf.
-template <bool kSlope>
-__device__ __forceinline__ float activated(float z, int act, float& slope) {
-    if (act == ADPSGD_ACT_NONE) {
-        slope = 1.0f;
-        return z;
-    }
-    if (act == ADPSGD_ACT_RELU) {
+template <bool kSlope, int kAct>
+__device__ __forceinline__ float activated(float z, float& slope) {
+    if (kAct == ADPSGD_ACT_RELU) {
         slope = z > 0.0f ? 1.0f : 0.0f;
         return z <= 0.0f ? 0.0f : z;                     // NaN stays
     }
-    if (act == ADPSGD_ACT_GELU) {
+    if (kAct == ADPSGD_ACT_GELU) {
         const float t = fabsf(z), u = __builtin_amdgcn_rcpf(fmaf(0.38f, t, 1.0f));
-        const float e = __builtin_amdgcn_exp2f(t * t * -0.7213475204444817f);
+        const float e = __builtin_amdgcn_exp2f(z * z * -0.7213475204444817f);
         float p = fmaf(u, 0.04894981298366624f, -0.16002513951519665f);
         p = fmaf(p, u, 0.11438935044517826f);
         p = fmaf(p, u, 0.05999139163590317f);
         p = fmaf(p, u, 0.1337908999955492f);
         p = fmaf(p, u, 0.15129931401177749f);
         p = fmaf(p, u, 0.15160565325274758f);
-        const float tail = e * (p * u), phi = z < 0.0f ? tail : 1.0f - tail;
+        const float phi = 0.5f + copysignf(fmaf(-(e * u), p, 0.5f), z);
         if (kSlope) slope = fmaf(z * 0.3989422804014327f, e, phi);
         return z * phi;
     }
-    const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
-    if (kSlope) slope = sig * fmaf(z, 1.0f - sig, 1.0f);
-    return z * sig;
+    const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)), y = z * sig;
+    if (kSlope) slope = fmaf(y, 1.0f - sig, sig);
+    return y;
 }
 
-// A slope (under 2 in magnitude) in 16 bits: sign, 3 bits of exponent (2^-6 to 1, and steps of 2^-18 below), 12 of fraction.  As
-// a power of two takes the exponent there the fp32 form of |s| 2^-120 is that format, with bits to spare.  Four times as fine as
-// fp16 where slopes are: dz, which is rounded to the type once, is not visibly further off for it.  0x7FFF is NaN.
-__device__ __forceinline__ uint16_t slope_word(float s) {
-    const uint32_t bits = __float_as_uint(fabsf(s) * 0x1p-120f), rounded = (bits + 0x3FFu + (bits >> 11 & 1u)) >> 11;
-    return static_cast<uint16_t>((s == s ? rounded : 0x7FFFu) | (__float_as_uint(s) >> 16 & 0x8000u));
+// Slopes in 16 bits for the backward pass: (w - 8192) 2^-15, within 2^-16 from -1/4 to 7/4 (they are from -0.13 to 1.13), and 0 for NaN,
+// which no slope comes to.  Beside the rounding of dz to its type that is nothing, except for slopes under 2^-7, where it is the larger
+// of the two.  A conversion of two and an FMA each; a form with an exponent took nine instructions, and tiles with gelu 24 us at their end.
+__device__ __forceinline__ v4u slope_words(const float* s) {
+    v4u w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = fmaf(s[2 * i], 32768.0f / 65535.0f, 8192.0f / 65535.0f), b = fmaf(s[2 * i + 1], 32768.0f / 65535.0f, 8192.0f / 65535.0f);
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b));
+    }
+    return w;
 }
-__device__ __forceinline__ float slope_of(uint16_t w) {
-    const uint32_t mag = w & 0x7FFFu;
-    const float s = __uint_as_float(mag << 11) * 0x1p120f;
-    return mag == 0x7FFFu ? NAN : __uint_as_float(__float_as_uint(s) | (w & 0x8000u) << 16);
+__device__ __forceinline__ float slope_of(uint32_t w) {
+    const float s = fmaf(static_cast<float>(w), 0x1p-15f, -0.25f);
+    return w == 0u ? NAN : s;
 }
 
 // How a product is cut: tiles of side x side, `splits` parts of k whose sums are joined afterwards.  `aligned`: as rows of
@@ -104,7 +106,7 @@ struct DensePlan {
 DensePlan dense_plan(int64_t I, int64_t J, int64_t K, bool aligned);
 inline bool large_fits(const DenseGemm& g) {
     auto rows = [](const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; };
-    return rows(g.a, g.lda, g.a_outer ? g.I : g.K) && rows(g.b, g.ldb, g.b_outer ? g.J : g.K) && g.K >= 1;
+    return rows(g.a, g.lda, g.a_outer ? g.I : g.K) && rows(g.b, g.ldb, g.b_outer ? g.J : g.K) && g.K >= 1 && g.J % 8 == 0;
 }
 
 template <class T>

@@ -221,11 +221,12 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
         for (int n = 0; n < kTJ; ++n) settle_mfma(acc[m][n]);
 
     // The results go through LDS, a wavefront's own 32 KB for 64 of its rows at a time: the end is a short loop over eight neighbouring
-    // results a lane instead of 256 copies of it, and rows are stored 256 bytes at a time.  Pieces of 16 bytes exchanged by the row.
+    // results a lane, and rows are stored 256 bytes at a time.  As 32 copies of the end in the place of the loop it took 20 us a tile
+    // (60 with an activation): the instructions had to come from memory.  Pieces of 16 bytes exchanged by the row.
     __syncthreads();                                     // the operands in LDS have been read by all
     float* own = reinterpret_cast<float*>(lds) + wave * (64 * 128);
     const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
-    const Ending<T> end(g, tj * kSide + wj + 8 * l);
+    const Ending<T, true> end(g, tj * kSide + wj + 8 * l);
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
 #pragma unroll
@@ -233,31 +234,21 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
 #pragma unroll
             for (int n = 0; n < kTJ; ++n) {
                 const int row = m * 16 + l, piece = (q * kTJ + n) ^ (row & 31);
-                *reinterpret_cast<v4f*>(own + row * 128 + piece * 4) = acc[part * 4 + m][n];
+                *reinterpret_cast<v4f*>(own + row * 128 + piece * 4) = acc[4 * part + m][n];
             }
         wave_lds_sync();
-        // four turns at a time, the residual rows of the next four on their way
         const int64_t i0 = ti * kSide + wi + part * 64 + q;
-        v4u next[4];
-        auto residual = [&](int first) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) next[u] = end.residual(i0 + (first + u) * 4);
-        };
-        residual(0);
+        v4u r0 = end.residual(i0), r1 = end.residual(i0 + 4);        // two turns ahead
 #pragma unroll 1
-        for (int first = 0; first < 16; first += 4) {
-            v4u r[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) r[u] = next[u];
-            residual(first + 4);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int row = (first + u) * 4 + q;
-                const v4f f0 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l) ^ (row & 31)) * 4);
-                const v4f f1 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l + 1) ^ (row & 31)) * 4);
-                float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-                end.finish(i0 + (first + u) * 4, f, r[u]);
-            }
+        for (int turn = 0; turn < 16; ++turn) {
+            const v4u r = r0;
+            r0 = r1;
+            r1 = end.residual(i0 + 4 * turn + 8);
+            const int row = turn * 4 + q;
+            const v4f f0 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l) ^ (row & 31)) * 4);
+            const v4f f1 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l + 1) ^ (row & 31)) * 4);
+            float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+            end.finish(i0 + 4 * turn, f, r);
         }
         wave_lds_sync();
     }

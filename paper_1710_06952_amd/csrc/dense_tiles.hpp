@@ -154,8 +154,20 @@ __device__ __forceinline__ void store_up_to(uint16_t* p, int64_t n, const uint16
     for (int v = 0; v < kN; ++v)
         if (v < n) p[v] = h[v];
 }
-// The end of eight neighbouring columns from j on: what all rows share is read once.
-template <class T>
+// Eight activations at once: the choice outside, so that their steps interleave.
+template <bool kSlope>
+__device__ __forceinline__ void activate8(float* f, float* slope, int act) {
+    auto all = [&](auto which) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) f[v] = activated<kSlope, decltype(which)::value>(f[v], slope[v]);
+    };
+    if (act == ADPSGD_ACT_RELU) all(std::integral_constant<int, ADPSGD_ACT_RELU>());
+    else if (act == ADPSGD_ACT_GELU) all(std::integral_constant<int, ADPSGD_ACT_GELU>());
+    else all(std::integral_constant<int, ADPSGD_ACT_SILU>());
+}
+
+// The end of eight neighbouring columns from j on: what all rows share is read once.  kWhole: J is a multiple of 8.
+template <class T, bool kWhole>
 struct Ending {
     const DenseGemm& g;
     int64_t j;
@@ -165,13 +177,21 @@ struct Ending {
     __device__ __forceinline__ Ending(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
         n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
         uint16_t h[8];
-        if (g.bias && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.bias) + j, n, h);
+        if (g.bias && n > 0) load(static_cast<const uint16_t*>(g.bias) + j, h);
 #pragma unroll
         for (int v = 0; v < 8; ++v) bias[v] = g.bias && v < n ? T::up(h[v]) : 0.0f;
     }
+    __device__ __forceinline__ void load(const uint16_t* p, uint16_t* h) const {
+        if (kWhole) __builtin_memcpy(h, p, 16);
+        else load_up_to<8>(p, n, h);
+    }
+    __device__ __forceinline__ void store(uint16_t* p, const uint16_t* h) const {
+        if (kWhole) __builtin_memcpy(p, h, 16);
+        else store_up_to<8>(p, n, h);
+    }
     __device__ __forceinline__ v4u residual(int64_t i) const {
         uint16_t h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (g.res && i < g.I && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, n, h);
+        if (g.res && i < g.I && n > 0) load(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, h);
         v4u r;
         __builtin_memcpy(&r, h, 16);
         return r;
@@ -183,20 +203,14 @@ struct Ending {
 #pragma unroll
         for (int v = 0; v < 8; ++v) f[v] += bias[v];
         if (g.act != ADPSGD_ACT_NONE) {
+            float slope[8];
             if (g.slope) {
-#pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                    float slope;
-                    f[v] = activated<true>(f[v], g.act, slope);
-                    h[v] = slope_word(slope);
-                }
-                store_up_to<8>(g.slope + at, n, h);
+                activate8<true>(f, slope, g.act);
+                const v4u w = slope_words(slope);
+                __builtin_memcpy(h, &w, 16);
+                store(g.slope + at, h);
             } else {
-#pragma unroll
-                for (int v = 0; v < 8; ++v) {
-                    float slope;
-                    f[v] = activated<false>(f[v], g.act, slope);
-                }
+                activate8<false>(f, slope, g.act);
             }
         }
         if (g.res) {
@@ -207,7 +221,7 @@ struct Ending {
         }
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] = T::down(f[v]);
-        store_up_to<8>(static_cast<uint16_t*>(g.out) + at, n, h);
+        store(static_cast<uint16_t*>(g.out) + at, h);
     }
 };
 
@@ -309,7 +323,7 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     }
 #pragma unroll
     for (int n = 0; n < kTJ; n += 2) {
-        const Ending<T> end(g, j + 4 * n);
+        const Ending<T, false> end(g, j + 4 * n);
         v4u r[kTI];
 #pragma unroll
         for (int m = 0; m < kTI; ++m) r[m] = end.residual(i0 + m * 16);
@@ -329,7 +343,7 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, cons
     const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t i = id / eights, j = id % eights * 8;
     if (i >= g.I) return;
-    const Ending<T> end(g, j);
+    const Ending<T, false> end(g, j);
     const v4u r = end.residual(i);
     float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) {
