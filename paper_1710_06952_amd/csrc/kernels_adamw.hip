@@ -180,12 +180,10 @@ __global__ __launch_bounds__(kT) void adamw_norm_kernel(const AdamwArgs a) {
     if (threadIdx.x == 0) {
         for (int w = 1; w < kT / 64; ++w) sum += at[w];
         __hip_atomic_store(a.norm_parts + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __threadfence();
-        turn = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        turn = count_done(a.ticket);
     }
     __syncthreads();
     if (turn + 1 != gridDim.x) return;
-    __threadfence();
     sum = 0.0;
     for (uint32_t b = threadIdx.x; b < gridDim.x; b += kT) sum += __hip_atomic_load(a.norm_parts + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sum = wave_sum(sum);

@@ -14,8 +14,8 @@
 // product, v_exp_f32, sum, twice for a gradient) take about half of the time that its bytes take.
 //
 // Rows begin at any multiple of the element (odd vocabularies): vectors of 16 bytes are read and written at such addresses too.
-// Exponentials, sums and the gradient are in 32 bits, what there is one of in a row (l, ratios, loss terms, coefficients) in 64,
-// as a ratio may stand next to the border of the clipping.  A row is summed in an order that depends on the sizes alone.
+// Exponentials, sums and the gradient are in 32 bits, log-probabilities, their sums over a sequence and the loss in 64.  A row is summed in an
+// order that depends on the sizes and the alignment of the rows alone.
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -24,7 +24,7 @@
 namespace adpsgd_impl {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = 1.925963033500e-8f;
 constexpr int kT = 256;
 constexpr int kUnroll = 4;              // vectors of a thread on their way at once
 constexpr int64_t kSplitBlocks = 1024;  // blocks that fill the chip: rows are split over the vocabulary up to this many
@@ -86,30 +86,33 @@ struct F16 {
     __device__ static void put(Raw* p, float f) { *p = __builtin_bit_cast(uint16_t, static_cast<_Float16>(f)); }
 };
 
-// Elements v kN .. of a row of V; beyond the end: `fill`, as bits of 32.
+// How a row of V elements is cut: vectors of kN whose addresses are multiples of 16 bytes, and what is left in front of and behind them,
+// less than a vector each, which the first threads of a block take as one element each.  (Ends taken inside of the vectors' code
+// made kernels of 40 KB whose registers did not suffice.)
 template <class E>
-__device__ __forceinline__ v4u load_vector(const typename E::Raw* row, int64_t v, int64_t V, uint32_t fill) {
-    const int64_t at = v * E::kN;
-    if (at + E::kN <= V) return *reinterpret_cast<const v4u_any*>(row + at);
-    v4u x = {fill, fill, fill, fill};
-    typename E::Raw part[E::kN];
-    __builtin_memcpy(part, &x, 16);
-#pragma unroll
-    for (int i = 0; i < E::kN; ++i)
-        if (at + i < V) part[i] = row[at + i];
-    __builtin_memcpy(&x, part, 16);
-    return x;
+struct Cut {
+    int head, vectors, tail;
+    __device__ __forceinline__ Cut(const void* row, int V) {
+        const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(typename E::Raw));
+        head = off == 0 ? 0 : E::kN - off;
+        head = head < V ? head : V;
+        vectors = (V - head) / E::kN;
+        tail = V - head - vectors * E::kN;
+    }
+    __device__ __forceinline__ int at(int v) const { return head + v * E::kN; }
+    // The element that a thread takes beside its vectors, or -1.
+    __device__ __forceinline__ int single() const {
+        const int t = threadIdx.x;
+        return t < E::kN ? (t < head ? t : -1) : t < 2 * E::kN && t - E::kN < tail ? at(vectors) + t - E::kN : -1;
+    }
+};
+template <class E>
+__device__ __forceinline__ v4u load_vector(const typename E::Raw* row, int at) {
+    return *reinterpret_cast<const v4u_any*>(row + at);
 }
 template <class E>
-__device__ __forceinline__ void store_vector(typename E::Raw* row, int64_t v, int64_t V, const float* f) {
-    const int64_t at = v * E::kN;
-    if (at + E::kN <= V) {
-        *reinterpret_cast<v4u_any*>(row + at) = E::pack(f);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < E::kN; ++i)
-        if (at + i < V) E::put(row + at + i, f[i]);
+__device__ __forceinline__ void store_vector(typename E::Raw* row, int at, const float* f) {
+    *reinterpret_cast<v4u_any*>(row + at) = E::pack(f);
 }
 template <class E>
 constexpr uint32_t kNothing = E::kN == 4 ? 0xFF800000u : 0u;       // two halves of -infinity ...
@@ -119,34 +122,40 @@ template <>
 constexpr uint32_t kNothing<F16> = 0xFC00FC00u;
 
 struct Stat {
-    float m, s;
+    float m, s;                 // the largest value, and the sum of exp(z - m)
 };
+// exp(d).  (2^(z log2 e - m') by an FMA is an instruction less, but a rounded m' stands for no m: at 1e9 its rounding is e^20.)
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// ... kFine: log2 e in two parts.  Its rounding to 32 bits is 1.3e-8 of d in every term of a sum, in the same direction, and sums of
+// log-probabilities over a sequence add that up.
+template <bool kFine>
+__device__ __forceinline__ float exp_in_sum(float d) { return __builtin_amdgcn_exp2f(kFine ? fmaf(d, kLog2eRest, d * kLog2e) : d * kLog2e); }
 // What the sum over values up to m is taken relative to: m, or 0 where there is nothing but -infinity.
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 __device__ __forceinline__ Stat joined(Stat a, Stat b) {
     const float m = fmaxf(a.m, b.m), base = base_of(m);
     return Stat{m, a.s * exp_of(a.m - base) + b.s * exp_of(b.m - base)};
 }
-__device__ __forceinline__ Stat wave_joined(Stat a) {
+__device__ __forceinline__ Stat of_one(float z) { return Stat{z, exp_of(z - base_of(z))}; }
+// Of each group of kLanes neighbouring lanes, to all of them.
+template <int kLanes>
+__device__ __forceinline__ Stat lanes_joined(Stat a) {
     float m = a.m;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    return Stat{m, wave_sum(a.s * exp_of(a.m - base_of(m)))};
+    for (int off = kLanes / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    float s = a.s * exp_of(a.m - base_of(m));
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+    return Stat{m, s};
 }
 // Of a block of kWaves wavefronts, to all threads; `at`: kWaves places in LDS.
 template <int kWaves>
 __device__ __forceinline__ Stat block_joined(Stat a, Stat* at) {
-    a = wave_joined(a);
+    a = lanes_joined<64>(a);
     if (kWaves == 1) return a;
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = a;
     __syncthreads();
-    float m = -INFINITY, s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, at[w].m);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s += at[w].s * exp_of(at[w].m - base_of(m));
-    return Stat{m, s};
+    return lanes_joined<kWaves>(at[threadIdx.x % kWaves]);
 }
 
 enum Mode { kScore, kPolicy, kPreference };
@@ -167,21 +176,41 @@ struct RowArgs {
     int splits;
 };
 
-__device__ __forceinline__ double log_prob(float at, Stat st) { return static_cast<double>(at - st.m) - log(static_cast<double>(st.s)); }
-
+// What there is one of in a row.  Its s is off by 1e-7, so logarithm and exponentials in 32 bits lose nothing as long as no large
+// number is rounded on the way: log s is taken apart into its exponent, in 64 bits, and the logarithm of a fraction.  (Those of 64 bits
+// take 40 registers, which the kernel that holds a row in registers does not have.)
+__device__ __forceinline__ double log_prob(float at, Stat st) {
+    int k;
+    const float f = frexpf(st.s, &k);                    // 1/2 <= f < 1
+    return static_cast<double>(at - st.m) - (static_cast<double>(k) * 0.6931471805599453 + static_cast<double>(logf(f)));
+}
+__device__ __forceinline__ float exp_near(float x) {     // the rounding of x log2 e made good
+    const float t = x * kLog2e, rest = fmaf(x, kLog2e, -t) + x * kLog2eRest, e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 126.0f ? fmaf(e, rest * 0.6931471805599453f, e) : e;
+}
+// exp(d) - 1 - d
+__device__ __forceinline__ float exp_less_line(float d) {
+    if (fabsf(d) > 0.25f) return exp_near(d) - 1.0f - d;
+    float p = fmaf(d, 1.0f / 40320.0f, 1.0f / 5040.0f);
+    p = fmaf(d, p, 1.0f / 720.0f);
+    p = fmaf(d, p, 1.0f / 120.0f);
+    p = fmaf(d, p, 1.0f / 24.0f);
+    p = fmaf(d, p, 1.0f / 6.0f);
+    p = fmaf(d, p, 0.5f);
+    return d * d * p;
+}
 // dL/dl and the loss term of one row, both times the number of counted rows.
-__device__ __forceinline__ void policy_row(const PolicyTerms& t, int64_t row, double l, double& slope, double& term) {
-    const double A = t.adv[row], rho = exp(l - static_cast<double>(t.old[row]));
-    const double free = rho * A;
+__device__ __forceinline__ void policy_row(const PolicyTerms& t, int64_t row, double l, float& slope, float& term) {
+    const float A = t.adv[row], rho = exp_near(static_cast<float>(l - static_cast<double>(t.old[row])));
+    const float free = rho * A;
     // fmin and fmax pass over a NaN: the ratio is kept as it is unless it is outside
-    const double inside = rho < 1.0 - t.clip_low ? 1.0 - t.clip_low : rho > 1.0 + t.clip_high ? 1.0 + t.clip_high : rho;
-    const double held = inside * A;
+    const float lo = 1.0f - t.clip_low, hi = 1.0f + t.clip_high, held = (rho < lo ? lo : rho > hi ? hi : rho) * A;
     term = held < free ? -held : -free;
-    slope = held < free ? 0.0 : -free;
+    slope = held < free ? 0.0f : -free;
     if (t.ref) {
-        const double d = static_cast<double>(t.ref[row]) - l, e = exp(d);
-        term += t.kl * (e - d - 1.0);
-        slope += t.kl * (1.0 - e);
+        const float d = static_cast<float>(static_cast<double>(t.ref[row]) - l), q = exp_less_line(d);
+        term = fmaf(t.kl, q, term);
+        slope = fmaf(-t.kl, q + d, slope);
     }
 }
 
@@ -203,44 +232,44 @@ __device__ __forceinline__ void finish_row(const RowArgs& a, int64_t row, Stat s
         a.coef[row] = 0.0f;
         return;
     }
-    double slope = 0.0, term = 0.0;
+    float slope = 0.0f, term = 0.0f;
     if (token >= 0) policy_row(a.policy, row, l, slope, term);
     a.logp[row] = static_cast<float>(l);
     a.term[row] = term;
-    a.coef[row] = static_cast<float>(slope * *a.share);
+    a.coef[row] = slope * *a.share;
 }
 
 // (m, s) of the vectors v0 <= v < v1 of a row that this thread takes
-template <class E>
-__device__ __forceinline__ Stat thread_stat(const typename E::Raw* row, int64_t v0, int64_t v1, int64_t V) {
+template <class E, bool kFine>
+__device__ __forceinline__ Stat thread_stat(const typename E::Raw* row, const Cut<E>& cut, int v0, int v1) {
     Stat st{-INFINITY, 0.0f};
-    for (int64_t v = v0 + threadIdx.x; v < v1; v += kT * kUnroll) {
+    for (int v = v0 + static_cast<int>(threadIdx.x); v < v1; v += kT * kUnroll) {
         v4u x[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             x[u] = v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
-            if (v + u * kT < v1) x[u] = load_vector<E>(row, v + u * kT, V, kNothing<E>);
+            if (v + u * kT < v1) x[u] = load_vector<E>(row, cut.at(v + u * kT));
         }
-        float f[kUnroll][E::kN], m = st.m;
+        float f[kUnroll][E::kN], top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             E::unpack(x[u], f[u]);
 #pragma unroll
-            for (int i = 0; i < E::kN; ++i) m = fmaxf(m, f[u][i]);
+            for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[u][i]);
         }
-        const float base = base_of(m);
+        const float m = fmaxf(st.m, top), base = base_of(m);
         float s = st.s * exp_of(st.m - base);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int i = 0; i < E::kN; ++i) s += exp_of(f[u][i] - base);
+            for (int i = 0; i < E::kN; ++i) s += exp_in_sum<kFine>(f[u][i] - base);
         st = Stat{m, s};
     }
     return st;
 }
 
 // grid: rows * splits.
-template <class E>
+template <class E, bool kFine>
 __global__ __launch_bounds__(kT) void row_stats_kernel(const RowArgs a) {
     __shared__ Stat at[kT / 64];
     const int64_t row = blockIdx.x / a.splits;
@@ -249,9 +278,12 @@ __global__ __launch_bounds__(kT) void row_stats_kernel(const RowArgs a) {
         if (a.splits == 1 && threadIdx.x == 0) finish_row<E>(a, row, Stat{0.0f, 1.0f});
         return;
     }
-    const int64_t vectors = (a.vocab + E::kN - 1) / E::kN, each = (vectors + a.splits - 1) / a.splits;
-    const int64_t v0 = part * each, v1 = v0 + each < vectors ? v0 + each : vectors;
-    const Stat st = block_joined<kT / 64>(thread_stat<E>(static_cast<const typename E::Raw*>(a.z) + row * a.ld, v0, v1, a.vocab), at);
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    const Cut<E> cut(z, static_cast<int>(a.vocab));
+    const int each = (cut.vectors + a.splits - 1) / a.splits, v0 = part * each, v1 = v0 + each < cut.vectors ? v0 + each : cut.vectors;
+    Stat st = thread_stat<E, kFine>(z, cut, v0, v1);
+    if (part == 0 && cut.single() >= 0) st = joined(st, of_one(E::get(z + cut.single())));
+    st = block_joined<kT / 64>(st, at);
     if (threadIdx.x == 0) {
         if (a.splits == 1) finish_row<E>(a, row, st);
         else a.parts[row * a.splits + part] = st;
@@ -266,17 +298,18 @@ __global__ __launch_bounds__(kT) void join_stats_kernel(const RowArgs a) {
     Stat st{-INFINITY, 0.0f};
     if (a.tokens[row] >= 0)
         for (int q = threadIdx.x & 63; q < a.splits; q += 64) st = joined(st, a.parts[row * a.splits + q]);
-    st = wave_joined(st);
+    st = lanes_joined<64>(st);
     if ((threadIdx.x & 63) == 0) finish_row<E>(a, row, st);
 }
 
-// d[i] = exp(z[i] - m) scale, and coef more at the token.
+__device__ __forceinline__ float gradient_at(float z, bool hot, float m, float scale, float coef) { return exp_of(z - m) * scale + (hot ? coef : 0.0f); }
+// d[i] = exp(z[i] - m) scale, and coef more at the token; the vector begins at `at`.
 template <class E>
-__device__ __forceinline__ void gradient_of(v4u x, int64_t v, int64_t token, float m, float scale, float coef, float* d) {
+__device__ __forceinline__ void gradient_of(v4u x, int at, int token, float m, float scale, float coef, float* d) {
     E::unpack(x, d);
 #pragma unroll
     for (int i = 0; i < E::kN; ++i) d[i] = exp_of(d[i] - m) * scale;
-    const int64_t here = token - v * E::kN;
+    const int here = token - at;
     if (here >= 0 && here < E::kN) {
 #pragma unroll
         for (int i = 0; i < E::kN; ++i) d[i] += here == i ? coef : 0.0f;
@@ -294,29 +327,33 @@ struct GradientArgs {
 };
 
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }      // NaN: below
+// The loss of the margins, by one wavefront.
+__device__ __forceinline__ void preference_loss(const float* margins, int64_t pairs, double smoothing, float* loss) {
+    double sum = 0.0;
+    for (int64_t q = threadIdx.x; q < pairs; q += 64) {
+        const double x = margins[q];
+        sum += x == x ? (1.0 - smoothing) * softplus(-x) + smoothing * softplus(x) : x;
+    }
+    sum = wave_sum(sum);
+    if (threadIdx.x == 0) *loss = static_cast<float>(sum / static_cast<double>(pairs));
+}
 
 // grid: rows * blocks.  The last rows first: they are the ones that the pass before has left in the last-level cache.
 template <class E>
 __global__ __launch_bounds__(kT) void logit_gradient_kernel(const GradientArgs g) {
     const RowArgs& a = g.row;
-    if (g.margins && blockIdx.x == 0 && threadIdx.x < 64) {
-        double sum = 0.0;
-        for (int64_t q = threadIdx.x; q < g.pairs; q += 64) {
-            const double x = g.margins[q];
-            sum += x == x ? (1.0 - g.smoothing) * softplus(-x) + g.smoothing * softplus(x) : x;
-        }
-        sum = wave_sum(sum);
-        if (threadIdx.x == 0) *g.loss = static_cast<float>(sum / static_cast<double>(g.pairs));
-    }
+    if (g.margins && blockIdx.x == 0 && threadIdx.x < 64) preference_loss(g.margins, g.pairs, g.smoothing, g.loss);
     const int64_t row = a.rows - 1 - blockIdx.x / g.blocks;
-    const int64_t vectors = (a.vocab + E::kN - 1) / E::kN;
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
     typename E::Raw* dz = static_cast<typename E::Raw*>(g.dz) + row * a.vocab;
+    const Cut<E> cut(dz, static_cast<int>(a.vocab));     // stores aligned; loads too where rows of both lie alike
     const int64_t token = a.tokens[row];
     const float coef = token < 0 ? 0.0f : a.coef[row];
     const Stat st = token < 0 ? Stat{0.0f, 1.0f} : a.stat[row];
     const float scale = -coef / st.s;
-    const int64_t v0 = (blockIdx.x % g.blocks) * (kT * kUnroll) + threadIdx.x;
+    const int v0 = static_cast<int>(blockIdx.x % g.blocks) * (kT * kUnroll) + static_cast<int>(threadIdx.x);
+    const int hot = token < a.vocab ? static_cast<int>(token) : -1, single = blockIdx.x % g.blocks == 0 ? cut.single() : -1;
+    if (single >= 0) E::put(dz + single, coef == 0.0f ? 0.0f : gradient_at(E::get(z + single), single == hot, st.m, scale, coef));
     v4u x[kUnroll];
     float d[E::kN];
     if (coef == 0.0f) {                 // nothing to read
@@ -324,17 +361,18 @@ __global__ __launch_bounds__(kT) void logit_gradient_kernel(const GradientArgs g
         for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
-            if (v0 + u * kT < vectors) store_vector<E>(dz, v0 + u * kT, a.vocab, d);
+            if (v0 + u * kT < cut.vectors) store_vector<E>(dz, cut.at(v0 + u * kT), d);
         return;
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-        if (v0 + u * kT < vectors) x[u] = load_vector<E>(z, v0 + u * kT, a.vocab, 0);
+        if (v0 + u * kT < cut.vectors) x[u] = load_vector<E>(z, cut.at(v0 + u * kT));
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-        if (v0 + u * kT < vectors) {
-            gradient_of<E>(x[u], v0 + u * kT, token, st.m, scale, coef, d);
-            store_vector<E>(dz, v0 + u * kT, a.vocab, d);
+        if (v0 + u * kT < cut.vectors) {
+            const int at = cut.at(v0 + u * kT);
+            gradient_of<E>(x[u], at, hot, st.m, scale, coef, d);
+            store_vector<E>(dz, at, d);
         }
 }
 
@@ -373,85 +411,90 @@ __global__ __launch_bounds__(kT) void mean_terms_kernel(const double* term, int6
     sum_terms<kT>(term, rows, share, loss, at);
 }
 
-// kWaves wavefronts a row, up to kHeld vectors a thread in registers; the last block to end adds the loss.
-template <class E, int kWaves, int kHeld>
-__global__ __launch_bounds__(kWaves * 64) void policy_rows_kernel(const GradientArgs g, uint32_t* ticket) {
+// kWaves wavefronts a row, up to kHeld vectors a thread in registers; the last block to end adds the loss.  kPerSimd wavefronts a SIMD:
+// with two blocks on a compute unit one loads or stores while the other computes, which its registers have to leave room for.
+template <class E, int kWaves, int kHeld, int kPerSimd>
+__global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(const GradientArgs g, uint32_t* ticket) {
     constexpr int kThreads = kWaves * 64;
     __shared__ Stat at[kWaves];
     __shared__ double sums[kWaves];
-    __shared__ float of_row[2];
+    __shared__ float of_row;
     __shared__ uint32_t turn;
     const RowArgs& a = g.row;
-    const int64_t row = blockIdx.x, vectors = (a.vocab + E::kN - 1) / E::kN;
+    const int64_t row = blockIdx.x;
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
     typename E::Raw* dz = static_cast<typename E::Raw*>(g.dz) + row * a.vocab;
+    const Cut<E> cut(dz, static_cast<int>(a.vocab));
     const int64_t token = a.tokens[row];
-    float coef = 0.0f, m = 0.0f, scale = 0.0f;
+    const int single = cut.single();
+    float coef = 0.0f, m = 0.0f, scale = 0.0f, alone = -INFINITY;
     v4u x[kHeld];
     if (token >= 0) {                   // uniform over the block
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
-            const int64_t v = u * kThreads + threadIdx.x;
+            const int v = u * kThreads + static_cast<int>(threadIdx.x);
             x[u] = v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
-            if (v < vectors) x[u] = load_vector<E>(z, v, a.vocab, kNothing<E>);
+            if (v < cut.vectors) x[u] = load_vector<E>(z, cut.at(v));
         }
-        float f[E::kN];
+        if (single >= 0) alone = E::get(z + single);
         Stat st{-INFINITY, 0.0f};
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
+            float f[E::kN], top = -INFINITY;
+            asm volatile("" : "+v"(x[u]));               // held packed, however it was come by
             E::unpack(x[u], f);
 #pragma unroll
-            for (int i = 0; i < E::kN; ++i) st.m = fmaxf(st.m, f[i]);
-        }
-        const float base = base_of(st.m);
+            for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[i]);
+            const float m = fmaxf(st.m, top), base = base_of(m);
+            st.s *= exp_of(st.m - base);
 #pragma unroll
-        for (int u = 0; u < kHeld; ++u) {
-            E::unpack(x[u], f);
-#pragma unroll
-            for (int i = 0; i < E::kN; ++i) st.s += exp_of(f[i] - base);
+            for (int i = 0; i < E::kN; ++i) st.s += exp_in_sum<false>(f[i] - base);
+            st.m = m;
+            __builtin_amdgcn_sched_barrier(0);           // one vector after the other: unpacked, they would not all fit
         }
+        if (single >= 0) st = joined(st, of_one(alone));
         st = block_joined<kWaves>(st, at);
-        if (threadIdx.x < 64) {         // 64-bit logarithm and exponentials: one wavefront's time, not the block's
+        if (threadIdx.x < 64) {
             const float value = token < a.vocab ? E::get(z + token) : NAN;
             const double l = log_prob(value, st);
-            double slope, term;
+            float slope, term;
             policy_row(a.policy, row, l, slope, term);
             if (threadIdx.x == 0) {
                 a.logp[row] = static_cast<float>(l);
-                __hip_atomic_store(a.term + row, term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                of_row[0] = static_cast<float>(slope * *a.share);
+                __hip_atomic_store(a.term + row, static_cast<double>(term), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                of_row = slope * *a.share;
             }
         }
         __syncthreads();
-        coef = of_row[0];
+        coef = of_row;
         m = st.m;
         scale = -coef / st.s;
     } else if (threadIdx.x == 0) {
         a.logp[row] = 0.0f;
         __hip_atomic_store(a.term + row, 0.0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    const int hot = token < a.vocab ? static_cast<int>(token) : -1;
     const bool zero = coef == 0.0f;     // NaN is not
+    if (single >= 0) E::put(dz + single, zero ? 0.0f : gradient_at(alone, single == hot, m, scale, coef));
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
-        const int64_t v = u * kThreads + threadIdx.x;
-        if (v < vectors) {
+        const int v = u * kThreads + static_cast<int>(threadIdx.x);
+        if (v < cut.vectors) {
             float d[E::kN];
             if (zero) {
 #pragma unroll
                 for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
             } else {
-                gradient_of<E>(x[u], v, token, m, scale, coef, d);
+                asm volatile("" : "+v"(x[u]));           // unpacked anew, not kept unpacked since the sum
+                gradient_of<E>(x[u], cut.at(v), hot, m, scale, coef, d);
             }
-            store_vector<E>(dz, v, a.vocab, d);
+            store_vector<E>(dz, cut.at(v), d);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
-    if (threadIdx.x == 0) {             // its term is in memory before it counts as done
-        __threadfence();
-        turn = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    if (threadIdx.x == 0) turn = count_done(ticket);     // after its term, which the same thread has stored
     __syncthreads();
     if (turn + 1 == gridDim.x) {
-        __threadfence();
         sum_terms<kThreads>(a.term, a.rows, a.share, g.loss, sums);
     }
 }
@@ -551,32 +594,33 @@ RowArgs row_args(const LossRows& a, Mode mode, const Workspace& w) {
 
 template <class E>
 void launch_stats(RowArgs r, hipStream_t s) {
-    r.splits = split_of(r.rows, (r.vocab + E::kN - 1) / E::kN);
-    hipLaunchKernelGGL(row_stats_kernel<E>, dim3(static_cast<uint32_t>(r.rows * r.splits)), dim3(kT), 0, s, r);
+    r.splits = split_of(r.rows, r.vocab / E::kN);
+    const dim3 grid(static_cast<uint32_t>(r.rows * r.splits));
+    if (r.mode == kPreference) hipLaunchKernelGGL((row_stats_kernel<E, true>), grid, dim3(kT), 0, s, r);
+    else hipLaunchKernelGGL((row_stats_kernel<E, false>), grid, dim3(kT), 0, s, r);
     if (r.splits > 1) hipLaunchKernelGGL(join_stats_kernel<E>, dim3(static_cast<uint32_t>((r.rows + kT / 64 - 1) / (kT / 64))), dim3(kT), 0, s, r);
 }
 template <class E>
 void launch_gradient(GradientArgs g, hipStream_t s) {
-    const int64_t vectors = (g.row.vocab + E::kN - 1) / E::kN;
-    g.blocks = (vectors + kT * kUnroll - 1) / (kT * kUnroll);
+    const int64_t vectors = g.row.vocab / E::kN;
+    g.blocks = std::max<int64_t>(1, (vectors + kT * kUnroll - 1) / (kT * kUnroll));
     hipLaunchKernelGGL(logit_gradient_kernel<E>, dim3(static_cast<uint32_t>(g.row.rows * g.blocks)), dim3(kT), 0, s, g);
 }
 
 template <class E>
 void launch_policy_of(GradientArgs g, uint32_t* ticket, hipStream_t s) {
-    const int64_t rows = g.row.rows, vectors = (g.row.vocab + E::kN - 1) / E::kN;
+    const int64_t rows = g.row.rows, vectors = g.row.vocab / E::kN;
     const dim3 grid(static_cast<uint32_t>(rows));
     hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, g.row.tokens, rows, const_cast<float*>(g.row.share), ticket);
-    if (vectors <= 256) hipLaunchKernelGGL((policy_rows_kernel<E, 1, 4>), grid, dim3(64), 0, s, g, ticket);
-    else if (vectors <= 1024) hipLaunchKernelGGL((policy_rows_kernel<E, 4, 4>), grid, dim3(256), 0, s, g, ticket);
-    else if (vectors <= 4096) hipLaunchKernelGGL((policy_rows_kernel<E, 8, 8>), grid, dim3(512), 0, s, g, ticket);
-    else if (vectors <= 8192) hipLaunchKernelGGL((policy_rows_kernel<E, 16, 8>), grid, dim3(1024), 0, s, g, ticket);
-    else if (vectors <= 16384) hipLaunchKernelGGL((policy_rows_kernel<E, 16, 16>), grid, dim3(1024), 0, s, g, ticket);
-    else {                               // more than a block's registers hold
+    if (vectors > 16384) {               // more than a block's registers hold
         launch_stats<E>(g.row, s);
         hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(kT), 0, s, g.row.term, rows, g.row.share, g.loss);
         launch_gradient<E>(g, s);
-    }
+    } else if (vectors <= 256) hipLaunchKernelGGL((policy_rows_kernel<E, 1, 4, 4>), grid, dim3(64), 0, s, g, ticket);
+    else if (vectors <= 1024) hipLaunchKernelGGL((policy_rows_kernel<E, 4, 4, 8>), grid, dim3(256), 0, s, g, ticket);
+    else if (vectors <= 4096) hipLaunchKernelGGL((policy_rows_kernel<E, 8, 8, 8>), grid, dim3(512), 0, s, g, ticket);
+    else if (vectors <= 8192) hipLaunchKernelGGL((policy_rows_kernel<E, 16, 8, 8>), grid, dim3(1024), 0, s, g, ticket);
+    else hipLaunchKernelGGL((policy_rows_kernel<E, 16, 16, 4>), grid, dim3(1024), 0, s, g, ticket);
 }
 template <class E>
 void launch_preference_of(const GradientArgs& g, const int64_t* offsets, const float* ref, double beta, float* sums, float* margins, hipStream_t s) {
@@ -587,13 +631,7 @@ void launch_preference_of(const GradientArgs& g, const int64_t* offsets, const f
 }
 
 __global__ __launch_bounds__(64) void preference_loss_kernel(const float* margins, int64_t pairs, double smoothing, float* loss) {
-    double sum = 0.0;
-    for (int64_t q = threadIdx.x; q < pairs; q += 64) {
-        const double x = margins[q];
-        sum += x == x ? (1.0 - smoothing) * softplus(-x) + smoothing * softplus(x) : x;
-    }
-    sum = wave_sum(sum);
-    if (threadIdx.x == 0) *loss = static_cast<float>(sum / static_cast<double>(pairs));
+    preference_loss(margins, pairs, smoothing, loss);
 }
 
 }  // namespace

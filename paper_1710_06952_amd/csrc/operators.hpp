@@ -38,7 +38,7 @@ int64_t loss_workspace_bytes(int64_t rows, int64_t vocab);
 hipError_t launch_log_probs(const LossRows& a, float* logp, void* ws, hipStream_t s);
 struct PolicyTerms {
     const float *old, *adv, *ref;
-    double clip_low, clip_high, kl;
+    float clip_low, clip_high, kl;
 };
 hipError_t launch_policy(const LossRows& a, const PolicyTerms& t, float* loss, void* dz, float* logp, void* ws, hipStream_t s);
 hipError_t launch_preference(const LossRows& a, const int64_t* offsets, int64_t pairs, const float* ref, double beta, double smoothing, float* loss,

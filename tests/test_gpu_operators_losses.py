@@ -224,6 +224,18 @@ def test_rows_that_cannot_be_answered():
     z = torch.full((2, 1024), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16, device="cuda:0")
     got = P.token_log_probs(z, torch.tensor([0, 1023], device="cuda:0"))
     assert torch.allclose(got, torch.full_like(got, -math.log(1024)), rtol=1e-6)
+    # ... of a row of each length of the kernels, and its gradient; the type's largest value
+    for V in (3, 40, 5000, 20_000, 40_000, 100_000, 140_000):
+        for dtype, lowest in ((torch.float32, torch.finfo(torch.float32).min), (torch.bfloat16, torch.finfo(torch.bfloat16).min), (torch.float32, -1e9)):
+            z = torch.full((2, V), lowest, dtype=dtype, device="cuda:0")
+            z[1, 2] = torch.finfo(dtype).max
+            tokens = torch.tensor([1, 2], device="cuda:0")
+            r = P.policy_loss_and_gradient(z, tokens, torch.tensor([-math.log(V), 0.0], device="cuda:0"), torch.ones(2, device="cuda:0"))
+            assert torch.allclose(r.log_probs, torch.tensor([-math.log(V), 0.0], device="cuda:0"), rtol=2e-6) and abs(float(r.loss) + 1) < 1e-5
+            want = torch.full((2, V), 0.5 / V, device="cuda:0")
+            want[0, 1] -= 0.5
+            want[1] = 0
+            assert torch.allclose(r.dlogits.float(), want, rtol=0.005, atol=1e-7), (V, dtype)
 
 
 def test_nothing_counted_and_no_rows():
