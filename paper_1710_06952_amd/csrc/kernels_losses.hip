@@ -26,6 +26,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = 1.925963033500e-8f;
 constexpr int kT = 256;
+constexpr int64_t kCountHere = 1024;    // rows that a block of the policy kernel counts itself: a launch less where launches are the time
 constexpr int kUnroll = 4;              // vectors of a thread on their way at once
 constexpr int64_t kSplitBlocks = 1024;  // blocks that fill the chip: rows are split over the vocabulary up to this many
 
@@ -100,19 +101,24 @@ struct Cut {
         tail = V - head - vectors * E::kN;
     }
     __device__ __forceinline__ int at(int v) const { return head + v * E::kN; }
+    // The vector that covers element e, or -1.
+    __device__ __forceinline__ int vector_of(int e) const { return e >= head && e < at(vectors) ? (e - head) / E::kN : -1; }
     // The element that a thread takes beside its vectors, or -1.
     __device__ __forceinline__ int single() const {
         const int t = threadIdx.x;
         return t < E::kN ? (t < head ? t : -1) : t < 2 * E::kN && t - E::kN < tail ? at(vectors) + t - E::kN : -1;
     }
 };
-template <class E>
+// Past the caches unless a later pass of the same call reads them again; gradients always.  8000 x 32 000 in fp16: 74 us for 84;
+// preference loss of 8 pairs over 50 001 tokens: 163 us for 198, and 183 where the first pass reads past the caches as well.
+template <class E, bool kAgain>
 __device__ __forceinline__ v4u load_vector(const typename E::Raw* row, int at) {
-    return *reinterpret_cast<const v4u_any*>(row + at);
+    const v4u_any* p = reinterpret_cast<const v4u_any*>(row + at);
+    return kAgain ? *p : __builtin_nontemporal_load(p);
 }
 template <class E>
 __device__ __forceinline__ void store_vector(typename E::Raw* row, int at, const float* f) {
-    *reinterpret_cast<v4u_any*>(row + at) = E::pack(f);
+    __builtin_nontemporal_store(E::pack(f), reinterpret_cast<v4u_any*>(row + at));
 }
 template <class E>
 constexpr uint32_t kNothing = E::kN == 4 ? 0xFF800000u : 0u;       // two halves of -infinity ...
@@ -200,15 +206,19 @@ __device__ __forceinline__ float exp_less_line(float d) {
     return d * d * p;
 }
 // dL/dl and the loss term of one row, both times the number of counted rows.
-__device__ __forceinline__ void policy_row(const PolicyTerms& t, int64_t row, double l, float& slope, float& term) {
-    const float A = t.adv[row], rho = exp_near(static_cast<float>(l - static_cast<double>(t.old[row])));
+struct RowNumbers {
+    float old, adv, ref;
+    __device__ __forceinline__ RowNumbers(const PolicyTerms& t, int64_t row) : old(t.old[row]), adv(t.adv[row]), ref(t.ref ? t.ref[row] : 0.0f) {}
+};
+__device__ __forceinline__ void policy_row(const PolicyTerms& t, const RowNumbers& n, double l, float& slope, float& term) {
+    const float A = n.adv, rho = exp_near(static_cast<float>(l - static_cast<double>(n.old)));
     const float free = rho * A;
     // fmin and fmax pass over a NaN: the ratio is kept as it is unless it is outside
     const float lo = 1.0f - t.clip_low, hi = 1.0f + t.clip_high, held = (rho < lo ? lo : rho > hi ? hi : rho) * A;
     term = held < free ? -held : -free;
     slope = held < free ? 0.0f : -free;
     if (t.ref) {
-        const float d = static_cast<float>(static_cast<double>(t.ref[row]) - l), q = exp_less_line(d);
+        const float d = static_cast<float>(static_cast<double>(n.ref) - l), q = exp_less_line(d);
         term = fmaf(t.kl, q, term);
         slope = fmaf(-t.kl, q + d, slope);
     }
@@ -233,7 +243,7 @@ __device__ __forceinline__ void finish_row(const RowArgs& a, int64_t row, Stat s
         return;
     }
     float slope = 0.0f, term = 0.0f;
-    if (token >= 0) policy_row(a.policy, row, l, slope, term);
+    if (token >= 0) policy_row(a.policy, RowNumbers(a.policy, row), l, slope, term);
     a.logp[row] = static_cast<float>(l);
     a.term[row] = term;
     a.coef[row] = slope * *a.share;
@@ -248,7 +258,7 @@ __device__ __forceinline__ Stat thread_stat(const typename E::Raw* row, const Cu
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             x[u] = v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
-            if (v + u * kT < v1) x[u] = load_vector<E>(row, cut.at(v + u * kT));
+            if (v + u * kT < v1) x[u] = load_vector<E, kFine>(row, cut.at(v + u * kT));
         }
         float f[kUnroll][E::kN], top = -INFINITY;
 #pragma unroll
@@ -303,17 +313,12 @@ __global__ __launch_bounds__(kT) void join_stats_kernel(const RowArgs a) {
 }
 
 __device__ __forceinline__ float gradient_at(float z, bool hot, float m, float scale, float coef) { return exp_of(z - m) * scale + (hot ? coef : 0.0f); }
-// d[i] = exp(z[i] - m) scale, and coef more at the token; the vector begins at `at`.
+// d[i] = exp(z[i] - m) scale
 template <class E>
-__device__ __forceinline__ void gradient_of(v4u x, int at, int token, float m, float scale, float coef, float* d) {
+__device__ __forceinline__ void gradient_of(v4u x, float m, float scale, float* d) {
     E::unpack(x, d);
 #pragma unroll
     for (int i = 0; i < E::kN; ++i) d[i] = exp_of(d[i] - m) * scale;
-    const int here = token - at;
-    if (here >= 0 && here < E::kN) {
-#pragma unroll
-        for (int i = 0; i < E::kN; ++i) d[i] += here == i ? coef : 0.0f;
-    }
 }
 
 struct GradientArgs {
@@ -366,60 +371,63 @@ __global__ __launch_bounds__(kT) void logit_gradient_kernel(const GradientArgs g
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-        if (v0 + u * kT < cut.vectors) x[u] = load_vector<E>(z, cut.at(v0 + u * kT));
+        if (v0 + u * kT < cut.vectors) x[u] = load_vector<E, false>(z, cut.at(v0 + u * kT));
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
         if (v0 + u * kT < cut.vectors) {
-            const int at = cut.at(v0 + u * kT);
-            gradient_of<E>(x[u], at, hot, st.m, scale, coef, d);
-            store_vector<E>(dz, at, d);
+            gradient_of<E>(x[u], st.m, scale, d);
+            store_vector<E>(dz, cut.at(v0 + u * kT), d);
         }
+    // the token's element once more, by the thread that has stored it without coef
+    const int back = cut.vector_of(hot) - v0;
+    if (cut.vector_of(hot) >= 0 && back >= 0 && back < kT * kUnroll && back % kT == 0) E::put(dz + hot, gradient_at(E::get(z + hot), true, st.m, scale, coef));
 }
 
 // ---- policy ----------------------------------------------------------------------------------------------
-// 1 / max(1, counted rows), and the ticket of the last block at zero.
-__global__ __launch_bounds__(1024) void count_rows_kernel(const int64_t* tokens, int64_t rows, float* share, uint32_t* ticket) {
-    __shared__ double at[16];
-    double n = 0.0;
-    for (int64_t i = threadIdx.x; i < rows; i += 1024) n += tokens[i] >= 0 ? 1.0 : 0.0;
+// Rows that count, to all threads of a block of kWaves wavefronts.
+template <int kWaves>
+__device__ __forceinline__ float counted_rows(const int64_t* tokens, int64_t rows, float* at) {
+    float n = 0.0f;                                      // up to 2^21: exact
+    for (int64_t i = threadIdx.x; i < rows; i += kWaves * 64) n += tokens[i] >= 0 ? 1.0f : 0.0f;
     n = wave_sum(n);
+    if (kWaves == 1) return n;
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = n;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w) n += at[w];
-        *share = static_cast<float>(1.0 / fmax(n, 1.0));
-        share[1] = static_cast<float>(fmax(n, 1.0));
-        *ticket = 0;
-    }
+    n = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) n += at[w];
+    return n;
 }
-
-// The mean of the loss terms, by one block, in an order that the number of rows gives.
-template <int kThreads>
-__device__ __forceinline__ void sum_terms(const double* term, int64_t rows, const float* share, float* loss, double* at) {
+// 1 / max(1, counted rows).
+__global__ __launch_bounds__(1024) void count_rows_kernel(const int64_t* tokens, int64_t rows, float* share) {
+    __shared__ float at[16];
+    const float n = counted_rows<16>(tokens, rows, at);
+    if (threadIdx.x == 0) *share = 1.0f / fmaxf(n, 1.0f);
+}
+// The mean of the loss terms, in an order that the number of rows gives.
+__global__ __launch_bounds__(1024) void mean_terms_kernel(const double* term, const int64_t* tokens, int64_t rows, float* loss) {
+    __shared__ float counts[16];
+    __shared__ double at[16];
+    const float n = counted_rows<16>(tokens, rows, counts);
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < rows; i += kThreads) sum += __hip_atomic_load(term + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int64_t i = threadIdx.x; i < rows; i += 1024) sum += term[i];
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 64; ++w) sum += at[w];
-        *loss = static_cast<float>(sum / static_cast<double>(share[1]));
+        for (int w = 1; w < 16; ++w) sum += at[w];
+        *loss = static_cast<float>(sum / static_cast<double>(fmaxf(n, 1.0f)));
     }
 }
-__global__ __launch_bounds__(kT) void mean_terms_kernel(const double* term, int64_t rows, const float* share, float* loss) {
-    __shared__ double at[kT / 64];
-    sum_terms<kT>(term, rows, share, loss, at);
-}
 
-// kWaves wavefronts a row, up to kHeld vectors a thread in registers; the last block to end adds the loss.  kPerSimd wavefronts a SIMD:
+// kWaves wavefronts a row, up to kHeld vectors a thread in registers.  kPerSimd wavefronts a SIMD:
 // with two blocks on a compute unit one loads or stores while the other computes, which its registers have to leave room for.
 template <class E, int kWaves, int kHeld, int kPerSimd>
-__global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(const GradientArgs g, uint32_t* ticket) {
+__global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(const GradientArgs g) {
     constexpr int kThreads = kWaves * 64;
     __shared__ Stat at[kWaves];
-    __shared__ double sums[kWaves];
+    __shared__ float counts[kWaves];
     __shared__ float of_row;
-    __shared__ uint32_t turn;
     const RowArgs& a = g.row;
     const int64_t row = blockIdx.x;
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
@@ -427,20 +435,30 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
     const Cut<E> cut(dz, static_cast<int>(a.vocab));
     const int64_t token = a.tokens[row];
     const int single = cut.single();
-    float coef = 0.0f, m = 0.0f, scale = 0.0f, alone = -INFINITY;
+    float coef = 0.0f, m = 0.0f, scale = 0.0f, alone = -INFINITY, value = 0.0f;
     v4u x[kHeld];
     if (token >= 0) {                   // uniform over the block
+        // in front of the row: behind it they would be waited for, and with them the whole row
+        value = token < a.vocab ? E::get(z + token) : NAN;
+        float share = a.rows <= kCountHere ? 0.0f : *a.share;
+        const RowNumbers numbers(a.policy, row);
+        if (single >= 0) alone = E::get(z + single);
+        __builtin_amdgcn_sched_barrier(0);
+        // No load under a condition (places beyond the end read the last vector), so that each is waited for by itself: behind
+        // branches all are waited for before the first is used.
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const int v = u * kThreads + static_cast<int>(threadIdx.x);
-            x[u] = v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
-            if (v < cut.vectors) x[u] = load_vector<E>(z, cut.at(v));
+            x[u] = load_vector<E, false>(z, cut.at(v < cut.vectors ? v : cut.vectors - 1));
         }
-        if (single >= 0) alone = E::get(z + single);
+        if (a.rows <= kCountHere) share = 1.0f / fmaxf(counted_rows<kWaves>(a.tokens, a.rows, counts), 1.0f);
+        __builtin_amdgcn_sched_barrier(0);
         Stat st{-INFINITY, 0.0f};
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             float f[E::kN], top = -INFINITY;
+            if ((u + 1) * kThreads > cut.vectors)        // uniform
+                x[u] = u * kThreads + static_cast<int>(threadIdx.x) < cut.vectors ? x[u] : v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
             asm volatile("" : "+v"(x[u]));               // held packed, however it was come by
             E::unpack(x[u], f);
 #pragma unroll
@@ -455,14 +473,13 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
         if (single >= 0) st = joined(st, of_one(alone));
         st = block_joined<kWaves>(st, at);
         if (threadIdx.x < 64) {
-            const float value = token < a.vocab ? E::get(z + token) : NAN;
             const double l = log_prob(value, st);
             float slope, term;
-            policy_row(a.policy, row, l, slope, term);
+            policy_row(a.policy, numbers, l, slope, term);
             if (threadIdx.x == 0) {
                 a.logp[row] = static_cast<float>(l);
-                __hip_atomic_store(a.term + row, static_cast<double>(term), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                of_row = slope * *a.share;
+                a.term[row] = term;
+                of_row = slope * share;
             }
         }
         __syncthreads();
@@ -471,7 +488,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
         scale = -coef / st.s;
     } else if (threadIdx.x == 0) {
         a.logp[row] = 0.0f;
-        __hip_atomic_store(a.term + row, 0.0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        a.term[row] = 0.0;
     }
     const int hot = token < a.vocab ? static_cast<int>(token) : -1;
     const bool zero = coef == 0.0f;     // NaN is not
@@ -486,17 +503,14 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
                 for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
             } else {
                 asm volatile("" : "+v"(x[u]));           // unpacked anew, not kept unpacked since the sum
-                gradient_of<E>(x[u], cut.at(v), hot, m, scale, coef, d);
+                gradient_of<E>(x[u], m, scale, d);
             }
             store_vector<E>(dz, cut.at(v), d);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    if (threadIdx.x == 0) turn = count_done(ticket);     // after its term, which the same thread has stored
-    __syncthreads();
-    if (turn + 1 == gridDim.x) {
-        sum_terms<kThreads>(a.term, a.rows, a.share, g.loss, sums);
-    }
+    // the token's element once more, by the thread that has stored it without coef
+    if (cut.vector_of(hot) >= 0 && cut.vector_of(hot) % kThreads == static_cast<int>(threadIdx.x)) E::put(dz + hot, gradient_at(value, true, m, scale, coef));
 }
 
 // ---- preference ------------------------------------------------------------------------------------------
@@ -554,8 +568,7 @@ struct Workspace {
     Stat* stat;
     double* term;
     float* coef;
-    float* share;           // 1 / counted and counted
-    uint32_t* ticket;
+    float* share;           // 1 / counted
     Stat* parts;
     int64_t bytes;
 };
@@ -570,8 +583,7 @@ Workspace laid_out(void* at, int64_t rows) {
     w.stat = reinterpret_cast<Stat*>(take(rows * sizeof(Stat)));
     w.term = reinterpret_cast<double*>(take(rows * sizeof(double)));
     w.coef = reinterpret_cast<float*>(take(rows * sizeof(float)));
-    w.share = reinterpret_cast<float*>(take(2 * sizeof(float)));
-    w.ticket = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+    w.share = reinterpret_cast<float*>(take(sizeof(float)));
     w.parts = reinterpret_cast<Stat*>(take(std::max(rows, kSplitBlocks) * sizeof(Stat)));      // rows * split_of(rows, .) at most
     return w;
 }
@@ -608,19 +620,20 @@ void launch_gradient(GradientArgs g, hipStream_t s) {
 }
 
 template <class E>
-void launch_policy_of(GradientArgs g, uint32_t* ticket, hipStream_t s) {
+void launch_policy_of(GradientArgs g, hipStream_t s) {
     const int64_t rows = g.row.rows, vectors = g.row.vocab / E::kN;
     const dim3 grid(static_cast<uint32_t>(rows));
-    hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, g.row.tokens, rows, const_cast<float*>(g.row.share), ticket);
-    if (vectors > 16384) {               // more than a block's registers hold
+    const bool apart = vectors < 2 || vectors > 16384;
+    if (apart || rows > kCountHere) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, g.row.tokens, rows, const_cast<float*>(g.row.share));
+    if (apart) {                         // perhaps none behind the first 16-byte address, or more than a block's registers hold
         launch_stats<E>(g.row, s);
-        hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(kT), 0, s, g.row.term, rows, g.row.share, g.loss);
         launch_gradient<E>(g, s);
-    } else if (vectors <= 256) hipLaunchKernelGGL((policy_rows_kernel<E, 1, 4, 4>), grid, dim3(64), 0, s, g, ticket);
-    else if (vectors <= 1024) hipLaunchKernelGGL((policy_rows_kernel<E, 4, 4, 8>), grid, dim3(256), 0, s, g, ticket);
-    else if (vectors <= 4096) hipLaunchKernelGGL((policy_rows_kernel<E, 8, 8, 8>), grid, dim3(512), 0, s, g, ticket);
-    else if (vectors <= 8192) hipLaunchKernelGGL((policy_rows_kernel<E, 16, 8, 8>), grid, dim3(1024), 0, s, g, ticket);
-    else hipLaunchKernelGGL((policy_rows_kernel<E, 16, 16, 4>), grid, dim3(1024), 0, s, g, ticket);
+    } else if (vectors <= 256) hipLaunchKernelGGL((policy_rows_kernel<E, 1, 4, 4>), grid, dim3(64), 0, s, g);
+    else if (vectors <= 1024) hipLaunchKernelGGL((policy_rows_kernel<E, 4, 4, 8>), grid, dim3(256), 0, s, g);
+    else if (vectors <= 4096) hipLaunchKernelGGL((policy_rows_kernel<E, 8, 8, 8>), grid, dim3(512), 0, s, g);
+    else if (vectors <= 8192) hipLaunchKernelGGL((policy_rows_kernel<E, 16, 8, 8>), grid, dim3(1024), 0, s, g);
+    else hipLaunchKernelGGL((policy_rows_kernel<E, 16, 16, 4>), grid, dim3(1024), 0, s, g);
+    hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(1024), 0, s, g.row.term, g.row.tokens, rows, g.loss);
 }
 template <class E>
 void launch_preference_of(const GradientArgs& g, const int64_t* offsets, const float* ref, double beta, float* sums, float* margins, hipStream_t s) {
@@ -657,11 +670,10 @@ hipError_t launch_policy(const LossRows& a, const PolicyTerms& t, float* loss, v
     g.dz = dz;
     g.loss = loss;
     if (a.rows == 0) {
-        hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, a.tokens, a.rows, w.share, w.ticket);
-        hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(kT), 0, s, w.term, a.rows, w.share, loss);
-    } else if (a.type == ADPSGD_TYPE_F32) launch_policy_of<F32>(g, w.ticket, s);
-    else if (a.type == ADPSGD_TYPE_BF16) launch_policy_of<Bf16>(g, w.ticket, s);
-    else launch_policy_of<F16>(g, w.ticket, s);
+        hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(1024), 0, s, w.term, a.tokens, a.rows, loss);
+    } else if (a.type == ADPSGD_TYPE_F32) launch_policy_of<F32>(g, s);
+    else if (a.type == ADPSGD_TYPE_BF16) launch_policy_of<Bf16>(g, s);
+    else launch_policy_of<F16>(g, s);
     return hipGetLastError();
 }
 
