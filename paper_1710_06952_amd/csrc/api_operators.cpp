@@ -210,7 +210,7 @@ extern "C" int adpsgd_preference_loss(const adpsgd_logits_t* o, const int64_t* o
 
 // ---- AdamW ----
 struct adpsgd_adamw {
-    DevBuf tables;                  // AdamwTensor, AdamwChunk, norm parts, factor, ticket, norm
+    DevBuf tables;                  // chunks, norm parts, factor, norm
     AdamwArgs a{};
     float* own_norm = nullptr;
     double beta1 = 0.0, beta2 = 0.0;
@@ -240,34 +240,29 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
         if (o->tensors > 0 && (!o->params || !o->grads || !o->weight_decay)) return refuse("adamw: params, grads or weight_decay is NULL");
         if (length > 0 && (!o->m || !o->v || !aligned16(o->m) || !aligned16(o->v))) return refuse("adamw: m or v is NULL or not 16-byte aligned");
         if (length > 0 && o->state_bits == 8 && (!o->exponents || !aligned_to(o->exponents, 2))) return refuse("adamw: exponents is NULL or not aligned to 2 bytes");
-        std::vector<AdamwTensor> tensors;
         std::vector<AdamwChunk> chunks;
         int64_t state = 0;
+        const int64_t p_size = size_of(o->param_type), g_size = size_of(o->grad_type);
         for (int32_t i = 0; i < o->tensors; ++i) {
             const int64_t n = o->sizes[i];
-            AdamwTensor t{};
-            t.p = o->params[i];
-            t.g = o->grads[i];
-            t.master = o->masters ? o->masters[i] : nullptr;
-            t.out = o->out ? o->out[i] : nullptr;
-            t.n = n;
-            t.state = state;
-            t.decay = o->weight_decay[i];
-            if (!std::isfinite(t.decay)) return refuse("adamw: weight_decay is not finite");
-            if (n > 0 && (!t.p || !t.g || (o->masters && !t.master) || (o->out && !t.out))) return refuse("adamw: a tensor is NULL");
-            if (!aligned_to(t.p, size_of(o->param_type)) || !aligned_to(t.g, size_of(o->grad_type)) || !aligned_to(t.master, 4) || !aligned_to(t.out, 4))
-                return refuse("adamw: a tensor is not aligned to its type");
-            const int64_t pieces = (n + kAdamwChunk - 1) / kAdamwChunk;
-            if (static_cast<int64_t>(chunks.size()) + pieces > (int64_t(1) << 23)) return refuse("adamw: more than 2^35 elements");
-            for (int64_t c = 0; c < pieces; ++c) chunks.push_back(AdamwChunk{i, static_cast<int32_t>(c)});
-            tensors.push_back(t);
+            char* p = static_cast<char*>(o->params[i]);
+            const char* g = static_cast<const char*>(o->grads[i]);
+            float* master = o->masters ? o->masters[i] : nullptr;
+            float* to = o->out ? o->out[i] : nullptr;
+            const float decay = o->weight_decay[i];
+            if (!std::isfinite(decay)) return refuse("adamw: weight_decay is not finite");
+            if (n > 0 && (!p || !g || (o->masters && !master) || (o->out && !to))) return refuse("adamw: a tensor is NULL");
+            if (!aligned_to(p, p_size) || !aligned_to(g, g_size) || !aligned_to(master, 4) || !aligned_to(to, 4)) return refuse("adamw: a tensor is not aligned to its type");
+            if (static_cast<int64_t>(chunks.size()) + n / kAdamwChunk >= (int64_t(1) << 23)) return refuse("adamw: more than 2^35 elements");
+            for (int64_t at = 0; at < n; at += kAdamwChunk)
+                chunks.push_back(AdamwChunk{p + at * p_size, g + at * g_size, master ? master + at : nullptr, to ? to + at : nullptr, state + at,
+                                            static_cast<int32_t>(std::min<int64_t>(n - at, kAdamwChunk)), decay});
             state += (n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock;
         }
-        const size_t tb = tensors.size() * sizeof(AdamwTensor), cb = chunks.size() * sizeof(AdamwChunk);
+        const size_t cb = chunks.size() * sizeof(AdamwChunk);
         const size_t own = kAdamwNormBlocks * sizeof(double) + 4 * sizeof(float);
-        std::vector<char> image(tb + cb + own, 0);         // the ticket at zero
-        if (tb) std::memcpy(image.data(), tensors.data(), tb);
-        if (cb) std::memcpy(image.data() + tb, chunks.data(), cb);
+        std::vector<char> image(cb + own, 0);
+        if (cb) std::memcpy(image.data(), chunks.data(), cb);
         adpsgd_adamw* h = new adpsgd_adamw;
         hipError_t e = h->tables.reserve(image.size());
         if (e == hipSuccess) e = hipMemcpy(h->tables.p, image.data(), image.size(), hipMemcpyHostToDevice);
@@ -277,13 +272,11 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
             return hip_fail(nullptr, e, "adamw: tables");
         }
         char* at = static_cast<char*>(h->tables.p);
-        h->a.tensors = reinterpret_cast<const AdamwTensor*>(at);
-        h->a.chunks = reinterpret_cast<const AdamwChunk*>(at + tb);
+        h->a.chunks = reinterpret_cast<const AdamwChunk*>(at);
         h->a.n_chunks = static_cast<int64_t>(chunks.size());
-        h->a.norm_parts = reinterpret_cast<double*>(at + tb + cb);
-        h->a.factor = reinterpret_cast<float*>(at + tb + cb + kAdamwNormBlocks * sizeof(double));
+        h->a.norm_parts = reinterpret_cast<double*>(at + cb);
+        h->a.factor = reinterpret_cast<float*>(at + cb + kAdamwNormBlocks * sizeof(double));
         h->own_norm = h->a.factor + 1;
-        h->a.ticket = reinterpret_cast<uint32_t*>(h->a.factor + 2);
         h->a.param_type = o->param_type;
         h->a.grad_type = o->grad_type;
         h->a.bits = o->state_bits;
@@ -294,6 +287,10 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
         h->a.exponents = o->exponents;
         h->a.beta1 = static_cast<float>(o->beta1);
         h->a.beta2 = static_cast<float>(o->beta2);
+        h->a.beta1_64 = o->beta1;
+        h->a.beta2_64 = o->beta2;
+        h->a.rest1_64 = 1.0 - o->beta1;
+        h->a.rest2_64 = 1.0 - o->beta2;
         h->a.rest1 = static_cast<float>(1.0 - o->beta1);
         h->a.rest2 = static_cast<float>(1.0 - o->beta2);
         h->a.eps = static_cast<float>(o->eps);

@@ -232,14 +232,6 @@ __device__ __forceinline__ void wave_lds_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Counts a thread block as done; returns how many were before it.  What the calling thread has stored before with agent-scope atomics
-// (which go past the L2 of an XCD) is in memory by then, so the block that is last may read it with such loads.  A release
-// would write back the whole L2 as well, for every block: a kernel of 4096 blocks that write 131 KB each took 640 us with it, 290 without.
-__device__ __forceinline__ uint32_t count_done(uint32_t* ticket) {
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-    return __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);

@@ -2,8 +2,8 @@
 //
 //   g' = f g;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2;  u = (m / c1) / (sqrt(v / c2) + eps);  p = p - lr (u + wd p)
 //
-// A table cuts the tensors into chunks of 4096 elements, one thread block each: a model of many small tensors is one grid, as a
-// single large tensor is.  A wavefront takes 256 consecutive elements at a time, four a lane, which is the block of elements that
+// A table cuts the tensors into chunks of up to 4096 elements, one thread block each: a model of many small tensors is one grid, as a
+// single large tensor is.  A whole chunk has no condition in front of its loads, so that all are on their way at once.  A wavefront takes 256 consecutive elements at a time, four a lane, which is the block of elements that
 // shares an exponent where the state has 8 bits: its largest magnitude is a reduction over the wavefront.
 //
 // Bound: memory, 28 bytes an element with everything in 32 bits (gradient 4, parameter 8, moments 16), 16 with bf16 parameters and
@@ -16,6 +16,7 @@
 // and hi is taken where share + (word + 1/2) / 2^16 >= 1, with 16 bits of a counter generator's word for each.  v > 0 is never
 // rounded to 0, so a direction is never divided by eps alone.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "operators.hpp"
@@ -63,19 +64,19 @@ struct TypeF16 {
     __device__ static void store(void* p, int64_t at, float x) { static_cast<uint16_t*>(p)[at] = down(x); }
 };
 
-// Four elements from `at` on of a tensor that ends at n; 0 beyond.
-template <class T>
-__device__ __forceinline__ v4f load_up_to(const void* p, int64_t at, int64_t n) {
-    if (at + 4 <= n) return T::load4(p, at);
+// Four elements from `at` on of n; beyond the end 0, or nothing.  kWhole: all of them are there.
+template <class T, bool kWhole>
+__device__ __forceinline__ v4f load_up_to(const void* p, int at, int n) {
+    if (kWhole || at + 4 <= n) return T::load4(p, at);
     v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (at + i < n) x[i] = T::load(p, at + i);
     return x;
 }
-template <class T>
-__device__ __forceinline__ void store_up_to(void* p, int64_t at, int64_t n, v4f x) {
-    if (at + 4 <= n) {
+template <class T, bool kWhole>
+__device__ __forceinline__ void store_up_to(void* p, int at, int n, v4f x) {
+    if (kWhole || at + 4 <= n) {
         T::store4(p, at, x);
         return;
     }
@@ -85,10 +86,19 @@ __device__ __forceinline__ void store_up_to(void* p, int64_t at, int64_t n, v4f 
 }
 
 // ---- e4m3 codes and exponents ----
+// The largest of a wavefront's values, not negative, by moves between lanes of a row and between rows (no LDS).
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-    return x;
+    auto with = [&](auto control) {
+        const int moved = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xF, 0xF, false);
+        x = fmaxf(x, __builtin_bit_cast(float, moved));
+    };
+    with(std::integral_constant<int, 0x111>());          // one lane up, two, four, eight within rows of 16
+    with(std::integral_constant<int, 0x112>());
+    with(std::integral_constant<int, 0x114>());
+    with(std::integral_constant<int, 0x118>());
+    with(std::integral_constant<int, 0x142>());          // the last of a row to the next, of two rows to the others
+    with(std::integral_constant<int, 0x143>());
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 __device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
 __device__ __forceinline__ float largest(v4f x) {
@@ -99,27 +109,27 @@ __device__ __forceinline__ int exponent_of(float x) { return x > 0.0f ? __builti
 __device__ __forceinline__ int scale_exponent(int top) { return (top < -43 ? -43 : top) - 7; }
 constexpr uint32_t kNanCode = 0x7F;
 
-// e4m3 code of y, 0 <= y < 256, rounded up where its share of the way to the next code and (word + 1/2) / 2^16 come to one
-__device__ __forceinline__ uint32_t code_up(float y, uint32_t word) {
-    const bool low = y < 0x1p-6f;                       // no exponent of their own: shifted to where the steps are the same
-    const uint32_t bits = __float_as_uint(low ? y + 0x1p-6f : y) + (word << 4) + 8u;
-    return (bits >> 20) - (low ? 121u << 3 : 120u << 3);
-}
 __device__ __forceinline__ float value_of(uint32_t code) { return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(code), 0); }
-__device__ __forceinline__ uint32_t moment_code(float m, int k, uint32_t word) {
-    const uint32_t sign = __float_as_uint(m) >> 31 << 7;
-    const uint32_t code = code_up(ldexpf(fabsf(m), -k), word);
-    return sign | (fabsf(m) < INFINITY ? code : kNanCode);
+// The draw decides by 2^-16 of a step, and a 32-bit m is off by up to 2^-20 of one: one element in a million would go the other way.
+// So moments are added in 64 bits here, of which the upper word is enough: 20 bits of fraction, 3 of them the code's, and what the other
+// 17 come to with 2 word + 1 is the carry.
+__device__ __forceinline__ uint32_t moment_code(double m, int k, uint32_t word) {
+    const double y = __builtin_amdgcn_ldexp(fabs(m), -k);
+    const bool low = y < 0x1p-6;                        // no exponent of their own: shifted to where the steps are the same
+    const uint32_t bits = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, low ? y + 0x1p-6 : y) >> 32) + 2 * word + 1;
+    const uint32_t code = (bits >> 17) - (low ? 1017u << 3 : 1016u << 3);
+    const uint32_t sign = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, m) >> 63) << 7;
+    return sign | (fabs(m) < INFINITY ? code : kNanCode);
 }
-__device__ __forceinline__ uint32_t square_code(float v, int k, uint32_t word) {
-    const float y2 = ldexpf(v, -2 * k);
-    const float y = sqrtf(y2);
+__device__ __forceinline__ uint32_t square_code(double v, int k, uint32_t word) {
+    const double y2 = __builtin_amdgcn_ldexp(v, -2 * k);
+    const float y = __builtin_amdgcn_sqrtf(static_cast<float>(y2));     // a step too far or too short is made good by the share
     const bool low = y < 0x1p-6f;
     const uint32_t below = (__float_as_uint(low ? y + 0x1p-6f : y) >> 20) - (low ? 121u << 3 : 120u << 3);
     const float lo = value_of(below), hi = value_of(below + 1);
     const float way = hi * hi - lo * lo, up = (static_cast<float>(word) + 0.5f) * 0x1p-16f;
-    uint32_t code = below + ((y2 - lo * lo) + up * way >= way ? 1u : 0u);
-    code = v > 0.0f && code == 0u ? 1u : code;
+    uint32_t code = below + (fmaf(up, way, static_cast<float>(y2 - static_cast<double>(lo * lo))) >= way ? 1u : 0u);
+    code = v > 0.0 && code == 0u ? 1u : code;
     return v < INFINITY ? code : kNanCode;              // NaN too
 }
 // The values of four codes, times 2^k.
@@ -132,15 +142,19 @@ __device__ __forceinline__ v4f squares_of(uint32_t codes, int k) {
     v *= v;                                             // exact: 8 bits
     return v4f{ldexpf(v.x, 2 * k), ldexpf(v.y, 2 * k), ldexpf(v.z, 2 * k), ldexpf(v.w, 2 * k)};
 }
+typedef double v4d __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ v4f rounded(v4d x) {
+    return v4f{static_cast<float>(x.x), static_cast<float>(x.y), static_cast<float>(x.z), static_cast<float>(x.w)};
+}
 // What a wavefront keeps of 256 moments: codes of its lanes' four, and the exponents.
 struct Kept {
     uint32_t m, v;
     int km, kv;
 };
-__device__ __forceinline__ Kept kept_of(v4f m, v4f v, v4u words) {
+__device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
     Kept k;
-    k.km = scale_exponent(exponent_of(wave_max(largest(m))));
-    const float top = wave_max(largest(v));
+    k.km = scale_exponent(exponent_of(wave_max(largest(rounded(m)))));
+    const float top = wave_max(largest(rounded(v)));
     k.kv = scale_exponent(top > 0.0f ? exponent_of(top) >> 1 : -1);     // floor(log2 sqrt v)
     k.m = k.v = 0;
 #pragma unroll
@@ -152,108 +166,139 @@ __device__ __forceinline__ Kept kept_of(v4f m, v4f v, v4u words) {
 }
 
 // ---- the norm ----
-// Sums of squares in 64 bits, block by block and then by the last block, in an order that the sizes give.
+// Sums of squares in 64 bits, block by block, then over the blocks, in an order that the sizes give.  The second sum is taken by a kernel of one
+// block, or, where the blocks are few, by every block of the step itself (a launch less).  A last block that takes it, found by a
+// counter that all blocks increment, cost 20 to 30 us with 1024 and 2048 of them.
+__device__ __forceinline__ double block_sum(double x, double* at) {
+    x = wave_sum(x);
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = at[0];
+#pragma unroll
+    for (int w = 1; w < kT / 64; ++w) x += at[w];
+    return x;
+}
+// The gradients' norm and their factor from the blocks' sums, to all threads.
+__device__ __forceinline__ float factor_of(const AdamwArgs& a, double* at, float& norm) {
+    double sum = 0.0;
+    for (int b = threadIdx.x; b < a.norm_blocks; b += kT) sum += a.norm_parts[b];
+    const double of = sqrt(block_sum(sum, at)) * fabs(static_cast<double>(a.grad_scale)), f = a.max_norm / (of + 1e-6);
+    norm = static_cast<float>(of);
+    return static_cast<float>(f > 1.0 ? 1.0 : f);                    // NaN stays
+}
+__global__ __launch_bounds__(kT) void adamw_factor_kernel(const AdamwArgs a) {
+    __shared__ double at[kT / 64];
+    float norm;
+    const float f = factor_of(a, at, norm);
+    if (threadIdx.x == 0) {
+        *a.norm = norm;
+        *a.factor = f;
+    }
+}
 template <class G>
 __global__ __launch_bounds__(kT) void adamw_norm_kernel(const AdamwArgs a) {
     __shared__ double at[kT / 64];
-    __shared__ uint32_t turn;
     double sum = 0.0;
-    for (int64_t c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
-        const AdamwChunk chunk = a.chunks[c];
-        const AdamwTensor& t = a.tensors[chunk.tensor];
-        const int64_t first = static_cast<int64_t>(chunk.index) * kAdamwChunk + threadIdx.x * kPerThread;
+    auto add = [&](const AdamwChunk& c, auto whole) {
         v4f g[kTurns];
 #pragma unroll
-        for (int u = 0; u < kTurns; ++u) {
-            const int64_t e = first + u * kT * kPerThread;
-            g[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            if (e < t.n) g[u] = load_up_to<G>(t.g, e, t.n);
-        }
+        for (int u = 0; u < kTurns; ++u) g[u] = load_up_to<G, decltype(whole)::value>(c.g, (u * kT + static_cast<int>(threadIdx.x)) * kPerThread, c.n);
 #pragma unroll
         for (int u = 0; u < kTurns; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum = fma(static_cast<double>(g[u][i]), static_cast<double>(g[u][i]), sum);
+    };
+    if (blockIdx.x < a.n_chunks) {
+        AdamwChunk next = a.chunks[blockIdx.x];
+        for (int64_t c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
+            const AdamwChunk chunk = next;
+            if (c + gridDim.x < a.n_chunks) next = a.chunks[c + gridDim.x];
+            if (chunk.n == kAdamwChunk) add(chunk, std::true_type());
+            else add(chunk, std::false_type());
+        }
     }
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kT / 64; ++w) sum += at[w];
-        __hip_atomic_store(a.norm_parts + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        turn = count_done(a.ticket);
-    }
-    __syncthreads();
-    if (turn + 1 != gridDim.x) return;
-    sum = 0.0;
-    for (uint32_t b = threadIdx.x; b < gridDim.x; b += kT) sum += __hip_atomic_load(a.norm_parts + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kT / 64; ++w) sum += at[w];
-        const double norm = sqrt(sum) * fabs(static_cast<double>(a.grad_scale));
-        const double f = a.max_norm / (norm + 1e-6);
-        *a.norm = static_cast<float>(norm);
-        *a.factor = static_cast<float>(f > 1.0 ? 1.0 : f);           // NaN stays
-        *a.ticket = 0;                                               // for the next step
-    }
+    sum = block_sum(sum, at);
+    if (threadIdx.x == 0) a.norm_parts[blockIdx.x] = sum;
 }
 
 // ---- the step ----
-template <class P, class G, bool kBytes, bool kMaster, bool kDirection>
-__global__ __launch_bounds__(kT) void adamw_step_kernel(const AdamwArgs a) {
-    const AdamwChunk chunk = a.chunks[blockIdx.x];
-    const AdamwTensor t = a.tensors[chunk.tensor];
-    const float f = a.max_norm > 0.0 ? *a.factor : 1.0f;
-    const int64_t first = static_cast<int64_t>(chunk.index) * kAdamwChunk + threadIdx.x * kPerThread;
+// Root and quotient by v_sqrt_f32 and v_rcp_f32, within 2^-22 (a v under 2^-126 counts as 0, whose root no eps over 1e-18 would feel).
+template <class P, class G, bool kBytes, bool kMaster, bool kDirection, bool kWhole>
+__device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk& t, double* sums) {
+    const int first = static_cast<int>(threadIdx.x) * kPerThread, padded = (t.n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock;
     v4f g[kTurns], p[kTurns], m32[kTurns], v32[kTurns];
     uint32_t m8[kTurns], v8[kTurns];
-    int km[kTurns], kv[kTurns];
+    uint16_t k8[kTurns];
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
-        const int64_t e = first + u * kT * kPerThread;
+        const int e = first + u * kT * kPerThread;
         const int64_t at = t.state + e;                   // the state is whole blocks of 256: no end inside four elements
-        if (e < (t.n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock) {      // uniform over a wavefront
+        if (kWhole || e < padded) {                       // uniform over a wavefront
+            g[u] = load_up_to<G, kWhole>(t.g, e, t.n);
+            p[u] = kMaster ? load_up_to<TypeF32, kWhole>(t.master, e, t.n) : load_up_to<P, kWhole>(t.p, e, t.n);
             if (kBytes) {
                 m8[u] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.m) + at);
                 v8[u] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + at);
-                const uint16_t k = *reinterpret_cast<const uint16_t*>(a.exponents + 2 * (at / kAdamwBlock));
-                km[u] = static_cast<int8_t>(k & 0xFF);
-                kv[u] = static_cast<int8_t>(k >> 8);
+                k8[u] = *reinterpret_cast<const uint16_t*>(a.exponents + 2 * (at / kAdamwBlock));
             } else {
                 m32[u] = *reinterpret_cast<const v4f*>(static_cast<const float*>(a.m) + at);
                 v32[u] = *reinterpret_cast<const v4f*>(static_cast<const float*>(a.v) + at);
             }
-            g[u] = load_up_to<G>(t.g, e, t.n);
-            p[u] = kMaster ? load_up_to<TypeF32>(t.master, e, t.n) : load_up_to<P>(t.p, e, t.n);
+        }
+    }
+    float f = 1.0f;                                       // the loads are on their way
+    if (a.max_norm > 0.0) {
+        if (a.norm_blocks <= kT) {
+            float norm;
+            f = factor_of(a, sums, norm);
+            if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = norm;
+        } else {
+            f = *a.factor;
         }
     }
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
-        const int64_t e = first + u * kT * kPerThread;
+        const int e = first + u * kT * kPerThread;
         const int64_t at = t.state + e;
-        if (e >= (t.n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock) continue;
-        v4f m = kBytes ? moments_of(m8[u], km[u]) : m32[u], v = kBytes ? squares_of(v8[u], kv[u]) : v32[u], q;
+        if (!kWhole && e >= padded) continue;
+        v4f m, v, q;
+        v4d m64, v64;
+        if (kBytes) {
+            const v4f m_old = moments_of(m8[u], static_cast<int8_t>(k8[u] & 0xFF)), v_old = squares_of(v8[u], static_cast<int8_t>(k8[u] >> 8));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double gi = g[u][i] * a.grad_scale * f;
+                m64[i] = fma(a.beta1_64, static_cast<double>(m_old[i]), a.rest1_64 * gi);
+                v64[i] = fma(a.beta2_64, static_cast<double>(v_old[i]), a.rest2_64 * gi * gi);
+            }
+            m = rounded(m64);
+            v = rounded(v64);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float gi = g[u][i] * a.grad_scale * f;
+                m[i] = fmaf(a.beta1, m32[u][i], a.rest1 * gi);
+                v[i] = fmaf(a.beta2, v32[u][i], a.rest2 * gi * gi);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float gi = g[u][i] * a.grad_scale * f;
-            m[i] = fmaf(a.beta1, m[i], a.rest1 * gi);
-            v[i] = fmaf(a.beta2, v[i], a.rest2 * gi * gi);
-            const float dir = m[i] * a.inv_c1 / (sqrtf(v[i] * a.inv_c2) + a.eps) + t.decay * p[u][i];
+            const float dir = m[i] * a.inv_c1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * a.inv_c2) + a.eps) + t.decay * p[u][i];
             q[i] = kDirection ? dir : p[u][i] - a.lr * dir;
+            asm volatile("" : "+v"(q[i]));                // rounded to 32 bits, as the master is, before the parameter's rounding
         }
         if (kDirection) {
-            store_up_to<TypeF32>(t.out, e, t.n, q);
+            store_up_to<TypeF32, kWhole>(t.out, e, t.n, q);
         } else {
-            if (kMaster) store_up_to<TypeF32>(t.master, e, t.n, q);
-            store_up_to<P>(t.p, e, t.n, q);
+            if (kMaster) store_up_to<TypeF32, kWhole>(t.master, e, t.n, q);
+            store_up_to<P, kWhole>(t.p, e, t.n, q);
         }
         if (kBytes) {
             const uint64_t lane = static_cast<uint64_t>(at) / 4;
             const v4u words = philox4x32_rounds<10>(static_cast<uint32_t>(lane), static_cast<uint32_t>(lane >> 32), static_cast<uint32_t>(a.step),
                                                     (static_cast<uint32_t>(a.step >> 32) & 0x00FFFFFFu) | kStreamMoments,
                                                     philox_keys<10>(static_cast<uint32_t>(a.seed), static_cast<uint32_t>(a.seed >> 32)));
-            const Kept k = kept_of(m, v, words);
+            const Kept k = kept_of(m64, v64, words);
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + at) = k.m;
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + at) = k.v;
             if ((threadIdx.x & 63) == 0)
@@ -264,21 +309,40 @@ __global__ __launch_bounds__(kT) void adamw_step_kernel(const AdamwArgs a) {
         }
     }
 }
+template <class P, class G, bool kBytes, bool kMaster, bool kDirection>
+__global__ __launch_bounds__(kT) void adamw_step_kernel(const AdamwArgs a) {
+    __shared__ double sums[kT / 64];
+    const AdamwChunk chunk = a.chunks[blockIdx.x];
+    if (chunk.n == kAdamwChunk) step_chunk<P, G, kBytes, kMaster, kDirection, true>(a, chunk, sums);
+    else step_chunk<P, G, kBytes, kMaster, kDirection, false>(a, chunk, sums);
+}
 
-// ---- the state in 8 bits from and to values; grid: ceil(length / 1024) ----
+// ---- the state in 8 bits from and to values; grid: ceil(length / 2048), ceil(length / 1024) ----
 __global__ __launch_bounds__(kT) void adamw_get_kernel(const uint8_t* m, const uint8_t* v, const int8_t* exponents, int64_t length, uint16_t* m_out, uint16_t* v_out) {
-    const int64_t at = 4 * (static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x);
+    typedef uint16_t v8h_any __attribute__((ext_vector_type(8), aligned(2)));
+    const int64_t at = 8 * (static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x);
     if (at >= length) return;
     const int8_t* k = exponents + 2 * (at / kAdamwBlock);
-    const v4f x = moments_of(*reinterpret_cast<const uint32_t*>(m + at), k[0]), y = squares_of(*reinterpret_cast<const uint32_t*>(v + at), k[1]);
-    TypeBf16::store4(m_out, at, x);
-    TypeBf16::store4(v_out, at, y);
+    const uint64_t cm = *reinterpret_cast<const uint64_t*>(m + at), cv = *reinterpret_cast<const uint64_t*>(v + at);
+    v8h_any x, y;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const v4f p = moments_of(static_cast<uint32_t>(cm >> (32 * h)), k[0]), q = squares_of(static_cast<uint32_t>(cv >> (32 * h)), k[1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[4 * h + i] = bf16_rne(p[i]);
+            y[4 * h + i] = bf16_rne(q[i]);
+        }
+    }
+    __builtin_nontemporal_store(x, reinterpret_cast<v8h_any*>(m_out + at));
+    __builtin_nontemporal_store(y, reinterpret_cast<v8h_any*>(v_out + at));
 }
 __global__ __launch_bounds__(kT) void adamw_set_kernel(const float* m, const float* v, int64_t length, uint8_t* m_out, uint8_t* v_out, int8_t* exponents) {
     const int64_t at = 4 * (static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x);
     if (at >= length) return;                            // whole wavefronts: the length is a multiple of 256
     const v4u half = {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};      // (word + 1/2) / 2^16 just under 1/2: to the nearest
-    const Kept k = kept_of(TypeF32::load4(m, at), TypeF32::load4(v, at), half);
+    const v4f x = TypeF32::load4(m, at), y = TypeF32::load4(v, at);
+    const Kept k = kept_of(v4d{x.x, x.y, x.z, x.w}, v4d{y.x, y.y, y.z, y.w}, half);
     *reinterpret_cast<uint32_t*>(m_out + at) = k.m;
     *reinterpret_cast<uint32_t*>(v_out + at) = k.v;
     if ((threadIdx.x & 63) == 0) {
@@ -312,12 +376,17 @@ void launch_step(const AdamwArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s) {
+hipError_t launch_adamw(const AdamwArgs& args, hipStream_t s) {
+    AdamwArgs a = args;
     if (a.max_norm > 0.0) {
-        const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(std::max<int64_t>(a.n_chunks, 1), kAdamwNormBlocks)));
-        if (a.grad_type == ADPSGD_TYPE_F32) hipLaunchKernelGGL(adamw_norm_kernel<TypeF32>, grid, dim3(kT), 0, s, a);
-        else if (a.grad_type == ADPSGD_TYPE_BF16) hipLaunchKernelGGL(adamw_norm_kernel<TypeBf16>, grid, dim3(kT), 0, s, a);
-        else hipLaunchKernelGGL(adamw_norm_kernel<TypeF16>, grid, dim3(kT), 0, s, a);
+        a.norm_blocks = static_cast<int32_t>(std::min<int64_t>(a.n_chunks, kAdamwNormBlocks));
+        const dim3 grid(static_cast<uint32_t>(a.norm_blocks));
+        if (a.n_chunks > 0) {
+            if (a.grad_type == ADPSGD_TYPE_F32) hipLaunchKernelGGL(adamw_norm_kernel<TypeF32>, grid, dim3(kT), 0, s, a);
+            else if (a.grad_type == ADPSGD_TYPE_BF16) hipLaunchKernelGGL(adamw_norm_kernel<TypeBf16>, grid, dim3(kT), 0, s, a);
+            else hipLaunchKernelGGL(adamw_norm_kernel<TypeF16>, grid, dim3(kT), 0, s, a);
+        }
+        if (a.n_chunks == 0 || a.norm_blocks > kT) hipLaunchKernelGGL(adamw_factor_kernel, dim3(1), dim3(kT), 0, s, a);
     }
     if (a.n_chunks > 0) {
         if (a.param_type == ADPSGD_TYPE_F32) launch_step<TypeF32>(a, s);
@@ -329,7 +398,7 @@ hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s) {
 
 hipError_t launch_adamw_get(const void* m, const void* v, const int8_t* exponents, int64_t length, uint16_t* m_out, uint16_t* v_out, hipStream_t s) {
     if (length > 0)
-        hipLaunchKernelGGL(adamw_get_kernel, dim3(static_cast<uint32_t>((length + 4 * kT - 1) / (4 * kT))), dim3(kT), 0, s, static_cast<const uint8_t*>(m),
+        hipLaunchKernelGGL(adamw_get_kernel, dim3(static_cast<uint32_t>((length + 8 * kT - 1) / (8 * kT))), dim3(kT), 0, s, static_cast<const uint8_t*>(m),
                            static_cast<const uint8_t*>(v), exponents, length, m_out, v_out);
     return hipGetLastError();
 }

@@ -45,39 +45,35 @@ hipError_t launch_preference(const LossRows& a, const int64_t* offsets, int64_t 
                              void* dz, float* sums, float* margins, void* ws, hipStream_t s);
 
 // ---- AdamW (kernels_adamw.hip) ----
-struct AdamwTensor {
+constexpr int kAdamwBlock = 256;    // elements that share an exponent
+constexpr int kAdamwChunk = 4096;   // elements of one thread block
+struct AdamwChunk {                 // of one tensor: where it begins
     void* p;
     const void* g;
     float* master;
     float* out;
-    int64_t n;
-    int64_t state;                  // of its first element, a multiple of 256
+    int64_t state;                  // a multiple of 256
+    int32_t n;
     float decay;
-    int32_t pad;
-};
-constexpr int kAdamwBlock = 256;    // elements that share an exponent
-constexpr int kAdamwChunk = 4096;   // elements of one thread block
-struct AdamwChunk {
-    int32_t tensor, index;          // the elements from index * kAdamwChunk on
 };
 struct AdamwArgs {
-    const AdamwTensor* tensors;
     const AdamwChunk* chunks;
     int64_t n_chunks;
     int32_t param_type, grad_type, bits;
     bool masters, direction;
     void *m, *v;
     int8_t* exponents;
+    double beta1_64, beta2_64, rest1_64, rest2_64;
     float beta1, beta2, rest1, rest2, eps, lr, inv_c1, inv_c2;     // rest: 1 - beta, inv_c: 1 / (1 - beta^step)
     float grad_scale;
     double max_norm;
     uint64_t seed, step;
-    double* norm_parts;             // kAdamwNormBlocks
+    double* norm_parts;             // kAdamwNormBlocks ...
+    int32_t norm_blocks;            // ... of which so many are used
     float* factor;                  // of the gradients in this step
-    uint32_t* ticket;
     float* norm;
 };
-constexpr int kAdamwNormBlocks = 1024;
+constexpr int kAdamwNormBlocks = 2048;      // eight for a compute unit: all are there at once
 hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s);
 hipError_t launch_adamw_get(const void* m, const void* v, const int8_t* exponents, int64_t length, uint16_t* m_out, uint16_t* v_out, hipStream_t s);
 hipError_t launch_adamw_set(const float* m, const float* v, int64_t length, void* m_out, void* v_out, int8_t* exponents, hipStream_t s);
