@@ -34,8 +34,8 @@ typedef uint16_t v4h_any __attribute__((ext_vector_type(4), aligned(2)));
 
 struct TypeF32 {
     using Raw = float;
-    __device__ static v4f load4(const void* p, int64_t at) { return *reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at); }
-    __device__ static void store4(void* p, int64_t at, v4f x) { *reinterpret_cast<v4f_any*>(static_cast<float*>(p) + at) = x; }
+    __device__ static v4f load4(const void* p, int64_t at) { return __builtin_nontemporal_load(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at)); }
+    __device__ static void store4(void* p, int64_t at, v4f x) { __builtin_nontemporal_store(x, reinterpret_cast<v4f_any*>(static_cast<float*>(p) + at)); }
     __device__ static float load(const void* p, int64_t at) { return static_cast<const float*>(p)[at]; }
     __device__ static void store(void* p, int64_t at, float x) { static_cast<float*>(p)[at] = x; }
 };
@@ -45,7 +45,7 @@ struct TypeBf16 {
         return v4f{bf16_to_float(h.x), bf16_to_float(h.y), bf16_to_float(h.z), bf16_to_float(h.w)};
     }
     __device__ static void store4(void* p, int64_t at, v4f x) {
-        *reinterpret_cast<v4h_any*>(static_cast<uint16_t*>(p) + at) = v4h_any{bf16_rne(x.x), bf16_rne(x.y), bf16_rne(x.z), bf16_rne(x.w)};
+        __builtin_nontemporal_store(v4h_any{bf16_rne(x.x), bf16_rne(x.y), bf16_rne(x.z), bf16_rne(x.w)}, reinterpret_cast<v4h_any*>(static_cast<uint16_t*>(p) + at));
     }
     __device__ static float load(const void* p, int64_t at) { return bf16_to_float(static_cast<const uint16_t*>(p)[at]); }
     __device__ static void store(void* p, int64_t at, float x) { static_cast<uint16_t*>(p)[at] = bf16_rne(x); }
@@ -86,11 +86,13 @@ __device__ __forceinline__ void store_up_to(void* p, int at, int n, v4f x) {
 }
 
 // ---- e4m3 codes and exponents ----
-// The largest of a wavefront's values, not negative, by moves between lanes of a row and between rows (no LDS).
-__device__ __forceinline__ float wave_max(float x) {
+// The largest of a wavefront's magnitudes, NaN if there is one, by moves between lanes of a row and between rows (no LDS).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float wave_largest(v4f v) {
+    float x = larger(larger(fabsf(v.x), fabsf(v.y)), larger(fabsf(v.z), fabsf(v.w)));
     auto with = [&](auto control) {
         const int moved = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(control)::value, 0xF, 0xF, false);
-        x = fmaxf(x, __builtin_bit_cast(float, moved));
+        x = larger(x, __builtin_bit_cast(float, moved));
     };
     with(std::integral_constant<int, 0x111>());          // one lane up, two, four, eight within rows of 16
     with(std::integral_constant<int, 0x112>());
@@ -100,9 +102,8 @@ __device__ __forceinline__ float wave_max(float x) {
     with(std::integral_constant<int, 0x143>());
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
-__device__ __forceinline__ float finite_or_0(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
-__device__ __forceinline__ float largest(v4f x) {
-    return fmaxf(fmaxf(finite_or_0(x.x), finite_or_0(x.y)), fmaxf(finite_or_0(x.z), finite_or_0(x.w)));
+__device__ __forceinline__ v4f finite_or_0(v4f x) {
+    return v4f{fabsf(x.x) < INFINITY ? x.x : 0.0f, fabsf(x.y) < INFINITY ? x.y : 0.0f, fabsf(x.z) < INFINITY ? x.z : 0.0f, fabsf(x.w) < INFINITY ? x.w : 0.0f};
 }
 // floor(log2 x), x finite and not negative; -1 for 0
 __device__ __forceinline__ int exponent_of(float x) { return x > 0.0f ? __builtin_amdgcn_frexp_expf(x) - 1 : -1; }
@@ -117,9 +118,9 @@ __device__ __forceinline__ uint32_t moment_code(double m, int k, uint32_t word) 
     const double y = __builtin_amdgcn_ldexp(fabs(m), -k);
     const bool low = y < 0x1p-6;                        // no exponent of their own: shifted to where the steps are the same
     const uint32_t bits = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, low ? y + 0x1p-6 : y) >> 32) + 2 * word + 1;
-    const uint32_t code = (bits >> 17) - (low ? 1017u << 3 : 1016u << 3);
+    const uint32_t code = ((bits >> 17) - (low ? 1017u << 3 : 1016u << 3)) & 0x7Fu;
     const uint32_t sign = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, m) >> 63) << 7;
-    return sign | (fabs(m) < INFINITY ? code : kNanCode);
+    return sign | code;
 }
 __device__ __forceinline__ uint32_t square_code(double v, int k, uint32_t word) {
     const double y2 = __builtin_amdgcn_ldexp(v, -2 * k);
@@ -129,8 +130,7 @@ __device__ __forceinline__ uint32_t square_code(double v, int k, uint32_t word) 
     const float lo = value_of(below), hi = value_of(below + 1);
     const float way = hi * hi - lo * lo, up = (static_cast<float>(word) + 0.5f) * 0x1p-16f;
     uint32_t code = below + (fmaf(up, way, static_cast<float>(y2 - static_cast<double>(lo * lo))) >= way ? 1u : 0u);
-    code = v > 0.0 && code == 0u ? 1u : code;
-    return v < INFINITY ? code : kNanCode;              // NaN too
+    return v > 0.0 && code == 0u ? 1u : code;
 }
 // The values of four codes, times 2^k.
 __device__ __forceinline__ v4f moments_of(uint32_t codes, int k) {
@@ -152,15 +152,28 @@ struct Kept {
     int km, kv;
 };
 __device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
+    const v4f m32 = rounded(m), v32 = rounded(v);
+    float top_m = wave_largest(m32), top_v = wave_largest(v32);
+    const bool all_finite = top_m < INFINITY && top_v < INFINITY;       // uniform; else the others decide, and NaN is kept as its code
+    if (!all_finite) {
+        top_m = wave_largest(finite_or_0(m32));
+        top_v = wave_largest(finite_or_0(v32));
+    }
     Kept k;
-    k.km = scale_exponent(exponent_of(wave_max(largest(rounded(m)))));
-    const float top = wave_max(largest(rounded(v)));
-    k.kv = scale_exponent(top > 0.0f ? exponent_of(top) >> 1 : -1);     // floor(log2 sqrt v)
+    k.km = scale_exponent(exponent_of(top_m));
+    k.kv = scale_exponent(top_v > 0.0f ? exponent_of(top_v) >> 1 : -1);     // floor(log2 sqrt v)
     k.m = k.v = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         k.m |= moment_code(m[i], k.km, words[i] >> 16) << (8 * i);
         k.v |= square_code(v[i], k.kv, words[i] & 0xFFFFu) << (8 * i);
+    }
+    if (!all_finite) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!(fabsf(m32[i]) < INFINITY)) k.m |= kNanCode << (8 * i);
+            if (!(v32[i] < INFINITY)) k.v |= kNanCode << (8 * i);
+        }
     }
     return k;
 }
@@ -237,12 +250,12 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
             g[u] = load_up_to<G, kWhole>(t.g, e, t.n);
             p[u] = kMaster ? load_up_to<TypeF32, kWhole>(t.master, e, t.n) : load_up_to<P, kWhole>(t.p, e, t.n);
             if (kBytes) {
-                m8[u] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.m) + at);
-                v8[u] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + at);
+                m8[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.m) + at));
+                v8[u] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v) + at));
                 k8[u] = *reinterpret_cast<const uint16_t*>(a.exponents + 2 * (at / kAdamwBlock));
             } else {
-                m32[u] = *reinterpret_cast<const v4f*>(static_cast<const float*>(a.m) + at);
-                v32[u] = *reinterpret_cast<const v4f*>(static_cast<const float*>(a.v) + at);
+                m32[u] = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(static_cast<const float*>(a.m) + at));
+                v32[u] = __builtin_nontemporal_load(reinterpret_cast<const v4f*>(static_cast<const float*>(a.v) + at));
             }
         }
     }
@@ -299,13 +312,13 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
                                                     (static_cast<uint32_t>(a.step >> 32) & 0x00FFFFFFu) | kStreamMoments,
                                                     philox_keys<10>(static_cast<uint32_t>(a.seed), static_cast<uint32_t>(a.seed >> 32)));
             const Kept k = kept_of(m64, v64, words);
-            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + at) = k.m;
-            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + at) = k.v;
+            __builtin_nontemporal_store(k.m, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + at));
+            __builtin_nontemporal_store(k.v, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + at));
             if ((threadIdx.x & 63) == 0)
                 *reinterpret_cast<uint16_t*>(a.exponents + 2 * (at / kAdamwBlock)) = static_cast<uint16_t>((k.km & 0xFF) | (k.kv & 0xFF) << 8);
         } else {
-            *reinterpret_cast<v4f*>(static_cast<float*>(a.m) + at) = m;
-            *reinterpret_cast<v4f*>(static_cast<float*>(a.v) + at) = v;
+            __builtin_nontemporal_store(m, reinterpret_cast<v4f*>(static_cast<float*>(a.m) + at));
+            __builtin_nontemporal_store(v, reinterpret_cast<v4f*>(static_cast<float*>(a.v) + at));
         }
     }
 }
