@@ -97,17 +97,11 @@ __device__ __forceinline__ float slope_of(uint32_t w) {
     return w == 0u ? NAN : s;
 }
 
-// How a product is cut: tiles of side x side, `splits` parts of k whose sums are joined afterwards.  `aligned`: as rows of
-// 16-byte pieces (large_fits), which the tiles of 256 need.
+// How a product is cut: tiles of side x side (0: columns, dense_narrow.hpp), `splits` parts of k whose sums are joined afterwards.
 struct DensePlan {
     int side;
     int splits;
 };
-DensePlan dense_plan(int64_t I, int64_t J, int64_t K, bool aligned);
-inline bool large_fits(const DenseGemm& g) {
-    auto rows = [](const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; };
-    return rows(g.a, g.lda, g.a_outer ? g.I : g.K) && rows(g.b, g.ldb, g.b_outer ? g.J : g.K) && g.K >= 1 && g.J % 8 == 0;
-}
 
 template <class T>
 void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);

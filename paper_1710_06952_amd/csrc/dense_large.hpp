@@ -1,9 +1,9 @@
-// Large tiled products D[i][j] = sum_k A(i, k) B(j, k): tiles of 256 x 256 by four wavefronts of 128 x 128, for operands whose rows
-// begin at multiples of 16 bytes.
+// Large tiled products D[i][j] = sum_k A(i, k) B(j, k), for operands whose rows begin at multiples of 16 bytes: tiles of 256 x 256 by four
+// wavefronts of 128 x 128, or of 128 x 128 by four of 64 x 64, two blocks on a compute unit, where the large ones are too few.
 //
-// A wavefront alone on its SIMD has 512 registers: 256 hold its results, and both halves of a step of 64 k fit beside them, so the
-// loads of one half are under way while the other is multiplied.  128 x 128 results of a wavefront read 128 KB of a step's operands from LDS
-// a compute unit, 64 x 128 would read 192.
+// Of the large tiles a wavefront is alone on its SIMD and has 512 registers: 256 hold its results, and both halves of a step of 64 k fit
+// beside them, so the loads of one half are under way while the other is multiplied.  128 x 128 results of a wavefront read 128 KB of a
+// step's operands from LDS a compute unit, 64 x 128 would read 192.
 //
 // Operands go from memory straight to LDS (buffer loads with the lds bit: 16 bytes a lane, a wavefront's 1024 bytes in a row), so
 // they cost no registers.  Two steps' operands are in LDS.  A turn of the loop:
@@ -31,9 +31,12 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 
 constexpr uint32_t kOutOfRange = 0x80000000u;
 
-template <bool kOuter, int kStep>
+// Rows are whole pieces: where a row's length is no multiple of 8 it has been copied with zeros behind it (dense_pack_kernel).
+__device__ __forceinline__ int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+
+template <bool kOuter, int kSide, int kStep>
 struct DirectOperand {
-    static constexpr int kSide = 256, kThreads = 256, kLoads = kSide * kBK / 8 / kThreads;
+    static constexpr int kThreads = 256, kLoads = kSide * kBK / 8 / kThreads;
     typedef Operand<kOuter, kSide, kThreads, kStep> Form;
     uint64_t base, end;         // bytes
     uint64_t advance;           // of a step
@@ -47,14 +50,14 @@ struct DirectOperand {
         const uint32_t pitch = static_cast<uint32_t>(ld * 2);
         if (!kOuter) {
             base = at + static_cast<uint64_t>(first) * pitch;
-            end = at + static_cast<uint64_t>(all - 1) * pitch + 2 * K;
+            end = at + static_cast<uint64_t>(all - 1) * pitch + 2 * up8(K);
             advance = 2 * kBK;
-            const int there = static_cast<int>((K - (K - 1) / kBK * kBK) / 8);       // pieces of the last step
+            const int there = static_cast<int>(up8(K - (K - 1) / kBK * kBK) / 8);    // pieces of the last step
 #pragma unroll
             for (int s = 0; s < 2; ++s) beyond[s] = ((threadIdx.x & 7) ^ Form::turn_of(s * 32 + (threadIdx.x >> 3))) < there ? 0u : kOutOfRange;
         } else {
             base = at + 2 * first;
-            end = at + static_cast<uint64_t>(K - 1) * pitch + 2 * all;
+            end = at + static_cast<uint64_t>(K - 1) * pitch + 2 * up8(all);
             advance = static_cast<uint64_t>(kBK) * pitch;
         }
         const int rows = static_cast<int>(all - first < kSide ? all - first : kSide);
@@ -70,14 +73,14 @@ struct DirectOperand {
             }
         }
     }
-    __device__ __forceinline__ void aim(int64_t step, int64_t steps, uint32_t lds) {
+    __device__ __forceinline__ void aim(int64_t step, int64_t steps, int64_t until, uint32_t lds) {
         const uint64_t from = base + static_cast<uint64_t>(step) * advance;
         const uint64_t left = end - from;
         const uint32_t range = left < kOutOfRange - 1 ? static_cast<uint32_t>(left) : kOutOfRange - 1;
         rsrc = v4su{static_cast<uint32_t>(from), static_cast<uint32_t>(from >> 32) & 0xFFFFu, range, 0x00020000u};
         to = lds;
         cut = step == steps - 1 ? 0xFFFFFFFFu : 0u;
-        none = step < steps ? 0u : kOutOfRange;
+        none = step < until ? 0u : kOutOfRange;
     }
     __device__ __forceinline__ void load(int s) const {
         const uint32_t at = offset[s] | (kOuter ? none : (beyond[s & 1] & cut) | none);
@@ -87,10 +90,10 @@ struct DirectOperand {
 
 // Where a lane reads its fragments of 16 rows and 32 k: what differs between fragments t and halves h by exchanged bits is a register,
 // the rest an immediate.  `flip` goes to the other step's operands.
-template <bool kOuter, int kStep>
+template <bool kOuter, int kSide, int kStep>
 struct FragmentReader {
-    typedef Operand<kOuter, 256, 256, kStep> Form;
-    static constexpr int kPlaces = !kOuter ? 2 : kStep == 0 ? 8 : 4;
+    typedef Operand<kOuter, kSide, 256, kStep> Form;
+    static constexpr int kTiles = kSide / 32, kPlaces = !kOuter ? 2 : kStep == 0 ? kTiles : kTiles / 2;
     uint32_t at[kPlaces];
 
     __device__ void start(uint32_t lds, int row0) {
@@ -108,7 +111,7 @@ struct FragmentReader {
     }
     __device__ __forceinline__ void flip() {
 #pragma unroll
-        for (int p = 0; p < kPlaces; ++p) at[p] ^= 0x10000u;
+        for (int p = 0; p < kPlaces; ++p) at[p] ^= 4u * kSide * kBK;       // the operands lie at the beginning of LDS
     }
     __device__ __forceinline__ v4u read(int t, int h) const {
         if (!kOuter) {
@@ -116,33 +119,33 @@ struct FragmentReader {
             return *(const __attribute__((address_space(3))) v4u*)(static_cast<uintptr_t>(at[h] + t * kBytes));
         }
         typedef short v4s __attribute__((ext_vector_type(4)));
-        const uint32_t from = (kStep == 0 ? at[t] : at[t / 2] + t % 2 * 8) + h * (32 * 512);
+        const uint32_t from = (kStep == 0 ? at[t] : at[t / 2] + t % 2 * 8) + h * (32 * 2 * kSide);
         v2u half[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            half[e] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(static_cast<uintptr_t>(from + e * (4 * 512)))));
+            half[e] = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(static_cast<uintptr_t>(from + e * (4 * 2 * kSide)))));
         return v4u{half[0].x, half[0].y, half[1].x, half[1].y};
     }
 };
 
-template <class T, bool kAOuter, bool kBOuter>
-__global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) {
-    constexpr int kSide = 256, kTI = 8, kTJ = 8, kHalf = kSide * kBK;
-    typedef DirectOperand<kAOuter, 0> OpA;
-    typedef DirectOperand<kBOuter, 4 * kTJ> OpB;
+template <class T, bool kAOuter, bool kBOuter, int kSide>
+__global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(const DenseGemm g, const int splits) {
+    constexpr int kTI = kSide / 32, kTJ = kTI, kHalf = kSide * kBK;
+    typedef DirectOperand<kAOuter, kSide, 0> OpA;
+    typedef DirectOperand<kBOuter, kSide, 4 * kTJ> OpB;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
     const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSide - 1) / kSide;
     int64_t ti, tj, split;
     place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
-    const int64_t steps = (g.K + kBK - 1) / kBK;
+    const int64_t steps = (g.K + kBK - 1) / kBK, s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
     OpA a;
     OpB b;
     a.start(g.a, g.lda, ti * kSide, g.I, g.K);
     b.start(g.b, g.ldb, tj * kSide, g.J, g.K);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = (wave >> 1) * 128, wj = (wave & 1) * 128;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = (wave >> 1) * (kSide / 2), wj = (wave & 1) * (kSide / 2);
     const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t*)lds)), place = at + wave * 1024;
-    FragmentReader<kAOuter, 0> read_a;
-    FragmentReader<kBOuter, 4 * kTJ> read_b;
+    FragmentReader<kAOuter, kSide, 0> read_a;
+    FragmentReader<kBOuter, kSide, 4 * kTJ> read_b;
     read_a.start(at, wi);
     read_b.start(at + 2 * kHalf, wj);
     v4f acc[kTI][kTJ];
@@ -153,9 +156,9 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
     v4u fa[2][kTI], fb[2][kTJ];
 
     auto aim = [&](int64_t step) {
-        const uint32_t to = place + static_cast<uint32_t>(step & 1) * (4 * kHalf);
-        a.aim(step, steps, to);
-        b.aim(step, steps, to + 2 * kHalf);
+        const uint32_t to = place + static_cast<uint32_t>((step - s0) & 1) * (4 * kHalf);
+        a.aim(step, steps, s1, to);
+        b.aim(step, steps, s1, to + 2 * kHalf);
     };
     auto request = [&](int h, int n) {                   // fragment n of 16, from LDS: those of B first, all products need them
         if (n < kTJ) fb[h][n] = read_b.read(n, h);
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
 #pragma unroll
             for (int n = 3 * m; n < 3 * m + 3; ++n)
                 if (n < kTI + kTJ) request(1 - h, n);
-            if (loads && m < 4) {
+            if (loads && m < kTI / 2) {
 #pragma unroll
                 for (int s = 2 * m; s < 2 * m + 2; ++s) {
                     a.load(s);
@@ -196,16 +199,16 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
             b.load(s);
         }
     };
-    aim(0);
+    aim(s0);
     all_loads();
     wait_loads();
     __syncthreads();
-    aim(1);
+    aim(s0 + 1);
     all_loads();
 #pragma unroll
     for (int n = 0; n < kTI + kTJ; ++n) request(0, n);
     // Behind the last step nothing is loaded (out of range), and what is requested is not used: one loop without ends of its own.
-    for (int64_t step = 0; step < steps; ++step) {
+    for (int64_t step = s0; step < s1; ++step) {
         multiply(0, false);
         wait_loads();
         __syncthreads();
@@ -220,48 +223,52 @@ __global__ __launch_bounds__(256, 1) void dense_large_kernel(const DenseGemm g) 
 #pragma unroll
         for (int n = 0; n < kTJ; ++n) settle_mfma(acc[m][n]);
 
-    // The results go through LDS, a wavefront's own 32 KB for 64 of its rows at a time: the end is a short loop over eight neighbouring
-    // results a lane, and rows are stored 256 bytes at a time.  As 32 copies of the end in the place of the loop it took 20 us a tile
-    // (60 with an activation): the instructions had to come from memory.  Pieces of 16 bytes exchanged by the row.
+    // The results go through LDS, 64 rows of a wavefront at a time: the end is a short loop over eight neighbouring results a lane, and rows
+    // are stored 128 or 256 bytes at a time.  As 32 copies of the end in the place of the loop it took 20 us a tile (60 with an
+    // activation): the instructions had to come from memory.  Pieces of 16 bytes exchanged by the row.
     __syncthreads();                                     // the operands in LDS have been read by all
-    float* own = reinterpret_cast<float*>(lds) + wave * (64 * 128);
-    const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
-    const Ending<T, true> end(g, tj * kSide + wj + 8 * l);
+    constexpr int kColumns = 16 * kTJ, kLanes = kColumns / 8, kRows = 64 / kLanes, kMask = kColumns / 4 - 1;
+    float* own = reinterpret_cast<float*>(lds) + wave * (64 * kColumns);
+    const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4, c = lane % kLanes, at_row = lane / kLanes;
+    const int64_t j = tj * kSide + wj + 8 * c;
+    const Ending<T> end(g, j);
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
+    for (int part = 0; part < kTI / 4; ++part) {
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int n = 0; n < kTJ; ++n) {
-                const int row = m * 16 + l, piece = (q * kTJ + n) ^ (row & 31);
-                *reinterpret_cast<v4f*>(own + row * 128 + piece * 4) = acc[4 * part + m][n];
+                const int row = m * 16 + l, piece = (q * kTJ + n) ^ (row & kMask);
+                *reinterpret_cast<v4f*>(own + row * kColumns + piece * 4) = acc[4 * part + m][n];
             }
         wave_lds_sync();
-        const int64_t i0 = ti * kSide + wi + part * 64 + q;
-        v4u r0 = end.residual(i0), r1 = end.residual(i0 + 4);        // two turns ahead
+        const int64_t i0 = ti * kSide + wi + part * 64 + at_row;
+        v4u r0 = end.residual(i0), r1 = end.residual(i0 + kRows);      // two turns ahead
 #pragma unroll 1
-        for (int turn = 0; turn < 16; ++turn) {
+        for (int turn = 0; turn < 64 / kRows; ++turn) {
             const v4u r = r0;
             r0 = r1;
-            r1 = end.residual(i0 + 4 * turn + 8);
-            const int row = turn * 4 + q;
-            const v4f f0 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l) ^ (row & 31)) * 4);
-            const v4f f1 = *reinterpret_cast<const v4f*>(own + row * 128 + ((2 * l + 1) ^ (row & 31)) * 4);
+            r1 = end.residual(i0 + kRows * (turn + 2));
+            const int row = turn * kRows + at_row;
+            const v4f f0 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c) ^ (row & kMask)) * 4);
+            const v4f f1 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c + 1) ^ (row & kMask)) * 4);
             float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-            end.finish(i0 + 4 * turn, f, r);
+            const int64_t i = i0 + kRows * turn;
+            if (splits > 1) store_part(g, split, i, j, f);
+            else end.finish(i, f, r);
         }
         wave_lds_sync();
     }
 }
 
-template <class T, bool kAOuter, bool kBOuter>
-void launch_large(const DenseGemm& g, hipStream_t s) {
-    const int64_t tiles = (g.I + 255) / 256 * ((g.J + 255) / 256);
-    constexpr int kBytes = 4 * 256 * kBK * 2;
-    auto kernel = dense_large_kernel<T, kAOuter, kBOuter>;
+template <class T, bool kAOuter, bool kBOuter, int kSide>
+void launch_large(const DenseGemm& g, int splits, hipStream_t s) {
+    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
+    constexpr int kBytes = 4 * kSide * kBK * 2;
+    auto kernel = dense_large_kernel<T, kAOuter, kBOuter, kSide>;
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     (void)allowed;                                       // a refusal shows at the launch
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles)), dim3(256), kBytes, s, g);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * splits)), dim3(256), kBytes, s, g, splits);
 }
 
 }  // namespace

@@ -166,8 +166,8 @@ __device__ __forceinline__ void activate8(float* f, float* slope, int act) {
     else all(std::integral_constant<int, ADPSGD_ACT_SILU>());
 }
 
-// The end of eight neighbouring columns from j on: what all rows share is read once.  kWhole: J is a multiple of 8.
-template <class T, bool kWhole>
+// The end of eight neighbouring columns from j on: what all rows share is read once.
+template <class T>
 struct Ending {
     const DenseGemm& g;
     int64_t j;
@@ -177,21 +177,13 @@ struct Ending {
     __device__ __forceinline__ Ending(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
         n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
         uint16_t h[8];
-        if (g.bias && n > 0) load(static_cast<const uint16_t*>(g.bias) + j, h);
+        if (g.bias && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.bias) + j, n, h);
 #pragma unroll
         for (int v = 0; v < 8; ++v) bias[v] = g.bias && v < n ? T::up(h[v]) : 0.0f;
     }
-    __device__ __forceinline__ void load(const uint16_t* p, uint16_t* h) const {
-        if (kWhole) __builtin_memcpy(h, p, 16);
-        else load_up_to<8>(p, n, h);
-    }
-    __device__ __forceinline__ void store(uint16_t* p, const uint16_t* h) const {
-        if (kWhole) __builtin_memcpy(p, h, 16);
-        else store_up_to<8>(p, n, h);
-    }
     __device__ __forceinline__ v4u residual(int64_t i) const {
         uint16_t h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (g.res && i < g.I && n > 0) load(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, h);
+        if (g.res && i < g.I && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, n, h);
         v4u r;
         __builtin_memcpy(&r, h, 16);
         return r;
@@ -208,7 +200,7 @@ struct Ending {
                 activate8<true>(f, slope, g.act);
                 const v4u w = slope_words(slope);
                 __builtin_memcpy(h, &w, 16);
-                store(g.slope + at, h);
+                store_up_to<8>(g.slope + at, n, h);
             } else {
                 activate8<false>(f, slope, g.act);
             }
@@ -221,9 +213,22 @@ struct Ending {
         }
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] = T::down(f[v]);
-        store(static_cast<uint16_t*>(g.out) + at, h);
+        store_up_to<8>(static_cast<uint16_t*>(g.out) + at, n, h);
     }
 };
+
+// Eight neighbouring sums of a part of k, for dense_join_kernel.
+__device__ __forceinline__ void store_part(const DenseGemm& g, int64_t split, int64_t i, int64_t j, const float* f) {
+    if (i >= g.I || j >= g.J) return;
+    float* out = g.partial + (split * g.I + i) * g.J + j;
+    if (j + 8 <= g.J) {
+        __builtin_memcpy(out, f, 32);
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+        if (j + v < g.J) out[v] = f[v];
+}
 
 // Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of
 // neighbouring ones, and a run goes down 8 tiles of i before it moves on in j, so that the tiles at work on an XCD share rows of both.
@@ -302,28 +307,9 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
     const int64_t j = tj * kSide + wj + q * (4 * kTJ), i0 = ti * kSide + wi + l;
     if (j >= g.J) return;
-    if (splits > 1) {
-#pragma unroll
-        for (int m = 0; m < kTI; ++m) {
-            const int64_t i = i0 + m * 16;
-            if (i >= g.I) continue;
-            float* out = g.partial + (split * g.I + i) * g.J + j;
-#pragma unroll
-            for (int n = 0; n < kTJ; ++n) {
-                if (j + 4 * n + 4 <= g.J) {
-                    __builtin_memcpy(out + 4 * n, &acc[m][n], 16);
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-                        if (j + 4 * n + v < g.J) out[4 * n + v] = acc[m][n][v];
-                }
-            }
-        }
-        return;
-    }
 #pragma unroll
     for (int n = 0; n < kTJ; n += 2) {
-        const Ending<T, false> end(g, j + 4 * n);
+        const Ending<T> end(g, j + 4 * n);
         v4u r[kTI];
 #pragma unroll
         for (int m = 0; m < kTI; ++m) r[m] = end.residual(i0 + m * 16);
@@ -332,7 +318,8 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
             float f[8];
 #pragma unroll
             for (int v = 0; v < 8; ++v) f[v] = acc[m][n + v / 4][v % 4];
-            end.finish(i0 + m * 16, f, r[m]);
+            if (splits > 1) store_part(g, split, i0 + m * 16, j + 4 * n, f);
+            else end.finish(i0 + m * 16, f, r[m]);
         }
     }
 }
@@ -343,7 +330,7 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, cons
     const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t i = id / eights, j = id % eights * 8;
     if (i >= g.I) return;
-    const Ending<T, false> end(g, j);
+    const Ending<T> end(g, j);
     const v4u r = end.residual(i);
     float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) {

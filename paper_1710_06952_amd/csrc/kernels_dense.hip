@@ -14,7 +14,8 @@ constexpr int kRowsAtOnce = 8;
 // dz = dy slope, rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 8 rows of a thread, then 64).
 // Memory: 6 bytes an element.  grid: (ceil(N / 256), strips).
 template <class T>
-__global__ __launch_bounds__(kT) void dense_dz_kernel(const uint16_t* dy, int64_t lddy, const uint16_t* slope, uint16_t* dz, double* sums, int64_t M, int64_t N) {
+__global__ __launch_bounds__(kT) void dense_dz_kernel(const uint16_t* dy, int64_t lddy, const uint16_t* slope, uint16_t* dz, double* sums, uint16_t* db, int64_t M,
+                                                     int64_t N) {
     __shared__ double at[kRowsAtOnce][kColumns];
     const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
     const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumns + 8 * cx;
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(kT) void dense_dz_kernel(const uint16_t* dy, int64_
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += static_cast<double>(part[i]);
     }
-    if (!sums) return;
+    if (!sums && !db) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) at[ry][8 * cx + i] = sum[i];
     __syncthreads();
@@ -78,7 +79,8 @@ __global__ __launch_bounds__(kT) void dense_dz_kernel(const uint16_t* dy, int64_
     if (column < N) {
         double s = 0.0;
         for (int r = 0; r < kRowsAtOnce; ++r) s += at[r][threadIdx.x];
-        sums[blockIdx.y * N + column] = s;
+        if (db) db[column] = T::down(static_cast<float>(s));        // the only strip
+        else sums[blockIdx.y * N + column] = s;
     }
 }
 template <class T>
@@ -98,8 +100,9 @@ void launch_dz_of(const void* dy, int64_t lddy, const uint16_t* slope, void* dz,
     const int strips = strips_of(M);
     if (strips > 0)
         hipLaunchKernelGGL(dense_dz_kernel<T>, dim3(static_cast<uint32_t>((N + kColumns - 1) / kColumns), strips), dim3(kT), 0, s,
-                           static_cast<const uint16_t*>(dy), lddy, slope, static_cast<uint16_t*>(dz), db ? sums : nullptr, M, N);
-    if (db) hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + kT - 1) / kT)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
+                           static_cast<const uint16_t*>(dy), lddy, slope, static_cast<uint16_t*>(dz), db ? sums : nullptr,
+                           strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
+    if (db && strips != 1) hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + kT - 1) / kT)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
 }
 
 }  // namespace
@@ -113,22 +116,95 @@ hipError_t launch_dense_dz(int32_t type, const void* dy, int64_t lddy, const uin
     return hipGetLastError();
 }
 
-DensePlan dense_plan(int64_t I, int64_t J, int64_t K, bool aligned) {
-    auto tiles = [&](int64_t side) { return ((I + side - 1) / side) * ((J + side - 1) / side); };
-    if (aligned && tiles(256) >= 128) return DensePlan{256, 1};
-    if (tiles(128) >= 128) return DensePlan{128, 1};
-    const int64_t steps = (K + 63) / 64, n = tiles(64);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(n, 1), steps / 4, 32}));
-    return DensePlan{64, static_cast<int>(splits)};
+namespace {
+
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+// The estimate of a cut, in microseconds, from measured steps of 64 k.  256: 1.45 us a step of a block that has a compute unit for itself and
+// 12 at both ends; 128: 0.75 with two blocks on a compute unit, and 8; 64: 0.8 with four, and 5.  Parts of k are written and read in 32 bits.
+double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
+    const double tiles = static_cast<double>((I + side - 1) / side) * static_cast<double>((J + side - 1) / side) * splits;
+    const double steps = static_cast<double>(((K + 63) / 64 + splits - 1) / splits);
+    const int at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
+    const double step = side == 256 ? 1.45 : side == 128 ? 0.75 : 0.8, ends = side == 256 ? 12.0 : side == 128 ? 8.0 : 5.0;
+    const double turns = std::max(1.0, tiles / at_once);                       // the last blocks are not all there at once, but they are faster
+    return turns * (steps * step + ends) + (splits > 1 ? 4.0 + 8.0 * splits * static_cast<double>(I) * static_cast<double>(J) / 4e6 : 0.0);
 }
-int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
-    const DensePlan p = dense_plan(I, J, K, false);       // aligned operands are cut into as many parts or none
-    return p.splits > 1 ? p.splits * I * J * static_cast<int64_t>(sizeof(float)) : 0;
+// `rows`: A has k inner.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
+DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool rows, bool direct) {
+    if (rows && I <= 64) return DensePlan{0, 1};
+    const int64_t steps = std::max<int64_t>(1, (K + 63) / 64);
+    DensePlan best{64, 1};
+    double least = 1e30;
+    for (int side : {64, 128, 256}) {
+        if (side > 64 && !direct) continue;
+        for (int splits : {1, 2, 4, 8, 16, 32}) {
+            if (splits > 1 && steps / splits < 4) break;
+            const double t = estimate(side, splits, I, J, K);
+            if (t < least) {
+                least = t;
+                best = DensePlan{side, splits};
+            }
+        }
+    }
+    return best;
 }
 
-hipError_t launch_dense_gemm(int32_t type, const DenseGemm& g, hipStream_t s) {
-    if (g.I == 0 || g.J == 0) return hipSuccess;
-    const DensePlan p = dense_plan(g.I, g.J, g.K, large_fits(g));
+// Rows of `inner` elements as whole 16-byte pieces with zeros at their ends.  grid: ceil(rows ceil(inner / 8) / 256).
+__global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t rows, int64_t inner) {
+    const int64_t pieces = (inner + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x;
+    const int64_t row = id / pieces, c = id % pieces * 8;
+    if (row >= rows) return;
+    const uint16_t* p = from + row * ld + c;
+    v8h h = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (c + 8 <= inner) {
+        h = __builtin_bit_cast(v8h, *reinterpret_cast<const v4u_any*>(p));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < inner) h[i] = p[i];
+    }
+    *reinterpret_cast<v4u*>(to + (row * pieces * 8 + c)) = __builtin_bit_cast(v4u, h);
+}
+
+bool whole_pieces(const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; }
+// Copies of operands whose rows are no whole pieces: they pay where the direct tiles do, from about 2^32 products on (2100 x 1030 x 4097:
+// 42 us with the copies, 63 with tiles of 64 from the operands as they are).
+bool worth_packing(int64_t I, int64_t J, int64_t K) { return static_cast<double>(I) * static_cast<double>(J) * static_cast<double>(K) >= 4294967296.0; }
+int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(inner)); }
+
+}  // namespace
+
+// Both ways of storing an operand, and operands that begin anywhere: what any of them may ask for.
+int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
+    int64_t parts = 0;
+    for (bool direct : {false, true}) parts = std::max<int64_t>(parts, plan_of(I, J, K, false, direct).splits);
+    const bool pack = (I % 8 || J % 8 || K % 8) && worth_packing(I, J, K);
+    const int64_t copies = pack ? std::max(packed_bytes(I, K), packed_bytes(K, I)) + std::max(packed_bytes(J, K), packed_bytes(K, J)) : 0;
+    return (parts > 1 ? up256(parts * I * J * static_cast<int64_t>(sizeof(float))) : 0) + copies;
+}
+
+hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s) {
+    if (given.I == 0 || given.J == 0) return hipSuccess;
+    DenseGemm g = given;
+    const int64_t a_inner = g.a_outer ? g.I : g.K, a_rows = g.a_outer ? g.K : g.I, b_inner = g.b_outer ? g.J : g.K, b_rows = g.b_outer ? g.K : g.J;
+    const bool a_whole = whole_pieces(g.a, g.lda, a_inner), b_whole = whole_pieces(g.b, g.ldb, b_inner);
+    const bool pack = !(a_whole && b_whole) && (g.I % 8 || g.J % 8 || g.K % 8) && worth_packing(g.I, g.J, g.K);
+    const bool direct = g.K >= 1 && ((a_whole && b_whole) || pack);
+    const DensePlan p = plan_of(g.I, g.J, g.K, !g.a_outer, direct);
+    if (p.side >= 128 && pack) {
+        char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * g.J * static_cast<int64_t>(sizeof(float))) : 0);
+        auto copy = [&](const void*& from, int64_t& ld, int64_t rows, int64_t inner) {
+            const uint32_t blocks = static_cast<uint32_t>((rows * (up8(inner) / 8) + kT - 1) / kT);
+            hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, static_cast<const uint16_t*>(from), ld, reinterpret_cast<uint16_t*>(at), rows, inner);
+            from = at;
+            ld = up8(inner);
+            at += packed_bytes(rows, inner);
+        };
+        if (!a_whole) copy(g.a, g.lda, a_rows, a_inner);
+        if (!b_whole) copy(g.b, g.ldb, b_rows, b_inner);
+    }
     if (type == ADPSGD_TYPE_BF16) launch_dense_tiles<Bf16>(g, p, s);
     else launch_dense_tiles<F16>(g, p, s);
     return hipGetLastError();

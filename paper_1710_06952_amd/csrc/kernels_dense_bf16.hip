@@ -1,13 +1,14 @@
 // The tiled products of dense layers in one of their types.
 #include "dense_large.hpp"
+#include "dense_narrow.hpp"
 
 namespace adpsgd_impl {
 namespace {
 
 template <class T, bool kAOuter, bool kBOuter>
 void launch_tiles_of(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
-    if (p.side == 256) launch_large<T, kAOuter, kBOuter>(g, s);
-    else if (p.side == 128) launch_tile<T, kAOuter, kBOuter, 128, 2, 2>(g, p.splits, s);
+    if (p.side == 256) launch_large<T, kAOuter, kBOuter, 256>(g, p.splits, s);
+    else if (p.side == 128) launch_large<T, kAOuter, kBOuter, 128>(g, p.splits, s);
     else launch_tile<T, kAOuter, kBOuter, 64, 2, 2>(g, p.splits, s);
 }
 
@@ -15,6 +16,10 @@ void launch_tiles_of(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
 
 template <class T>
 void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
+    if (p.side == 0) {
+        launch_narrow<T>(g, s);
+        return;
+    }
     if (g.a_outer) launch_tiles_of<T, true, true>(g, p, s);
     else if (g.b_outer) launch_tiles_of<T, false, true>(g, p, s);
     else launch_tiles_of<T, false, false>(g, p, s);

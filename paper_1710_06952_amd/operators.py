@@ -31,12 +31,11 @@ PreferenceLoss = namedtuple("PreferenceLoss", "loss dlogits log_probs margins")
 
 def _call(device, fn, *args):
     """One library call on the device's current stream."""
-    stream = torch.cuda.current_stream(device).cuda_stream
     if torch.cuda.current_device() == device.index:
-        rc = fn(*args, stream)
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, stream)
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
     if rc != B.OK:
         raise B.AdpsgdError(rc, (B.lib().adpsgd_last_error(None) or b"").decode())
 
@@ -65,10 +64,12 @@ def _ptr(t):
 
 def _as_rows(t):
     """t as a matrix whose last dimension is contiguous, and its leading dimension."""
-    t = t.reshape(-1, t.shape[-1])
-    if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        t = t.contiguous()
-    return t, max(t.stride(0), t.shape[1])
+    if t.dim() != 2:
+        t = t.reshape(-1, t.shape[-1])
+    n, (step, inner) = t.shape[1], t.stride()
+    if (inner != 1 and n > 1) or (step < n and t.shape[0] > 1):
+        t, step = t.contiguous(), n
+    return t, max(step, n)
 
 
 def _as_weights(w):
@@ -182,14 +183,13 @@ def dense(x, w, bias=None, *, residual=None, activation="none"):
     return _forward(x, w, bias, residual, activation, False)[0]
 
 
-@torch.no_grad()
 def dense_forward(x, w, bias=None, *, residual=None, activation="none"):
     """(y, slope): the forward pass without autograd, and what dense_gradients needs (None without an activation)."""
     _check_dense(x, w, bias, residual, activation)
-    return _forward(x, w, bias, residual, activation, True)
+    with torch.no_grad():
+        return _forward(x, w, bias, residual, activation, True)
 
 
-@torch.no_grad()
 def dense_gradients(dy, x, w, slope, *, activation="none", need=(True, True, True)):
     """(dx, dw, dbias) for dy; None where ``need`` says so.  The residual's gradient is dy."""
     _check_dense(x, w, None, dy, activation)
@@ -199,7 +199,8 @@ def dense_gradients(dy, x, w, slope, *, activation="none", need=(True, True, Tru
             raise ValueError("slope must be what dense_forward returned")
     if not any(need):
         return None, None, None
-    return _backward(dy, x, w, slope if activation != "none" else None, activation, *need)
+    with torch.no_grad():
+        return _backward(dy, x, w, slope if activation != "none" else None, activation, *need)
 
 
 # ---- losses over a vocabulary -----------------------------------------------------------------------------------
@@ -211,62 +212,58 @@ def _logits(logits, tokens):
     if logits.dim() != 2 or logits.shape[1] < 1:
         raise ValueError("logits must be rows x vocabulary, are %s" % (tuple(logits.shape),))
     rows, vocab = logits.shape
-    tokens = _vector("tokens", tokens, rows, torch.int64, logits.device)
-    z, ld = _as_rows(logits.detach())
+    device = logits.device
+    tokens = _vector("tokens", tokens, rows, torch.int64, device)
+    z, ld = _as_rows(logits)
     size = B.lib().adpsgd_loss_workspace_bytes(rows, vocab)
     if size < 0:
         raise B.AdpsgdError(B.ERR_ARG, "logits: %d rows of %d are too many" % (rows, vocab))
-    space = torch.empty(size, dtype=torch.uint8, device=z.device)
-    return B.Logits(_TYPES[z.dtype], 0, rows, vocab, z.data_ptr(), ld, tokens.data_ptr(), space.data_ptr(), size), (z, tokens, space)
+    space = torch.empty(size, dtype=torch.uint8, device=device)
+    return (B.Logits(_TYPES[z.dtype], 0, rows, vocab, z.data_ptr(), ld, tokens.data_ptr(), space.data_ptr(), size), rows, device, (z, tokens, space))
 
 
-@torch.no_grad()
 def token_log_probs(logits, tokens):
-    """log softmax(logits)[i, tokens[i]] as float32; 0 where tokens[i] is negative (that row is not read)."""
-    args, keep = _logits(logits, tokens)
-    out = torch.empty(args.rows, dtype=torch.float32, device=logits.device)
-    _call(logits.device, B.lib().adpsgd_token_log_probs, C.byref(args), out.data_ptr())
+    """log softmax(logits)[i, tokens[i]] as float32, without autograd; 0 where tokens[i] is negative (that row is not read)."""
+    args, rows, dev, keep = _logits(logits, tokens)
+    out = torch.empty(rows, dtype=torch.float32, device=dev)
+    _call(dev, B.lib().adpsgd_token_log_probs, C.byref(args), out.data_ptr())
     del keep
     return out
 
 
-@torch.no_grad()
 def policy_loss_and_gradient(logits, tokens, old_log_probs, advantages, ref_log_probs=None, *, clip=(0.2, 0.2), kl_coef=0.0):
     """Clipped policy loss with a KL term (see adpsgd_policy_loss), a mean over the rows whose token is not negative, and its
     gradient for the logits.  loss is a scalar tensor; dlogits has the logits' shape and type; log_probs is float32."""
-    args, keep = _logits(logits, tokens)
-    rows, dev = args.rows, logits.device
+    args, rows, dev, keep = _logits(logits, tokens)
     old = _vector("old_log_probs", old_log_probs, rows, torch.float32, dev)
     adv = _vector("advantages", advantages, rows, torch.float32, dev)
     ref = None if ref_log_probs is None else _vector("ref_log_probs", ref_log_probs, rows, torch.float32, dev)
-    out = torch.empty(rows + 1, dtype=torch.float32, device=dev)
+    loss, logp = torch.empty((), dtype=torch.float32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev)
     dz = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-    _call(dev, B.lib().adpsgd_policy_loss, C.byref(args), old.data_ptr(), adv.data_ptr(), _ptr(ref), clip[0], clip[1], kl_coef,
-          out.data_ptr() + 4 * rows, dz.data_ptr(), out.data_ptr())
+    _call(dev, B.lib().adpsgd_policy_loss, C.byref(args), old.data_ptr(), adv.data_ptr(), _ptr(ref), clip[0], clip[1], kl_coef, loss.data_ptr(),
+          dz.data_ptr(), logp.data_ptr())
     del keep
-    return PolicyLoss(out[rows], dz, out[:rows])
+    return PolicyLoss(loss, dz, logp)
 
 
-@torch.no_grad()
 def preference_loss_and_gradient(logits, tokens, offsets, ref_log_probs, *, beta=0.1, label_smoothing=0.0):
     """Preference loss of paired answers (see adpsgd_preference_loss) and its gradient for the logits.  The rows of sequence q are
     offsets[q] .. offsets[q + 1]; the first half of the sequences are the chosen answers, the other half their rejected ones in
     the same order.  ref_log_probs: sums over each sequence under the reference model.  log_probs are those sums under this one."""
-    args, keep = _logits(logits, tokens)
-    dev = logits.device
+    args, rows, dev, keep = _logits(logits, tokens)
     _on_gpu("offsets", offsets, dev)
     if offsets.dim() != 1 or offsets.dtype != torch.int64 or offsets.numel() < 3 or offsets.numel() % 2 == 0:
         raise ValueError("offsets must be 2 pairs + 1 int64, are %s %s" % (tuple(offsets.shape), offsets.dtype))
     pairs = offsets.numel() // 2
     offsets = offsets.contiguous()
     ref = _vector("ref_log_probs", ref_log_probs, 2 * pairs, torch.float32, dev)
-    out = torch.empty(3 * pairs + 1, dtype=torch.float32, device=dev)
+    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)  # noqa: E731
+    loss, sums, margins = new(), new(2 * pairs), new(pairs)
     dz = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-    at = out.data_ptr()
-    _call(dev, B.lib().adpsgd_preference_loss, C.byref(args), offsets.data_ptr(), pairs, ref.data_ptr(), beta, label_smoothing, at + 12 * pairs,
-          dz.data_ptr(), at, at + 8 * pairs)
+    _call(dev, B.lib().adpsgd_preference_loss, C.byref(args), offsets.data_ptr(), pairs, ref.data_ptr(), beta, label_smoothing, loss.data_ptr(),
+          dz.data_ptr(), sums.data_ptr(), margins.data_ptr())
     del keep
-    return PreferenceLoss(out[3 * pairs], dz, out[:2 * pairs], out[2 * pairs:3 * pairs])
+    return PreferenceLoss(loss, dz, sums, margins)
 
 
 # ---- AdamW ------------------------------------------------------------------------------------------------------
