@@ -19,7 +19,7 @@ struct Bf16 {
     __device__ static v4f mfma(v4u a, v4u b, v4f c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8, a), __builtin_bit_cast(V8, b), c, 0, 0, 0);
     }
-    // c in accumulation registers, and in the same ones before and after; wait_mfma and settle_mfma before c is read
+    // c in accumulation registers, and in the same ones before and after; wait_mfma before c is read
     __device__ static void mfma_in_place(v4u a, v4u b, v4f& c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 struct F16 {
@@ -33,9 +33,8 @@ struct F16 {
 };
 
 // An instruction that reads the result of a matrix instruction has to come some cycles later, which the compiler sees to for its
-// own only: 32 cycles cover every form.  One wait, then every result that it is for.
+// own only: 32 cycles cover every form.
 __device__ __forceinline__ void wait_mfma() { asm volatile("s_nop 15\n\ts_nop 15"); }
-__device__ __forceinline__ void settle_mfma(v4f& c) { asm volatile("" : "+a"(c)); }
 
 // Eight values rounded.
 template <class T>

@@ -29,6 +29,10 @@ __device__ __forceinline__ void load_to_lds(v4su rsrc, uint32_t offset, uint32_t
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
+// 16 bytes from accumulation registers to LDS: written out, as the compiler would copy all results to vector registers in front of the loop.
+__device__ __forceinline__ void write_result(uint32_t lds, v4f c) { asm volatile("ds_write_b128 %0, %1" : : "v"(lds), "a"(c) : "memory"); }
+__device__ __forceinline__ void wait_results() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
 constexpr uint32_t kOutOfRange = 0x80000000u;
 
 // Rows are whole pieces: where a row's length is no multiple of 8 it has been copied with zeros behind it (dense_pack_kernel).
@@ -218,53 +222,59 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
     }
     wait_loads();
     wait_mfma();
-#pragma unroll
-    for (int m = 0; m < kTI; ++m)
-#pragma unroll
-        for (int n = 0; n < kTJ; ++n) settle_mfma(acc[m][n]);
 
-    // The results go through LDS, 64 rows of a wavefront at a time: the end is a short loop over eight neighbouring results a lane, and rows
-    // are stored 128 or 256 bytes at a time.  As 32 copies of the end in the place of the loop it took 20 us a tile (60 with an
-    // activation): the instructions had to come from memory.  Pieces of 16 bytes exchanged by the row.
+    // The end.  A store is waited for together with the loads behind it, so the residual's rows are loaded in front of the first store, into
+    // the LDS that the operands have left; with loads two turns ahead every turn waited for the stores of the one before, 25 us a tile with
+    // gelu.  The results go through LDS, 16 rows of a wavefront at a time: one short loop over eight neighbouring results a lane, which
+    // stores rows of 128 or 256 bytes.  As 32 copies of the loop's body it took 60 us a tile: the instructions had to come from memory.
     __syncthreads();                                     // the operands in LDS have been read by all
-    constexpr int kColumns = 16 * kTJ, kLanes = kColumns / 8, kRows = 64 / kLanes, kMask = kColumns / 4 - 1;
-    float* own = reinterpret_cast<float*>(lds) + wave * (64 * kColumns);
+    constexpr int kColumns = 16 * kTJ, kLanes = kColumns / 8, kRows = 64 / kLanes, kTurns = 16 * kTI / kRows, kMask = kColumns / 4 - 1;
     const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4, c = lane % kLanes, at_row = lane / kLanes;
-    const int64_t j = tj * kSide + wj + 8 * c;
-    const Ending<T> end(g, j);
+    v4u* kept = reinterpret_cast<v4u*>(lds) + wave * (kTurns * 64) + lane;                     // a lane's own
+    float* own = reinterpret_cast<float*>(reinterpret_cast<v4u*>(lds) + 4 * kTurns * 64) + wave * (16 * kColumns);
+    const uint32_t stage = at + (4 * kTurns * 64) * 16 + wave * (16 * kColumns * 4) + l * (kColumns * 4) + (((q * kTJ) ^ (l & kMask)) * 16);
+    const int64_t i0 = ti * kSide + wi + at_row, j = tj * kSide + wj + 8 * c;
+    auto finish_rows = [&](auto whole) {
+        const Ending<T, decltype(whole)::value> end(g, j);
+        if (g.res) {
+            if (end.n > 0) {
+                v4u r[kTurns];
 #pragma unroll
-    for (int part = 0; part < kTI / 4; ++part) {
+                for (int t = 0; t < kTurns; ++t) r[t] = end.residual_row(i0 + kRows * t);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < kTJ; ++n) {
-                const int row = m * 16 + l, piece = (q * kTJ + n) ^ (row & kMask);
-                *reinterpret_cast<v4f*>(own + row * kColumns + piece * 4) = acc[4 * part + m][n];
+                for (int t = 0; t < kTurns; ++t) kept[t * 64] = r[t];
             }
-        wave_lds_sync();
-        const int64_t i0 = ti * kSide + wi + part * 64 + at_row;
-        v4u r0 = end.residual(i0), r1 = end.residual(i0 + kRows);      // two turns ahead
-#pragma unroll 1
-        for (int turn = 0; turn < 64 / kRows; ++turn) {
-            const v4u r = r0;
-            r0 = r1;
-            r1 = end.residual(i0 + kRows * (turn + 2));
-            const int row = turn * kRows + at_row;
-            const v4f f0 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c) ^ (row & kMask)) * 4);
-            const v4f f1 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c + 1) ^ (row & kMask)) * 4);
-            float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-            const int64_t i = i0 + kRows * turn;
-            if (splits > 1) store_part(g, split, i, j, f);
-            else end.finish(i, f, r);
         }
-        wave_lds_sync();
-    }
+#pragma unroll 1
+        for (int m = 0; m < kTI; ++m) {
+#pragma unroll
+            for (int k = 0; k < kTI; ++k)
+                if (m == k) {
+#pragma unroll
+                    for (int n = 0; n < kTJ; ++n) write_result(stage ^ (n * 16), acc[k][n]);      // pieces exchanged by the row
+                }
+            wait_results();
+#pragma unroll 1
+            for (int turn = 0; turn < 16 / kRows; ++turn) {
+                const int row = turn * kRows + at_row, t = m * (16 / kRows) + turn;
+                const v4f f0 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c) ^ (row & kMask)) * 4);
+                const v4f f1 = *reinterpret_cast<const v4f*>(own + row * kColumns + ((2 * c + 1) ^ (row & kMask)) * 4);
+                const v4u r = kept[t * 64];
+                float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
+                if (splits > 1) store_part(g, split, i0 + kRows * t, j, f);
+                else end.finish(i0 + kRows * t, f, r);
+            }
+            wave_lds_sync();
+        }
+    };
+    if (g.J % 8 == 0) finish_rows(std::true_type());
+    else finish_rows(std::false_type());
 }
 
 template <class T, bool kAOuter, bool kBOuter, int kSide>
 void launch_large(const DenseGemm& g, int splits, hipStream_t s) {
     const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
-    constexpr int kBytes = 4 * kSide * kBK * 2;
+    constexpr int kBytes = kSide == 256 ? 160 * 1024 : 4 * kSide * kBK * 2;       // two steps' operands; the end of the large tiles needs more
     auto kernel = dense_large_kernel<T, kAOuter, kBOuter, kSide>;
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     (void)allowed;                                       // a refusal shows at the launch

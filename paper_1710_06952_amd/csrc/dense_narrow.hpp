@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kNarrowWaves * 64) void dense_narrow_kernel(const D
     for (int id = threadIdx.x; id < 16 * kTI * kEights; id += kNarrowWaves * 64) {
         const int i = id / kEights, c = id % kEights * 8;
         if (i >= g.I || j0 + c >= g.J) continue;
-        const Ending<T> end(g, j0 + c);
+        const Ending<T, false> end(g, j0 + c);
         const v4u r = end.residual(i);
         float f[8];
 #pragma unroll

@@ -166,8 +166,8 @@ __device__ __forceinline__ void activate8(float* f, float* slope, int act) {
     else all(std::integral_constant<int, ADPSGD_ACT_SILU>());
 }
 
-// The end of eight neighbouring columns from j on: what all rows share is read once.
-template <class T>
+// The end of eight neighbouring columns from j on: what all rows share is read once.  kWhole: J is a multiple of 8.
+template <class T, bool kWhole>
 struct Ending {
     const DenseGemm& g;
     int64_t j;
@@ -177,13 +177,29 @@ struct Ending {
     __device__ __forceinline__ Ending(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
         n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
         uint16_t h[8];
-        if (g.bias && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.bias) + j, n, h);
+        if (g.bias && n > 0) load(static_cast<const uint16_t*>(g.bias) + j, h);
 #pragma unroll
         for (int v = 0; v < 8; ++v) bias[v] = g.bias && v < n ? T::up(h[v]) : 0.0f;
     }
+    __device__ __forceinline__ void load(const uint16_t* p, uint16_t* h) const {
+        if (kWhole) __builtin_memcpy(h, p, 16);
+        else load_up_to<8>(p, n, h);
+    }
+    __device__ __forceinline__ void store(uint16_t* p, const uint16_t* h) const {
+        if (kWhole) __builtin_memcpy(p, h, 16);
+        else store_up_to<8>(p, n, h);
+    }
+    // Where there is a residual and a column (n > 0); a row beyond the end reads the last one.
+    __device__ __forceinline__ v4u residual_row(int64_t i) const {
+        uint16_t h[8];
+        load(static_cast<const uint16_t*>(g.res) + (i < g.I ? i : g.I - 1) * g.ldres + j, h);
+        v4u r;
+        __builtin_memcpy(&r, h, 16);
+        return r;
+    }
     __device__ __forceinline__ v4u residual(int64_t i) const {
         uint16_t h[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (g.res && i < g.I && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, n, h);
+        if (g.res && i < g.I && n > 0) load(static_cast<const uint16_t*>(g.res) + i * g.ldres + j, h);
         v4u r;
         __builtin_memcpy(&r, h, 16);
         return r;
@@ -200,7 +216,7 @@ struct Ending {
                 activate8<true>(f, slope, g.act);
                 const v4u w = slope_words(slope);
                 __builtin_memcpy(h, &w, 16);
-                store_up_to<8>(g.slope + at, n, h);
+                store(g.slope + at, h);
             } else {
                 activate8<false>(f, slope, g.act);
             }
@@ -213,7 +229,7 @@ struct Ending {
         }
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] = T::down(f[v]);
-        store_up_to<8>(static_cast<uint16_t*>(g.out) + at, n, h);
+        store(static_cast<uint16_t*>(g.out) + at, h);
     }
 };
 
@@ -230,16 +246,17 @@ __device__ __forceinline__ void store_part(const DenseGemm& g, int64_t split, in
         if (j + v < g.J) out[v] = f[v];
 }
 
-// Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of
-// neighbouring ones, and a run goes down 8 tiles of i before it moves on in j, so that the tiles at work on an XCD share rows of both.
+// Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of neighbouring
+// ones, and a run goes through 4 tiles of j before it moves on in i, so that the tiles at work on an XCD share rows of both and
+// those at work on all of them write whole rows of D.
 __device__ __forceinline__ void place_of(int64_t b, int64_t blocks, int64_t tiles_i, int64_t tiles_j, int64_t& ti, int64_t& tj, int64_t& split) {
     const int64_t q = blocks / 8, r = blocks % 8, xcd = b % 8;
     const int64_t id = xcd * q + (xcd < r ? xcd : r) + b / 8;
     split = id / (tiles_i * tiles_j);
-    const int64_t t = id % (tiles_i * tiles_j), group = t / (8 * tiles_j), first = group * 8;
-    const int64_t size = tiles_i - first < 8 ? tiles_i - first : 8, in = t % (8 * tiles_j);
-    ti = first + in % size;
-    tj = in / size;
+    const int64_t t = id % (tiles_i * tiles_j), group = t / (4 * tiles_i), first = group * 4;
+    const int64_t size = tiles_j - first < 4 ? tiles_j - first : 4, in = t % (4 * tiles_i);
+    tj = first + in % size;
+    ti = in / size;
 }
 
 // kSide x kSide tiles, kWI x kWJ wavefronts
@@ -309,7 +326,7 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     if (j >= g.J) return;
 #pragma unroll
     for (int n = 0; n < kTJ; n += 2) {
-        const Ending<T> end(g, j + 4 * n);
+        const Ending<T, false> end(g, j + 4 * n);
         v4u r[kTI];
 #pragma unroll
         for (int m = 0; m < kTI; ++m) r[m] = end.residual(i0 + m * 16);
@@ -330,7 +347,7 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, cons
     const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t i = id / eights, j = id % eights * 8;
     if (i >= g.I) return;
-    const Ending<T> end(g, j);
+    const Ending<T, false> end(g, j);
     const v4u r = end.residual(i);
     float f[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     for (int s = 0; s < splits; ++s) {
