@@ -8,88 +8,95 @@ namespace adpsgd_impl {
 namespace {
 
 constexpr int kT = 256;
-constexpr int kColumns = 256;           // of a block: 32 threads of eight
-constexpr int kRowsAtOnce = 8;
 
 // dz = dy slope, rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 8 rows of a thread, then 64).
-// Memory: 6 bytes an element.  grid: (ceil(N / 256), strips).
-template <class T>
+// Memory: 6 bytes an element.  kAcross threads of eight columns in a block: 32, or 8 where there is one strip only (64 x 1024: a quarter of
+// the rows for a thread and four times the blocks).  grid: (ceil(N / (8 kAcross)), strips).
+template <class T, int kAcross>
 __global__ __launch_bounds__(kT) void dense_dz_kernel(const uint16_t* dy, int64_t lddy, const uint16_t* slope, uint16_t* dz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
+    constexpr int kColumns = 8 * kAcross, kRowsAtOnce = kT / kAcross;
     __shared__ double at[kRowsAtOnce][kColumns];
-    const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+    const int cx = threadIdx.x % kAcross, ry = threadIdx.x / kAcross;
     const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumns + 8 * cx;
     const int64_t m0 = M * blockIdx.y / gridDim.y, m1 = M * (blockIdx.y + 1) / gridDim.y;
-    const bool whole = j + 8 <= N;
     double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int64_t first = m0 + ry; first < m1; first += 4 * kRowsAtOnce) {
-        float part[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        v4u d[4], w[4];
+    // Four rows at a time; rows beyond the strip are its last one again and count nothing, so that no load stands behind a condition
+    // (there they are waited for together with the stores before).
+    auto rows = [&](auto whole_columns) {
+        constexpr bool kWhole = decltype(whole_columns)::value;
+        auto load = [&](const uint16_t* p) {
+            if (kWhole) return static_cast<v4u>(__builtin_nontemporal_load(reinterpret_cast<const v4u_any*>(p)));
+            v8h h = {0, 0, 0, 0, 0, 0, 0, 0};
+            for (int i = 0; i < 8; ++i)
+                if (j + i < N) h[i] = p[i];
+            return __builtin_bit_cast(v4u, h);
+        };
+        for (int64_t first = m0 + ry; first < m1; first += 4 * kRowsAtOnce) {
+            float part[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            v4u d[4], w[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t m = first + u * kRowsAtOnce;
-            d[u] = w[u] = v4u{0, 0, 0, 0};
-            if (m >= m1 || j >= N) continue;
-            if (whole) {
-                d[u] = *reinterpret_cast<const v4u_any*>(dy + m * lddy + j);
-                if (slope) w[u] = *reinterpret_cast<const v4u_any*>(slope + m * N + j);
-            } else {
-                v8h a = {0, 0, 0, 0, 0, 0, 0, 0}, b = a;
-                for (int i = 0; i < 8; ++i)
-                    if (j + i < N) {
-                        a[i] = dy[m * lddy + j + i];
-                        if (slope) b[i] = slope[m * N + j + i];
+            for (int u = 0; u < 4; ++u) {
+                const int64_t m = first + u * kRowsAtOnce < m1 ? first + u * kRowsAtOnce : m1 - 1;
+                d[u] = load(dy + m * lddy + j);
+                if (slope) w[u] = load(slope + m * N + j);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t m = first + u * kRowsAtOnce;
+                if (m >= m1) break;
+                float f[8];
+                unpack8<T>(d[u], f);
+                if (slope) {
+                    const v8h s = __builtin_bit_cast(v8h, w[u]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] *= slope_of(s[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) part[i] += f[i];
+                if (dz) {
+                    const v4u p = pack8<T>(f);
+                    if (kWhole) {
+                        *reinterpret_cast<v4u_any*>(dz + m * N + j) = p;
+                    } else {
+                        const v8h h = __builtin_bit_cast(v8h, p);
+                        for (int i = 0; i < 8; ++i)
+                            if (j + i < N) dz[m * N + j + i] = h[i];
                     }
-                d[u] = __builtin_bit_cast(v4u, a);
-                w[u] = __builtin_bit_cast(v4u, b);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t m = first + u * kRowsAtOnce;
-            if (m >= m1 || j >= N) continue;
-            float f[8];
-            unpack8<T>(d[u], f);
-            if (slope) {
-                const v8h s = __builtin_bit_cast(v8h, w[u]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= slope_of(s[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) part[i] += f[i];
-            if (dz) {
-                const v4u p = pack8<T>(f);
-                if (whole) {
-                    *reinterpret_cast<v4u_any*>(dz + m * N + j) = p;
-                } else {
-                    const v8h h = __builtin_bit_cast(v8h, p);
-                    for (int i = 0; i < 8; ++i)
-                        if (j + i < N) dz[m * N + j + i] = h[i];
                 }
             }
-        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += static_cast<double>(part[i]);
-    }
+            for (int i = 0; i < 8; ++i) sum[i] += static_cast<double>(part[i]);
+        }
+    };
+    if (j + 8 <= N) rows(std::true_type());
+    else if (j < N) rows(std::false_type());
     if (!sums && !db) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) at[ry][8 * cx + i] = sum[i];
     __syncthreads();
     const int64_t column = static_cast<int64_t>(blockIdx.x) * kColumns + threadIdx.x;
-    if (column < N) {
+    if (static_cast<int>(threadIdx.x) < kColumns && column < N) {
         double s = 0.0;
         for (int r = 0; r < kRowsAtOnce; ++r) s += at[r][threadIdx.x];
         if (db) db[column] = T::down(static_cast<float>(s));        // the only strip
         else sums[blockIdx.y * N + column] = s;
     }
 }
+// Sums of the strips, four threads a column.  grid: ceil(N / 64).
 template <class T>
 __global__ __launch_bounds__(kT) void dense_db_kernel(const double* sums, int strips, int64_t N, uint16_t* db) {
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x;
-    if (j >= N) return;
+    __shared__ double at[4][64];
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
+    const int part = threadIdx.x >> 6;
     double s = 0.0;
-    for (int r = 0; r < strips; ++r) s += sums[r * N + j];
-    db[j] = T::down(static_cast<float>(s));
+    if (j < N) {
+#pragma unroll 8
+        for (int r = part; r < strips; r += 4) s += sums[r * N + j];
+    }
+    at[part][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (part == 0 && j < N) db[j] = T::down(static_cast<float>(((s + at[1][threadIdx.x]) + at[2][threadIdx.x]) + at[3][threadIdx.x]));
 }
 
 // Strips of 256 rows, as many as 64: with N = 8192 four blocks for a compute unit.
@@ -98,11 +105,13 @@ int strips_of(int64_t M) { return static_cast<int>(std::min<int64_t>((M + 255) /
 template <class T>
 void launch_dz_of(const void* dy, int64_t lddy, const uint16_t* slope, void* dz, void* db, double* sums, int64_t M, int64_t N, hipStream_t s) {
     const int strips = strips_of(M);
-    if (strips > 0)
-        hipLaunchKernelGGL(dense_dz_kernel<T>, dim3(static_cast<uint32_t>((N + kColumns - 1) / kColumns), strips), dim3(kT), 0, s,
-                           static_cast<const uint16_t*>(dy), lddy, slope, static_cast<uint16_t*>(dz), db ? sums : nullptr,
-                           strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
-    if (db && strips != 1) hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + kT - 1) / kT)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
+    auto go = [&](auto kernel, int64_t columns) {
+        hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((N + columns - 1) / columns), strips), dim3(kT), 0, s, static_cast<const uint16_t*>(dy), lddy, slope,
+                           static_cast<uint16_t*>(dz), db ? sums : nullptr, strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
+    };
+    if (strips == 1) go(dense_dz_kernel<T, 8>, 64);
+    else if (strips > 1) go(dense_dz_kernel<T, 32>, 256);
+    if (db && strips != 1) hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + 63) / 64)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
 }
 
 }  // namespace
@@ -121,15 +130,18 @@ namespace {
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
-// The estimate of a cut, in microseconds, from measured steps of 64 k.  256: 1.45 us a step of a block that has a compute unit for itself and
-// 12 at both ends; 128: 0.75 with two blocks on a compute unit, and 8; 64: 0.8 with four, and 5.  Parts of k are written and read in 32 bits.
+// The estimate of a cut, in microseconds, from measured calls: a step of 64 k of a block, with so many of them on a compute unit, and both ends
+// of a block.  Tiles of 256 take 1.5 a step and 24; of 128 0.65 alone and 1.0 by two, and 6; of 64 0.5 alone to 0.93 by four, and 3.
+// Against 4096^3: 120 (measured 125), 140 (151) and 260 (260); 2048^3: 72 (50), 27 (29), 33 (35); 1024^3: 48 (33), 16 (14), 11 (10.5);
+// 512 x 8192 x 512 in eight parts of tiles of 64: 20.  Parts of k are written and read in 32 bits at 5 TB/s, and a launch more.
 double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
+    constexpr double kUnits = 256.0;
     const double tiles = static_cast<double>((I + side - 1) / side) * static_cast<double>((J + side - 1) / side) * splits;
     const double steps = static_cast<double>(((K + 63) / 64 + splits - 1) / splits);
-    const int at_once = side == 256 ? 256 : side == 128 ? 512 : 1024;
-    const double step = side == 256 ? 1.45 : side == 128 ? 0.75 : 0.8, ends = side == 256 ? 12.0 : side == 128 ? 8.0 : 5.0;
-    const double turns = std::max(1.0, tiles / at_once);                       // the last blocks are not all there at once, but they are faster
-    return turns * (steps * step + ends) + (splits > 1 ? 4.0 + 8.0 * splits * static_cast<double>(I) * static_cast<double>(J) / 4e6 : 0.0);
+    const double most = side == 256 ? 1.0 : side == 128 ? 2.0 : 4.0, ends = side == 256 ? 24.0 : side == 128 ? 6.0 : 3.0;
+    const double together = std::min(most, std::max(1.0, tiles / kUnits)), turns = std::max(1.0, tiles / (kUnits * most));
+    const double step = side == 256 ? 1.5 : side == 128 ? 0.30 + 0.35 * together : 0.357 + 0.143 * together;
+    return turns * (steps * step + ends) + (splits > 1 ? 4.0 + 8.0 * splits * static_cast<double>(I) * static_cast<double>(J) / 5e6 : 0.0);
 }
 // `rows`: A has k inner.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
 DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool rows, bool direct) {
@@ -170,7 +182,7 @@ __global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, in
 
 bool whole_pieces(const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; }
 // Copies of operands whose rows are no whole pieces: they pay where the direct tiles do, from about 2^32 products on (2100 x 1030 x 4097:
-// 42 us with the copies, 63 with tiles of 64 from the operands as they are).
+// dx 60 us with the copies, 257 with tiles of 64 from the operands as they are).
 bool worth_packing(int64_t I, int64_t J, int64_t K) { return static_cast<double>(I) * static_cast<double>(J) * static_cast<double>(K) >= 4294967296.0; }
 int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(inner)); }
 
