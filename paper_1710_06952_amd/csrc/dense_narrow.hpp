@@ -1,7 +1,7 @@
 // Products with few rows, D[i][j] = sum_k A(i, k) B(j, k), I <= 64: B is read once and its bytes are the time.
 //
 // A block owns up to 64 columns and all rows; its eight wavefronts take steps of k in turn and their sums are joined through LDS, so a call is
-// one launch.  Matrix operands come from memory straight into registers, no LDS in between: B is used once.
+// one launch, unless columns are few and k is long: then several blocks share the steps, and dense_join_kernel adds their sums.  Matrix operands come from memory straight into registers, no LDS in between: B is used once.
 //   k inner  a lane reads 16 neighbouring k of a row in two loads; four lanes together 128 bytes, a line.  Which 8 of 32 k a lane holds is
 //            of no account as long as A's lanes hold the same.
 //   k outer  a lane reads kV neighbouring j at 8 k (16 lanes 128 or 64 bytes of a k) and exchanges halves of registers, 4 v_perm_b32 a
@@ -37,12 +37,12 @@ __device__ __forceinline__ v2u load_some(const uint16_t* row, int64_t start, int
 
 // kTI: tiles of 16 rows; kV: columns of a lane's operands, 16 kV of a block
 template <class T, bool kBOuter, int kTI, int kV>
-__global__ __launch_bounds__(kNarrowWaves * 64) void dense_narrow_kernel(const DenseGemm g) {
+__global__ __launch_bounds__(kNarrowWaves * 64) void dense_narrow_kernel(const DenseGemm g, const int splits) {
     constexpr int kColumns = 16 * kV, kStep = kBOuter ? 32 : 64, kPitch = kColumns + 4;
     __shared__ __attribute__((aligned(16))) float sums[kNarrowWaves][16 * kTI][kPitch];
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
     int64_t none, tile, split;
-    place_of(blockIdx.x, gridDim.x, 1, gridDim.x, none, tile, split);        // neighbouring columns on one XCD: they share lines where k is outer
+    place_of(blockIdx.x, gridDim.x, 1, gridDim.x / splits, none, tile, split);        // neighbouring columns on one XCD: they share lines where k is outer
     const int64_t j0 = tile * kColumns;
     const uint16_t* a[kTI];
 #pragma unroll
@@ -57,13 +57,13 @@ __global__ __launch_bounds__(kNarrowWaves * 64) void dense_narrow_kernel(const D
         for (int n = 0; n < kV; ++n) acc[m][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     // this wavefront's steps: kTogether at a time, then one by one, and the end of k where it is not a whole step
     constexpr int kTogether = kTI == 1 && !kBOuter ? 4 : 2;
-    const int64_t whole = g.K / kStep;
+    const int64_t whole = g.K / kStep, until = whole * (split + 1) / splits;
     auto walk = [&](auto go) {
-        int64_t s = wave;
-        for (; s + (kTogether - 1) * kNarrowWaves < whole; s += kTogether * kNarrowWaves) go(s, std::integral_constant<int, kTogether>(), std::false_type());
+        int64_t s = whole * split / splits + wave;
+        for (; s + (kTogether - 1) * kNarrowWaves < until; s += kTogether * kNarrowWaves) go(s, std::integral_constant<int, kTogether>(), std::false_type());
 #pragma unroll 1
-        for (; s < whole; s += kNarrowWaves) go(s, std::integral_constant<int, 1>(), std::false_type());
-        if (whole * kStep < g.K && whole % kNarrowWaves == wave) go(whole, std::integral_constant<int, 1>(), std::true_type());
+        for (; s < until; s += kNarrowWaves) go(s, std::integral_constant<int, 1>(), std::false_type());
+        if (whole * kStep < g.K && split + 1 == splits && wave == 0) go(whole, std::integral_constant<int, 1>(), std::true_type());
     };
 
     if constexpr (!kBOuter) {
@@ -155,24 +155,25 @@ __global__ __launch_bounds__(kNarrowWaves * 64) void dense_narrow_kernel(const D
         for (int w = 1; w < kNarrowWaves; ++w)
 #pragma unroll
             for (int v = 0; v < 8; ++v) f[v] += sums[w][i][c + v];
-        end.finish(i, f, r);
+        if (splits > 1) store_part(g, split, i, j0 + c, f);
+        else end.finish(i, f, r);
     }
 }
 
 template <class T, bool kBOuter, int kTI, int kV>
-void launch_narrow_of(const DenseGemm& g, hipStream_t s) {
-    const dim3 grid(static_cast<uint32_t>((g.J + 16 * kV - 1) / (16 * kV)));
-    hipLaunchKernelGGL((dense_narrow_kernel<T, kBOuter, kTI, kV>), grid, dim3(kNarrowWaves * 64), 0, s, g);
+void launch_narrow_of(const DenseGemm& g, int splits, hipStream_t s) {
+    const dim3 grid(static_cast<uint32_t>((g.J + 16 * kV - 1) / (16 * kV) * splits));
+    hipLaunchKernelGGL((dense_narrow_kernel<T, kBOuter, kTI, kV>), grid, dim3(kNarrowWaves * 64), 0, s, g, splits);
 }
 template <class T>
-void launch_narrow(const DenseGemm& g, hipStream_t s) {
+void launch_narrow(const DenseGemm& g, int splits, hipStream_t s) {
     if (g.b_outer) {                                     // lines of 128 bytes where that leaves a block for every compute unit
         const bool wide = g.J >= 64 * 256;
-        if (g.I <= 16) wide ? launch_narrow_of<T, true, 1, 4>(g, s) : launch_narrow_of<T, true, 1, 2>(g, s);
-        else launch_narrow_of<T, true, 4, 2>(g, s);
+        if (g.I <= 16) wide ? launch_narrow_of<T, true, 1, 4>(g, splits, s) : launch_narrow_of<T, true, 1, 2>(g, splits, s);
+        else launch_narrow_of<T, true, 4, 2>(g, splits, s);
     } else {                                             // every block reads all of A: more columns where that is not little
-        if (g.I <= 16) launch_narrow_of<T, false, 1, 1>(g, s);
-        else launch_narrow_of<T, false, 4, 2>(g, s);
+        if (g.I <= 16) launch_narrow_of<T, false, 1, 1>(g, splits, s);
+        else launch_narrow_of<T, false, 4, 2>(g, splits, s);
     }
 }
 

@@ -145,8 +145,11 @@ double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
 }
 // `rows`: A has k inner.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
 DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool rows, bool direct) {
-    if (rows && I <= 64) return DensePlan{0, 1};
     const int64_t steps = std::max<int64_t>(1, (K + 63) / 64);
+    if (rows && I <= 64) {               // a wavefront's steps of 64 k take 1 to 2 us each with few blocks: shared from eight on (47 x 477 x 6060: dx 52 to 16 us)
+        const int64_t blocks = (J + 31) / 32, shares = std::min<int64_t>(std::min<int64_t>(256 / blocks, steps / 16), 32);
+        return DensePlan{0, steps >= 64 && shares > 1 ? static_cast<int>(shares) : 1};
+    }
     DensePlan best{64, 1};
     double least = 1e30;
     for (int side : {64, 128, 256}) {
@@ -192,6 +195,7 @@ int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(
 int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
     int64_t parts = 0;
     for (bool direct : {false, true}) parts = std::max<int64_t>(parts, plan_of(I, J, K, false, direct).splits);
+    parts = std::max<int64_t>(parts, plan_of(I, J, K, true, false).splits);
     const bool pack = (I % 8 || J % 8 || K % 8) && worth_packing(I, J, K);
     const int64_t copies = pack ? std::max(packed_bytes(I, K), packed_bytes(K, I)) + std::max(packed_bytes(J, K), packed_bytes(K, J)) : 0;
     return (parts > 1 ? up256(parts * I * J * static_cast<int64_t>(sizeof(float))) : 0) + copies;

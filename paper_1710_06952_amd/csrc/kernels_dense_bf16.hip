@@ -16,11 +16,8 @@ void launch_tiles_of(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
 
 template <class T>
 void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s) {
-    if (p.side == 0) {
-        launch_narrow<T>(g, s);
-        return;
-    }
-    if (g.a_outer) launch_tiles_of<T, true, true>(g, p, s);
+    if (p.side == 0) launch_narrow<T>(g, p.splits, s);
+    else if (g.a_outer) launch_tiles_of<T, true, true>(g, p, s);
     else if (g.b_outer) launch_tiles_of<T, false, true>(g, p, s);
     else launch_tiles_of<T, false, false>(g, p, s);
     if (p.splits > 1)

@@ -13,7 +13,7 @@ ACTS = ["none", "relu", "gelu", "silu"]
 # (M, K, N): one of everything, odd sizes, ends inside tiles and vectors, few rows, split sums, tiles of 64, 128 and 256
 SIZES = [(1, 1, 1), (1, 8, 64), (3, 7, 5), (2, 64, 9), (16, 8, 520), (64, 784, 1024), (130, 257, 391), (257, 63, 129), (300, 1000, 10), (33, 2049, 65),
          (1, 4096, 768), (5, 4100, 72), (40, 6, 1000), (1100, 200, 2000), (1101, 203, 2001), (2049, 72, 4100), (2100, 1030, 4097), (2056, 72, 4104),
-         (2952, 2824, 3096), (1701, 1703, 1705), (256, 8192, 256), (520, 4096, 392), (72, 1024, 8192), (8192, 136, 264)]
+         (2952, 2824, 3096), (1701, 1703, 1705), (256, 8192, 256), (520, 4096, 392), (72, 1024, 8192), (8192, 136, 264), (47, 6060, 477), (3, 8191, 66), (64, 5000, 40)]
 
 
 def half(t):
