@@ -151,6 +151,9 @@ struct Kept {
     uint32_t m, v;
     int km, kv;
 };
+// kAgain: the values may be what a state stood for, and are kept as they are then.  Its largest may be a code that was rounded up to 256; with
+// the exponent one higher that 256 gives, the smallest codes of its block would not all be there.
+template <bool kAgain>
 __device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
     const v4f m32 = rounded(m), v32 = rounded(v);
     float top_m = wave_largest(m32), top_v = wave_largest(v32);
@@ -160,8 +163,13 @@ __device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
         top_v = wave_largest(finite_or_0(v32));
     }
     Kept k;
-    k.km = scale_exponent(exponent_of(top_m));
-    k.kv = scale_exponent(top_v > 0.0f ? exponent_of(top_v) >> 1 : -1);     // floor(log2 sqrt v)
+    int em = exponent_of(top_m), ev = exponent_of(top_v);
+    if (kAgain) {                                        // 2^n as if it were a little less
+        if (top_m > 0.0f && ldexpf(1.0f, em) == top_m) --em;
+        if (top_v > 0.0f && ldexpf(1.0f, ev) == top_v) --ev;
+    }
+    k.km = scale_exponent(em);
+    k.kv = scale_exponent(top_v > 0.0f ? ev >> 1 : -1);     // floor(log2 sqrt v)
     k.m = k.v = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -311,7 +319,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
             const v4u words = philox4x32_rounds<10>(static_cast<uint32_t>(lane), static_cast<uint32_t>(lane >> 32), static_cast<uint32_t>(a.step),
                                                     (static_cast<uint32_t>(a.step >> 32) & 0x00FFFFFFu) | kStreamMoments,
                                                     philox_keys<10>(static_cast<uint32_t>(a.seed), static_cast<uint32_t>(a.seed >> 32)));
-            const Kept k = kept_of(m64, v64, words);
+            const Kept k = kept_of<false>(m64, v64, words);
             __builtin_nontemporal_store(k.m, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.m) + at));
             __builtin_nontemporal_store(k.v, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v) + at));
             if ((threadIdx.x & 63) == 0)
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(kT) void adamw_set_kernel(const float* m, const flo
     if (at >= length) return;                            // whole wavefronts: the length is a multiple of 256
     const v4u half = {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};      // (word + 1/2) / 2^16 just under 1/2: to the nearest
     const v4f x = TypeF32::load4(m, at), y = TypeF32::load4(v, at);
-    const Kept k = kept_of(v4d{x.x, x.y, x.z, x.w}, v4d{y.x, y.y, y.z, y.w}, half);
+    const Kept k = kept_of<true>(v4d{x.x, x.y, x.z, x.w}, v4d{y.x, y.y, y.z, y.w}, half);
     *reinterpret_cast<uint32_t*>(m_out + at) = k.m;
     *reinterpret_cast<uint32_t*>(v_out + at) = k.v;
     if ((threadIdx.x & 63) == 0) {

@@ -189,6 +189,25 @@ def test_stored_state_goes_on_as_if_it_had_not_been_stored():
         assert all(torch.equal(p, q) for p, q in zip(b.opt.moments(), c.opt.moments())) and c.opt.steps == 5
 
 
+def test_loaded_moments_are_kept_as_they_are():
+    """What a state stands for comes back from load_moments bit for bit, blocks among it whose largest value was rounded up."""
+    import torch
+    import paper_1710_06952_amd as P
+    n = 256 * 200
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(11)
+    grad = torch.randn(n, generator=g, device="cuda:0") * torch.exp(4 * torch.randn(n, generator=g, device="cuda:0"))
+    grad.view(-1, 256)[:50, 7] = 255.9 * 2.0 ** torch.randint(5, 9, (50,), generator=g, device="cuda:0")      # the largest, just under a power of two
+    a, b = (P.AdamW([torch.zeros(n, device="cuda:0")], [grad], state_bits=8, betas=(0.0, 0.0)) for _ in range(2))
+    a.step()
+    m, v = a.moments()
+    top = m.float().abs().view(-1, 256).amax(1)
+    assert (torch.frexp(top)[0] == 0.5).any()            # powers of two are among the largest values
+    for mt, vt in ((m, v), (m.float(), v.float())):
+        b.load_moments(mt, vt, 1)
+        assert all(torch.equal(p, q) for p, q in zip(b.moments(), (m, v)))
+
+
 def test_gradients_that_are_not_finite():
     import torch
     for bits in (32, 8):

@@ -205,7 +205,9 @@ def test_rows_that_cannot_be_answered():
             print(V, dtype, flush=True)
             z = torch.randn(8, V, device="cuda:0").to(dtype)
             tokens = torch.arange(8, device="cuda:0")
+            one = torch.ones(8, device="cuda:0")
             good = P.token_log_probs(z, tokens)
+            before = P.policy_loss_and_gradient(z, tokens, good, one).log_probs
             z[1] = -math.inf
             z[2, 2] = -math.inf
             tokens[3] = V
@@ -213,10 +215,9 @@ def test_rows_that_cannot_be_answered():
             z[5, 9] = math.inf
             got = P.token_log_probs(z, tokens)
             assert torch.isnan(got[[1, 3, 4, 5]]).all() and got[2] == -math.inf and torch.equal(got[[0, 6, 7]], good[[0, 6, 7]])
-            one = torch.ones(8, device="cuda:0")
             r = P.policy_loss_and_gradient(z, tokens, good, one)
             assert torch.isnan(r.loss) and torch.isnan(r.dlogits[[1, 3, 4, 5]]).any(1).all()
-            assert torch.isfinite(r.dlogits[[0, 2, 6, 7]]).all() and torch.equal(r.log_probs[[0, 6, 7]], good[[0, 6, 7]])
+            assert torch.isfinite(r.dlogits[[0, 2, 6, 7]]).all() and torch.equal(r.log_probs[[0, 6, 7]], before[[0, 6, 7]])
             tokens[[1, 3, 4, 5]] = -1                    # not counted: nothing of them is left
             r = P.policy_loss_and_gradient(z, tokens, good, one)
             assert torch.isfinite(r.loss) and torch.isfinite(r.dlogits).all() and not r.dlogits[[1, 3, 4, 5]].any()
