@@ -12,6 +12,11 @@
 //     request step s + 2 from memory into the place of step s;  request half 0 of step s + 1 from LDS;  multiply half 1.
 // The pieces of 16 bytes are exchanged as in dense_tiles.hpp, here by the addresses that the lanes load from.
 //
+// Bound: the matrix cores, at the clock that their power leaves.  8192^3 in bf16 takes 850 us, 1.30 PFLOP/s (a library's product 680 to 790); a tile
+// of 256 takes 1.45 us a step, 1.5 PFLOP/s over the chip, and 24 us at its ends, which with four tiles of K = 2048 for a compute unit
+// are a third of the time (274 us; with gelu, slopes and a residual 345: the activation is 20 instructions an element).  Two blocks on a
+// compute unit would hide the ends, but tiles of 128 take 1.4 times as long for the same products: their fragments come from LDS twice as often.
+//
 // What lies beyond the ends: rows of an operand with k inner are the last row again; pieces beyond the end of k, and rows of k beyond the
 // end where k is outer, are out of the buffer's range, for which the load delivers zeros.
 #pragma once
@@ -23,11 +28,13 @@ namespace {
 
 typedef uint32_t v4su __attribute__((ext_vector_type(4)));
 
-// 16 bytes a lane from `rsrc` + offset to LDS at `lds` + 16 lane.  No register is written; the wait is `wait_loads`.
+// 16 bytes a lane from `rsrc` + offset to LDS at `lds` + 16 lane.  No register is written; the wait is `wait_loads`.  Between the write of M0
+// and the load that reads it the hardware wants another instruction.
 __device__ __forceinline__ void load_to_lds(v4su rsrc, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(rsrc), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(offset), "s"(rsrc), "s"(lds) : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+// ... and for this wavefront's reads of the LDS that the next loads go to.
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }
 
 // 16 bytes from accumulation registers to LDS: written out, as the compiler would copy all results to vector registers in front of the loop.
 __device__ __forceinline__ void write_result(uint32_t lds, v4f c) { asm volatile("ds_write_b128 %0, %1" : : "v"(lds), "a"(c) : "memory"); }

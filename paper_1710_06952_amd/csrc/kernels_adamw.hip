@@ -3,11 +3,14 @@
 //   g' = f g;  m = b1 m + (1 - b1) g';  v = b2 v + (1 - b2) g'^2;  u = (m / c1) / (sqrt(v / c2) + eps);  p = p - lr (u + wd p)
 //
 // A table cuts the tensors into chunks of up to 4096 elements, one thread block each: a model of many small tensors is one grid, as a
-// single large tensor is.  A whole chunk has no condition in front of its loads, so that all are on their way at once.  A wavefront takes 256 consecutive elements at a time, four a lane, which is the block of elements that
-// shares an exponent where the state has 8 bits: its largest magnitude is a reduction over the wavefront.
+// single large tensor is.  A whole chunk has no condition in front of its loads, so that all are on their way at once.  A wavefront
+// takes 256 consecutive elements at a time, four a lane, which is the block of elements that shares an exponent where the state has 8
+// bits: its largest magnitude is a reduction over the wavefront.
 //
 // Bound: memory, 28 bytes an element with everything in 32 bits (gradient 4, parameter 8, moments 16), 16 with bf16 parameters and
 // gradients, fp32 masters and 8-bit moments.  With clipping the gradients are read once more before that, by adamw_norm_kernel.
+// Measured: 25.6 M parameters in 32 bits 118 us (6.1 TB/s) and 16 + 5 for the norm; 67 M with 8-bit moments 187 to 235 us (5.7 to 4.6 TB/s:
+// 440 instructions for four elements a lane are as long as their bytes) and 28 + 5 for the norm.
 //
 // 8 bits.  A block's scale is 2^k, so that its largest value y 2^k has 128 <= y < 256 (k >= -50).  The codes are e4m3, not
 // negative: between two neighbours lo and hi the share of the way is
