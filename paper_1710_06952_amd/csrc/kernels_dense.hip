@@ -146,7 +146,7 @@ double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
 // `rows`: A has k inner.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
 DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool rows, bool direct) {
     const int64_t steps = std::max<int64_t>(1, (K + 63) / 64);
-    if (rows && I <= 64) {               // a wavefront's steps of 64 k take 1 to 2 us each with few blocks: shared from eight on (47 x 477 x 6060: dx 52 to 16 us)
+    if (rows && I <= 64) {               // a wavefront's steps of 64 k take 1 to 2 us each with few blocks: shared from eight on (47 x 477 x 6060: dx 52 to 24 us)
         const int64_t blocks = (J + 31) / 32, shares = std::min<int64_t>(std::min<int64_t>(256 / blocks, steps / 16), 32);
         return DensePlan{0, steps >= 64 && shares > 1 ? static_cast<int>(shares) : 1};
     }

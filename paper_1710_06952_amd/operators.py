@@ -30,12 +30,13 @@ PreferenceLoss = namedtuple("PreferenceLoss", "loss dlogits log_probs margins")
 
 
 def _call(device, fn, *args):
-    """One library call on the device's current stream."""
+    """One library call on the device's current stream.  The stream is asked for as the number it is: a Stream object takes
+    2.5 us to make, a sixth of what the smallest calls take in all."""
     if torch.cuda.current_device() == device.index:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     if rc != B.OK:
         raise B.AdpsgdError(rc, (B.lib().adpsgd_last_error(None) or b"").decode())
 
