@@ -125,6 +125,7 @@ __device__ __forceinline__ uint32_t moment_code(double m, int k, uint32_t word) 
     const uint32_t sign = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, m) >> 63) << 7;
     return sign | code;
 }
+// v finite and not negative: another one has no code of seven bits, and its upper bits would be those of the next element.
 __device__ __forceinline__ uint32_t square_code(double v, int k, uint32_t word) {
     const double y2 = __builtin_amdgcn_ldexp(v, -2 * k);
     const float y = __builtin_amdgcn_sqrtf(static_cast<float>(y2));     // a step too far or too short is made good by the share
@@ -164,6 +165,9 @@ __device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
     if (!all_finite) {
         top_m = wave_largest(finite_or_0(m32));
         top_v = wave_largest(finite_or_0(v32));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (!(v32[i] < INFINITY)) v[i] = 0.0;
     }
     Kept k;
     int em = exponent_of(top_m), ev = exponent_of(top_v);

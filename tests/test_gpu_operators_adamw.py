@@ -269,3 +269,30 @@ def test_capture_is_refused_and_other_streams_work():
     a.opt.close()
     with pytest.raises(RuntimeError, match="closed"):
         a.opt.step()
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan, 1e25])
+@pytest.mark.parametrize("place", range(4))
+def test_a_moment_that_is_not_finite_leaves_its_neighbours(place, value):
+    """In 8 bits, four elements share a word: the codes of the other three are those of a run without it."""
+    import torch
+    import paper_1710_06952_amd as P
+    n = 768
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(place)
+    grad = 0.01 * torch.randn(n, generator=g, device="cuda:0")
+    at = 256 + 4 * 7 + place
+    grad[at] = 0.0
+    bad = grad.clone()
+    bad[at] = value
+    a, b = (P.AdamW([torch.zeros(n, device="cuda:0")], [x], state_bits=8, seed=3) for x in (grad, bad))
+    others = torch.arange(n, device="cuda:0") != at
+    for _ in range(3):
+        a.step()
+        b.step()
+        (m, v), (mb, vb) = a.moments(), b.moments()
+        assert torch.isnan(vb[at]) and torch.equal(v[others], vb[others])
+        assert value == 1e25 or (torch.isnan(mb[at]) and torch.equal(m[others], mb[others]))      # a finite m sets its block's exponent
+    c = P.AdamW([torch.zeros(n, device="cuda:0")], [bad], state_bits=8, seed=3)
+    c.load_moments(mb, vb, 3)
+    assert all(torch.equal(p.nan_to_num(77.0), q.nan_to_num(77.0)) for p, q in zip(c.moments(), (mb, vb)))
