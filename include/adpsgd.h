@@ -575,7 +575,7 @@ int adpsgd_adamw_get_steps(const adpsgd_adamw_t* h, int64_t* out);
 int adpsgd_adamw_set_steps(adpsgd_adamw_t* h, int64_t steps);
 
 /* state_bits 8: the values that the state stands for, state_length bf16 each (which hold them exactly), and the state from fp32
- * values, each to the nearest (ADPSGD_ERR_STATE with 32). */
+ * values, each to the nearest; a v under 0 is kept as NaN (ADPSGD_ERR_STATE with 32). */
 int adpsgd_adamw_get_moments(adpsgd_adamw_t* h, uint16_t* m, uint16_t* v, void* stream);
 int adpsgd_adamw_set_moments(adpsgd_adamw_t* h, const float* m, const float* v, void* stream);
 

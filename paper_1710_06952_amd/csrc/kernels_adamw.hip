@@ -369,7 +369,10 @@ __global__ __launch_bounds__(kT) void adamw_set_kernel(const float* m, const flo
     const int64_t at = 4 * (static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x);
     if (at >= length) return;                            // whole wavefronts: the length is a multiple of 256
     const v4u half = {0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu};      // (word + 1/2) / 2^16 just under 1/2: to the nearest
-    const v4f x = TypeF32::load4(m, at), y = TypeF32::load4(v, at);
+    const v4f x = TypeF32::load4(m, at);
+    v4f y = TypeF32::load4(v, at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.0f ? NAN : y[i];         // what its root is
     const Kept k = kept_of<true>(v4d{x.x, x.y, x.z, x.w}, v4d{y.x, y.y, y.z, y.w}, half);
     *reinterpret_cast<uint32_t*>(m_out + at) = k.m;
     *reinterpret_cast<uint32_t*>(v_out + at) = k.v;

@@ -296,3 +296,16 @@ def test_a_moment_that_is_not_finite_leaves_its_neighbours(place, value):
     c = P.AdamW([torch.zeros(n, device="cuda:0")], [bad], state_bits=8, seed=3)
     c.load_moments(mb, vb, 3)
     assert all(torch.equal(p.nan_to_num(77.0), q.nan_to_num(77.0)) for p, q in zip(c.moments(), (mb, vb)))
+
+
+def test_loaded_squares_under_zero_are_kept_as_nan():
+    import torch
+    import paper_1710_06952_amd as P
+    p = torch.zeros(256, device="cuda:0")
+    opt = P.AdamW([p], [p.clone()], state_bits=8)
+    m, v = torch.ones(256, device="cuda:0"), torch.ones(256, device="cuda:0")
+    v[9] = -300.0
+    opt.load_moments(m, v, 1)
+    got = opt.moments()
+    assert torch.isnan(got[1][9]) and int(torch.isnan(got[1]).sum()) == 1 and torch.equal(got[0].float(), m)
+    assert (got[1].float()[torch.arange(256, device="cuda:0") != 9] == 1.0).all()
