@@ -260,7 +260,7 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
             state += (n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock;
         }
         const size_t cb = chunks.size() * sizeof(AdamwChunk);
-        const size_t own = kAdamwNormBlocks * sizeof(double) + 4 * sizeof(float);
+        const size_t own = (kAdamwNormBlocks + 1) * sizeof(double) + sizeof(float);
         std::vector<char> image(cb + own, 0);
         if (cb) std::memcpy(image.data(), chunks.data(), cb);
         adpsgd_adamw* h = new adpsgd_adamw;
@@ -275,8 +275,8 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
         h->a.chunks = reinterpret_cast<const AdamwChunk*>(at);
         h->a.n_chunks = static_cast<int64_t>(chunks.size());
         h->a.norm_parts = reinterpret_cast<double*>(at + cb);
-        h->a.factor = reinterpret_cast<float*>(at + cb + kAdamwNormBlocks * sizeof(double));
-        h->own_norm = h->a.factor + 1;
+        h->a.factor = h->a.norm_parts + kAdamwNormBlocks;
+        h->own_norm = reinterpret_cast<float*>(h->a.factor + 1);
         h->a.param_type = o->param_type;
         h->a.grad_type = o->grad_type;
         h->a.bits = o->state_bits;
@@ -324,6 +324,7 @@ extern "C" int adpsgd_adamw_step(adpsgd_adamw_t* h, double lr, double max_norm, 
         AdamwArgs a = h->a;
         a.lr = static_cast<float>(lr);
         a.grad_scale = static_cast<float>(grad_scale);
+        a.grad_scale_64 = grad_scale;
         a.max_norm = max_norm;
         a.norm = norm ? norm : h->own_norm;
         const int64_t t = h->steps + 1;

@@ -115,7 +115,7 @@ constexpr uint32_t kNanCode = 0x7F;
 
 __device__ __forceinline__ float value_of(uint32_t code) { return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(code), 0); }
 // The draw decides by 2^-16 of a step, and a 32-bit m is off by up to 2^-20 of one: one element in a million would go the other way.
-// So moments are added in 64 bits here, of which the upper word is enough: 20 bits of fraction, 3 of them the code's, and what the other
+// So gradients are scaled and moments added in 64 bits here, of which the upper word is enough: 20 bits of fraction, 3 of them the code's, and what the other
 // 17 come to with 2 word + 1 is the carry.
 __device__ __forceinline__ uint32_t moment_code(double m, int k, uint32_t word) {
     const double y = __builtin_amdgcn_ldexp(fabs(m), -k);
@@ -207,17 +207,17 @@ __device__ __forceinline__ double block_sum(double x, double* at) {
     return x;
 }
 // The gradients' norm and their factor from the blocks' sums, to all threads.
-__device__ __forceinline__ float factor_of(const AdamwArgs& a, double* at, float& norm) {
+__device__ __forceinline__ double factor_of(const AdamwArgs& a, double* at, float& norm) {
     double sum = 0.0;
     for (int b = threadIdx.x; b < a.norm_blocks; b += kT) sum += a.norm_parts[b];
-    const double of = sqrt(block_sum(sum, at)) * fabs(static_cast<double>(a.grad_scale)), f = a.max_norm / (of + 1e-6);
+    const double of = sqrt(block_sum(sum, at)) * fabs(a.grad_scale_64), f = a.max_norm / (of + 1e-6);
     norm = static_cast<float>(of);
-    return static_cast<float>(f > 1.0 ? 1.0 : f);                    // NaN stays
+    return f > 1.0 ? 1.0 : f;                            // NaN stays
 }
 __global__ __launch_bounds__(kT) void adamw_factor_kernel(const AdamwArgs a) {
     __shared__ double at[kT / 64];
     float norm;
-    const float f = factor_of(a, at, norm);
+    const double f = factor_of(a, at, norm);
     if (threadIdx.x == 0) {
         *a.norm = norm;
         *a.factor = f;
@@ -274,7 +274,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
             }
         }
     }
-    float f = 1.0f;                                       // the loads are on their way
+    double f = 1.0;                                       // the loads are on their way
     if (a.max_norm > 0.0) {
         if (a.norm_blocks <= kT) {
             float norm;
@@ -284,6 +284,8 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
             f = *a.factor;
         }
     }
+    const float f32 = static_cast<float>(f);
+    const double scale = a.grad_scale_64 * f;
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
         const int e = first + u * kT * kPerThread;
@@ -295,7 +297,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
             const v4f m_old = moments_of(m8[u], static_cast<int8_t>(k8[u] & 0xFF)), v_old = squares_of(v8[u], static_cast<int8_t>(k8[u] >> 8));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const double gi = g[u][i] * a.grad_scale * f;
+                const double gi = scale * static_cast<double>(g[u][i]);
                 m64[i] = fma(a.beta1_64, static_cast<double>(m_old[i]), a.rest1_64 * gi);
                 v64[i] = fma(a.beta2_64, static_cast<double>(v_old[i]), a.rest2_64 * gi * gi);
             }
@@ -304,7 +306,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float gi = g[u][i] * a.grad_scale * f;
+                const float gi = g[u][i] * a.grad_scale * f32;
                 m[i] = fmaf(a.beta1, m32[u][i], a.rest1 * gi);
                 v[i] = fmaf(a.beta2, v32[u][i], a.rest2 * gi * gi);
             }

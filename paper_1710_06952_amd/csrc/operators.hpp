@@ -66,11 +66,11 @@ struct AdamwArgs {
     double beta1_64, beta2_64, rest1_64, rest2_64;
     float beta1, beta2, rest1, rest2, eps, lr, inv_c1, inv_c2;     // rest: 1 - beta, inv_c: 1 / (1 - beta^step)
     float grad_scale;
-    double max_norm;
+    double grad_scale_64, max_norm;
     uint64_t seed, step;
     double* norm_parts;             // kAdamwNormBlocks ...
     int32_t norm_blocks;            // ... of which so many are used
-    float* factor;                  // of the gradients in this step
+    double* factor;                 // of the gradients in this step
     float* norm;
 };
 constexpr int kAdamwNormBlocks = 2048;      // eight for a compute unit: all are there at once
