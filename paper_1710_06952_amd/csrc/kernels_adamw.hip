@@ -177,6 +177,8 @@ __device__ __forceinline__ Kept kept_of(v4d m, v4d v, v4u words) {
     }
     k.km = scale_exponent(em);
     k.kv = scale_exponent(top_v > 0.0f ? ev >> 1 : -1);     // floor(log2 sqrt v)
+    if (top_v == 0.0f && __ballot(v[0] > 0.0 || v[1] > 0.0 || v[2] > 0.0 || v[3] > 0.0) != 0)
+        k.kv = scale_exponent(-75);                      // squares that 32 bits do not hold are no block of zeros
     k.m = k.v = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

@@ -344,3 +344,16 @@ def test_draws_decide_as_in_64_bits():
     off = int((opt.moments()[0].double() != want).sum())
     print(off, "differ", flush=True)
     assert off == 0
+
+
+def test_squares_that_32_bits_do_not_hold():
+    """A block whose squares are all under 2^-149 has the smallest scale, 2^-50, not that of a block of zeros."""
+    import torch
+    import paper_1710_06952_amd as P
+    g = torch.zeros(512, device="cuda:0")
+    g[:256] = 1e-24
+    g[300] = 1e-24
+    opt = P.AdamW([torch.zeros(512, device="cuda:0")], [g], state_bits=8)
+    opt.step()
+    v = opt.moments()[1].double()
+    assert (v[g != 0] == 2.0 ** -118).all() and not v[g == 0].any()
