@@ -552,7 +552,7 @@ typedef struct {
     float* const* masters;           /* host, or NULL                                                        */
     float* const* out;               /* host, or NULL                                                        */
     const float* weight_decay;       /* host: of each tensor                                                 */
-    double beta1, beta2, eps;        /* 0 <= beta < 1, eps > 0                                               */
+    double beta1, beta2, eps;        /* 0 <= beta < 1, eps >= 2^-126                                       */
     uint64_t seed;
     void* m;                         /* state_bits 32: state_length floats, 8: state_length bytes; zero at the start ... */
     void* v;

@@ -234,7 +234,7 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
         if (o->tensors < 0 || !is_type(o->param_type) || !is_type(o->grad_type)) return refuse("adamw: unknown type, or a negative number of tensors");
         if (o->state_bits != 8 && o->state_bits != 32) return refuse("adamw: state_bits must be 8 or 32");
         if (!(o->beta1 >= 0.0 && o->beta1 < 1.0 && o->beta2 >= 0.0 && o->beta2 < 1.0 && o->eps > 0.0 && o->eps < INFINITY)) return refuse("adamw: 0 <= beta < 1 and eps > 0");
-        if (!(static_cast<float>(o->eps) > 0.0f)) return refuse("adamw: eps is 0 in 32 bits");
+        if (!(static_cast<float>(o->eps) >= std::numeric_limits<float>::min())) return refuse("adamw: eps is under 2^-126, the smallest normal number of 32 bits");
         const int64_t length = adpsgd_adamw_state_length(o->sizes, o->tensors);
         if (length < 0) return refuse("adamw: a size is negative or over 2^40");
         if (o->tensors > 0 && (!o->params || !o->grads || !o->weight_decay)) return refuse("adamw: params, grads or weight_decay is NULL");
@@ -294,6 +294,7 @@ extern "C" int adpsgd_adamw_create(adpsgd_adamw_t** out, const adpsgd_adamw_opts
         h->a.rest1 = static_cast<float>(1.0 - o->beta1);
         h->a.rest2 = static_cast<float>(1.0 - o->beta2);
         h->a.eps = static_cast<float>(o->eps);
+        h->a.root = o->eps < 1e-18 ? 0x1p-15f : 1.0f;
         h->a.seed = o->seed;
         h->beta1 = o->beta1;
         h->beta2 = o->beta2;
@@ -330,7 +331,7 @@ extern "C" int adpsgd_adamw_step(adpsgd_adamw_t* h, double lr, double max_norm, 
         const int64_t t = h->steps + 1;
         a.step = static_cast<uint64_t>(t);
         a.inv_c1 = static_cast<float>(1.0 / (1.0 - std::pow(h->beta1, static_cast<double>(t))));
-        a.inv_c2 = static_cast<float>(1.0 / (1.0 - std::pow(h->beta2, static_cast<double>(t))));
+        a.inv_c2 = static_cast<float>(1.0 / (1.0 - std::pow(h->beta2, static_cast<double>(t)))) / (a.root * a.root);
         e = launch_adamw(a, s);
         if (e != hipSuccess) return hip_fail(nullptr, e, "adamw step");
         h->steps = t;

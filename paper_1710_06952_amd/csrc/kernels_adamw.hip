@@ -252,7 +252,8 @@ __global__ __launch_bounds__(kT) void adamw_norm_kernel(const AdamwArgs a) {
 }
 
 // ---- the step ----
-// Root and quotient by v_sqrt_f32 and v_rcp_f32, within 2^-22 (a v under 2^-126 counts as 0, whose root no eps over 1e-18 would feel).
+// Root and quotient by v_sqrt_f32 and v_rcp_f32, within 2^-22.  v_sqrt_f32 takes a v under 2^-126 as 0, whose root an eps over 1e-18 does not feel;
+// beside a smaller one v is taken times 2^30 and the root times 2^-15 (inv_c2 and root), which v up to 2^98 allow.
 template <class P, class G, bool kBytes, bool kMaster, bool kDirection, bool kWhole>
 __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk& t, double* sums) {
     const int first = static_cast<int>(threadIdx.x) * kPerThread, padded = (t.n + kAdamwBlock - 1) / kAdamwBlock * kAdamwBlock;
@@ -315,7 +316,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwChunk&
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float dir = m[i] * a.inv_c1 * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i] * a.inv_c2) + a.eps) + t.decay * p[u][i];
+            const float dir = m[i] * a.inv_c1 * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i] * a.inv_c2), a.root, a.eps)) + t.decay * p[u][i];
             q[i] = kDirection ? dir : p[u][i] - a.lr * dir;
             asm volatile("" : "+v"(q[i]));                // rounded to 32 bits, as the master is, before the parameter's rounding
         }

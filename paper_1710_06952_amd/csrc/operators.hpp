@@ -64,7 +64,8 @@ struct AdamwArgs {
     void *m, *v;
     int8_t* exponents;
     double beta1_64, beta2_64, rest1_64, rest2_64;
-    float beta1, beta2, rest1, rest2, eps, lr, inv_c1, inv_c2;     // rest: 1 - beta, inv_c: 1 / (1 - beta^step)
+    float beta1, beta2, rest1, rest2, eps, lr, inv_c1, inv_c2;     // rest: 1 - beta, inv_c: 1 / (1 - beta^step), inv_c2 divided by root^2
+    float root;                     // times the root of v inv_c2
     float grad_scale;
     double grad_scale_64, max_norm;
     uint64_t seed, step;

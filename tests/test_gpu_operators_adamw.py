@@ -357,3 +357,16 @@ def test_squares_that_32_bits_do_not_hold():
     opt.step()
     v = opt.moments()[1].double()
     assert (v[g != 0] == 2.0 ** -118).all() and not v[g == 0].any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_small_eps_beside_small_squares(bits):
+    """v under 2^-126 counts with its root: u = 1, not m / eps."""
+    import torch
+    import paper_1710_06952_amd as P
+    g = torch.full((256,), 2e-20, device="cuda:0")
+    out = torch.zeros(256, device="cuda:0")
+    opt = P.AdamW([torch.zeros(256, device="cuda:0")], [g], state_bits=bits, eps=1e-30, out=[out])
+    opt.step()
+    # v = 4e-43 is a multiple of 2^-149 to 1.7e-3, its root to half of that
+    assert float((out - 1.0).abs().max()) < 1e-3, out[0]

@@ -161,3 +161,9 @@ def test_shapes_and_types():
     with pytest.raises(ValueError, match="steps"):
         opt.load_moments(new(256), new(256), -1)
     assert opt.steps == 0
+
+
+def test_an_eps_that_is_no_normal_number():
+    h = C.c_void_p(1)
+    refused(B.lib().adpsgd_adamw_create(C.byref(h), C.byref(adamw_args(eps=1e-40))), "eps")
+    assert not h.value
