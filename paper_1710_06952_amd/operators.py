@@ -320,6 +320,9 @@ class AdamW:
         if rc != B.OK:
             raise B.AdpsgdError(rc, (B.lib().adpsgd_last_error(None) or b"").decode())
         self._h = h
+        # what a step writes, for autograd's check of tensors that were saved for a backward pass
+        params, _, masters, out = self._tensors
+        self._written = params + (masters or []) if out is None else out
 
     def close(self):
         h, self._h = getattr(self, "_h", None), None
@@ -347,6 +350,7 @@ class AdamW:
         the norm before that is returned as a scalar tensor (None with 0: no clipping, no norm)."""
         norm = torch.empty((), dtype=torch.float32, device=self.device) if max_norm else None
         _call(self.device, B.lib().adpsgd_adamw_step, self._open(), self.lr, max_norm, grad_scale, _ptr(norm))
+        torch.autograd.graph.increment_version(self._written)
         return norm
 
     def moments(self):

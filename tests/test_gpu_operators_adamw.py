@@ -370,3 +370,32 @@ def test_a_small_eps_beside_small_squares(bits):
     opt.step()
     # v = 4e-43 is a multiple of 2^-149 to 1.7e-3, its root to half of that
     assert float((out - 1.0).abs().max()) < 1e-3, out[0]
+
+
+def test_a_step_is_seen_by_autograd():
+    import torch
+    import paper_1710_06952_amd as P
+    x, w = (torch.ones(n, 16, dtype=torch.bfloat16, device="cuda:0", requires_grad=True) for n in (8, 24))
+    y = P.dense(x, w)
+    opt = P.AdamW([w], [torch.ones_like(w)])
+    before = w._version
+    opt.step()
+    assert w._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward(torch.ones_like(y))
+    flat = torch.zeros(600, dtype=torch.bfloat16, device="cuda:0")
+    master, out = torch.zeros(600, device="cuda:0"), torch.zeros(600, device="cuda:0")
+    views = lambda t: [t[:300], t[300:]]  # noqa: E731
+    opt = P.AdamW(views(flat), views(flat.clone()), masters=views(master))
+    at = flat._version, master._version
+    opt.step()
+    assert flat._version > at[0] and master._version > at[1]
+    opt = P.AdamW(views(flat), views(flat.clone()), out=views(out))
+    at = flat._version, out._version
+    opt.step()
+    assert flat._version == at[0] and out._version > at[1]             # a direction leaves the parameters
+    with torch.inference_mode():
+        p = torch.zeros(5, device="cuda:0")
+        opt = P.AdamW([p], [torch.ones(5, device="cuda:0")])
+        opt.step()
+    opt.step()
