@@ -384,10 +384,14 @@ class AdamW:
         return dict({k: t.clone() for k, t in parts.items() if t is not None}, steps=self.steps)
 
     def load_state_dict(self, state):
-        for k, t in (("m", self._m), ("v", self._v), ("exponents", self._exponents)):
-            if t is None:
-                continue
-            if state[k].shape != t.shape or state[k].dtype != t.dtype:
-                raise ValueError("%s of the stored state is %s %s, here %s %s" % (k, tuple(state[k].shape), state[k].dtype, tuple(t.shape), t.dtype))
-            t.copy_(state[k])
-        B.lib().adpsgd_adamw_set_steps(self._open(), int(state["steps"]))
+        """Continue from a state_dict.  One that does not fit is refused and changes nothing."""
+        h = self._open()
+        parts = [(k, t, state[k]) for k, t in (("m", self._m), ("v", self._v), ("exponents", self._exponents)) if t is not None]
+        steps = int(state["steps"])
+        for k, t, stored in parts:
+            if stored.shape != t.shape or stored.dtype != t.dtype:
+                raise ValueError("%s of the stored state is %s %s, here %s %s" % (k, tuple(stored.shape), stored.dtype, tuple(t.shape), t.dtype))
+        if B.lib().adpsgd_adamw_set_steps(h, steps) != B.OK:
+            raise ValueError("the stored state has %d steps" % steps)
+        for _, t, stored in parts:
+            t.copy_(stored)

@@ -399,3 +399,19 @@ def test_a_step_is_seen_by_autograd():
         opt = P.AdamW([p], [torch.ones(5, device="cuda:0")])
         opt.step()
     opt.step()
+
+
+def test_a_stored_state_that_does_not_fit_changes_nothing():
+    import torch
+    for bits in (32, 8):
+        a = Model([700], "float32", "float32", False, False, bits, seed=9)
+        a.opt.step()
+        want = a.opt.state_dict()
+        good = {k: (v + 1 if isinstance(v, int) else torch.ones_like(v)) for k, v in want.items()}
+        last = "v" if bits == 32 else "exponents"
+        for bad, kind in (({**good, last: good[last][:-1]}, ValueError), ({**good, last: good[last].double()}, ValueError), ({k: v for k, v in good.items() if k != last}, KeyError),
+                          ({k: v for k, v in good.items() if k != "steps"}, KeyError), ({**good, "steps": -1}, ValueError)):
+            with pytest.raises(kind):
+                a.opt.load_state_dict(bad)
+            got = a.opt.state_dict()
+            assert got["steps"] == 1 and all(torch.equal(want[k], got[k]) for k in want if k != "steps")
