@@ -329,7 +329,7 @@ class AdamW:
         if h:
             try:
                 B.lib().adpsgd_adamw_destroy(h)
-            except TypeError:                   # interpreter shutdown: the module globals are already gone
+            except (AttributeError, TypeError):    # interpreter shutdown: the module globals are already gone
                 pass
 
     __del__ = close

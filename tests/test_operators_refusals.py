@@ -167,3 +167,13 @@ def test_an_eps_that_is_no_normal_number():
     h = C.c_void_p(1)
     refused(B.lib().adpsgd_adamw_create(C.byref(h), C.byref(adamw_args(eps=1e-40))), "eps")
     assert not h.value
+
+
+def test_an_optimizer_that_outlives_the_module(monkeypatch):
+    """At the interpreter's end the module's names are None, and a collected optimizer says nothing."""
+    from paper_1710_06952_amd import operators
+    opt = operators.AdamW.__new__(operators.AdamW)
+    opt._h = C.c_void_p(NOWHERE)
+    monkeypatch.setattr(operators, "B", None)
+    opt.close()
+    assert opt._h is None
