@@ -19,6 +19,7 @@ from collections import namedtuple
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -44,6 +45,8 @@ def _call(device, fn, *args):
 def _on_gpu(name, t, device=None):
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a tensor" % name)
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:      # read through its address, it would lose the tangent
+        raise NotImplementedError("%s has a tangent: the operators have no derivatives in forward mode" % name)
     if not t.is_cuda:
         raise ValueError("%s must be on the GPU: the HIP library is the only implementation" % name)
     if device is not None and t.device != device:
@@ -168,7 +171,7 @@ class _Dense(torch.autograd.Function):
 
 
 def dense(x, w, bias=None, *, residual=None, activation="none"):
-    """act(x w^T + bias) + residual in one pass, differentiable (once) in all four.
+    """act(x w^T + bias) + residual in one pass, differentiable (once, in reverse mode) in all four.
 
     x (..., in), w (out, in) as it is or as the transpose of an (in, out) tensor, bias (out), residual (..., out), all
     bfloat16 or all float16; activation "none", "relu", "gelu" (z Phi(z)) or "silu".  Products are added in 32 bits and

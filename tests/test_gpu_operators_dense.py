@@ -259,3 +259,22 @@ def test_capture_with_autograd_is_refused():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(y, P.dense(x, w, b))
+
+
+def test_forward_mode_is_refused():
+    import torch
+    import paper_1710_06952_amd as P
+    from torch.autograd import forward_ad
+    x, w, b, r, dy = make(8, 16, 24, torch.bfloat16, "nk", seed=9)
+    t = torch.arange(8, device="cuda:0")
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        db = forward_ad.make_dual(b, torch.ones_like(b))
+        for call in (lambda: P.dense(dual, w), lambda: P.dense(x, w, db), lambda: P.dense_forward(dual, w), lambda: P.token_log_probs(dual, t)):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+        P.dense(x, w)
+    with pytest.raises(Exception):
+        torch.func.vmap(lambda q: P.dense(q, w))(x[None])
+    with pytest.raises(Exception):
+        torch.func.jvp(lambda q: P.dense(q, w), (x,), (torch.ones_like(x),))

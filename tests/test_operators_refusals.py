@@ -177,3 +177,17 @@ def test_an_optimizer_that_outlives_the_module(monkeypatch):
     monkeypatch.setattr(operators, "B", None)
     opt.close()
     assert opt._h is None
+
+
+def test_forward_mode():
+    import torch
+    from torch.autograd import forward_ad
+    x, w, t = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(3, 8, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: P.dense(dual, w), lambda: P.dense_forward(dual, w), lambda: P.token_log_probs(dual, t), lambda: P.AdamW([dual], [x]),
+                     lambda: P.policy_loss_and_gradient(dual, t, x[:, 0], x[:, 0])):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+        with pytest.raises(ValueError, match="GPU"):
+            P.dense(x, w)
