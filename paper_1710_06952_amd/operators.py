@@ -66,23 +66,28 @@ def _ptr(t):
 
 # ---- dense layers -----------------------------------------------------------------------------------------------
 
-def _as_rows(t):
-    """t as a matrix whose last dimension is contiguous, and its leading dimension."""
+_REACH = 1 << 22        # elements from one row of a dense operand to the next, at most
+
+
+def _as_rows(t, reach=_REACH):
+    """t as a matrix whose last dimension is contiguous, and its leading dimension.  The stride of a dimension of size 1 says nothing."""
     if t.dim() != 2:
         t = t.reshape(-1, t.shape[-1])
     n, (step, inner) = t.shape[1], t.stride()
-    if (inner != 1 and n > 1) or (step < n and t.shape[0] > 1):
+    if t.shape[0] <= 1:
+        step = n
+    if (inner != 1 and n > 1) or not n <= step <= reach:
         t, step = t.contiguous(), n
-    return t, max(step, n)
+    return t, step
 
 
 def _as_weights(w):
     """w (out x in) as it is stored: the tensor, its leading dimension, and whether it lies in x out."""
-    N, K = w.shape
-    if (w.stride(1) == 1 or K == 1) and (N == 1 or w.stride(0) >= K):
-        return w, max(w.stride(0), K), 0
-    if (w.stride(0) == 1 or N == 1) and (K == 1 or w.stride(1) >= N):
-        return w, max(w.stride(1), N), 1
+    (N, K), (out, inner) = w.shape, w.stride()
+    if (inner == 1 or K == 1) and (N == 1 or K <= out <= _REACH):
+        return w, K if N == 1 else out, 0
+    if (out == 1 or N == 1) and (K == 1 or N <= inner <= _REACH):
+        return w, N if K == 1 else inner, 1
     return w.contiguous(), K, 0
 
 
@@ -218,7 +223,7 @@ def _logits(logits, tokens):
     rows, vocab = logits.shape
     device = logits.device
     tokens = _vector("tokens", tokens, rows, torch.int64, device)
-    z, ld = _as_rows(logits)
+    z, ld = _as_rows(logits, 1 << 40)
     size = B.lib().adpsgd_loss_workspace_bytes(rows, vocab)
     if size < 0:
         raise B.AdpsgdError(B.ERR_ARG, "logits: %d rows of %d are too many" % (rows, vocab))

@@ -278,3 +278,29 @@ def test_forward_mode_is_refused():
         torch.func.vmap(lambda q: P.dense(q, w))(x[None])
     with pytest.raises(Exception):
         torch.func.jvp(lambda q: P.dense(q, w), (x,), (torch.ones_like(x),))
+
+
+def test_dimensions_of_one_and_far_rows():
+    """The stride of a dimension of size 1 says nothing, and rows that lie further apart than the kernels reach are copied."""
+    import torch
+    import paper_1710_06952_amd as P
+    K, N, far = 40, 24, (1 << 22) + 8
+    x, w, b, r, dy = make(3, K, N, torch.bfloat16, "nk", seed=10)
+    def apart(t):
+        big = torch.full((t.shape[0], far), math.nan, dtype=t.dtype, device=t.device)
+        big[:, :t.shape[1]] = t
+        return big[:, :t.shape[1]]
+    for rows in (1, 3):
+        xs, rs, dys = x[:rows], r[:rows], dy[:rows]
+        want, slope = P.dense_forward(xs, w, b, residual=rs, activation="silu")
+        grads = P.dense_gradients(dys, xs, w, slope, activation="silu")
+        got, slope = P.dense_forward(apart(xs), w, b, residual=apart(rs), activation="silu")
+        assert torch.equal(got, want)
+        assert all(torch.equal(p, q) for p, q in zip(P.dense_gradients(apart(dys), apart(xs), w, slope, activation="silu"), grads))
+    want = P.dense(x, w, b)
+    assert torch.equal(P.dense(x, apart(w), b), want) and torch.equal(P.dense(x, apart(w.t().contiguous()).t(), b), want)
+    assert torch.equal(P.dense(x, apart(w[:1]), b[:1]), P.dense(x, w[:1], b[:1]))
+    one = P.dense(x[:, :1], w[:, :1])
+    assert torch.equal(P.dense(x[:, :1].contiguous(), apart(w[:, :1].t().contiguous()).t()), one)
+    tokens = torch.tensor([5], device="cuda:0")
+    assert torch.equal(P.token_log_probs(apart(x[:1]), tokens), P.token_log_probs(x[:1], tokens))
