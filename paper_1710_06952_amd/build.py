@@ -19,7 +19,8 @@ SOURCES = ["api.cpp", "api_sync.cpp", "api_diag.cpp", "schedule.cpp", "planner.c
            "kernels_mlp.hip", "kernels_diag.hip", "kernels_sync.hip", "api_operators.cpp", "kernels_losses.hip", "kernels_adamw.hip",
            "kernels_dense.hip", "kernels_dense_bf16.hip", "kernels_dense_f16.hip"]
 HEADERS = ["internal.hpp", "strips.hpp", "onepass.hpp", "exchange.hpp", "handle.hpp", "device_common.hpp", "chains.hpp",
-           "operators.hpp", "dense.hpp", "dense_tiles.hpp", "dense_large.hpp", "dense_narrow.hpp"]
+           "operators.hpp", "dense.hpp", "dense_tiles.hpp", "dense_large.hpp", "dense_narrow.hpp",
+           "per_device.hpp"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 instructions

@@ -5,6 +5,7 @@
 
 #include "device_common.hpp"
 #include "operators.hpp"
+#include "per_device.hpp"
 
 namespace adpsgd_impl {
 
@@ -102,7 +103,15 @@ struct DensePlan {
     int splits;
 };
 
+// Dynamic LDS over 64 KB for a kernel, on the current device; `done`: the kernel's own.
+inline hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
+    int device = -1;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    return once_a_device(done, device, hipSuccess, [&] { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+}
+
 template <class T>
-void launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
+hipError_t launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 
 }  // namespace adpsgd_impl

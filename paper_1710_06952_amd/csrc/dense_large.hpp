@@ -279,13 +279,15 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
 }
 
 template <class T, bool kAOuter, bool kBOuter, int kSide>
-void launch_large(const DenseGemm& g, int splits, hipStream_t s) {
+hipError_t launch_large(const DenseGemm& g, int splits, hipStream_t s) {
     const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
     constexpr int kBytes = kSide == 256 ? 160 * 1024 : 4 * kSide * kBK * 2;       // two steps' operands; the end of the large tiles needs more
     auto kernel = dense_large_kernel<T, kAOuter, kBOuter, kSide>;
-    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    (void)allowed;                                       // a refusal shows at the launch
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * splits)), dim3(256), kBytes, s, g, splits);
+    return hipSuccess;
 }
 
 }  // namespace

@@ -371,13 +371,15 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, cons
 }
 
 template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
-void launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
+hipError_t launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
     const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
     constexpr int kBytes = 4 * kSide * kBK * 2;
     auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ>;
-    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    (void)allowed;                                       // a refusal shows at the launch
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(tiles * splits)), dim3(kWI * kWJ * 64), kBytes, s, g, splits);
+    return hipSuccess;
 }
 }  // namespace
 }  // namespace adpsgd_impl

@@ -221,9 +221,7 @@ hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s
         if (!a_whole) copy(g.a, g.lda, a_rows, a_inner);
         if (!b_whole) copy(g.b, g.ldb, b_rows, b_inner);
     }
-    if (type == ADPSGD_TYPE_BF16) launch_dense_tiles<Bf16>(g, p, s);
-    else launch_dense_tiles<F16>(g, p, s);
-    return hipGetLastError();
+    return type == ADPSGD_TYPE_BF16 ? launch_dense_tiles<Bf16>(g, p, s) : launch_dense_tiles<F16>(g, p, s);
 }
 
 }  // namespace adpsgd_impl
