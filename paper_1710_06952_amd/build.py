@@ -20,7 +20,7 @@ SOURCES = ["api.cpp", "api_sync.cpp", "api_diag.cpp", "schedule.cpp", "planner.c
            "kernels_dense.hip", "kernels_dense_bf16.hip", "kernels_dense_f16.hip"]
 HEADERS = ["internal.hpp", "strips.hpp", "onepass.hpp", "exchange.hpp", "handle.hpp", "device_common.hpp", "chains.hpp",
            "operators.hpp", "dense.hpp", "dense_tiles.hpp", "dense_large.hpp", "dense_narrow.hpp",
-           "per_device.hpp"]
+           "dense_launch.hpp", "per_device.hpp"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 instructions
