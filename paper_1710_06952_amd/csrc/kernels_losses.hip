@@ -207,7 +207,7 @@ __device__ __forceinline__ double log_of(float s) {
     return fma(static_cast<double>(k), 0.6931471805599453, 2.0 * u * fma(y, p, 1.0));
 }
 __device__ __forceinline__ double log_prob(float at, Stat st) {
-    const double l = static_cast<double>(at - st.m) - log_of(st.s);
+    const double l = static_cast<double>(at) - static_cast<double>(st.m) - log_of(st.s);
     return st.s < INFINITY ? l : NAN;                    // NaN too, of which frexp says nothing
 }
 // Exponentials of what there is one of in a row: s is off by 1e-7, so 32 bits lose nothing.

@@ -306,3 +306,22 @@ def test_capture_and_other_streams():
             want = every()
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(replayed, want)), k
+
+
+def test_differences_to_the_largest_logit_are_in_64_bits():
+    """The margin is a difference of sums of log-probabilities: what rounding a difference of two fp32 logits to 32 bits is off by, the same in
+    every row of one side, would add up in it."""
+    import torch
+    import paper_1710_06952_amd as P
+    n = 300
+    z = torch.zeros(2 * n, 2, device="cuda:0")
+    z[:, 1] = 16.0
+    z[:n, 0] = 0.45 * 2.0 ** -20                         # 16 less this is within half a step of 32 bits of 16: rounded, the difference is 16
+    tokens = torch.zeros(2 * n, dtype=torch.int64, device="cuda:0")
+    offsets = torch.tensor([0, n, 2 * n], device="cuda:0")
+    z64 = z.double()
+    l = z64[:, 0] - torch.logsumexp(z64, 1)
+    sums = torch.stack([l[:n].sum(), l[n:].sum()])
+    r = P.preference_loss_and_gradient(z, tokens, offsets, torch.zeros(2, device="cuda:0"), beta=1.0)
+    # of a row: s = 1 + 1e-7 is rounded to 32 bits the same on both sides
+    assert abs(float(r.margins[0]) - float(sums[0] - sums[1])) <= n * 2.0 ** -30
