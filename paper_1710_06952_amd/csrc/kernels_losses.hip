@@ -339,13 +339,19 @@ __global__ __launch_bounds__(kT) void join_stats_kernel(const RowArgs a) {
     if ((threadIdx.x & 63) == 0) finish_row<E>(a, row, st);
 }
 
-__device__ __forceinline__ float gradient_at(float z, bool hot, float m, float scale, float coef) { return exp_of(z - m) * scale + (hot ? coef : 0.0f); }
+// In the gradient the rounding of log2 e is 1.3e-8 of z - m, in the same direction in every element: 1e-7 where fp32 holds it, nothing in 16 bits.
+template <class E>
+__device__ __forceinline__ float exp_in_gradient(float d) { return exp_in_sum<E::kN == 4>(d); }
+template <class E>
+__device__ __forceinline__ float gradient_at(float z, bool hot, float m, float scale, float coef) {
+    return exp_in_gradient<E>(z - m) * scale + (hot ? coef : 0.0f);
+}
 // d[i] = exp(z[i] - m) scale
 template <class E>
 __device__ __forceinline__ void gradient_of(v4u x, float m, float scale, float* d) {
     E::unpack(x, d);
 #pragma unroll
-    for (int i = 0; i < E::kN; ++i) d[i] = exp_of(d[i] - m) * scale;
+    for (int i = 0; i < E::kN; ++i) d[i] = exp_in_gradient<E>(d[i] - m) * scale;
 }
 
 struct GradientArgs {
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(kT) void logit_gradient_kernel(const GradientArgs g
     const float scale = -coef / st.s;
     const int v0 = static_cast<int>(blockIdx.x % g.blocks) * (kT * kUnroll) + static_cast<int>(threadIdx.x);
     const int hot = token < a.vocab ? static_cast<int>(token) : -1, single = blockIdx.x % g.blocks == 0 ? cut.single() : -1;
-    if (single >= 0) E::put(dz + single, coef == 0.0f ? 0.0f : gradient_at(E::get(z + single), single == hot, st.m, scale, coef));
+    if (single >= 0) E::put(dz + single, coef == 0.0f ? 0.0f : gradient_at<E>(E::get(z + single), single == hot, st.m, scale, coef));
     v4u x[kUnroll];
     float d[E::kN];
     if (coef == 0.0f) {                 // nothing to read
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(kT) void logit_gradient_kernel(const GradientArgs g
         }
     // the token's element once more, by the thread that has stored it without coef
     const int back = cut.vector_of(hot) - v0;
-    if (cut.vector_of(hot) >= 0 && back >= 0 && back < kT * kUnroll && back % kT == 0) E::put(dz + hot, gradient_at(E::get(z + hot), true, st.m, scale, coef));
+    if (cut.vector_of(hot) >= 0 && back >= 0 && back < kT * kUnroll && back % kT == 0) E::put(dz + hot, gradient_at<E>(E::get(z + hot), true, st.m, scale, coef));
 }
 
 // ---- policy ----------------------------------------------------------------------------------------------
@@ -520,7 +526,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
     }
     const int hot = token < a.vocab ? static_cast<int>(token) : -1;
     const bool zero = coef == 0.0f;     // NaN is not
-    if (single >= 0) E::put(dz + single, zero ? 0.0f : gradient_at(alone, single == hot, m, scale, coef));
+    if (single >= 0) E::put(dz + single, zero ? 0.0f : gradient_at<E>(alone, single == hot, m, scale, coef));
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
         const int v = u * kThreads + static_cast<int>(threadIdx.x);
@@ -538,7 +544,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void policy_rows_kernel(cons
         __builtin_amdgcn_sched_barrier(0);
     }
     // the token's element once more, by the thread that has stored it without coef
-    if (cut.vector_of(hot) >= 0 && cut.vector_of(hot) % kThreads == static_cast<int>(threadIdx.x)) E::put(dz + hot, gradient_at(value, true, m, scale, coef));
+    if (cut.vector_of(hot) >= 0 && cut.vector_of(hot) % kThreads == static_cast<int>(threadIdx.x)) E::put(dz + hot, gradient_at<E>(value, true, m, scale, coef));
 }
 
 // ---- preference ------------------------------------------------------------------------------------------

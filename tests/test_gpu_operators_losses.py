@@ -325,3 +325,30 @@ def test_differences_to_the_largest_logit_are_in_64_bits():
     r = P.preference_loss_and_gradient(z, tokens, offsets, torch.zeros(2, device="cuda:0"), beta=1.0)
     # of a row: s = 1 + 1e-7 is rounded to 32 bits the same on both sides
     assert abs(float(r.margins[0]) - float(sums[0] - sums[1])) <= n * 2.0 ** -30
+
+
+def test_fp32_gradients_do_not_lean():
+    """Rounding log2 e to 32 bits is 1.3e-8 of z - m in every term, in the same direction: 1.2e-7 between the means of terms at 3 and 12 under the
+    largest.  Without it the mean of 10 000 roundings of up to 2e-6 is within 5e-8 of that of another 10 000."""
+    import torch
+    import paper_1710_06952_amd as P
+    for V in (2048, 70_001):                             # a row in registers, and two passes
+        g = torch.Generator(device="cuda:0")
+        g.manual_seed(V)
+        z = 2 * torch.randn(64, V, generator=g, device="cuda:0")
+        tokens = torch.zeros(64, dtype=torch.int64, device="cuda:0")
+        z[:, 0] = 8.0
+        l, lse, _ = log_probs(z, tokens)
+        one = torch.ones(64, device="cuda:0")
+        offsets = torch.arange(0, 65, device="cuda:0")
+        for dz in (P.policy_loss_and_gradient(z, tokens, l.float(), one).dlogits, P.preference_loss_and_gradient(z, tokens, offsets, torch.zeros(64, device="cuda:0")).dlogits):
+            p = torch.exp(z.double() - lse[:, None])
+            p[:, 0] = math.nan
+            rel = dz.double() / p                        # the row's coefficient, and what the terms are off by
+            d = z.amax(1, keepdim=True) - z
+            near, far = ((d > lo) & (d < hi) for lo, hi in ((2.5, 5.0), (11.0, 14.0)))
+            both = near.any(1) & far.any(1)
+            mean = lambda at: torch.where(at, rel, 0.0).sum(1) / at.sum(1)  # noqa: E731
+            of = (mean(far) / mean(near) - 1.0)[both]
+            print(V, int(near.sum()), int(far.sum()), float(of.mean()), flush=True)
+            assert abs(float(of.mean())) <= 5e-8
