@@ -71,7 +71,7 @@ __device__ __forceinline__ float activated(float z, float& slope) {
         p = fmaf(p, u, 0.1337908999955492f);
         p = fmaf(p, u, 0.15129931401177749f);
         p = fmaf(p, u, 0.15160565325274758f);
-        const float phi = 0.5f + copysignf(fmaf(-(e * u), p, 0.5f), z);
+        const float tail = e * u * p, phi = z < 0.0f ? tail : 1.0f - tail;
         if (kSlope) slope = fmaf(z * 0.3989422804014327f, e, phi);
         return z * phi;
     }
