@@ -487,8 +487,8 @@ typedef struct {
 /* Host only: the workspace of a forward (backward = 0) or backward call of these sizes; -1 where an argument is refused. */
 int64_t adpsgd_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward);
 
-/* y: M x N, contiguous.  slope (or NULL): M x N 16-bit words, contiguous, receives act'(z) for the backward call (in steps
- * of 2^-15). */
+/* y: M x N, contiguous.  slope (or NULL): M x N 16-bit words, contiguous, receives act'(z) for the backward call (its root, in
+ * steps of 1 / 46000). */
 int adpsgd_dense_forward(const adpsgd_dense_t* o, void* y, uint16_t* slope, void* stream);
 
 /* Gradients for dy (M x N, row m at dy + m lddy): dx (M x K, contiguous), dw (as w is stored: N x K or K x N, contiguous) and db (N);

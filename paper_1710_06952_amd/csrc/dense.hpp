@@ -80,21 +80,23 @@ __device__ __forceinline__ float activated(float z, float& slope) {
     return y;
 }
 
-// Slopes in 16 bits for the backward pass: (w - 8192) 2^-15, within 2^-16 from -1/4 to 7/4 (they are from -0.13 to 1.13), and 0 for NaN,
-// which no slope comes to.  Beside the rounding of dz to its type that is nothing, except for slopes under 2^-7, where it is the larger
-// of the two.  A conversion of two and an FMA each; a form with an exponent took nine instructions, and tiles with gelu 24 us at their end.
+// Slopes in 16 bits for the backward pass: their roots, signs kept, in steps of 1 / 46000 (roots are from -0.359 to 1.063: words 80 to 65479), and 0
+// for NaN, which no slope comes to.  A slope s is within 2.2e-5 |s|^1/2 (1.2e-10 where its word is that of 0): 2^-15.5 at 1, and no more than half a step
+// of fp16 down to 2^-9, of bf16 to 2^-15; beside the rounding of dz to its type that is little.  In steps of s itself (2^-15) the same 16 bits
+// were coarser than fp16 under 2^-5, and in the tails of gelu and silu nothing was left.  0 and 1 are exact.
+constexpr float kRootSteps = 46000.0f, kRootZero = 16600.0f;
 __device__ __forceinline__ v4u slope_words(const float* s) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = fmaf(copysignf(__builtin_amdgcn_sqrtf(fabsf(s[i])), s[i]), kRootSteps / 65535.0f, kRootZero / 65535.0f);
     v4u w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = fmaf(s[2 * i], 32768.0f / 65535.0f, 8192.0f / 65535.0f), b = fmaf(s[2 * i + 1], 32768.0f / 65535.0f, 8192.0f / 65535.0f);
-        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(a, b));
-    }
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pknorm_u16(r[2 * i], r[2 * i + 1]));
     return w;
 }
 __device__ __forceinline__ float slope_of(uint32_t w) {
-    const float s = fmaf(static_cast<float>(w), 0x1p-15f, -0.25f);
-    return w == 0u ? NAN : s;
+    const float r = (static_cast<float>(w) - kRootZero) * (1.0f / kRootSteps);
+    return w == 0u ? NAN : r * fabsf(r);
 }
 
 // How a product is cut: tiles of side x side (0: columns, dense_narrow.hpp), `splits` parts of k whose sums are joined afterwards.

@@ -320,3 +320,24 @@ def test_values_far_from_0(act, dtype):
     tiny = 2.0 ** -25 if T == torch.float16 else 1e-38
     off = (y[0].double() - a).abs()
     assert (off <= 1.01 * half(T) * a.abs() + 1.2e-5 * a.abs() + tiny).all(), float((off / a.abs().clamp(min=1e-30)).max())
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_slopes_far_from_0(act, dtype):
+    """Products of one term, so z is exact.  db is the slope where dy is 1: its root is kept in steps of 1 / 46000, half of which is 2.2e-5 of the
+    root in the slope, and its square where nothing else is left; beside that 1.2e-5 as for y, and where terms cancel 2^-22."""
+    import torch
+    import paper_1710_06952_amd as P
+    T = getattr(torch, dtype)
+    z = torch.linspace(-9.0, 9.0, 2048, device="cuda:0").to(T)[:, None].contiguous()
+    one = torch.ones(1, 1, dtype=T, device="cuda:0")
+    y, slope = P.dense_forward(one, z, activation=act)
+    s = activation(z[:, 0].double(), act)[1]
+    db = P.dense_gradients(torch.ones_like(y), one, z, slope, activation=act)[2]
+    tiny = 2.0 ** -25 if T == torch.float16 else 1e-38
+    bound = 1.01 * half(T) * s.abs() + 1.01 * (1.2e-5 * s.abs() + 2.2e-5 * s.abs().sqrt()) + 1.2e-10 + tiny + torch.where(z[:, 0].abs() < 3, 2.0 ** -22, 0.0)
+    if act == "relu":
+        bound = torch.zeros_like(bound)                  # 0 and 1 are kept as they are
+    off = (db.double() - s).abs()
+    assert (off <= bound).all(), float((off / bound).max())
