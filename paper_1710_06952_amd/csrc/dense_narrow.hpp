@@ -1,4 +1,4 @@
-// Products with few rows, D[i][j] = sum_k A(i, k) B(j, k), I <= 64: B is read once and its bytes are the time.
+// Products with few rows, D[i][j] = sum_k A(i, k) B(j, k), I <= 64 (few_rows in kernels_dense.hip): B is read once and its bytes are the time.
 //
 // A block owns up to 64 columns and all rows; its eight wavefronts take steps of k in turn and their sums are joined through LDS, so a call is
 // one launch, unless columns are few and k is long: then several blocks share the steps, and dense_join_kernel adds their sums.  Matrix operands come from memory straight into registers, no LDS in between: B is used once.

@@ -143,10 +143,20 @@ double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
     const double step = side == 256 ? 1.5 : side == 128 ? 0.30 + 0.35 * together : 0.357 + 0.143 * together;
     return turns * (steps * step + ends) + (splits > 1 ? 4.0 + 8.0 * splits * static_cast<double>(I) * static_cast<double>(J) / 5e6 : 0.0);
 }
-// `rows`: A has k inner.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
-DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool rows, bool direct) {
+// Whether a product goes to the kernel for few rows; `b_whole`: B's rows are whole 16-byte pieces.  Microseconds there and in tiles, I x K x J:
+//   from 9 rows on up to 2^24 weights: 16 x 8192 x 8192 41 and 34, 64 rows 52 and 39; 64 x 4096 x 6144 27 and 22, 64 x 4096 x 4096 19.1 and 18.7,
+//     64 x 2048 x 4096 14.4 and 14.0, 64 x 1024 x 8192 9.2 and 13.2; one row 14 and 19 for 4096 x 6144, 35 and 33 for 8192 x 8192
+//   from 17 rows on whole pieces only: 32 x 2001 x 5003 27 and 21, 64 x 255 x 1021 9.3 and 6.3, 64 x 504 x 504 (whole) 5.8 and 7.1
+//   k outer, a last block that the end of the columns cuts and K over 1024: 1 x 3000 x 5008 30 and 17, 16 x 3001 x 3001 52 and 21; 1 x 3000 x 5024 (not
+//     cut) 9.7 and 16, 16 x 1000 x 1000 9.1 and 10.1
+bool few_rows(int64_t I, int64_t J, int64_t K, bool b_outer, bool b_whole) {
+    if (I > 64 || (I > 16 && !b_whole) || (I > 8 && J * K > (int64_t(1) << 24))) return false;
+    return !(b_outer && J % 32 != 0 && K > 1024);
+}
+// `few`: for the kernel of few rows.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
+DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct) {
     const int64_t steps = std::max<int64_t>(1, (K + 63) / 64);
-    if (rows && I <= 64) {               // a wavefront's steps of 64 k take 1 to 2 us each with few blocks: shared from eight on (47 x 477 x 6060: dx 52 to 24 us)
+    if (few) {                           // a wavefront's steps of 64 k take 1 to 2 us each with few blocks: shared from eight on (64 x 8192 x 1024: 15 us, 45 unshared)
         const int64_t blocks = (J + 31) / 32, shares = std::min<int64_t>(std::min<int64_t>(256 / blocks, steps / 16), 32);
         return DensePlan{0, steps >= 64 && shares > 1 ? static_cast<int>(shares) : 1};
     }
@@ -195,7 +205,7 @@ int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(
 int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
     int64_t parts = 0;
     for (bool direct : {false, true}) parts = std::max<int64_t>(parts, plan_of(I, J, K, false, direct).splits);
-    parts = std::max<int64_t>(parts, plan_of(I, J, K, true, false).splits);
+    if (I <= 64) parts = std::max<int64_t>(parts, plan_of(I, J, K, true, false).splits);
     const bool pack = (I % 8 || J % 8 || K % 8) && worth_packing(I, J, K);
     const int64_t copies = pack ? std::max(packed_bytes(I, K), packed_bytes(K, I)) + std::max(packed_bytes(J, K), packed_bytes(K, J)) : 0;
     return (parts > 1 ? up256(parts * I * J * static_cast<int64_t>(sizeof(float))) : 0) + copies;
@@ -208,7 +218,7 @@ hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s
     const bool a_whole = whole_pieces(g.a, g.lda, a_inner), b_whole = whole_pieces(g.b, g.ldb, b_inner);
     const bool pack = !(a_whole && b_whole) && (g.I % 8 || g.J % 8 || g.K % 8) && worth_packing(g.I, g.J, g.K);
     const bool direct = g.K >= 1 && ((a_whole && b_whole) || pack);
-    const DensePlan p = plan_of(g.I, g.J, g.K, !g.a_outer, direct);
+    const DensePlan p = plan_of(g.I, g.J, g.K, !g.a_outer && few_rows(g.I, g.J, g.K, g.b_outer, b_whole), direct);
     if (p.side >= 128 && pack) {
         char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * g.J * static_cast<int64_t>(sizeof(float))) : 0);
         auto copy = [&](const void*& from, int64_t& ld, int64_t rows, int64_t inner) {

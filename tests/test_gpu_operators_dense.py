@@ -341,3 +341,19 @@ def test_slopes_far_from_0(act, dtype):
         bound = torch.zeros_like(bound)                  # 0 and 1 are kept as they are
     off = (db.double() - s).abs()
     assert (off <= bound).all(), float((off / bound).max())
+
+
+@pytest.mark.parametrize("size", [(8, 4096, 4104), (9, 4096, 4104), (9, 4096, 4096), (64, 4096, 4096), (64, 4104, 4096), (17, 72, 104), (17, 73, 101), (16, 73, 101),
+                                  (5, 1032, 1001), (5, 1024, 1001), (30, 1032, 1032)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+def test_both_sides_of_few_rows(size, layout):
+    """Sizes next to the lines between the kernel for few rows and the tiles."""
+    import torch
+    import paper_1710_06952_amd as P
+    print(size, layout, flush=True)
+    x, w, b, r, dy = make(*size, torch.float16, layout, seed=11)
+    want = reference(x, w, b, r, dy, "silu")
+    y, slope = P.dense_forward(x, w, b, residual=r, activation="silu")
+    close("y", y, want["y"])
+    for name, g in zip(("dx", "dw", "db"), P.dense_gradients(dy, x, w, slope, activation="silu")):
+        close(name, g, want[name])
