@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
         multiply(1, true);
     }
     wait_loads();
-    wait_mfma();
+    wait_mfma();                                         // the compiler may copy a result in front of it, but none of the last eight: a test looks
 
     // The end.  A store is waited for together with the loads behind it, so the residual's rows are loaded in front of the first store, into
     // the LDS that the operands have left; with loads two turns ahead every turn waited for the stores of the one before, 25 us a tile with
