@@ -415,3 +415,11 @@ def test_a_stored_state_that_does_not_fit_changes_nothing():
                 a.opt.load_state_dict(bad)
             got = a.opt.state_dict()
             assert got["steps"] == 1 and all(torch.equal(want[k], got[k]) for k in want if k != "steps")
+
+
+@pytest.mark.parametrize("param", ["bfloat16", "float16"])
+@pytest.mark.parametrize("direction", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_without_masters(param, direction, bits):
+    """Parameters of 16 bits that are stepped themselves, gradients of the same type."""
+    test_steps([5, 256, 257, 3, 4096, 4097], (param, param, False), direction, bits)
