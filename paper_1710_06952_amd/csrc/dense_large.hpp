@@ -14,7 +14,7 @@
 //
 // Bound: the matrix cores, at the clock that their power leaves.  8192^3 in bf16 takes 850 us, 1.30 PFLOP/s (a library's product 680 to 790); a tile
 // of 256 takes 1.45 us a step, 1.5 PFLOP/s over the chip, and 24 us at its ends, which with four tiles of K = 2048 for a compute unit
-// are a third of the time (274 us; with gelu, slopes and a residual 345: the activation is 20 instructions an element).  Two blocks on a
+// are a third of the time (274 us; with gelu, slopes and a residual 327, 343 to 368 between other kernels: the activation is 25 instructions an element).  Two blocks on a
 // compute unit would hide the ends, but tiles of 128 take 1.4 times as long for the same products: their fragments come from LDS twice as often.
 //
 // What lies beyond the ends: rows of an operand with k inner are the last row again; pieces beyond the end of k, and rows of k beyond the

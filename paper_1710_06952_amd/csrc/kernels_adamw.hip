@@ -9,7 +9,7 @@
 //
 // Bound: memory, 28 bytes an element with everything in 32 bits (gradient 4, parameter 8, moments 16), 16 with bf16 parameters and
 // gradients, fp32 masters and 8-bit moments.  With clipping the gradients are read once more before that, by adamw_norm_kernel.
-// Measured: 25.6 M parameters in 32 bits 118 us (6.1 TB/s) and 16 + 5 for the norm; 67 M with 8-bit moments 187 to 235 us (5.7 to 4.6 TB/s:
+// Measured: 25.6 M parameters in 32 bits 118 us (6.1 TB/s) and 16 + 5 for the norm; 67 M with 8-bit moments 190 to 240 us (5.6 to 4.5 TB/s:
 // 440 instructions for four elements a lane are as long as their bytes) and 28 + 5 for the norm.
 //
 // 8 bits.  A block's scale is 2^k, so that its largest value y 2^k has 128 <= y < 256 (k >= -50).  The codes are e4m3, not
