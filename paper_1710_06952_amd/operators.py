@@ -283,7 +283,7 @@ class AdamW:
     params, grads: lists of contiguous tensors, each list of one type; they are read and written where they lie, for the life of
     the object.  masters: float32 copies that are stepped, with the params as their roundings.  out: float32 tensors that
     receive the direction u + weight_decay p in place of a step.  weight_decay: a number, or one for each tensor.  state_bits 32 or
-    8.  ``lr`` may be changed between steps."""
+    8.  ``lr`` may be changed between steps.  A step raises the versions of the tensors that it writes, as other changes in place do."""
 
     def __init__(self, params, grads, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state_bits=32, masters=None, out=None, seed=0):
         self._h = None
@@ -324,6 +324,7 @@ class AdamW:
                            self._m.data_ptr(), self._v.data_ptr(), _ptr(self._exponents))
         h = C.c_void_p()
         with torch.cuda.device(dev):
+            torch.cuda.current_stream().synchronize()       # the state is there for whatever stream the steps are on
             rc = B.lib().adpsgd_adamw_create(C.byref(h), C.byref(opts))
         if rc != B.OK:
             raise B.AdpsgdError(rc, (B.lib().adpsgd_last_error(None) or b"").decode())

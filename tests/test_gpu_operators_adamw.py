@@ -423,3 +423,19 @@ def test_a_stored_state_that_does_not_fit_changes_nothing():
 def test_steps_without_masters(param, direction, bits):
     """Parameters of 16 bits that are stepped themselves, gradients of the same type."""
     test_steps([5, 256, 257, 3, 4096, 4097], (param, param, False), direction, bits)
+
+
+def test_a_state_made_on_one_stream_is_there_for_another():
+    """The zeros that a state begins with are the optimizer's own, so no caller can wait for them."""
+    import torch
+    import paper_1710_06952_amd as P
+    p, g = torch.zeros(3000, device="cuda:0"), torch.ones(3000, device="cuda:0")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(100_000_000)                   # the zeros come some 50 ms later
+        opts = [P.AdamW([p], [g], state_bits=bits) for bits in (32, 8)]
+    for opt in opts:
+        opt.step()
+    torch.cuda.synchronize()
+    for opt in opts:
+        assert all(bool((t[:3000] > 0).all()) for t in opt.moments())
