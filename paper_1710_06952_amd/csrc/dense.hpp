@@ -105,6 +105,9 @@ struct DensePlan {
     int splits;
 };
 
+// Columns of a block of the kernel for few rows with k outer: lines of 128 bytes where that leaves a block for every compute unit.
+inline int64_t narrow_columns(int64_t I, int64_t J) { return I <= 16 && J >= 64 * 256 ? 64 : 32; }
+
 // Dynamic LDS over 64 KB for a kernel, on the current device; `done`: the kernel's own.
 inline hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
     int device = -1;

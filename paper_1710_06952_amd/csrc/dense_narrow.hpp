@@ -171,9 +171,9 @@ void launch_narrow_of(const DenseGemm& g, int splits, hipStream_t s) {
 }
 template <class T>
 void launch_narrow(const DenseGemm& g, int splits, hipStream_t s) {
-    if (g.b_outer) {                                     // lines of 128 bytes where that leaves a block for every compute unit
-        const bool wide = g.J >= 64 * 256;
-        if (g.I <= 16) wide ? launch_narrow_of<T, true, 1, 4>(g, splits, s) : launch_narrow_of<T, true, 1, 2>(g, splits, s);
+    if (g.b_outer) {
+        if (narrow_columns(g.I, g.J) == 64) launch_narrow_of<T, true, 1, 4>(g, splits, s);
+        else if (g.I <= 16) launch_narrow_of<T, true, 1, 2>(g, splits, s);
         else launch_narrow_of<T, true, 4, 2>(g, splits, s);
     } else {                                             // every block reads all of A: more columns where that is not little
         if (g.I <= 16) launch_narrow_of<T, false, 1, 1>(g, splits, s);

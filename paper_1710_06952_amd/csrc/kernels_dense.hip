@@ -146,14 +146,16 @@ double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
     return turns * (steps * step + ends) + (splits > 1 ? 4.0 + 8.0 * splits * static_cast<double>(I) * static_cast<double>(J) / 5e6 : 0.0);
 }
 // Whether a product goes to the kernel for few rows; `b_whole`: B's rows are whole 16-byte pieces.  Microseconds there and in tiles, I x K x J:
-//   from 9 rows on up to 2^24 weights: 16 x 8192 x 8192 41 and 34, 64 rows 52 and 39; 64 x 4096 x 6144 27 and 22, 64 x 4096 x 4096 19.1 and 18.7,
-//     64 x 2048 x 4096 14.4 and 14.0, 64 x 1024 x 8192 9.2 and 13.2; one row 14 and 19 for 4096 x 6144, 35 and 33 for 8192 x 8192
-//   from 17 rows on whole pieces only: 32 x 2001 x 5003 27 and 21, 64 x 255 x 1021 9.3 and 6.3, 64 x 504 x 504 (whole) 5.8 and 7.1
-//   k outer, a last block that the end of the columns cuts and K over 1024: 1 x 3000 x 5008 30 and 17, 16 x 3001 x 3001 52 and 21; 1 x 3000 x 5024 (not
-//     cut) 9.7 and 16, 16 x 1000 x 1000 9.1 and 10.1
+//   up to 16 rows: 1 x 4096 x 6144 14 and 19, 16 x 1024 x 1024 4.8 and 9, 16 x 2048 x 8192 11 and 16, 8 x 8192 x 12288 48 and 53, 16 x 16384 x 16384
+//     136 and 141; the other way round between 2^25 and 2^26 weights with nearly 16 rows (16 x 8192 x 8192 41 and 34, 8 rows 36 and 34)
+//   up to 64 rows, to 2^24 weights: 64 x 4096 x 6144 27 and 22, 64 x 8192 x 8192 52 and 39; 64 x 4096 x 4096 19.1 and 18.7, 64 x 2048 x 4096 14.4 and
+//     14.0, 17 x 4096 x 4096 16 and 19, 64 x 1024 x 8192 9.2 and 13.2; whole pieces only: 32 x 2001 x 5003 27 and 21, 64 x 255 x 1021 9.3 and 6.3;
+//     64 x 504 x 504 (whole) 5.8 and 7.1
+//   k outer, a last block that the end of the columns cuts and K over 1024: 1 x 3000 x 5008 30 and 17, 16 x 3001 x 3001 52 and 21,
+//     1 x 4096 x 16416 52 and 42; 1 x 3000 x 5024 (not cut) 9.7 and 16, 16 x 1000 x 1000 9.1 and 10.1
 bool few_rows(int64_t I, int64_t J, int64_t K, bool b_outer, bool b_whole) {
-    if (I > 64 || (I > 16 && !b_whole) || (I > 8 && J * K > (int64_t(1) << 24))) return false;
-    return !(b_outer && J % 32 != 0 && K > 1024);
+    if (I > 64 || (I > 16 && (!b_whole || J * K > (int64_t(1) << 24)))) return false;
+    return !(b_outer && J % narrow_columns(I, J) != 0 && K > 1024);
 }
 // `few`: for the kernel of few rows.  `direct`: the tiles of 256 and 128, whose operands go straight to LDS, can be had.
 DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct) {

@@ -344,7 +344,7 @@ def test_slopes_far_from_0(act, dtype):
 
 
 @pytest.mark.parametrize("size", [(8, 4096, 4104), (9, 4096, 4104), (9, 4096, 4096), (64, 4096, 4096), (64, 4104, 4096), (17, 72, 104), (17, 73, 101), (16, 73, 101),
-                                  (5, 1032, 1001), (5, 1024, 1001), (30, 1032, 1032)], ids=lambda s: "x".join(map(str, s)))
+                                  (5, 1032, 1001), (5, 1024, 1001), (30, 1032, 1032), (3, 1040, 16416), (3, 1040, 16448), (3, 1024, 16416)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("layout", ["nk", "kn"])
 def test_both_sides_of_few_rows(size, layout):
     """Sizes next to the lines between the kernel for few rows and the tiles."""
