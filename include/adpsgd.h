@@ -497,6 +497,34 @@ int adpsgd_dense_forward(const adpsgd_dense_t* o, void* y, uint16_t* slope, void
 int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, int64_t lddy, const uint16_t* slope, void* dx, void* dw, void* db,
                           void* stream);
 
+/* Layer norm over rows of n elements:  y = (x - mean) / sqrt(var + eps) w + b,  var the mean of (x - mean)^2.  x, y and their
+ * gradients are of one type, w and b both of param_type: that type or F32.  Means and variances are in 32 bits with the mean in two parts, so a
+ * mean far from 0 costs no accuracy.  A row with a value that is not finite is NaN. */
+typedef struct {
+    int32_t type;            /* ADPSGD_TYPE_*                                                                */
+    int32_t param_type;      /* the same, or ADPSGD_TYPE_F32                                                 */
+    int64_t rows, n;         /* 0 <= rows <= 2^31, 1 <= n <= 2^28                                            */
+    const void* x;           /* rows x n, row i at x + i ldx                                                 */
+    int64_t ldx;
+    const void* w;           /* n, or NULL: 1                                                                */
+    const void* b;           /* n, or NULL: 0; not without w                                                 */
+    double eps;              /* >= 2^-126                                                                    */
+    void* workspace;         /* of the backward call: adpsgd_layer_norm_workspace_bytes, 16-byte aligned; may be used again in stream order */
+    int64_t workspace_bytes;
+} adpsgd_layer_norm_t;
+
+/* Host only: the workspace of a backward call with dw or db (else none is needed); -1 where an argument is refused. */
+int64_t adpsgd_layer_norm_workspace_bytes(int32_t type, int64_t rows, int64_t n);
+
+/* y: rows x n, contiguous.  stats (or NULL): 3 x rows floats for the backward call (the mean in two parts, 1 / sqrt(var + eps)). */
+int adpsgd_layer_norm_forward(const adpsgd_layer_norm_t* o, void* y, float* stats, void* stream);
+
+/* Gradients for dy (rows x n, row i at dy + i lddy): dx (rows x n, contiguous, the type of x), dw and db (n, param_type); each may be
+ * NULL.  stats: as the forward call wrote them.  b and eps are not read.  dw and db are added in 32 bits over up to 128 rows and in 64 from there
+ * on, in an order that the sizes give. */
+int adpsgd_layer_norm_backward(const adpsgd_layer_norm_t* o, const void* dy, int64_t lddy, const float* stats, void* dx, void* dw, void* db,
+                               void* stream);
+
 /* Logits of `rows` positions over a vocabulary: row i at z + i ld.  tokens: one of the vocabulary for each row; a negative one is a
  * position that does not count (its row is not read: log-probability 0, gradient 0, no share in a loss), one beyond the vocabulary
  * makes its results NaN.  Logits of -infinity are tokens that cannot be; where a row has nothing else its results are NaN. */

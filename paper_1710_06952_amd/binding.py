@@ -28,6 +28,7 @@ EXPORTS = [
     "adpsgd_synth_gradient", "adpsgd_run_sync_steps", "adpsgd_run_sync_steps_with", "adpsgd_metropolis_weights",
     "adpsgd_get_event_count", "adpsgd_set_event_count", "adpsgd_verify_plan", "adpsgd_objective", "adpsgd_objective_weighted", "adpsgd_count_nonfinite",
     "adpsgd_dense_workspace_bytes", "adpsgd_dense_forward", "adpsgd_dense_backward", "adpsgd_loss_workspace_bytes", "adpsgd_token_log_probs",
+    "adpsgd_layer_norm_workspace_bytes", "adpsgd_layer_norm_forward", "adpsgd_layer_norm_backward",
     "adpsgd_policy_loss", "adpsgd_preference_loss", "adpsgd_adamw_state_length", "adpsgd_adamw_create", "adpsgd_adamw_destroy", "adpsgd_adamw_step",
     "adpsgd_adamw_get_steps", "adpsgd_adamw_set_steps", "adpsgd_adamw_get_moments", "adpsgd_adamw_set_moments",
 ]
@@ -89,6 +90,11 @@ class Dense(C.Structure):
                 ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("w_transposed", C.c_int32),
                 ("reserved", C.c_int32), ("b", C.c_void_p), ("r", C.c_void_p), ("ldr", C.c_int64), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_int64)]
+
+
+class LayerNorm(C.Structure):
+    _fields_ = [("type", C.c_int32), ("param_type", C.c_int32), ("rows", C.c_int64), ("n", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("w", C.c_void_p), ("b", C.c_void_p), ("eps", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
 class Logits(C.Structure):
@@ -171,6 +177,9 @@ def lib():
         L.adpsgd_dense_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.adpsgd_dense_forward.argtypes = [P(Dense), vp, vp, vp]
         L.adpsgd_dense_backward.argtypes = [P(Dense), vp, i64, vp, vp, vp, vp, vp]
+        L.adpsgd_layer_norm_workspace_bytes.argtypes = [i32, i64, i64]
+        L.adpsgd_layer_norm_forward.argtypes = [P(LayerNorm), vp, vp, vp]
+        L.adpsgd_layer_norm_backward.argtypes = [P(LayerNorm), vp, i64, vp, vp, vp, vp, vp]
         L.adpsgd_loss_workspace_bytes.argtypes = [i64, i64]
         L.adpsgd_token_log_probs.argtypes = [P(Logits), vp, vp]
         L.adpsgd_policy_loss.argtypes = [P(Logits), vp, vp, vp, f32, f32, f32, vp, vp, vp, vp]
@@ -184,7 +193,8 @@ def lib():
         L.adpsgd_adamw_set_steps.argtypes = [vp, i64]
         L.adpsgd_adamw_get_moments.argtypes = [vp, vp, vp, vp]
         L.adpsgd_adamw_set_moments.argtypes = [vp, vp, vp, vp]
-        for name in ("adpsgd_dense_workspace_bytes", "adpsgd_loss_workspace_bytes", "adpsgd_adamw_state_length"):
+        for name in ("adpsgd_dense_workspace_bytes", "adpsgd_loss_workspace_bytes", "adpsgd_adamw_state_length",
+                     "adpsgd_layer_norm_workspace_bytes"):
             getattr(L, name).restype = i64
         _lib = L
     return _lib

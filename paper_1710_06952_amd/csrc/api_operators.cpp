@@ -68,6 +68,23 @@ const char* dense_fault(const adpsgd_dense_t* o) {
     return nullptr;
 }
 
+// ---- layer norm ----
+bool norm_sizes(int64_t rows, int64_t n) {
+    return rows >= 0 && rows <= (int64_t(1) << 31) && n >= 1 && n <= (int64_t(1) << 28) && rows <= (int64_t(1) << 43) / n;
+}
+const char* norm_fault(const adpsgd_layer_norm_t* o) {
+    if (!o) return "layer_norm: no arguments";
+    if (!is_type(o->type) || (o->param_type != o->type && o->param_type != ADPSGD_TYPE_F32)) return "layer_norm: unknown type, or param_type neither that type nor F32";
+    if (!norm_sizes(o->rows, o->n)) return "layer_norm: rows <= 2^31, 1 <= n <= 2^28 and no more than 2^43 elements";
+    if (o->ldx < o->n || o->ldx > (int64_t(1) << 40)) return "layer_norm: the leading dimension is not n .. 2^40";
+    if (o->rows > 0 && !o->x) return "layer_norm: x is NULL";
+    if (o->b && !o->w) return "layer_norm: b without w";
+    const int64_t size = size_of(o->type), of_params = size_of(o->param_type);
+    if (!aligned_to(o->x, size) || !aligned_to(o->w, of_params) || !aligned_to(o->b, of_params)) return "layer_norm: a tensor is not aligned to its type";
+    return nullptr;
+}
+NormRows norm_rows(const adpsgd_layer_norm_t* o) { return NormRows{o->type, o->param_type, o->rows, o->n, o->x, o->ldx, o->w}; }
+
 // ---- losses ----
 bool loss_sizes(int64_t rows, int64_t vocab) {
     return rows >= 0 && vocab >= 1 && vocab <= (int64_t(1) << 30) && rows <= (int64_t(1) << 21) && rows * ((vocab + 4095) / 4096) <= (int64_t(1) << 23);
@@ -162,6 +179,36 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
             if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
         }
         return ADPSGD_OK;
+    });
+}
+
+extern "C" int64_t adpsgd_layer_norm_workspace_bytes(int32_t type, int64_t rows, int64_t n) {
+    return is_type(type) && norm_sizes(rows, n) ? norm_workspace_bytes(type, rows, n) : -1;
+}
+
+extern "C" int adpsgd_layer_norm_forward(const adpsgd_layer_norm_t* o, void* y, float* stats, void* stream) {
+    return guarded([&]() -> int {
+        if (const char* why = norm_fault(o)) return refuse(why);
+        if (!(o->eps < INFINITY) || !(static_cast<float>(o->eps) >= std::numeric_limits<float>::min())) return refuse("layer_norm: eps must be finite and 2^-126 or more");
+        if (o->rows > 0 && !y) return refuse("layer_norm: y is NULL");
+        if (!aligned_to(y, size_of(o->type)) || !aligned_to(stats, 4)) return refuse("layer_norm: a tensor is not aligned to its type");
+        return ended(launch_norm(norm_rows(o), o->b, o->eps, y, stats, static_cast<hipStream_t>(stream)), "layer_norm forward");
+    });
+}
+
+extern "C" int adpsgd_layer_norm_backward(const adpsgd_layer_norm_t* o, const void* dy, int64_t lddy, const float* stats, void* dx, void* dw, void* db,
+                                          void* stream) {
+    return guarded([&]() -> int {
+        if (const char* why = norm_fault(o)) return refuse(why);
+        if (o->rows > 0 && (!dy || !stats)) return refuse("layer_norm: dy or stats is NULL");
+        if (lddy < o->n || lddy > (int64_t(1) << 40)) return refuse("layer_norm: the leading dimension of dy is not n .. 2^40");
+        if (dw && !o->w) return refuse("layer_norm: dw without w");
+        const int64_t size = size_of(o->type), of_params = size_of(o->param_type);
+        if (!aligned_to(dy, size) || !aligned_to(dx, size) || !aligned_to(stats, 4) || !aligned_to(dw, of_params) || !aligned_to(db, of_params))
+            return refuse("layer_norm: a tensor is not aligned to its type");
+        const int64_t bytes = dw || db ? norm_workspace_bytes(o->type, o->rows, o->n) : 0;
+        if (o->workspace_bytes < bytes || (bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("layer_norm: workspace missing, not 16-byte aligned or too small");
+        return ended(launch_norm_gradient(norm_rows(o), dy, lddy, stats, dx, dw, db, o->workspace, static_cast<hipStream_t>(stream)), "layer_norm backward");
     });
 }
 

@@ -27,6 +27,18 @@ hipError_t launch_dense_dz(int32_t type, const void* dy, int64_t lddy, const uin
                            hipStream_t s);
 int64_t dense_sums_bytes(int64_t M, int64_t N);
 
+// ---- layer norm (kernels_norm.hip) ----
+struct NormRows {
+    int32_t type, param_type;
+    int64_t rows, n;
+    const void* x;
+    int64_t ldx;
+    const void* w;                  // n, or nullptr
+};
+int64_t norm_workspace_bytes(int32_t type, int64_t rows, int64_t n);       // of a gradient
+hipError_t launch_norm(const NormRows& r, const void* b, double eps, void* y, float* stats, hipStream_t s);
+hipError_t launch_norm_gradient(const NormRows& r, const void* dy, int64_t lddy, const float* stats, void* dx, void* dw, void* db, void* ws, hipStream_t s);
+
 // ---- losses over a vocabulary (kernels_losses.hip) ----
 struct LossRows {
     int32_t type;

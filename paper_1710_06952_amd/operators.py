@@ -212,6 +212,115 @@ def dense_gradients(dy, x, w, slope, *, activation="none", need=(True, True, Tru
         return _backward(dy, x, w, slope if activation != "none" else None, activation, *need)
 
 
+# ---- layer norm -------------------------------------------------------------------------------------------------
+
+_FAR = 1 << 40          # elements from one row to the next, at most, where rows are walked one by one
+
+
+def _check_norm(x, w, b, dy=None):
+    _on_gpu("x", x)
+    if x.dtype not in _TYPES:
+        raise TypeError("layer_norm takes float32, bfloat16 or float16, not %s" % x.dtype)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x is %s: the last dimension is what is normalised" % (tuple(x.shape),))
+    if b is not None and w is None:
+        raise ValueError("a bias without a weight")
+    for name, t in (("weight", w), ("bias", b)):
+        if t is None:
+            continue
+        _on_gpu(name, t, x.device)
+        if t.dtype not in (x.dtype, torch.float32) or t.dtype != w.dtype:
+            raise TypeError("x is %s, %s is %s: weight and bias are both of that type or both float32" % (x.dtype, name, t.dtype))
+        if t.shape != x.shape[-1:]:
+            raise ValueError("%s is %s, x %s" % (name, tuple(t.shape), tuple(x.shape)))
+    if dy is not None:
+        _on_gpu("dy", dy, x.device)
+        if dy.dtype != x.dtype or dy.shape != x.shape:
+            raise ValueError("dy is %s %s, must be as x, %s %s" % (tuple(dy.shape), dy.dtype, tuple(x.shape), x.dtype))
+
+
+def _norm_args(x, w, b, eps):
+    xm, ldx = _as_rows(x, _FAR)
+    rows, n = xm.shape
+    kind = _TYPES[x.dtype]
+    w, b = (None if t is None else t.contiguous() for t in (w, b))
+    return B.LayerNorm(kind, kind if w is None else _TYPES[w.dtype], rows, n, xm.data_ptr(), ldx, _ptr(w), _ptr(b), eps, None, 0), (xm, w, b)
+
+
+def _norm_forward(x, w, b, eps, want_stats):
+    args, keep = _norm_args(x, w, b, eps)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty(3, args.rows, dtype=torch.float32, device=x.device) if want_stats else None
+    _call(x.device, B.lib().adpsgd_layer_norm_forward, C.byref(args), y.data_ptr(), _ptr(stats))
+    del keep
+    return y, stats
+
+
+def _norm_backward(dy, x, w, stats, need_dx, need_dw, need_db):
+    args, keep = _norm_args(x, w, None, 1.0)
+    dym, lddy = _as_rows(dy, _FAR)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
+    dw, db = (torch.empty_like(w, memory_format=torch.contiguous_format) if needed and w is not None else None for needed in (need_dw, need_db))
+    space = None
+    if dw is not None or db is not None:
+        size = B.lib().adpsgd_layer_norm_workspace_bytes(args.type, args.rows, args.n)
+        if size > 0:
+            space = torch.empty(size, dtype=torch.uint8, device=x.device)
+            args.workspace, args.workspace_bytes = space.data_ptr(), size
+    _call(x.device, B.lib().adpsgd_layer_norm_backward, C.byref(args), dym.data_ptr(), lddy, stats.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db))
+    del keep, space
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, b, eps):
+        y, stats = _norm_forward(x, w, b, eps, True)
+        ctx.save_for_backward(x, w, stats)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, w, stats = ctx.saved_tensors
+        return (*_norm_backward(dy, x, w, stats, *ctx.needs_input_grad[:3]), None)
+
+
+def layer_norm(x, weight=None, bias=None, *, eps=1e-5):
+    """(x - mean) / sqrt(var + eps) weight + bias over the last dimension, differentiable (once, in reverse mode) in all three.
+
+    x (..., n) float32, bfloat16 or float16; weight and bias (n) both of that type or both float32, bias only with a weight.  Means,
+    variances and sums are in 32 bits or more, results are rounded once.  With gradients, 12 bytes a row are kept for the
+    backward pass.  Under capture of a HIP graph the differentiable form is refused, as dense's is: layer_norm_forward and
+    layer_norm_gradients can be captured."""
+    _check_norm(x, weight, bias)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("layer_norm with gradients cannot be captured: capture layer_norm_forward and layer_norm_gradients")
+        return _LayerNorm.apply(x, weight, bias, eps)
+    return _norm_forward(x, weight, bias, eps, False)[0]
+
+
+def layer_norm_forward(x, weight=None, bias=None, *, eps=1e-5):
+    """(y, stats): the forward pass without autograd, and what layer_norm_gradients needs."""
+    _check_norm(x, weight, bias)
+    with torch.no_grad():
+        return _norm_forward(x, weight, bias, eps, True)
+
+
+def layer_norm_gradients(dy, x, weight, stats, *, need=(True, True, True)):
+    """(dx, dweight, dbias) for dy; None where ``need`` says so, and without a weight for the last two."""
+    _check_norm(x, weight, None, dy)
+    _on_gpu("stats", stats, x.device)
+    if stats.dtype != torch.float32 or stats.shape != (3, x.numel() // x.shape[-1]) or not stats.is_contiguous():
+        raise ValueError("stats must be what layer_norm_forward returned")
+    need = (need[0], need[1] and weight is not None, need[2] and weight is not None)
+    if not any(need):
+        return None, None, None
+    with torch.no_grad():
+        return _norm_backward(dy, x, weight, stats, *need)
+
+
 # ---- losses over a vocabulary -----------------------------------------------------------------------------------
 
 def _logits(logits, tokens):

@@ -1,0 +1,83 @@
+"""What layer norm, the gated projections and the distillation loss refuse, at the C entries (host checks, before anything touches a GPU) and in Python."""
+import ctypes as C
+
+import pytest
+
+import paper_1710_06952_amd as P
+from paper_1710_06952_amd import binding as B
+
+NOWHERE = 1 << 20                                        # an aligned address that is never read
+
+
+def refused(rc, word):
+    assert rc == B.ERR_ARG
+    assert word in B.lib().adpsgd_last_error(None).decode(), B.lib().adpsgd_last_error(None)
+
+
+def norm_args(**kw):
+    o = dict(type=B.TYPE_BF16, param_type=B.TYPE_BF16, rows=4, n=16, x=NOWHERE, ldx=16, w=NOWHERE, b=NOWHERE, eps=1e-5, workspace=NOWHERE,
+             workspace_bytes=1 << 20)
+    o.update(kw)
+    return B.LayerNorm(**o)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(type=5), "type"), (dict(param_type=B.TYPE_F16), "type"), (dict(type=B.TYPE_F32), "type"), (dict(rows=-1), "rows"), (dict(n=0), "rows"), (dict(n=(1 << 28) + 1, ldx=1 << 29), "rows"),
+    (dict(rows=(1 << 31) + 1), "rows"), (dict(rows=1 << 30, n=1 << 20, ldx=1 << 20), "rows"), (dict(ldx=15), "leading"), (dict(ldx=1 << 41), "leading"), (dict(x=None), "NULL"),
+    (dict(w=None), "without w"), (dict(x=NOWHERE + 1), "aligned"), (dict(w=NOWHERE + 1), "aligned"), (dict(param_type=B.TYPE_F32, b=NOWHERE + 2), "aligned")])
+def test_layer_norm(change, word):
+    L = B.lib()
+    refused(L.adpsgd_layer_norm_forward(C.byref(norm_args(**change)), NOWHERE, NOWHERE, None), word)
+    refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(**change)), NOWHERE, 1 << 20, NOWHERE, NOWHERE, NOWHERE, NOWHERE, None), word)
+
+
+def test_layer_norm_calls():
+    L, at = B.lib(), NOWHERE
+    refused(L.adpsgd_layer_norm_forward(None, at, at, None), "no arguments")
+    for eps in (0.0, -1e-5, 1e-40, float("inf"), float("nan")):
+        refused(L.adpsgd_layer_norm_forward(C.byref(norm_args(eps=eps)), at, at, None), "eps")
+    refused(L.adpsgd_layer_norm_forward(C.byref(norm_args()), None, at, None), "y is NULL")
+    refused(L.adpsgd_layer_norm_forward(C.byref(norm_args()), at + 1, at, None), "aligned")
+    refused(L.adpsgd_layer_norm_forward(C.byref(norm_args()), at, at + 2, None), "aligned")
+    o = norm_args()
+    refused(L.adpsgd_layer_norm_backward(C.byref(o), None, 16, at, at, at, at, None), "dy or stats")
+    refused(L.adpsgd_layer_norm_backward(C.byref(o), at, 16, None, at, at, at, None), "dy or stats")
+    refused(L.adpsgd_layer_norm_backward(C.byref(o), at, 15, at, at, at, at, None), "leading dimension of dy")
+    refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(w=None, b=None)), at, 16, at, at, at, None, None), "dw without w")
+    refused(L.adpsgd_layer_norm_backward(C.byref(o), at, 16, at, at, at + 1, at, None), "aligned")
+    for short in (dict(workspace_bytes=8), dict(workspace=None), dict(workspace=at + 8)):
+        refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(**short)), at, 16, at, None, at, None, None), "workspace")
+    assert L.adpsgd_layer_norm_forward(C.byref(norm_args(rows=0, x=None)), None, None, None) == B.OK       # no rows: nothing to do
+    assert L.adpsgd_layer_norm_backward(C.byref(norm_args(rows=0, x=None)), None, 16, None, None, None, None, None) == B.OK
+    assert L.adpsgd_layer_norm_workspace_bytes(9, 4, 16) == L.adpsgd_layer_norm_workspace_bytes(0, -1, 16) == L.adpsgd_layer_norm_workspace_bytes(0, 4, 0) == -1
+    assert L.adpsgd_layer_norm_workspace_bytes(0, 0, 16) == 0 and L.adpsgd_layer_norm_workspace_bytes(1, 4, 16) >= 128
+
+
+def test_layer_norm_tensors_that_are_not_on_a_gpu():
+    import torch
+    x, w = torch.zeros(4, 8), torch.zeros(8)
+    for call in (lambda: P.layer_norm(x, w), lambda: P.layer_norm_forward(x, w, w), lambda: P.layer_norm_gradients(x, x, w, torch.zeros(3, 4))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    with pytest.raises(TypeError, match="tensor"):
+        P.layer_norm([1.0])
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level():
+        with pytest.raises(NotImplementedError, match="forward mode"):
+            P.layer_norm(forward_ad.make_dual(x, x), w)
+
+
+@pytest.mark.gpu
+def test_layer_norm_shapes_and_types():
+    import torch
+    new = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda:0")  # noqa: E731
+    x, w, stats = new(4, 8), new(8), new(3, 4, dtype=torch.float32)
+    for call, kind, word in [
+            (lambda: P.layer_norm(x.double()), TypeError, "float32"), (lambda: P.layer_norm(x, w.half()), TypeError, "both"), (lambda: P.layer_norm(x.float(), w), TypeError, "both"),
+            (lambda: P.layer_norm(x, w, w.float()), TypeError, "both"), (lambda: P.layer_norm(x, None, w), ValueError, "without a weight"),
+            (lambda: P.layer_norm(x, new(7)), ValueError, "weight is"), (lambda: P.layer_norm(x, w, new(1, 8)), ValueError, "bias is"), (lambda: P.layer_norm(x, w.cpu()), ValueError, "GPU"),
+            (lambda: P.layer_norm(new(4, 0)), ValueError, "last dimension"), (lambda: P.layer_norm(x, eps=0.0), P.AdpsgdError, "eps"),
+            (lambda: P.layer_norm_gradients(x.float(), x, w, stats), ValueError, "dy is"), (lambda: P.layer_norm_gradients(x[:3], x, w, stats), ValueError, "dy is"),
+            (lambda: P.layer_norm_gradients(x, x, w, stats[:, :3]), ValueError, "stats"), (lambda: P.layer_norm_gradients(x, x, w, stats.half()), ValueError, "stats")]:
+        with pytest.raises(kind, match=word):
+            call()
