@@ -192,6 +192,7 @@ extern "C" int adpsgd_layer_norm_forward(const adpsgd_layer_norm_t* o, void* y, 
         if (!(o->eps < INFINITY) || !(static_cast<float>(o->eps) >= std::numeric_limits<float>::min())) return refuse("layer_norm: eps must be finite and 2^-126 or more");
         if (o->rows > 0 && !y) return refuse("layer_norm: y is NULL");
         if (!aligned_to(y, size_of(o->type)) || !aligned_to(stats, 4)) return refuse("layer_norm: a tensor is not aligned to its type");
+        if (o->rows == 0) return ADPSGD_OK;
         return ended(launch_norm(norm_rows(o), o->b, o->eps, y, stats, static_cast<hipStream_t>(stream)), "layer_norm forward");
     });
 }
@@ -208,6 +209,7 @@ extern "C" int adpsgd_layer_norm_backward(const adpsgd_layer_norm_t* o, const vo
             return refuse("layer_norm: a tensor is not aligned to its type");
         const int64_t bytes = dw || db ? norm_workspace_bytes(o->type, o->rows, o->n) : 0;
         if (o->workspace_bytes < bytes || (bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("layer_norm: workspace missing, not 16-byte aligned or too small");
+        if (!dw && !db && (o->rows == 0 || !dx)) return ADPSGD_OK;
         return ended(launch_norm_gradient(norm_rows(o), dy, lddy, stats, dx, dw, db, o->workspace, static_cast<hipStream_t>(stream)), "layer_norm backward");
     });
 }

@@ -564,8 +564,7 @@ hipError_t launch_norm(const NormRows& r, const void* b, double eps, void* y, fl
     a.ldx = r.ldx; a.rows = r.rows; a.n = static_cast<int>(r.n);
     a.eps = static_cast<float>(eps);
     a.y = y; a.stats = stats;
-    if (r.rows > 0)
-        with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_of<decltype(e), decltype(w)>(a, s); });
+    with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_of<decltype(e), decltype(w)>(a, s); });
     return hipGetLastError();
 }
 
@@ -576,8 +575,7 @@ hipError_t launch_norm_gradient(const NormRows& r, const void* dy, int64_t lddy,
     a.stats = stats;
     a.dx = dx;
     a.sums = dw || db ? static_cast<float*>(ws) : nullptr;
-    if (dx || dw || db)
-        with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_gradient_of<decltype(e), decltype(w)>(r.type, a, dw, db, s); });
+    with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_gradient_of<decltype(e), decltype(w)>(r.type, a, dw, db, s); });
     return hipGetLastError();
 }
 
