@@ -497,6 +497,24 @@ int adpsgd_dense_forward(const adpsgd_dense_t* o, void* y, uint16_t* slope, void
 int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, int64_t lddy, const uint16_t* slope, void* dx, void* dw, void* db,
                           void* stream);
 
+/* Gated projections, the first half of a feed-forward block (its second half is a dense layer):
+ *   g = x Wg^T + bg,  u = x Wu^T + bu,  h = act(g) u
+ * in one pass over x.  The arguments are those of a dense layer with N the columns of h: w has 2 N rows (w_transposed: rows of 2 N), Wg's and then
+ * Wu's, b is [bg | bu] or NULL, r is NULL.  g, u and their product are in 32 bits, h is rounded once. */
+
+/* Host only: the workspace of a forward (backward = 0) or backward call of these sizes; -1 where an argument is refused. */
+int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward);
+
+/* h: M x N, contiguous.  slopes (or NULL): M x 2 N 16-bit words, contiguous, receives dh/dg and dh/du for the backward call (fp16: as
+ * they are; bf16: the fp16 roots of their magnitudes with their signs). */
+int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream);
+
+/* Gradients for dh (M x N, row m at dh + m lddh): dx (M x K, contiguous), dw (as w is stored, contiguous) and db (2 N); each may be NULL.
+ * slopes: as the forward call wrote them.  dz = [dh dh/dg | dh dh/du] is rounded to the type once for the two products; db adds it before
+ * that rounding. */
+int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, int64_t lddh, const uint16_t* slopes, void* dx, void* dw, void* db,
+                          void* stream);
+
 /* Layer norm over rows of n elements:  y = (x - mean) / sqrt(var + eps) w + b,  var the mean of (x - mean)^2.  x, y and their
  * gradients are of one type, w and b both of param_type: that type or F32.  Means and variances are in 32 bits with the mean in two parts, so a
  * mean far from 0 costs no accuracy.  A row with a value that is not finite is NaN. */

@@ -68,6 +68,49 @@ const char* dense_fault(const adpsgd_dense_t* o) {
     return nullptr;
 }
 
+// ---- gated projections ----
+const char* gated_fault(const adpsgd_dense_t* o) {
+    if (!o) return "gated: no arguments";
+    if (o->type != ADPSGD_TYPE_BF16 && o->type != ADPSGD_TYPE_F16) return "gated: type must be BF16 or F16";
+    if (o->activation < ADPSGD_ACT_NONE || o->activation > ADPSGD_ACT_SILU) return "gated: unknown activation";
+    if (o->N < 1 || o->N >= kMostSide || !dense_sizes(o->M, 2 * o->N, o->K)) return "gated: M >= 0, N >= 1, K >= 1, and no product of two of M, 2 N and K over 2^34";
+    if (o->ldx < o->K || o->ldw < (o->w_transposed ? 2 * o->N : o->K)) return "gated: a leading dimension is too small";
+    if (o->ldx > kMostStride || o->ldw > kMostStride || 2 * o->N > kMostStride || o->K > kMostStride) return "gated: rows of more than 2^22 elements";
+    if (o->r) return "gated: there is no residual";
+    if (!o->w || (o->M > 0 && !o->x)) return "gated: x or w is NULL";
+    if (!aligned_to(o->x, 2) || !aligned_to(o->w, 2) || !aligned_to(o->b, 2)) return "gated: a tensor is not aligned to its type";
+    return nullptr;
+}
+// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.
+hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, void* dx, void* dw, void* partial, int64_t partial_bytes, hipStream_t s) {
+    DenseGemm g{};
+    g.act = ADPSGD_ACT_NONE;
+    g.partial = static_cast<float*>(partial);
+    g.partial_bytes = partial_bytes;
+    if (dx && o->M > 0) {
+        g.a = dz; g.lda = lddz; g.a_outer = false;
+        g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed == 0;
+        g.I = o->M; g.J = o->K; g.K = N;
+        g.out = dx;
+        hipError_t e = launch_dense_gemm(o->type, g, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dw) {
+        g.a_outer = g.b_outer = true;
+        g.K = o->M;
+        g.out = dw;
+        if (o->w_transposed) {
+            g.a = o->x; g.lda = o->ldx; g.I = o->K;
+            g.b = dz; g.ldb = lddz; g.J = N;
+        } else {
+            g.a = dz; g.lda = lddz; g.I = N;
+            g.b = o->x; g.ldb = o->ldx; g.J = o->K;
+        }
+        return launch_dense_gemm(o->type, g, s);
+    }
+    return hipSuccess;
+}
+
 // ---- layer norm ----
 bool norm_sizes(int64_t rows, int64_t n) {
     return rows >= 0 && rows <= (int64_t(1) << 31) && n >= 1 && n <= (int64_t(1) << 28) && rows <= (int64_t(1) << 43) / n;
@@ -152,33 +195,49 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
             hipError_t e = launch_dense_dz(o->type, dy, lddy, of, own ? ws + at.dz : nullptr, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
             if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
         }
+        return ended(backward_products(o, o->N, dz, lddz, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
+    });
+}
+
+extern "C" int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward) {
+    if (N < 1 || N >= kMostSide || !dense_sizes(M, 2 * N, K)) return -1;
+    return backward ? backward_space(M, 2 * N, K).bytes : up256(gated_partial_bytes(M, N, K));
+}
+
+extern "C" int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream) {
+    return guarded([&]() -> int {
+        if (const char* why = gated_fault(o)) return refuse(why);
+        if (o->M == 0) return ADPSGD_OK;
+        if (!h || !aligned_to(h, 2) || !aligned_to(slopes, 2)) return refuse("gated: h is NULL, or not aligned to its type");
+        const int64_t bytes = up256(gated_partial_bytes(o->M, o->N, o->K));
+        if (o->workspace_bytes < bytes || (bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("gated: workspace missing, not 16-byte aligned or too small");
         DenseGemm g{};
-        g.act = ADPSGD_ACT_NONE;
-        g.partial = reinterpret_cast<float*>(ws + at.partial);
-        g.partial_bytes = at.bytes - at.partial;
-        if (dx && o->M > 0) {
-            g.a = dz; g.lda = lddz; g.a_outer = false;
-            g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed == 0;
-            g.I = o->M; g.J = o->K; g.K = o->N;
-            g.out = dx;
-            hipError_t e = launch_dense_gemm(o->type, g, s);
-            if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
-        }
-        if (dw) {
-            g.a_outer = g.b_outer = true;
-            g.K = o->M;
-            g.out = dw;
-            if (o->w_transposed) {
-                g.a = o->x; g.lda = o->ldx; g.I = o->K;
-                g.b = dz; g.ldb = lddz; g.J = o->N;
-            } else {
-                g.a = dz; g.lda = lddz; g.I = o->N;
-                g.b = o->x; g.ldb = o->ldx; g.J = o->K;
-            }
-            hipError_t e = launch_dense_gemm(o->type, g, s);
-            if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
-        }
-        return ADPSGD_OK;
+        g.a = o->x; g.lda = o->ldx;
+        g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed != 0;
+        g.I = o->M; g.J = o->N; g.K = o->K;
+        g.act = o->activation;
+        g.bias = o->b;
+        g.out = h; g.slope = slopes;
+        g.partial = static_cast<float*>(o->workspace); g.partial_bytes = bytes;
+        return ended(launch_gated_gemm(o->type, g, static_cast<hipStream_t>(stream)), "gated forward");
+    });
+}
+
+extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, int64_t lddh, const uint16_t* slopes, void* dx, void* dw, void* db, void* stream) {
+    return guarded([&]() -> int {
+        if (const char* why = gated_fault(o)) return refuse(why);
+        if (o->M > 0 && (!dh || !slopes)) return refuse("gated: dh or slopes is NULL");
+        if (lddh < o->N || lddh > kMostStride) return refuse("gated: the leading dimension of dh is not N .. 2^22");
+        if (!aligned_to(dh, 2) || !aligned_to(slopes, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(db, 2)) return refuse("gated: a tensor is not aligned to its type");
+        const BackwardSpace at = backward_space(o->M, 2 * o->N, o->K);
+        if (o->workspace_bytes < at.bytes || (at.bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("gated: workspace missing, not 16-byte aligned or too small");
+        if (!dx && !dw && !db) return ADPSGD_OK;
+        hipStream_t s = static_cast<hipStream_t>(stream);
+        char* ws = static_cast<char*>(o->workspace);
+        void* dz = dx || dw ? ws + at.dz : nullptr;
+        hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
+        if (e == hipSuccess) e = backward_products(o, 2 * o->N, dz, 2 * o->N, dx, dw, ws + at.partial, at.bytes - at.partial, s);
+        return ended(e, "gated backward");
     });
 }
 

@@ -99,6 +99,20 @@ __device__ __forceinline__ float slope_of(uint32_t w) {
     return w == 0u ? NAN : r * fabsf(r);
 }
 
+// Slopes of gated projections.  What the backward pass needs of a result h = act(g) u is dh/dg = u act'(g) and dh/du = act(g), kept in 16 bits each.  fp16: as they are.  bf16: their roots with
+// their signs, in fp16: a slope is within 2^-10 of itself, where bf16 would add 2^-8 to what dz is rounded by, from 4e-9 to 2^32 (down to 4e-15 in
+// larger steps, infinite above).
+template <class T>
+__device__ __forceinline__ uint16_t gated_slope_word(float s) {
+    if constexpr (std::is_same<T, Bf16>::value) s = copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s);
+    return F16::down(s);
+}
+template <class T>
+__device__ __forceinline__ float gated_slope(uint16_t w) {
+    const float r = F16::up(w);
+    return std::is_same<T, Bf16>::value ? r * fabsf(r) : r;
+}
+
 // How a product is cut: tiles of side x side (0: columns, dense_narrow.hpp), `splits` parts of k whose sums are joined afterwards.
 struct DensePlan {
     int side;
@@ -116,7 +130,24 @@ inline hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int
     return once_a_device(done, device, hipSuccess, [&] { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
+// Whether a product goes to the kernel for few rows, how it is cut, and copies of operands whose rows are no whole pieces (kernels_dense.hip).
+bool few_rows(int64_t I, int64_t J, int64_t K, bool b_outer, bool b_whole);
+DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct);
+bool whole_pieces(const void* p, int64_t ld, int64_t inner);
+bool worth_packing(int64_t I, int64_t J, int64_t K);
+int64_t packed_bytes(int64_t rows, int64_t inner);
+// rows x inner at `from` to rows of ldto elements at `to`, whole pieces with zeros at their ends
+void launch_pack(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t inner, hipStream_t s);
+
+// Strips that a pass over dy sums by itself (256 rows each, as many as 64: with N = 8192 four blocks for a compute unit), and their sums.
+int strips_of(int64_t M);
+template <class T>
+void launch_dense_db(const double* sums, int strips, int64_t N, void* db, hipStream_t s);
+
 template <class T>
 hipError_t launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
+
+template <class T>
+hipError_t launch_gated_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 
 }  // namespace adpsgd_impl

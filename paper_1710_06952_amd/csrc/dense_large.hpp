@@ -45,7 +45,9 @@ constexpr uint32_t kOutOfRange = 0x80000000u;
 // Rows are whole pieces: where a row's length is no multiple of 8 it has been copied with zeros behind it (dense_pack_kernel).
 __device__ __forceinline__ int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 
-template <bool kOuter, int kSide, int kStep>
+// kGated: kSide / 2 gates and their partners `up` elements behind them (dense_tiles.hpp).  With k inner a wavefront's eight rows of a load are of one
+// kind, so the partners are a matter of where its loads begin; with k outer of a lane's offset.
+template <bool kOuter, int kSide, int kStep, bool kGated = false>
 struct DirectOperand {
     static constexpr int kThreads = 256, kLoads = kSide * kBK / 8 / kThreads;
     typedef Operand<kOuter, kSide, kThreads, kStep> Form;
@@ -56,8 +58,9 @@ struct DirectOperand {
     v4su rsrc;                  // of the step that is being loaded ...
     uint32_t to, cut, none;     // ... its place in LDS, all ones in the last step, and kOutOfRange behind it
 
-    __device__ void start(const void* p, int64_t ld, int64_t first, int64_t all, int64_t K) {
-        const uint64_t at = reinterpret_cast<uint64_t>(p);
+    __device__ void start(const void* p, int64_t ld, int64_t first, int64_t all, int64_t K, int64_t up = 0) {
+        constexpr int kMost = kGated ? kSide / 2 : kSide;
+        const uint64_t at = reinterpret_cast<uint64_t>(p) + (kGated && !kOuter && (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 1) ? 2 * up : 0);
         const uint32_t pitch = static_cast<uint32_t>(ld * 2);
         if (!kOuter) {
             base = at + static_cast<uint64_t>(first) * pitch;
@@ -68,19 +71,20 @@ struct DirectOperand {
             for (int s = 0; s < 2; ++s) beyond[s] = ((threadIdx.x & 7) ^ Form::turn_of(s * 32 + (threadIdx.x >> 3))) < there ? 0u : kOutOfRange;
         } else {
             base = at + 2 * first;
-            end = at + static_cast<uint64_t>(K - 1) * pitch + 2 * up8(all);
+            end = at + static_cast<uint64_t>(K - 1) * pitch + 2 * (up8(all) + (kGated ? up : 0));
             advance = static_cast<uint64_t>(kBK) * pitch;
         }
-        const int rows = static_cast<int>(all - first < kSide ? all - first : kSide);
+        const int rows = static_cast<int>(all - first < kMost ? all - first : kMost);
 #pragma unroll
         for (int s = 0; s < kLoads; ++s) {
             const int id = s * kThreads + static_cast<int>(threadIdx.x);
             if (!kOuter) {
                 const int row = id >> 3, piece = (id & 7) ^ Form::turn_of(row);
-                offset[s] = static_cast<uint32_t>(row < rows ? row : rows - 1) * pitch + piece * 16;
+                const int from = kGated ? gated_row(row) : row;
+                offset[s] = static_cast<uint32_t>(from < rows ? from : rows - 1) * pitch + piece * 16;
             } else {
                 const int k = id / Form::kPieces, piece = (id % Form::kPieces) ^ Form::piece_of(k);
-                offset[s] = static_cast<uint32_t>(k) * pitch + piece * 16;
+                offset[s] = static_cast<uint32_t>(k) * pitch + (kGated ? gated_row(piece * 8) * 2 + (gated_kind(piece * 8) ? static_cast<uint32_t>(2 * up) : 0u) : piece * 16);
             }
         }
     }
@@ -139,20 +143,21 @@ struct FragmentReader {
     }
 };
 
-template <class T, bool kAOuter, bool kBOuter, int kSide>
+template <class T, bool kAOuter, bool kBOuter, int kSide, bool kGated = false>
 __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(const DenseGemm g, const int splits) {
     constexpr int kTI = kSide / 32, kTJ = kTI, kHalf = kSide * kBK;
     typedef DirectOperand<kAOuter, kSide, 0> OpA;
-    typedef DirectOperand<kBOuter, kSide, 4 * kTJ> OpB;
+    constexpr int kSideJ = kGated ? kSide / 2 : kSide;                   // results of a tile's row
+    typedef DirectOperand<kBOuter, kSide, 4 * kTJ, kGated> OpB;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
-    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSide - 1) / kSide;
+    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSideJ - 1) / kSideJ;
     int64_t ti, tj, split;
     place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
     const int64_t steps = (g.K + kBK - 1) / kBK, s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
     OpA a;
     OpB b;
     a.start(g.a, g.lda, ti * kSide, g.I, g.K);
-    b.start(g.b, g.ldb, tj * kSide, g.J, g.K);
+    b.start(g.b, g.ldb, tj * kSideJ, g.J, g.K, g.b_up);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = (wave >> 1) * (kSide / 2), wj = (wave & 1) * (kSide / 2);
     const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint16_t*)lds)), place = at + wave * 1024;
     FragmentReader<kAOuter, kSide, 0> read_a;
@@ -240,6 +245,44 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
     v4u* kept = reinterpret_cast<v4u*>(lds) + wave * (kTurns * 64) + lane;                     // a lane's own
     float* own = reinterpret_cast<float*>(reinterpret_cast<v4u*>(lds) + 4 * kTurns * 64) + wave * (16 * kColumns);
     const uint32_t stage = at + (4 * kTurns * 64) * 16 + wave * (16 * kColumns * 4) + l * (kColumns * 4) + (((q * kTJ) ^ (l & kMask)) * 16);
+    if constexpr (kGated) {
+        // A lane takes eight neighbouring gates and the eight partners behind them, half as many lanes a row.
+        constexpr int kPairs = kColumns / 16, kAtOnce = 64 / kPairs;
+        const int pair = lane % kPairs, first = lane / kPairs;
+        const int64_t gi0 = ti * kSide + wi + first, gj = tj * kSideJ + wj / 2 + 8 * pair;
+        auto finish_gated = [&](auto whole) {
+            const GatedEnding<T, decltype(whole)::value> end(g, gj);
+#pragma unroll 1
+            for (int m = 0; m < kTI; ++m) {
+#pragma unroll
+                for (int k = 0; k < kTI; ++k)
+                    if (m == k) {
+#pragma unroll
+                        for (int n = 0; n < kTJ; ++n) write_result(stage ^ (n * 16), acc[k][n]);
+                    }
+                wait_results();
+#pragma unroll 1
+                for (int turn = 0; turn < 16 / kAtOnce; ++turn) {
+                    const int row = turn * kAtOnce + first;
+                    float f[16];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const v4f part = *reinterpret_cast<const v4f*>(own + row * kColumns + ((4 * pair + v) ^ (row & kMask)) * 4);
+                        f[4 * v] = part.x;
+                        f[4 * v + 1] = part.y;
+                        f[4 * v + 2] = part.z;
+                        f[4 * v + 3] = part.w;
+                    }
+                    if (splits > 1) store_gated_part(g, split, gi0 + m * 16 + turn * kAtOnce, gj, f, f + 8);
+                    else end.finish(gi0 + m * 16 + turn * kAtOnce, f, f + 8);
+                }
+                wave_lds_sync();
+            }
+        };
+        if (g.J % 8 == 0) finish_gated(std::true_type());
+        else finish_gated(std::false_type());
+        return;
+    }
     const int64_t i0 = ti * kSide + wi + at_row, j = tj * kSide + wj + 8 * c;
     auto finish_rows = [&](auto whole) {
         const Ending<T, decltype(whole)::value> end(g, j);
@@ -278,11 +321,12 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
     else finish_rows(std::false_type());
 }
 
-template <class T, bool kAOuter, bool kBOuter, int kSide>
+template <class T, bool kAOuter, bool kBOuter, int kSide, bool kGated = false>
 hipError_t launch_large(const DenseGemm& g, int splits, hipStream_t s) {
-    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
+    constexpr int kSideJ = kGated ? kSide / 2 : kSide;
+    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSideJ - 1) / kSideJ);
     constexpr int kBytes = kSide == 256 ? 160 * 1024 : 4 * kSide * kBK * 2;       // two steps' operands; the end of the large tiles needs more
-    auto kernel = dense_large_kernel<T, kAOuter, kBOuter, kSide>;
+    auto kernel = dense_large_kernel<T, kAOuter, kBOuter, kSide, kGated>;
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
     if (e != hipSuccess) return e;

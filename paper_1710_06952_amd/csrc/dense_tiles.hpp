@@ -53,21 +53,30 @@ __device__ __forceinline__ v4u load_cut(const uint16_t* row, int64_t start, int6
     return v4u{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
-// One operand: kRows rows (of i or j) by 64 k, loaded by kThreads threads; kStep: 4 TJ of the permuted operand, or 0.
-template <bool kOuter, int kRows, int kThreads, int kStep>
+// Rows of a tile of gated weights: eight gates, their eight partners, eight gates ...  Row r is the partner of a gate or a gate itself
+// (kind), and the number of that gate in the tile.
+__device__ __forceinline__ int gated_kind(int r) { return r >> 3 & 1; }
+__device__ __forceinline__ int gated_row(int r) { return (r >> 4) * 8 + (r & 7); }
+
+// One operand: kRows rows (of i or j) by 64 k, loaded by kThreads threads; kStep: 4 TJ of the permuted operand, or 0.  kGated: kRows / 2 gates
+// and their partners `up` elements behind them.
+template <bool kOuter, int kRows, int kThreads, int kStep, bool kGated = false>
 struct Operand {
     static constexpr int kVectors = kRows * kBK / 8 / kThreads;      // of a thread
     static constexpr int kPieces = kRows / 8;                        // of a k where k is outer
     static_assert(kRows * kBK / 8 % kThreads == 0, "");
     const uint16_t* base;       // row 0 of the tile at k 0
     int64_t ld, rows, depth;    // rows of the tile that are there
+    int64_t up;
     bool edge;
     v4u x[kVectors];
 
-    __device__ void start(const void* p, int64_t stride, int64_t first, int64_t all, int64_t K) {
+    __device__ void start(const void* p, int64_t stride, int64_t first, int64_t all, int64_t K, int64_t partner = 0) {
+        constexpr int kMost = kGated ? kRows / 2 : kRows;
         ld = stride;
-        rows = all - first < kRows ? all - first : kRows;
-        edge = rows < kRows;
+        up = partner;
+        rows = all - first < kMost ? all - first : kMost;
+        edge = rows < kMost;
         depth = K;
         base = static_cast<const uint16_t*>(p) + (kOuter ? first : first * stride);
     }
@@ -85,18 +94,18 @@ struct Operand {
         for (int s = 0; s < kVectors; ++s) {
             const int id = s * kThreads + static_cast<int>(threadIdx.x);
             if (!kOuter) {
-                int row = id >> 3;
+                int row = kGated ? gated_row(id >> 3) : id >> 3;
                 row = row < rows ? row : static_cast<int>(rows) - 1;
                 const int64_t k = step * kBK + (id & 7) * 8;
-                const uint16_t* p = base + static_cast<int64_t>(row) * ld;
+                const uint16_t* p = base + static_cast<int64_t>(row) * ld + (kGated && gated_kind(id >> 3) ? up : 0);
                 x[s] = last ? load_cut(p, k, depth) : *reinterpret_cast<const v4u_any*>(p + k);
             } else {
                 const int64_t k = step * kBK + id / kPieces;
-                const int at = id % kPieces * 8;
+                const int at = kGated ? gated_row(id % kPieces * 8) : id % kPieces * 8;
                 if (last && k >= depth) {
                     x[s] = v4u{0, 0, 0, 0};
                 } else {
-                    const uint16_t* p = base + k * ld;
+                    const uint16_t* p = base + k * ld + (kGated && gated_kind(id % kPieces * 8) ? up : 0);
                     x[s] = edge ? load_cut(p, at, rows) : *reinterpret_cast<const v4u_any*>(p + at);
                 }
             }
@@ -250,6 +259,74 @@ __device__ __forceinline__ void store_part(const DenseGemm& g, int64_t split, in
         if (j + v < g.J) out[v] = f[v];
 }
 
+// ---- gated projections: act(gate) partner ----
+// The end of eight neighbouring results from column j on.  kWhole: J is a multiple of 8.
+template <class T, bool kWhole>
+struct GatedEnding {
+    const DenseGemm& g;
+    int64_t j;
+    int n;                      // columns that are there, up to 8
+    float bias[2][8];
+
+    __device__ __forceinline__ GatedEnding(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
+        n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            uint16_t h[8];
+            if (g.bias && n > 0) load_up_to<8>(static_cast<const uint16_t*>(g.bias) + kind * g.J + j, n, h);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) bias[kind][v] = g.bias && v < n ? T::up(h[v]) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t* p, const uint16_t* h) const {
+        if (kWhole) __builtin_memcpy(p, h, 16);
+        else store_up_to<8>(p, n, h);
+    }
+    __device__ __forceinline__ void finish(int64_t i, float* gate, float* up) const {
+        if (i >= g.I || n <= 0) return;
+        uint16_t h[8];
+        float slope[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            gate[v] += bias[0][v];
+            up[v] += bias[1][v];
+            slope[v] = 1.0f;
+        }
+        if (g.slope) {
+            if (g.act != ADPSGD_ACT_NONE) activate8<true>(gate, slope, g.act);
+            uint16_t* at = g.slope + i * (2 * g.J) + j;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) h[v] = gated_slope_word<T>(up[v] * slope[v]);
+            store(at, h);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) h[v] = gated_slope_word<T>(gate[v]);
+            store(at + g.J, h);
+        } else if (g.act != ADPSGD_ACT_NONE) {
+            activate8<false>(gate, slope, g.act);
+        }
+#pragma unroll
+        for (int v = 0; v < 8; ++v) h[v] = T::down(gate[v] * up[v]);
+        store(static_cast<uint16_t*>(g.out) + i * g.J + j, h);
+    }
+};
+// Eight neighbouring sums of a part of k, gates [split][i][j] and their partners J behind them, for gated_join_kernel.
+__device__ __forceinline__ void store_gated_part(const DenseGemm& g, int64_t split, int64_t i, int64_t j, const float* gate, const float* up) {
+    if (i >= g.I || j >= g.J) return;
+    float* out = g.partial + (split * g.I + i) * (2 * g.J) + j;
+    const int n = g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
+    if (n == 8) {
+        __builtin_memcpy(out, gate, 32);
+        __builtin_memcpy(out + g.J, up, 32);
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+        if (v < n) {
+            out[v] = gate[v];
+            out[g.J + v] = up[v];
+        }
+}
+
 // Blocks go to the eight XCDs in turn, each with an L2 of its own: block b takes the tile that gives every XCD a run of neighbouring
 // ones, and a run goes through 4 tiles of j before it moves on in i, so that the tiles at work on an XCD share rows of both and
 // those at work on all of them write whole rows of D.
@@ -263,22 +340,23 @@ __device__ __forceinline__ void place_of(int64_t b, int64_t blocks, int64_t tile
     ti = in / size;
 }
 
-// kSide x kSide tiles, kWI x kWJ wavefronts
-template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
+// kSide x kSide tiles, kWI x kWJ wavefronts.  kGated: of kSide / 2 results and their partners.
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false>
 __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseGemm g, const int splits) {
     constexpr int kThreads = kWI * kWJ * 64, kTI = kSide / kWI / 16, kTJ = kSide / kWJ / 16;
     typedef Operand<kAOuter, kSide, kThreads, 0> OpA;
-    typedef Operand<kBOuter, kSide, kThreads, 4 * kTJ> OpB;
+    typedef Operand<kBOuter, kSide, kThreads, 4 * kTJ, kGated> OpB;
+    constexpr int kSideJ = kGated ? kSide / 2 : kSide;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
     constexpr int kHalf = kSide * kBK;                                   // elements of one operand's step
-    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSide - 1) / kSide;
+    const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSideJ - 1) / kSideJ;
     int64_t ti, tj, split;
     place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
     const int64_t steps = (g.K + kBK - 1) / kBK, s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
     OpA a;
     OpB b;
     a.start(g.a, g.lda, ti * kSide, g.I, g.K);
-    b.start(g.b, g.ldb, tj * kSide, g.J, g.K);
+    b.start(g.b, g.ldb, tj * kSideJ, g.J, g.K, g.b_up);
     const int wave = threadIdx.x >> 6, wi = wave / kWJ * (kTI * 16), wj = wave % kWJ * (kTJ * 16);
     v4f acc[kTI][kTJ];
 #pragma unroll
@@ -326,6 +404,20 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     }
 
     const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
+    if constexpr (kGated) {                              // a lane has eight neighbouring gates and their partners
+        static_assert(kTJ == 4 && kWJ == 1, "");
+        const GatedEnding<T, false> end(g, tj * kSideJ + q * 8);
+#pragma unroll
+        for (int m = 0; m < kTI; ++m) {
+            const int64_t i = ti * kSide + wi + l + m * 16;
+            float f[2][8];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) f[v / 8][v % 8] = acc[m][v / 4][v % 4];
+            if (splits > 1) store_gated_part(g, split, i, end.j, f[0], f[1]);
+            else end.finish(i, f[0], f[1]);
+        }
+        return;
+    }
     const int64_t j = tj * kSide + wj + q * (4 * kTJ), i0 = ti * kSide + wi + l;
     if (j >= g.J) return;
 #pragma unroll
@@ -370,11 +462,32 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const DenseGemm g, cons
     end.finish(i, f, r);
 }
 
-template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ>
+// The same for gated projections.
+template <class T>
+__global__ __launch_bounds__(256) void gated_join_kernel(const DenseGemm g, const int splits) {
+    const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t i = id / eights, j = id % eights * 8;
+    if (i >= g.I) return;
+    const GatedEnding<T, false> end(g, j);
+    float f[2][8] = {};
+    for (int s = 0; s < splits; ++s) {
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            const float* p = g.partial + (s * g.I + i) * (2 * g.J) + kind * g.J + j;
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                if (v < end.n) f[kind][v] += p[v];
+        }
+    }
+    end.finish(i, f[0], f[1]);
+}
+
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false>
 hipError_t launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
-    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSide - 1) / kSide);
+    constexpr int kSideJ = kGated ? kSide / 2 : kSide;
+    const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSideJ - 1) / kSideJ);
     constexpr int kBytes = 4 * kSide * kBK * 2;
-    auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ>;
+    auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ, kGated>;
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
     if (e != hipSuccess) return e;

@@ -101,8 +101,17 @@ __global__ __launch_bounds__(kT) void dense_db_kernel(const double* sums, int st
     if (part == 0 && j < N) db[j] = T::down(static_cast<float>(((s + at[1][threadIdx.x]) + at[2][threadIdx.x]) + at[3][threadIdx.x]));
 }
 
-// Strips of 256 rows, as many as 64: with N = 8192 four blocks for a compute unit.
+}  // namespace
+
 int strips_of(int64_t M) { return static_cast<int>(std::min<int64_t>((M + 255) / 256, 64)); }
+template <class T>
+void launch_dense_db(const double* sums, int strips, int64_t N, void* db, hipStream_t s) {
+    hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + 63) / 64)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
+}
+template void launch_dense_db<Bf16>(const double* sums, int strips, int64_t N, void* db, hipStream_t s);
+template void launch_dense_db<F16>(const double* sums, int strips, int64_t N, void* db, hipStream_t s);
+
+namespace {
 
 template <class T>
 void launch_dz_of(const void* dy, int64_t lddy, const uint16_t* slope, void* dz, void* db, double* sums, int64_t M, int64_t N, hipStream_t s) {
@@ -113,7 +122,7 @@ void launch_dz_of(const void* dy, int64_t lddy, const uint16_t* slope, void* dz,
     };
     if (strips == 1) go(dense_dz_kernel<T, 8>, 64);
     else if (strips > 1) go(dense_dz_kernel<T, 32>, 256);
-    if (db && strips != 1) hipLaunchKernelGGL(dense_db_kernel<T>, dim3(static_cast<uint32_t>((N + 63) / 64)), dim3(kT), 0, s, sums, strips, N, static_cast<uint16_t*>(db));
+    if (db && strips != 1) launch_dense_db<T>(sums, strips, N, db, s);
 }
 
 }  // namespace
@@ -153,6 +162,7 @@ double estimate(int side, int splits, int64_t I, int64_t J, int64_t K) {
 //     64 x 504 x 504 (whole) 5.8 and 7.1
 //   k outer, a last block that the end of the columns cuts and K over 1024: 1 x 3000 x 5008 30 and 17, 16 x 3001 x 3001 52 and 21,
 //     1 x 4096 x 16416 52 and 42; 1 x 3000 x 5024 (not cut) 9.7 and 16, 16 x 1000 x 1000 9.1 and 10.1
+}  // namespace
 bool few_rows(int64_t I, int64_t J, int64_t K, bool b_outer, bool b_whole) {
     if (I > 64 || (I > 16 && (!b_whole || J * K > (int64_t(1) << 24)))) return false;
     return !(b_outer && J % narrow_columns(I, J) != 0 && K > 1024);
@@ -180,8 +190,9 @@ DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct) {
     return best;
 }
 
+namespace {
 // Rows of `inner` elements as whole 16-byte pieces with zeros at their ends.  grid: ceil(rows ceil(inner / 8) / 256).
-__global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t rows, int64_t inner) {
+__global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t ldto, int64_t rows, int64_t inner) {
     const int64_t pieces = (inner + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x;
     const int64_t row = id / pieces, c = id % pieces * 8;
     if (row >= rows) return;
@@ -194,16 +205,19 @@ __global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, in
         for (int i = 0; i < 8; ++i)
             if (c + i < inner) h[i] = p[i];
     }
-    *reinterpret_cast<v4u*>(to + (row * pieces * 8 + c)) = __builtin_bit_cast(v4u, h);
+    *reinterpret_cast<v4u*>(to + (row * ldto + c)) = __builtin_bit_cast(v4u, h);
 }
+}  // namespace
 
 bool whole_pieces(const void* p, int64_t ld, int64_t inner) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && inner % 8 == 0; }
 // Copies of operands whose rows are no whole pieces: they pay where the direct tiles do, from about 2^32 products on (2100 x 1030 x 4097:
 // dx 60 us with the copies, 257 with tiles of 64 from the operands as they are).
 bool worth_packing(int64_t I, int64_t J, int64_t K) { return static_cast<double>(I) * static_cast<double>(J) * static_cast<double>(K) >= 4294967296.0; }
 int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(inner)); }
-
-}  // namespace
+void launch_pack(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t inner, hipStream_t s) {
+    const uint32_t blocks = static_cast<uint32_t>((rows * (up8(inner) / 8) + kT - 1) / kT);
+    hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, static_cast<const uint16_t*>(from), ld, static_cast<uint16_t*>(to), ldto, rows, inner);
+}
 
 // Both ways of storing an operand, and operands that begin anywhere: what any of them may ask for.
 int64_t dense_partial_bytes(int64_t I, int64_t J, int64_t K) {
@@ -226,8 +240,7 @@ hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s
     if (p.side >= 128 && pack) {
         char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * g.J * static_cast<int64_t>(sizeof(float))) : 0);
         auto copy = [&](const void*& from, int64_t& ld, int64_t rows, int64_t inner) {
-            const uint32_t blocks = static_cast<uint32_t>((rows * (up8(inner) / 8) + kT - 1) / kT);
-            hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, static_cast<const uint16_t*>(from), ld, reinterpret_cast<uint16_t*>(at), rows, inner);
+            launch_pack(from, ld, at, up8(inner), rows, inner, s);
             from = at;
             ld = up8(inner);
             at += packed_bytes(rows, inner);

@@ -1,0 +1,169 @@
+// Gated projections, the first half of a feed-forward block:  g = x Wg^T + bg,  u = x Wu^T + bu,  h = act(g) u.
+//
+// Both products are one pass over x: a tile holds eight gates, their eight partners, eight gates ... (gated_row in dense_tiles.hpp), so that a gate
+// and its partner end in the same lane, and activation and product are the epilogue of the matrix product of dense layers.  Neither g nor u goes to memory; a
+// backward pass gets dh/dg = u act'(g) and dh/du = act(g) in 16 bits each.  Then
+//   dz = [dh u act'(g) | dh act(g)],  db = sum over rows of dz      (this file)
+//   dx = dz w,  dw = dz^T x                                         the products of dense layers, over 2 N
+//
+// Bound: the matrix cores, with few rows the bytes of the weights.
+#include <algorithm>
+
+#include "dense.hpp"
+
+namespace adpsgd_impl {
+namespace {
+
+constexpr int kT = 256;
+
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t gated_partial_bytes(int64_t I, int64_t J, int64_t K) {
+    int64_t parts = 0;
+    for (bool direct : {false, true}) parts = std::max<int64_t>(parts, plan_of(I, 2 * J, K, false, direct).splits);
+    if (I <= 64) parts = std::max<int64_t>(parts, plan_of(I, 2 * J, K, true, false).splits);
+    const bool pack = (J % 8 || K % 8) && worth_packing(I, 2 * J, K);
+    const int64_t copies = pack ? packed_bytes(I, K) + std::max(packed_bytes(2 * J, K), packed_bytes(K, 2 * up8(J))) : 0;
+    return (parts > 1 ? up256(parts * I * 2 * J * static_cast<int64_t>(sizeof(float))) : 0) + copies;
+}
+
+// As launch_dense_gemm, for 2 J columns.
+hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s) {
+    DenseGemm g = given;
+    g.b_up = g.b_outer ? g.J : g.J * g.ldb;
+    const bool a_whole = whole_pieces(g.a, g.lda, g.K), b_whole = whole_pieces(g.b, g.ldb, g.b_outer ? g.J : g.K);
+    const bool pack = !(a_whole && b_whole) && (g.J % 8 || g.K % 8) && worth_packing(g.I, 2 * g.J, g.K);
+    const DensePlan p = plan_of(g.I, 2 * g.J, g.K, few_rows(g.I, 2 * g.J, g.K, g.b_outer, b_whole), (a_whole && b_whole) || pack);
+    if (p.side >= 128 && pack) {
+        char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * 2 * g.J * static_cast<int64_t>(sizeof(float))) : 0);
+        if (!a_whole) {
+            launch_pack(g.a, g.lda, at, up8(g.K), g.I, g.K, s);
+            g.a = at;
+            g.lda = up8(g.K);
+            at += packed_bytes(g.I, g.K);
+        }
+        if (!b_whole && g.b_outer) {                     // gates and partners each in whole pieces
+            const int64_t half = up8(g.J);
+            for (int kind = 0; kind < 2; ++kind)
+                launch_pack(static_cast<const uint16_t*>(g.b) + kind * g.J, g.ldb, at + kind * 2 * half, 2 * half, g.K, g.J, s);
+            g.b = at;
+            g.ldb = 2 * half;
+            g.b_up = half;
+        } else if (!b_whole) {
+            launch_pack(g.b, g.ldb, at, up8(g.K), 2 * g.J, g.K, s);
+            g.b = at;
+            g.ldb = up8(g.K);
+            g.b_up = g.J * g.ldb;
+        }
+    }
+    return type == ADPSGD_TYPE_BF16 ? launch_gated_tiles<Bf16>(g, p, s) : launch_gated_tiles<F16>(g, p, s);
+}
+
+namespace {
+
+// dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
+// Memory: 2 + 4 + 4 bytes a result.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
+template <class T, int kAcross>
+__global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, double* sums, uint16_t* db, int64_t M,
+                                                     int64_t N) {
+    constexpr int kColumns = 8 * kAcross, kRowsAtOnce = kT / kAcross;
+    __shared__ double at[kRowsAtOnce][kColumns];
+    const int cx = threadIdx.x % kAcross, ry = threadIdx.x / kAcross;
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumns + 8 * cx;
+    const int64_t m0 = M * blockIdx.y / gridDim.y, m1 = M * (blockIdx.y + 1) / gridDim.y;
+    double sum[2][8] = {};
+    auto rows = [&](auto whole_columns) {
+        constexpr bool kWhole = decltype(whole_columns)::value;
+        auto load = [&](const uint16_t* p) {
+            if (kWhole) return static_cast<v4u>(__builtin_nontemporal_load(reinterpret_cast<const v4u_any*>(p)));
+            v8h h = {0, 0, 0, 0, 0, 0, 0, 0};
+            for (int i = 0; i < 8; ++i)
+                if (j + i < N) h[i] = p[i];
+            return __builtin_bit_cast(v4u, h);
+        };
+        for (int64_t first = m0 + ry; first < m1; first += 4 * kRowsAtOnce) {
+            float part[2][8] = {};
+            v4u d[4], w[4][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {                // rows beyond the strip: its last one again, which counts nothing
+                const int64_t m = first + u * kRowsAtOnce < m1 ? first + u * kRowsAtOnce : m1 - 1;
+                d[u] = load(dh + m * lddh + j);
+#pragma unroll
+                for (int kind = 0; kind < 2; ++kind) w[u][kind] = load(slopes + (2 * m + kind) * N + j);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t m = first + u * kRowsAtOnce;
+                if (m >= m1) break;
+                float dy[8];
+                unpack8<T>(d[u], dy);
+#pragma unroll
+                for (int kind = 0; kind < 2; ++kind) {
+                    const v8h s = __builtin_bit_cast(v8h, w[u][kind]);
+                    float f[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        f[i] = dy[i] * gated_slope<T>(s[i]);
+                        part[kind][i] += f[i];
+                    }
+                    if (!dz) continue;
+                    uint16_t* to = dz + (2 * m + kind) * N + j;
+                    const v4u p = pack8<T>(f);
+                    if (kWhole) {
+                        *reinterpret_cast<v4u_any*>(to) = p;
+                    } else {
+                        const v8h h = __builtin_bit_cast(v8h, p);
+                        for (int i = 0; i < 8; ++i)
+                            if (j + i < N) to[i] = h[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[kind][i] += static_cast<double>(part[kind][i]);
+        }
+    };
+    if (j + 8 <= N) rows(std::true_type());
+    else if (j < N) rows(std::false_type());
+    if (!sums && !db) return;
+    for (int kind = 0; kind < 2; ++kind) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) at[ry][8 * cx + i] = sum[kind][i];
+        __syncthreads();
+        const int64_t column = static_cast<int64_t>(blockIdx.x) * kColumns + threadIdx.x;
+        if (static_cast<int>(threadIdx.x) < kColumns && column < N) {
+            double s = 0.0;
+            for (int r = 0; r < kRowsAtOnce; ++r) s += at[r][threadIdx.x];
+            if (db) db[kind * N + column] = T::down(static_cast<float>(s));      // the only strip
+            else sums[(2 * blockIdx.y + kind) * N + column] = s;
+        }
+    }
+}
+
+template <class T>
+void launch_dz_of(const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* db, double* sums, int64_t M, int64_t N, hipStream_t s) {
+    const int strips = strips_of(M);
+    auto go = [&](auto kernel, int64_t columns) {
+        hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((N + columns - 1) / columns), strips), dim3(kT), 0, s, static_cast<const uint16_t*>(dh), lddh, slopes,
+                           static_cast<uint16_t*>(dz), db ? sums : nullptr, strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
+    };
+    if (strips == 1) go(gated_dz_kernel<T, 8>, 64);
+    else if (strips > 1) go(gated_dz_kernel<T, 32>, 256);
+    if (db && strips != 1) launch_dense_db<T>(sums, strips, 2 * N, db, s);
+}
+
+}  // namespace
+
+hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* db, double* sums, int64_t M, int64_t N,
+                           hipStream_t s) {
+    if (type == ADPSGD_TYPE_BF16) launch_dz_of<Bf16>(dh, lddh, slopes, dz, db, sums, M, N, s);
+    else launch_dz_of<F16>(dh, lddh, slopes, dz, db, sums, M, N, s);
+    return hipGetLastError();
+}
+
+}  // namespace adpsgd_impl

@@ -212,6 +212,116 @@ def dense_gradients(dy, x, w, slope, *, activation="none", need=(True, True, Tru
         return _backward(dy, x, w, slope if activation != "none" else None, activation, *need)
 
 
+# ---- gated projections ------------------------------------------------------------------------------------------
+
+def _check_gated(x, w, b, activation):
+    _on_gpu("x", x)
+    for name, t in (("w", w), ("bias", b)):
+        if t is None and name != "w":
+            continue
+        _on_gpu(name, t, x.device)
+        if t.dtype != x.dtype:
+            raise TypeError("x is %s, %s is %s" % (x.dtype, name, t.dtype))
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("gated takes bfloat16 or float16, not %s" % x.dtype)
+    if activation not in _ACTIVATIONS:
+        raise ValueError("activation must be one of %s" % ", ".join(_ACTIVATIONS))
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1] or w.shape[0] < 2 or w.shape[0] % 2 or w.shape[1] < 1:
+        raise ValueError("x is %s, w %s: w must be 2 out x in, the gates' rows and then their partners'" % (tuple(x.shape), tuple(w.shape)))
+    if b is not None and b.shape != (w.shape[0],):
+        raise ValueError("bias is %s, w %s" % (tuple(b.shape), tuple(w.shape)))
+
+
+def _gated_args(x, w, activation, backward):
+    xm, ldx = _as_rows(x)
+    ws, ldw, transposed = _as_weights(w)
+    M, K, N = xm.shape[0], xm.shape[1], w.shape[0] // 2
+    size = B.lib().adpsgd_gated_workspace_bytes(M, N, K, backward)
+    if size < 0:
+        raise B.AdpsgdError(B.ERR_ARG, "gated: M = %d, N = %d, K = %d is too large" % (M, N, K))
+    space = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    args = B.Dense(_TYPES[x.dtype], _ACTIVATIONS[activation], M, N, K, xm.data_ptr(), ldx, ws.data_ptr(), ldw, transposed, 0, None, None, 0, _ptr(space),
+                   size)
+    return args, (xm, ws, space)
+
+
+def _gated_forward(x, w, b, activation, want_slopes):
+    args, keep = _gated_args(x, w, activation, 0)
+    h = torch.empty(*x.shape[:-1], args.N, dtype=x.dtype, device=x.device)
+    slopes = torch.empty(args.M, 2 * args.N, dtype=torch.int16, device=x.device) if want_slopes else None
+    if b is not None:
+        b = b.contiguous()
+        args.b = b.data_ptr()
+    if args.M:
+        _call(x.device, B.lib().adpsgd_gated_forward, C.byref(args), h.data_ptr(), _ptr(slopes))
+    del keep
+    return h, slopes
+
+
+def _gated_backward(dh, x, w, slopes, need_dx, need_dw, need_db):
+    args, keep = _gated_args(x, w, "none", 1)
+    dhm, lddh = _as_rows(dh)
+    M, N, K = args.M, args.N, args.K
+    new = lambda *shape: torch.empty(*shape, dtype=x.dtype, device=x.device)  # noqa: E731
+    dx = new(*x.shape) if need_dx else None
+    dw = (new(K, 2 * N).t() if args.w_transposed else new(2 * N, K)) if need_dw else None
+    db = new(2 * N) if need_db else None
+    _call(x.device, B.lib().adpsgd_gated_backward, C.byref(args), dhm.data_ptr(), lddh, slopes.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db))
+    del keep
+    return dx, dw, db
+
+
+class _Gated(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, b, activation):
+        h, slopes = _gated_forward(x, w, b, activation, True)
+        ctx.save_for_backward(x, w, slopes)
+        return h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        return (*_gated_backward(dh, *ctx.saved_tensors, *ctx.needs_input_grad[:3]), None)
+
+
+def gated(x, w, bias=None, *, activation="silu"):
+    """act(x wg^T + bg) (x wu^T + bu) in one pass, the first half of a feed-forward block; differentiable (once, in reverse mode) in
+    all three.  Its second half is dense(h, w2, residual=...).
+
+    x (..., in), w (2 out, in) the rows of wg and then those of wu, as it is or as the transpose of an (in, 2 out) tensor, bias (2 out)
+    likewise, all bfloat16 or all float16; the result is (..., out).  Activations as dense's.  Both products and theirs are in 32 bits and
+    the result is rounded once.  With gradients, 4 bytes an output are kept for the backward pass.  Under capture of a HIP graph the
+    differentiable form is refused, as dense's is: gated_forward and gated_gradients can be captured."""
+    _check_gated(x, w, bias, activation)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias)):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("gated with gradients cannot be captured: capture gated_forward and gated_gradients")
+        return _Gated.apply(x, w, bias, activation)
+    return _gated_forward(x, w, bias, activation, False)[0]
+
+
+def gated_forward(x, w, bias=None, *, activation="silu"):
+    """(h, slopes): the forward pass without autograd, and what gated_gradients needs."""
+    _check_gated(x, w, bias, activation)
+    with torch.no_grad():
+        return _gated_forward(x, w, bias, activation, True)
+
+
+def gated_gradients(dh, x, w, slopes, *, need=(True, True, True)):
+    """(dx, dw, dbias) for dh; None where ``need`` says so.  The activation is in the slopes."""
+    _check_gated(x, w, None, "none")
+    _on_gpu("dh", dh, x.device)
+    _on_gpu("slopes", slopes, x.device)
+    if dh.dtype != x.dtype or dh.shape != (*x.shape[:-1], w.shape[0] // 2):
+        raise ValueError("dh is %s %s, must be as the result" % (tuple(dh.shape), dh.dtype))
+    if slopes.dtype != torch.int16 or slopes.shape != (x.numel() // x.shape[-1], w.shape[0]) or not slopes.is_contiguous():
+        raise ValueError("slopes must be what gated_forward returned")
+    if not any(need):
+        return None, None, None
+    with torch.no_grad():
+        return _gated_backward(dh, x, w, slopes, *need)
+
+
 # ---- layer norm -------------------------------------------------------------------------------------------------
 
 _FAR = 1 << 40          # elements from one row to the next, at most, where rows are walked one by one

@@ -81,3 +81,69 @@ def test_layer_norm_shapes_and_types():
             (lambda: P.layer_norm_gradients(x, x, w, stats[:, :3]), ValueError, "stats"), (lambda: P.layer_norm_gradients(x, x, w, stats.half()), ValueError, "stats")]:
         with pytest.raises(kind, match=word):
             call()
+
+
+def gated_args(**kw):
+    o = dict(type=B.TYPE_BF16, activation=B.ACT_SILU, M=4, N=8, K=16, x=NOWHERE, ldx=16, w=NOWHERE, ldw=16, w_transposed=0, workspace=NOWHERE,
+             workspace_bytes=1 << 30)
+    o.update(kw)
+    return B.Dense(**o)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(type=B.TYPE_F32), "type"), (dict(activation=9), "activation"), (dict(M=-1), "M >= 0"), (dict(N=0), "M >= 0"), (dict(K=0), "M >= 0"), (dict(N=1 << 62), "M >= 0"),
+    (dict(ldx=15), "leading"), (dict(ldw=15), "leading"), (dict(w_transposed=1, ldw=15), "leading"), (dict(r=NOWHERE, ldr=8), "residual"), (dict(ldx=(1 << 22) + 1), "2^22"),
+    (dict(N=(1 << 21) + 1), "2^22"), (dict(M=1 << 30, N=1 << 10), "2^34"), (dict(x=None), "NULL"), (dict(w=None), "NULL"), (dict(x=NOWHERE + 1), "aligned"),
+    (dict(b=NOWHERE + 1), "aligned")])
+def test_gated(change, word):
+    L = B.lib()
+    refused(L.adpsgd_gated_forward(C.byref(gated_args(**change)), NOWHERE, None, None), word)
+    refused(L.adpsgd_gated_backward(C.byref(gated_args(**change)), NOWHERE, 1 << 22, NOWHERE, NOWHERE, NOWHERE, NOWHERE, None), word)
+
+
+def test_gated_calls():
+    L, at = B.lib(), NOWHERE
+    refused(L.adpsgd_gated_forward(None, at, None, None), "no arguments")
+    refused(L.adpsgd_gated_forward(C.byref(gated_args()), None, None, None), "h is NULL")
+    refused(L.adpsgd_gated_forward(C.byref(gated_args()), at, at + 1, None), "aligned")
+    refused(L.adpsgd_gated_backward(C.byref(gated_args()), at, 8, None, at, None, None, None), "slopes")
+    refused(L.adpsgd_gated_backward(C.byref(gated_args()), None, 8, at, at, None, None, None), "dh")
+    refused(L.adpsgd_gated_backward(C.byref(gated_args()), at, 7, at, at, None, None, None), "leading dimension of dh")
+    refused(L.adpsgd_gated_backward(C.byref(gated_args()), at, 8, at, at + 1, None, None, None), "aligned")
+    for short in (dict(workspace_bytes=8), dict(workspace=None), dict(workspace=at + 4)):
+        refused(L.adpsgd_gated_backward(C.byref(gated_args(**short)), at, 8, at, at, None, None, None), "workspace")
+    refused(L.adpsgd_gated_forward(C.byref(gated_args(K=1 << 13, ldx=1 << 13, ldw=1 << 13, workspace_bytes=8)), at, None, None), "workspace")
+    assert L.adpsgd_gated_forward(C.byref(gated_args(M=0, x=None)), None, None, None) == B.OK        # no rows: nothing to do
+    assert L.adpsgd_gated_backward(C.byref(gated_args()), at, 8, at, None, None, None, None) == B.OK       # nothing asked for
+    for sizes in ((-1, 1, 1), (1, 0, 1), (1, 1, 0), (1 << 31, 1, 1), (1 << 20, 1 << 20, 1), (1, 1 << 62, 1)):
+        assert L.adpsgd_gated_workspace_bytes(*sizes, 0) == -1 and L.adpsgd_gated_workspace_bytes(*sizes, 1) == -1
+    assert L.adpsgd_gated_workspace_bytes(64, 1024, 784, 1) >= 4 * 64 * 1024
+
+
+def test_gated_tensors_that_are_not_on_a_gpu():
+    import torch
+    x, w = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(6, 8, dtype=torch.bfloat16)
+    for call in (lambda: P.gated(x, w), lambda: P.gated_forward(x, w), lambda: P.gated_gradients(x[:, :3], x, w, torch.zeros(4, 6, dtype=torch.int16))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    with pytest.raises(TypeError, match="tensor"):
+        P.gated([1.0], w)
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level():
+        with pytest.raises(NotImplementedError, match="forward mode"):
+            P.gated(forward_ad.make_dual(x, x), w)
+
+
+@pytest.mark.gpu
+def test_gated_shapes_and_types():
+    import torch
+    new = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda:0")  # noqa: E731
+    x, w, dh, slopes = new(4, 8), new(6, 8), new(4, 3), new(4, 6, dtype=torch.int16)
+    for call, kind, word in [
+            (lambda: P.gated(x, new(6, 9)), ValueError, "2 out x in"), (lambda: P.gated(x, new(5, 8)), ValueError, "2 out x in"), (lambda: P.gated(x, new(0, 8)), ValueError, "2 out x in"),
+            (lambda: P.gated(x.float(), w.float()), TypeError, "float32"), (lambda: P.gated(x, w.half()), TypeError, "float16"), (lambda: P.gated(x, w, new(3)), ValueError, "bias"),
+            (lambda: P.gated(x, w, activation="tanh"), ValueError, "activation"), (lambda: P.gated(x, w.cpu()), ValueError, "GPU"),
+            (lambda: P.gated_gradients(new(4, 6), x, w, slopes), ValueError, "dh is"), (lambda: P.gated_gradients(dh.half(), x, w, slopes), ValueError, "dh is"),
+            (lambda: P.gated_gradients(dh, x, w, slopes[:, :3]), ValueError, "slopes"), (lambda: P.gated_gradients(dh, x, w, slopes.half()), ValueError, "slopes")]:
+        with pytest.raises(kind, match=word):
+            call()
