@@ -578,6 +578,31 @@ int adpsgd_policy_loss(const adpsgd_logits_t* o, const float* old_log_probs, con
 int adpsgd_preference_loss(const adpsgd_logits_t* o, const int64_t* offsets, int64_t pairs, const float* ref_log_probs, float beta,
                            float label_smoothing, float* loss, void* dlogits, float* log_probs, float* margins, void* stream);
 
+/* Distillation from a teacher's top logits.  A row has k entries (a token and the teacher's logit for it); an entry with a negative token is not used,
+ * one of -infinity has no weight, entries of the same token add up, and a token beyond the vocabulary makes the row's results NaN.  With p = softmax(t / T) over a
+ * row's entries, q_T = softmax(z / T) and q = softmax(z) over the vocabulary, and c the counted rows (tokens as for the losses above):
+ *   KL_i = sum_j p_j (log p_j - log q_T[v_j])            0 where no entry is used, NaN where all that are have no weight
+ *   loss = 1/max(1, c) sum_i [ (1 - hard_weight) T^2 KL_i - hard_weight log q[tokens[i]] ]
+ * An entry with weight whose logit is -infinity makes the loss infinite, and its gradient is finite. */
+typedef struct {
+    int32_t type;            /* of the teacher's logits: ADPSGD_TYPE_*                                       */
+    int32_t reserved;
+    int64_t k;               /* entries of a row, 1 .. 1024                                                  */
+    const int64_t* tokens;   /* rows x k, row i at tokens + i ld_tokens                                      */
+    int64_t ld_tokens;
+    const void* z;           /* rows x k, row i at z + i ld                                                  */
+    int64_t ld;
+} adpsgd_teacher_t;
+
+/* Host only: the workspace of the call below (in place of adpsgd_loss_workspace_bytes); -1 where an argument is refused. */
+int64_t adpsgd_distillation_workspace_bytes(int64_t rows, int64_t vocab, int64_t k);
+
+/* dlogits (rows x vocab, contiguous, the type of z) receives the gradient of loss_scale times the loss (fp16: a mean over many rows leaves nothing of
+ * an unscaled one), loss (1) the loss, divergences (rows) KL, log_probs (rows) log q[tokens[i]]: NULL where hard_weight is 0, and only
+ * there.  2^-20 <= temperature <= 2^20, 0 <= hard_weight < 1, |loss_scale| <= 2^60. */
+int adpsgd_distillation_loss(const adpsgd_logits_t* o, const adpsgd_teacher_t* teacher, double temperature, double hard_weight, double loss_scale,
+                             float* loss, void* dlogits, float* divergences, float* log_probs, void* stream);
+
 /* AdamW over many tensors at once.  With g' = f grad_scale g, f = min(1, max_norm / (|grad_scale g| + 1e-6)) over all tensors
  * (1 where max_norm is 0), t the number of the step from 1:
  *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,  u = (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)

@@ -12,7 +12,7 @@ from .engine import Engine  # noqa: F401
 from . import step_sizes  # noqa: F401
 
 _OPERATORS = ("dense", "dense_forward", "dense_gradients", "token_log_probs", "policy_loss_and_gradient", "preference_loss_and_gradient", "AdamW",
-              "gated", "gated_forward", "gated_gradients", "layer_norm", "layer_norm_forward", "layer_norm_gradients")
+              "distillation_loss_and_gradient", "gated", "gated_forward", "gated_gradients", "layer_norm", "layer_norm_forward", "layer_norm_gradients")
 
 
 def __getattr__(name):                  # these need torch, which the host-only entry points do not

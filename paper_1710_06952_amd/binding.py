@@ -28,7 +28,7 @@ EXPORTS = [
     "adpsgd_synth_gradient", "adpsgd_run_sync_steps", "adpsgd_run_sync_steps_with", "adpsgd_metropolis_weights",
     "adpsgd_get_event_count", "adpsgd_set_event_count", "adpsgd_verify_plan", "adpsgd_objective", "adpsgd_objective_weighted", "adpsgd_count_nonfinite",
     "adpsgd_dense_workspace_bytes", "adpsgd_dense_forward", "adpsgd_dense_backward", "adpsgd_loss_workspace_bytes", "adpsgd_token_log_probs",
-    "adpsgd_gated_workspace_bytes", "adpsgd_gated_forward", "adpsgd_gated_backward",
+    "adpsgd_distillation_workspace_bytes", "adpsgd_distillation_loss", "adpsgd_gated_workspace_bytes", "adpsgd_gated_forward", "adpsgd_gated_backward",
     "adpsgd_layer_norm_workspace_bytes", "adpsgd_layer_norm_forward", "adpsgd_layer_norm_backward",
     "adpsgd_policy_loss", "adpsgd_preference_loss", "adpsgd_adamw_state_length", "adpsgd_adamw_create", "adpsgd_adamw_destroy", "adpsgd_adamw_step",
     "adpsgd_adamw_get_steps", "adpsgd_adamw_set_steps", "adpsgd_adamw_get_moments", "adpsgd_adamw_set_moments",
@@ -101,6 +101,11 @@ class LayerNorm(C.Structure):
 class Logits(C.Structure):
     _fields_ = [("type", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("vocab", C.c_int64), ("z", C.c_void_p),
                 ("ld", C.c_int64), ("tokens", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("type", C.c_int32), ("reserved", C.c_int32), ("k", C.c_int64), ("tokens", C.c_void_p), ("ld_tokens", C.c_int64), ("z", C.c_void_p),
+                ("ld", C.c_int64)]
 
 
 class AdamwOpts(C.Structure):
@@ -188,6 +193,8 @@ def lib():
         L.adpsgd_token_log_probs.argtypes = [P(Logits), vp, vp]
         L.adpsgd_policy_loss.argtypes = [P(Logits), vp, vp, vp, f32, f32, f32, vp, vp, vp, vp]
         L.adpsgd_preference_loss.argtypes = [P(Logits), vp, i64, vp, f32, f32, vp, vp, vp, vp, vp]
+        L.adpsgd_distillation_workspace_bytes.argtypes = [i64, i64, i64]
+        L.adpsgd_distillation_loss.argtypes = [P(Logits), P(Teacher), f64, f64, f64, vp, vp, vp, vp, vp]
         L.adpsgd_adamw_state_length.argtypes = [P(i64), i32]
         L.adpsgd_adamw_create.argtypes = [P(vp), P(AdamwOpts)]
         L.adpsgd_adamw_destroy.argtypes = [vp]
@@ -198,7 +205,7 @@ def lib():
         L.adpsgd_adamw_get_moments.argtypes = [vp, vp, vp, vp]
         L.adpsgd_adamw_set_moments.argtypes = [vp, vp, vp, vp]
         for name in ("adpsgd_dense_workspace_bytes", "adpsgd_loss_workspace_bytes", "adpsgd_adamw_state_length",
-                     "adpsgd_gated_workspace_bytes", "adpsgd_layer_norm_workspace_bytes"):
+                     "adpsgd_distillation_workspace_bytes", "adpsgd_gated_workspace_bytes", "adpsgd_layer_norm_workspace_bytes"):
             getattr(L, name).restype = i64
         _lib = L
     return _lib

@@ -16,7 +16,7 @@ STREAM_BENCH = HERE / "stream_bench"       # stand-alone streaming microbenchmar
 
 SOURCES = ["api.cpp", "api_sync.cpp", "api_diag.cpp", "schedule.cpp", "planner.cpp", "strips.cpp", "onepass.cpp", "kernels_fused.hip", "kernels_columns.hip",
            "kernels_strips.hip", "kernels_grad_linear.hip", "kernels_onepass.hip",
-           "kernels_mlp.hip", "kernels_diag.hip", "kernels_sync.hip", "api_operators.cpp", "kernels_losses.hip", "kernels_adamw.hip", "kernels_norm.hip",
+           "kernels_mlp.hip", "kernels_diag.hip", "kernels_sync.hip", "api_operators.cpp", "kernels_losses.hip", "kernels_adamw.hip", "kernels_norm.hip", "kernels_distill.hip",
            "kernels_dense.hip", "kernels_dense_bf16.hip", "kernels_dense_f16.hip",
            "kernels_gated.hip", "kernels_gated_bf16.hip", "kernels_gated_f16.hip"]
 HEADERS = ["internal.hpp", "strips.hpp", "onepass.hpp", "exchange.hpp", "handle.hpp", "device_common.hpp", "chains.hpp",

@@ -132,7 +132,7 @@ NormRows norm_rows(const adpsgd_layer_norm_t* o) { return NormRows{o->type, o->p
 bool loss_sizes(int64_t rows, int64_t vocab) {
     return rows >= 0 && vocab >= 1 && vocab <= (int64_t(1) << 30) && rows <= (int64_t(1) << 21) && rows * ((vocab + 4095) / 4096) <= (int64_t(1) << 23);
 }
-const char* logits_fault(const adpsgd_logits_t* o) {
+const char* logits_fault(const adpsgd_logits_t* o, int64_t bytes = -1) {      // bytes: of the workspace, where it is not that of the losses alone
     if (!o) return "logits: no arguments";
     if (!is_type(o->type)) return "logits: unknown type";
     if (!loss_sizes(o->rows, o->vocab)) return "logits: rows <= 2^21, 1 <= vocab <= 2^30 and rows * ceil(vocab / 4096) <= 2^23";
@@ -140,7 +140,7 @@ const char* logits_fault(const adpsgd_logits_t* o) {
     if (o->ld > (int64_t(1) << 40)) return "logits: the leading dimension is too large";
     if (o->rows > 0 && (!o->z || !o->tokens)) return "logits: z or tokens is NULL";
     if (!aligned_to(o->z, size_of(o->type)) || !aligned_to(o->tokens, 8)) return "logits: a tensor is not aligned to its type";
-    if (!o->workspace || !aligned16(o->workspace) || o->workspace_bytes < loss_workspace_bytes(o->rows, o->vocab)) return "logits: workspace missing, not 16-byte aligned or too small";
+    if (!o->workspace || !aligned16(o->workspace) || o->workspace_bytes < (bytes < 0 ? loss_workspace_bytes(o->rows, o->vocab) : bytes)) return "logits: workspace missing, not 16-byte aligned or too small";
     return nullptr;
 }
 LossRows rows_of(const adpsgd_logits_t* o) { return LossRows{o->type, o->rows, o->vocab, o->ld, o->z, o->tokens}; }
@@ -313,6 +313,36 @@ extern "C" int adpsgd_preference_loss(const adpsgd_logits_t* o, const int64_t* o
         return ended(launch_preference(rows_of(o), offsets, pairs, ref_log_probs, beta, label_smoothing, loss, dlogits, log_probs, margins, o->workspace,
                                        static_cast<hipStream_t>(stream)),
                      "preference_loss");
+    });
+}
+
+constexpr int64_t kMostEntries = 1024;
+
+extern "C" int64_t adpsgd_distillation_workspace_bytes(int64_t rows, int64_t vocab, int64_t k) {
+    return loss_sizes(rows, vocab) && k >= 1 && k <= kMostEntries ? distill_workspace_bytes(rows, k) : -1;
+}
+
+extern "C" int adpsgd_distillation_loss(const adpsgd_logits_t* o, const adpsgd_teacher_t* t, double temperature, double hard_weight, double loss_scale, float* loss,
+                                        void* dlogits, float* divergences, float* log_probs, void* stream) {
+    return guarded([&]() -> int {
+        if (!t) return refuse("distillation_loss: no teacher");
+        if (t->k < 1 || t->k > kMostEntries) return refuse("distillation_loss: 1 <= k <= 1024");
+        const bool sizes = o && loss_sizes(o->rows, o->vocab);
+        if (const char* why = logits_fault(o, sizes ? distill_workspace_bytes(o->rows, t->k) : 0)) return refuse(why);
+        if (!is_type(t->type)) return refuse("distillation_loss: unknown type of the teacher's logits");
+        if (t->ld < t->k || t->ld_tokens < t->k || t->ld > (int64_t(1) << 40) || t->ld_tokens > (int64_t(1) << 40)) return refuse("distillation_loss: a leading dimension is not k .. 2^40");
+        if (!(temperature >= 0x1p-20 && temperature <= 0x1p20)) return refuse("distillation_loss: 2^-20 <= temperature <= 2^20");
+        if (!(hard_weight >= 0.0 && hard_weight < 1.0)) return refuse("distillation_loss: 0 <= hard_weight < 1");
+        if (!(std::fabs(loss_scale) <= 0x1p60)) return refuse("distillation_loss: loss_scale is over 2^60");
+        if ((hard_weight > 0.0) != (log_probs != nullptr) && o->rows > 0) return refuse("distillation_loss: log_probs belongs to a hard_weight over 0");
+        if (!loss || (o->rows > 0 && (!t->tokens || !t->z || !dlogits || !divergences))) return refuse("distillation_loss: a tensor is NULL");
+        if (!aligned_to(t->tokens, 8) || !aligned_to(t->z, size_of(t->type)) || !aligned_to(loss, 4) || !aligned_to(divergences, 4) || !aligned_to(log_probs, 4) ||
+            !aligned_to(dlogits, size_of(o->type)))
+            return refuse("distillation_loss: a tensor is not aligned to its type");
+        const TeacherRows rows{t->type, t->k, t->tokens, t->ld_tokens, t->z, t->ld};
+        return ended(launch_distill(rows_of(o), rows, temperature, hard_weight, loss_scale, loss, dlogits, divergences, log_probs, o->workspace,
+                                    static_cast<hipStream_t>(stream)),
+                     "distillation_loss");
     });
 }
 

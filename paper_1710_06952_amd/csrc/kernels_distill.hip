@@ -1,0 +1,578 @@
+// Distillation from a teacher's top logits, and its gradient for the logits.
+//
+// A row has logits z and up to k entries (v_j, t_j) of the teacher.  With p = softmax(t / T) over its entries, q_T = softmax(z / T), q = softmax(z):
+//   KL = sum_j p_j (log p_j - log q_T[v_j])
+//      = [sum_j p_j t_j / T - log Z] - sum_j p_j z[v_j] / T + m / T + log s        Z of the entries, m and s of the row: the first part needs no pass over z
+//   dL/dz = cs (q_T - sum_j p_j onehot(v_j)) + ch (q - onehot(token)),   cs = (1 - a) T / counted,  ch = a / counted
+//
+//   teacher_rows     p and the first part of KL, one wavefront a row; entries of the same token become one, and the token itself is the last
+//   distill_rows     statistics, KL and gradient with the row held in registers: the logits are read once
+//   stats, finish, gradient, entries: the same in passes, for rows that registers do not hold, and for few rows, which are split over the chip
+//
+// The gradient of all elements is stored without the entries first; behind a barrier the few that have an entry are stored again.  (The pass
+// would have to look for its own elements among the entries.)
+//
+// Exponentials, sums of a row and the gradient are in 32 bits, what there is one of in a row or an entry in 64.  Orders depend on the sizes and the
+// alignment of the gradient alone.
+//
+// Bound: memory, 2 or 4 bytes an element in and out.
+#include <cmath>
+
+#include "loss_rows.hpp"
+
+namespace adpsgd_impl {
+namespace {
+
+constexpr int kUnroll = 4;              // vectors of a thread on their way at once
+constexpr int64_t kCountHere = 1024;    // rows that a block counts itself: a launch less where launches are the time
+constexpr int64_t kSplitBlocks = 1024;  // blocks that fill the chip: rows are split over the vocabulary up to this many
+
+struct Entry {
+    int v;                      // of the vocabulary, or -1: nothing
+    float p;
+};
+// log2 e / T in two parts, the second positive: a difference of -infinity is e^-infinity by both.
+struct Heat {
+    float hi, lo;
+};
+struct Stat2 {
+    float m, s, s1;             // the largest value, sum exp((z - m) / T), sum exp(z - m)
+};
+struct DistillArgs {
+    const void* z;
+    const int64_t* tokens;
+    int64_t rows, vocab, ld;
+    const void* t;              // teacher
+    int32_t t_type;
+    const int64_t* t_tokens;
+    int64_t k, ld_t, ld_tokens;
+    double T, inv_T, soft, hard;        // soft: 1 - a, hard: a
+    float cs, ch;               // times 1 / counted
+    Heat heat;
+    const float* share;         // 1 / counted, where rows > kCountHere
+    Entry* entries;             // [row][k + 1]
+    double* first;              // of KL: its first part
+    double* term;
+    Stat2 *stat, *parts;        // in passes: of rows, of parts of rows
+    float2* coef;               // in passes: cs / s, ch / s1 of a row
+    int splits;
+    int64_t blocks;             // of a row, in the gradient's pass
+    void* dz;
+    float *kl, *logp;           // logp may be nullptr
+};
+
+template <bool kFine>
+__device__ __forceinline__ float warm(float d, const Heat& h) { return __builtin_amdgcn_exp2f(kFine ? fmaf(d, h.hi, d * h.lo) : d * h.hi); }
+template <bool kTwo>
+__device__ __forceinline__ Stat2 joined2(Stat2 a, Stat2 b, const Heat& h) {
+    const float m = fmaxf(a.m, b.m), base = base_of(m);
+    Stat2 r{m, a.s * warm<true>(a.m - base, h) + b.s * warm<true>(b.m - base, h), 0.0f};
+    if (kTwo) r.s1 = a.s1 * exp_in_sum<true>(a.m - base) + b.s1 * exp_in_sum<true>(b.m - base);
+    return r;
+}
+__device__ __forceinline__ Stat2 of_one2(float z, const Heat& h) { return Stat2{z, warm<true>(z - base_of(z), h), exp_in_sum<true>(z - base_of(z))}; }
+template <bool kTwo, int kLanes>
+__device__ __forceinline__ Stat2 lanes_joined2(Stat2 a, const Heat& h) {
+    float m = a.m;
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    float s = a.s * warm<true>(a.m - base_of(m), h), s1 = kTwo ? a.s1 * exp_in_sum<true>(a.m - base_of(m)) : 0.0f;
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1) {
+        s += __shfl_xor(s, off, 64);
+        if (kTwo) s1 += __shfl_xor(s1, off, 64);
+    }
+    return Stat2{m, s, s1};
+}
+template <bool kTwo, int kWaves>
+__device__ __forceinline__ Stat2 block_joined2(Stat2 a, const Heat& h, Stat2* at) {
+    a = lanes_joined2<kTwo, 64>(a, h);
+    if (kWaves == 1) return a;
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = a;
+    __syncthreads();
+    return lanes_joined2<kTwo, kWaves>(at[threadIdx.x % kWaves], h);
+}
+
+// ---- the teacher's rows ------------------------------------------------------------------------------------
+// exp(x) of what there is one of in an entry: x in 64 bits as a rounding and its rest.
+__device__ __forceinline__ float exp_of_entry(double x) {
+    const float hi = static_cast<float>(x), t = hi * kLog2e;
+    const float rest = fmaf(hi, kLog2e, -t) + hi * kLog2eRest + static_cast<float>(x - static_cast<double>(hi)) * kLog2e, e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 126.0f ? fmaf(e, rest * 0.6931471805599453f, e) : e;
+}
+__device__ __forceinline__ float teacher_logit(const void* t, int32_t type, int64_t at) {
+    if (type == ADPSGD_TYPE_F32) return F32::get(static_cast<const float*>(t) + at);
+    const uint16_t* p = static_cast<const uint16_t*>(t) + at;
+    return type == ADPSGD_TYPE_BF16 ? Bf16::get(p) : F16::get(p);
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+}
+
+// Words of LDS for a row: entries (token, value, place in the table) and a table of twice as many places (token, first entry).
+__host__ __device__ constexpr int teacher_places(int k) {
+    int n = 64;
+    while (n < 2 * (k + 1)) n *= 2;
+    return n;
+}
+static_assert(64 * 1024 > 4 * (3 * 1025 + 2 * 4096), "the words of 1024 entries");
+__host__ __device__ constexpr int teacher_words(int k) { return 3 * (k + 1) + 2 * teacher_places(k); }
+
+// One wavefront a row; as many in a block, up to four, as have their words in 64 KB.
+template <class E>
+__global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) {
+    extern __shared__ int words[];
+    const int lane = threadIdx.x & 63, k = static_cast<int>(a.k), places = teacher_places(k);
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    if (row >= a.rows) return;
+    const int64_t token = a.tokens[row];
+    if (token < 0) return;                               // nothing of the row is read
+    int* token_of = words + (threadIdx.x >> 6) * teacher_words(k);
+    float* value = reinterpret_cast<float*>(token_of + (k + 1));
+    int *place_of_entry = token_of + 2 * (k + 1), *key = token_of + 3 * (k + 1), *owner = key + places;
+    for (int i = lane; i < places; i += 64) {
+        key[i] = -1;
+        owner[i] = k + 1;
+    }
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    bool beyond = false, some = false;
+    float top = -INFINITY;
+    for (int j = lane; j < k; j += 64) {
+        const int64_t v = a.t_tokens[row * a.ld_tokens + j];
+        const float t = v < 0 ? -INFINITY : teacher_logit(a.t, a.t_type, row * a.ld_t + j);
+        token_of[j] = v < 0 || v >= a.vocab ? -1 : static_cast<int>(v);
+        value[j] = t;
+        beyond = beyond || v >= a.vocab;
+        some = some || v >= 0;
+        top = t != t ? NAN : top != top ? top : fmaxf(top, t);       // fmax passes over a NaN
+    }
+    if (lane == 0) {                                     // the row's own token, an entry that weighs nothing
+        token_of[k] = token < a.vocab ? static_cast<int>(token) : -1;
+        value[k] = 0.0f;
+    }
+    beyond = __any(beyond || top != top);
+    some = __any(some);
+    top = wave_max(top);
+    wave_lds_sync();
+    double Z = 0.0, with_t = 0.0, with_z = 0.0;
+    for (int j = lane; j < k; j += 64) {
+        const int v = token_of[j];
+        const double x = (static_cast<double>(value[j]) - static_cast<double>(top)) * a.inv_T;
+        const float e = v < 0 ? 0.0f : exp_of_entry(x);
+        value[j] = e;
+        if (e != 0.0f) {
+            Z += static_cast<double>(e);
+            with_t += static_cast<double>(e) * x;
+            with_z += static_cast<double>(e) * static_cast<double>(E::get(z + v));
+        }
+    }
+    Z = wave_sum(Z);
+    with_t = wave_sum(with_t);
+    with_z = wave_sum(with_z);
+    // one entry for each token: the first of its entries
+    for (int j = lane; j <= k; j += 64) {
+        const int v = token_of[j];
+        int at = -1;
+        if (v >= 0) {
+            at = static_cast<int>(static_cast<uint32_t>(v) * 2654435761u >> 7) & (places - 1);
+            for (;;) {                                   // less than half of the places are taken
+                const int was = atomicCAS(&key[at], -1, v);
+                if (was == -1 || was == v) break;
+                at = (at + 1) & (places - 1);
+            }
+            atomicMin(&owner[at], j);
+        }
+        place_of_entry[j] = at;
+    }
+    wave_lds_sync();
+    bool twice = false;
+    for (int j = lane; j <= k; j += 64) twice = twice || (place_of_entry[j] >= 0 && owner[place_of_entry[j]] != j);
+    twice = __any(twice);
+    const double scale = 1.0 / Z;
+    const bool bad = beyond || (some && !(Z > 0.0 && Z < INFINITY));
+    Entry* out = a.entries + row * (k + 1);
+    for (int j = lane; j <= k; j += 64) {
+        const int at = place_of_entry[j];
+        Entry e{at >= 0 && owner[at] == j ? token_of[j] : -1, 0.0f};
+        if (e.v >= 0) {
+            double w = value[j];
+            if (twice)
+                for (int i = j + 1; i <= k; ++i) w += place_of_entry[i] == at ? static_cast<double>(value[i]) : 0.0;
+            e.p = some ? static_cast<float>(w * scale) : 0.0f;
+        }
+        out[j] = e;
+    }
+    if (lane == 0) {
+        const float near = static_cast<float>(Z);
+        const double log_Z = log_of(near) + (Z - static_cast<double>(near)) * scale;
+        // infinity tells that there is no entry; NaN is one
+        a.first[row] = bad ? static_cast<double>(NAN) : some ? with_t * scale - log_Z - with_z * scale * a.inv_T : static_cast<double>(-INFINITY);
+    }
+}
+
+// ---- what one thread does once for a row --------------------------------------------------------------------
+struct RowEnd {
+    float cs, ch;               // of exp((z - m) / T) and exp(z - m): cs / s, ch / s1
+    float cp, ct;               // of an entry's p, of the token
+};
+template <bool kTwo>
+__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, float at, const Stat2& st, float share, bool writes) {
+    const double first = a.first[row];
+    const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0.0f && st.s < INFINITY;
+    double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of(st.s) : 0.0, logp = 0.0;
+    if (!good || first != first) kl = NAN;
+    if (a.hard > 0.0) {
+        const float s1 = kTwo ? st.s1 : st.s;
+        logp = static_cast<double>(at) - static_cast<double>(st.m) - log_of(s1);
+        if (!(s1 > 0.0f && s1 < INFINITY)) logp = NAN;
+    } else if (at != at) {
+        kl = NAN;                                        // the token is beyond the vocabulary
+    }
+    if (writes) {
+        a.kl[row] = static_cast<float>(kl);
+        if (a.logp) a.logp[row] = static_cast<float>(logp);
+        a.term[row] = a.soft * a.T * a.T * kl - (a.hard > 0.0 ? a.hard * logp : 0.0);
+    }
+    RowEnd e;
+    e.cp = there ? a.cs * share : 0.0f;
+    e.ct = a.ch * share;
+    if (kl != kl || logp != logp) e.cp = NAN;
+    e.cs = e.cp / st.s;
+    e.ch = kTwo ? e.ct / st.s1 : 0.0f;
+    if (!kTwo) e.cs += e.ct / st.s;                      // one softmax for both
+    return e;
+}
+template <class E, bool kTwo>
+__device__ __forceinline__ float slope_at(float z, float m, const RowEnd& e, const Heat& h) {
+    float d = warm<E::kN == 4>(z - m, h) * e.cs;
+    if (kTwo) d = fmaf(exp_in_gradient<E>(z - m), e.ch, d);
+    return d;
+}
+template <class E, bool kTwo>
+__device__ __forceinline__ void slopes_of(v4u x, float m, const RowEnd& e, const Heat& h, float* d) {
+    E::unpack(x, d);
+#pragma unroll
+    for (int i = 0; i < E::kN; ++i) d[i] = slope_at<E, kTwo>(d[i], m, e, h);
+}
+// The elements that have an entry, by threads threadIdx.x, + threads, ...
+template <class E, bool kTwo>
+__device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row, int64_t token, float m, const RowEnd& e, int from, int threads) {
+    const Entry* list = a.entries + row * (a.k + 1);
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
+    for (int j = from; j <= a.k; j += threads) {
+        const Entry n = list[j];
+        if (n.v >= 0) E::put(dz + n.v, slope_at<E, kTwo>(E::get(z + n.v), m, e, a.heat) - e.cp * n.p - (n.v == token ? e.ct : 0.0f));
+    }
+}
+
+// ---- rows held in registers -----------------------------------------------------------------------------------
+// kWaves wavefronts a row, up to kHeld vectors a thread; as policy_rows_kernel of the policy loss.
+template <class E, bool kTwo, int kWaves, int kHeld, int kPerSimd>
+__global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(const DistillArgs a) {
+    constexpr int kThreads = kWaves * 64;
+    __shared__ Stat2 at[kWaves];
+    __shared__ float counts[kWaves];
+    __shared__ RowEnd of_row;
+    const int64_t row = blockIdx.x;
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
+    const Cut<E> cut(dz, static_cast<int>(a.vocab));
+    const int64_t token = a.tokens[row];
+    const int single = cut.single();
+    RowEnd end{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = 0.0f, alone = -INFINITY;
+    v4u x[kHeld];
+    if (token >= 0) {                   // uniform over the block
+        const float value = token < a.vocab ? E::get(z + token) : NAN;
+        float share = a.rows <= kCountHere ? 0.0f : *a.share;
+        if (single >= 0) alone = E::get(z + single);
+        __builtin_amdgcn_sched_barrier(0);
+        // no load under a condition: each is waited for by itself
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            const int v = u * kThreads + static_cast<int>(threadIdx.x);
+            x[u] = load_vector<E, false>(z, cut.at(v < cut.vectors ? v : cut.vectors - 1));
+        }
+        if (a.rows <= kCountHere) share = 1.0f / fmaxf(counted_rows<kWaves>(a.tokens, a.rows, counts), 1.0f);
+        __builtin_amdgcn_sched_barrier(0);
+        Stat2 st{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+            float f[E::kN], top = -INFINITY;
+            if ((u + 1) * kThreads > cut.vectors)        // uniform
+                x[u] = u * kThreads + static_cast<int>(threadIdx.x) < cut.vectors ? x[u] : v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
+            asm volatile("" : "+v"(x[u]));               // held packed, however it was come by
+            E::unpack(x[u], f);
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[i]);
+            const float most = fmaxf(st.m, top), base = base_of(most);
+            float part = 0.0f, part1 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) {
+                part += warm<true>(f[i] - base, a.heat);
+                if (kTwo) part1 += exp_in_sum<false>(f[i] - base);
+            }
+            st.s = fmaf(st.s, warm<true>(st.m - base, a.heat), part);
+            if (kTwo) st.s1 = fmaf(st.s1, exp_in_sum<true>(st.m - base), part1);
+            st.m = most;
+            __builtin_amdgcn_sched_barrier(0);           // one vector after the other: unpacked, they would not all fit
+        }
+        if (single >= 0) st = joined2<kTwo>(st, of_one2(alone, a.heat), a.heat);
+        st = block_joined2<kTwo, kWaves>(st, a.heat, at);
+        if (threadIdx.x < 64) {
+            const RowEnd e = end_of_row<kTwo>(a, row, value, st, share, threadIdx.x == 0);
+            if (threadIdx.x == 0) of_row = e;
+        }
+        __syncthreads();
+        end = of_row;
+        m = st.m;
+    } else if (threadIdx.x == 0) {
+        a.kl[row] = 0.0f;
+        if (a.logp) a.logp[row] = 0.0f;
+        a.term[row] = 0.0;
+    }
+    const bool zero = end.cs == 0.0f && end.ch == 0.0f;  // NaN is not
+    if (single >= 0) E::put(dz + single, zero ? 0.0f : slope_at<E, kTwo>(alone, m, end, a.heat));
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        const int v = u * kThreads + static_cast<int>(threadIdx.x);
+        if (v < cut.vectors) {
+            float d[E::kN];
+            if (zero) {
+#pragma unroll
+                for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
+            } else {
+                asm volatile("" : "+v"(x[u]));           // unpacked anew, not kept unpacked since the sum
+                slopes_of<E, kTwo>(x[u], m, end, a.heat, d);
+            }
+            store_vector<E>(dz, cut.at(v), d);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (token < 0) return;
+    __syncthreads();
+    store_entries<E, kTwo>(a, row, token, m, end, static_cast<int>(threadIdx.x), kThreads);
+}
+
+// ---- in passes ------------------------------------------------------------------------------------------------
+// grid: rows * splits.
+template <class E, bool kTwo>
+__global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a) {
+    __shared__ Stat2 at[kT / 64];
+    const int64_t row = blockIdx.x / a.splits;
+    const int part = blockIdx.x % a.splits;
+    if (a.tokens[row] < 0) return;
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    const Cut<E> cut(static_cast<const typename E::Raw*>(a.dz) + row * a.vocab, static_cast<int>(a.vocab));    // as the gradient's pass
+    const int each = (cut.vectors + a.splits - 1) / a.splits, v0 = part * each, v1 = v0 + each < cut.vectors ? v0 + each : cut.vectors;
+    float most = -INFINITY;
+    double sum = 0.0, sum1 = 0.0;                        // 32 terms at a time in 32 bits, their sums in 64
+    for (int v = v0 + static_cast<int>(threadIdx.x); v < v1; v += kT * kUnroll) {
+        v4u x[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            x[u] = v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
+            if (v + u * kT < v1) x[u] = load_vector<E, true>(z, cut.at(v + u * kT));
+        }
+        float f[kUnroll][E::kN], top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            E::unpack(x[u], f[u]);
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[u][i]);
+        }
+        const float m = fmaxf(most, top), base = base_of(m);
+        float part[kUnroll], part1[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            part[u] = part1[u] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) {
+                part[u] += warm<true>(f[u][i] - base, a.heat);
+                if (kTwo) part1[u] += exp_in_sum<true>(f[u][i] - base);
+            }
+        }
+        static_assert(kUnroll == 4, "");
+        sum = sum * static_cast<double>(warm<true>(most - base, a.heat)) + static_cast<double>((part[0] + part[1]) + (part[2] + part[3]));
+        if (kTwo) sum1 = sum1 * static_cast<double>(exp_in_sum<true>(most - base)) + static_cast<double>((part1[0] + part1[1]) + (part1[2] + part1[3]));
+        most = m;
+    }
+    Stat2 st{most, static_cast<float>(sum), static_cast<float>(sum1)};
+    if (part == 0 && cut.single() >= 0) st = joined2<kTwo>(st, of_one2(E::get(z + cut.single()), a.heat), a.heat);
+    st = block_joined2<kTwo, kT / 64>(st, a.heat, at);
+    if (threadIdx.x == 0) a.parts[row * a.splits + part] = st;
+}
+
+// The parts of a row joined and what there is one of: one wavefront a row.
+template <class E, bool kTwo>
+__global__ __launch_bounds__(kT) void distill_finish_kernel(const DistillArgs a) {
+    __shared__ float counts[kT / 64];
+    const float share = a.rows <= kCountHere ? 1.0f / fmaxf(counted_rows<kT / 64>(a.tokens, a.rows, counts), 1.0f) : *a.share;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kT / 64) + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const int64_t token = a.tokens[row];
+    if (token < 0) {
+        if (lane == 0) {
+            a.kl[row] = 0.0f;
+            if (a.logp) a.logp[row] = 0.0f;
+            a.term[row] = 0.0;
+        }
+        return;
+    }
+    Stat2 st{-INFINITY, 0.0f, 0.0f};
+    for (int q = lane; q < a.splits; q += 64) st = joined2<kTwo>(st, a.parts[row * a.splits + q], a.heat);
+    st = lanes_joined2<kTwo, 64>(st, a.heat);
+    const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
+    const RowEnd e = end_of_row<kTwo>(a, row, at, st, share, lane == 0);
+    if (lane == 0) {
+        a.stat[row] = Stat2{st.m, e.cp, e.ct};
+        a.coef[row] = make_float2(e.cs, e.ch);
+    }
+}
+__device__ __forceinline__ RowEnd kept_end(const DistillArgs& a, int64_t row, float& m) {
+    const Stat2 st = a.stat[row];
+    const float2 c = a.coef[row];
+    m = st.m;
+    return RowEnd{c.x, c.y, st.s, st.s1};
+}
+
+// grid: rows * blocks.  The last rows first: they are the ones that the pass before has left in the last-level cache.
+template <class E, bool kTwo>
+__global__ __launch_bounds__(kT) void distill_gradient_kernel(const DistillArgs a) {
+    const int64_t row = a.rows - 1 - blockIdx.x / a.blocks;
+    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
+    typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
+    const Cut<E> cut(dz, static_cast<int>(a.vocab));
+    float m = 0.0f;
+    const RowEnd e = a.tokens[row] < 0 ? RowEnd{0.0f, 0.0f, 0.0f, 0.0f} : kept_end(a, row, m);
+    const bool zero = e.cs == 0.0f && e.ch == 0.0f;
+    const int v0 = static_cast<int>(blockIdx.x % a.blocks) * (kT * kUnroll) + static_cast<int>(threadIdx.x);
+    const int single = blockIdx.x % a.blocks == 0 ? cut.single() : -1;
+    if (single >= 0) E::put(dz + single, zero ? 0.0f : slope_at<E, kTwo>(E::get(z + single), m, e, a.heat));
+    v4u x[kUnroll];
+    float d[E::kN];
+    if (zero) {                         // nothing to read
+#pragma unroll
+        for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (v0 + u * kT < cut.vectors) store_vector<E>(dz, cut.at(v0 + u * kT), d);
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+        if (v0 + u * kT < cut.vectors) x[u] = load_vector<E, true>(z, cut.at(v0 + u * kT));
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+        if (v0 + u * kT < cut.vectors) {
+            slopes_of<E, kTwo>(x[u], m, e, a.heat, d);
+            store_vector<E>(dz, cut.at(v0 + u * kT), d);
+        }
+}
+// One wavefront a row.
+template <class E, bool kTwo>
+__global__ __launch_bounds__(kT) void distill_entries_kernel(const DistillArgs a) {
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kT / 64) + (threadIdx.x >> 6);
+    if (row >= a.rows) return;
+    const int64_t token = a.tokens[row];
+    if (token < 0) return;
+    float m;
+    const RowEnd e = kept_end(a, row, m);
+    store_entries<E, kTwo>(a, row, token, m, e, threadIdx.x & 63, 64);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------
+int split_of(int64_t rows, int64_t vectors) {
+    const int64_t most = kSplitBlocks / std::max<int64_t>(rows, 1);
+    return static_cast<int>(std::max<int64_t>(1, std::min(most, vectors / (2 * kT))));
+}
+
+struct Workspace {
+    Entry* entries;
+    double *first, *term;
+    Stat2 *stat, *parts;
+    float2* coef;
+    float* share;
+    int64_t bytes;
+};
+Workspace laid_out(void* at, int64_t rows, int64_t k) {
+    char* p = static_cast<char*>(at);
+    Workspace w{};
+    auto take = [&](int64_t bytes) {
+        char* q = p + w.bytes;
+        w.bytes += up16(bytes);
+        return q;
+    };
+    w.entries = reinterpret_cast<Entry*>(take(rows * (k + 1) * sizeof(Entry)));
+    w.first = reinterpret_cast<double*>(take(rows * sizeof(double)));
+    w.term = reinterpret_cast<double*>(take(rows * sizeof(double)));
+    w.stat = reinterpret_cast<Stat2*>(take(rows * sizeof(Stat2)));
+    w.parts = reinterpret_cast<Stat2*>(take(std::max(rows, kSplitBlocks) * sizeof(Stat2)));    // rows * split_of(rows, .) at most
+    w.coef = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
+    w.share = reinterpret_cast<float*>(take(sizeof(float)));
+    return w;
+}
+
+template <class E, bool kTwo>
+void launch_rows(DistillArgs a, hipStream_t s) {
+    const int64_t rows = a.rows, vectors = a.vocab / E::kN;
+    const dim3 grid(static_cast<uint32_t>(rows)), waves(static_cast<uint32_t>((rows + kT / 64 - 1) / (kT / 64)));
+    const bool apart = vectors < 2 || vectors > 16384 || (rows <= 32 && vectors >= 2048);
+    if (apart) {                         // perhaps none behind the first 16-byte address, or more than a block's registers hold, or few rows
+        a.splits = split_of(rows, vectors);
+        a.blocks = std::max<int64_t>(1, (vectors + kT * kUnroll - 1) / (kT * kUnroll));
+        hipLaunchKernelGGL((distill_stats_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.splits)), dim3(kT), 0, s, a);
+        hipLaunchKernelGGL((distill_finish_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
+        hipLaunchKernelGGL((distill_gradient_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.blocks)), dim3(kT), 0, s, a);
+        hipLaunchKernelGGL((distill_entries_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
+    } else if (vectors <= 256) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 1, 4, 4>), grid, dim3(64), 0, s, a);
+    else if (vectors <= 1024) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 4, 4, 8>), grid, dim3(256), 0, s, a);
+    else if (vectors <= 4096) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 8, 8, 8>), grid, dim3(512), 0, s, a);
+    else if (vectors <= 8192) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 8, 8>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 16, 4>), grid, dim3(1024), 0, s, a);
+}
+template <class E>
+void launch_of(const DistillArgs& a, hipStream_t s) {
+    const int bytes = teacher_words(static_cast<int>(a.k)) * static_cast<int>(sizeof(int));
+    int waves = 4;
+    while (waves > 1 && waves * bytes > 64 * 1024) waves /= 2;
+    hipLaunchKernelGGL(teacher_rows_kernel<E>, dim3(static_cast<uint32_t>((a.rows + waves - 1) / waves)), dim3(waves * 64), waves * bytes, s, a);
+    if (a.hard > 0.0 && a.T != 1.0) launch_rows<E, true>(a, s);
+    else launch_rows<E, false>(a, s);
+}
+
+}  // namespace
+
+int64_t distill_workspace_bytes(int64_t rows, int64_t k) { return laid_out(nullptr, rows, k).bytes; }
+
+hipError_t launch_distill(const LossRows& r, const TeacherRows& t, double temperature, double hard_weight, double loss_scale, float* loss, void* dz, float* kl,
+                          float* logp, void* ws, hipStream_t s) {
+    const Workspace w = laid_out(ws, r.rows, t.k);
+    DistillArgs a{};
+    a.z = r.z; a.tokens = r.tokens; a.rows = r.rows; a.vocab = r.vocab; a.ld = r.ld;
+    a.t = t.z; a.t_type = t.type; a.t_tokens = t.tokens; a.k = t.k; a.ld_t = t.ld; a.ld_tokens = t.ld_tokens;
+    a.T = temperature; a.inv_T = 1.0 / temperature; a.soft = 1.0 - hard_weight; a.hard = hard_weight;
+    a.cs = static_cast<float>((1.0 - hard_weight) * temperature * loss_scale);
+    a.ch = static_cast<float>(hard_weight * loss_scale);
+    const double heat = 1.4426950408889634 / temperature;
+    a.heat.hi = static_cast<float>(heat);
+    if (static_cast<double>(a.heat.hi) >= heat) a.heat.hi = std::nextafterf(a.heat.hi, 0.0f);
+    a.heat.lo = static_cast<float>(heat - static_cast<double>(a.heat.hi));
+    a.share = w.share;
+    a.entries = w.entries; a.first = w.first; a.term = w.term; a.stat = w.stat; a.parts = w.parts; a.coef = w.coef;
+    a.dz = dz; a.kl = kl; a.logp = logp;
+    if (r.rows > kCountHere) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, r.tokens, r.rows, w.share);
+    if (r.rows > 0) {
+        if (r.type == ADPSGD_TYPE_F32) launch_of<F32>(a, s);
+        else if (r.type == ADPSGD_TYPE_BF16) launch_of<Bf16>(a, s);
+        else launch_of<F16>(a, s);
+    }
+    hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(1024), 0, s, w.term, r.tokens, r.rows, loss);
+    return hipGetLastError();
+}
+
+}  // namespace adpsgd_impl

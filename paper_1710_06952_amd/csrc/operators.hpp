@@ -64,6 +64,18 @@ hipError_t launch_policy(const LossRows& a, const PolicyTerms& t, float* loss, v
 hipError_t launch_preference(const LossRows& a, const int64_t* offsets, int64_t pairs, const float* ref, double beta, double smoothing, float* loss,
                              void* dz, float* sums, float* margins, void* ws, hipStream_t s);
 
+struct TeacherRows {                // kernels_distill.hip
+    int32_t type;
+    int64_t k;
+    const int64_t* tokens;
+    int64_t ld_tokens;
+    const void* z;
+    int64_t ld;
+};
+int64_t distill_workspace_bytes(int64_t rows, int64_t k);
+hipError_t launch_distill(const LossRows& r, const TeacherRows& t, double temperature, double hard_weight, double loss_scale, float* loss, void* dz, float* kl,
+                          float* logp, void* ws, hipStream_t s);
+
 // ---- AdamW (kernels_adamw.hip) ----
 constexpr int kAdamwBlock = 256;    // elements that share an exponent
 constexpr int kAdamwChunk = 4096;   // elements of one thread block

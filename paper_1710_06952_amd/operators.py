@@ -27,6 +27,7 @@ _TYPES = {torch.float32: B.TYPE_F32, torch.bfloat16: B.TYPE_BF16, torch.float16:
 _ACTIVATIONS = {"none": B.ACT_NONE, "relu": B.ACT_RELU, "gelu": B.ACT_GELU, "silu": B.ACT_SILU}
 
 PolicyLoss = namedtuple("PolicyLoss", "loss dlogits log_probs")
+DistillationLoss = namedtuple("DistillationLoss", "loss dlogits divergences log_probs")
 PreferenceLoss = namedtuple("PreferenceLoss", "loss dlogits log_probs margins")
 
 
@@ -433,7 +434,7 @@ def layer_norm_gradients(dy, x, weight, stats, *, need=(True, True, True)):
 
 # ---- losses over a vocabulary -----------------------------------------------------------------------------------
 
-def _logits(logits, tokens):
+def _logits(logits, tokens, workspace_bytes=None):
     _on_gpu("logits", logits)
     if logits.dtype not in _TYPES:
         raise TypeError("logits must be float32, bfloat16 or float16, not %s" % logits.dtype)
@@ -443,9 +444,9 @@ def _logits(logits, tokens):
     device = logits.device
     tokens = _vector("tokens", tokens, rows, torch.int64, device)
     z, ld = _as_rows(logits, 1 << 40)
-    size = B.lib().adpsgd_loss_workspace_bytes(rows, vocab)
+    size = (workspace_bytes or B.lib().adpsgd_loss_workspace_bytes)(rows, vocab)
     if size < 0:
-        raise B.AdpsgdError(B.ERR_ARG, "logits: %d rows of %d are too many" % (rows, vocab))
+        raise B.AdpsgdError(B.ERR_ARG, "logits: %d rows of %d are too many%s" % (rows, vocab, ", or more than 1024 entries" if workspace_bytes else ""))
     space = torch.empty(size, dtype=torch.uint8, device=device)
     return (B.Logits(_TYPES[z.dtype], 0, rows, vocab, z.data_ptr(), ld, tokens.data_ptr(), space.data_ptr(), size), rows, device, (z, tokens, space))
 
@@ -492,6 +493,40 @@ def preference_loss_and_gradient(logits, tokens, offsets, ref_log_probs, *, beta
           dz.data_ptr(), sums.data_ptr(), margins.data_ptr())
     del keep
     return PreferenceLoss(loss, dz, sums, margins)
+
+
+def _teacher_rows(name, t, rows, device):
+    """t as rows x k with a contiguous last dimension, and its leading dimension."""
+    _on_gpu(name, t, device)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < 1:
+        raise ValueError("%s is %s, must be rows x entries of %d rows" % (name, tuple(t.shape), rows))
+    return _as_rows(t, _FAR)
+
+
+def distillation_loss_and_gradient(logits, tokens, teacher_tokens, teacher_logits, *, temperature=1.0, hard_weight=0.0, loss_scale=1.0):
+    """(1 - hard_weight) T^2 KL(teacher || softmax(logits / T)) - hard_weight log softmax(logits)[token] (see adpsgd_distillation_loss), a mean over the
+    rows whose token is not negative, and its gradient for the logits.
+
+    The teacher of a row is the softmax of teacher_logits / T (rows x k, any of the types) over its entries teacher_tokens (rows x k,
+    int64): its k <= 1024 largest logits, say; an entry with a negative token is not used.  loss is a scalar tensor; dlogits has the logits'
+    shape and type, and is the gradient of loss_scale times the loss, for logits in float16 (AdamW.step's grad_scale takes it off again); divergences
+    (KL of each row) and log_probs (of the tokens; None where hard_weight is 0) are float32."""
+    _on_gpu("logits", logits)
+    tt, ld_tokens = _teacher_rows("teacher_tokens", teacher_tokens, logits.shape[0] if logits.dim() else 0, logits.device)
+    tz, ld = _teacher_rows("teacher_logits", teacher_logits, tt.shape[0], logits.device)
+    if tt.dtype != torch.int64 or tz.dtype not in _TYPES or tz.shape != tt.shape:
+        raise TypeError("teacher_tokens must be int64 and teacher_logits of the same shape, float32, bfloat16 or float16: they are %s %s, %s %s"
+                        % (tuple(tt.shape), tt.dtype, tuple(tz.shape), tz.dtype))
+    k = tt.shape[1]
+    args, rows, dev, keep = _logits(logits, tokens, lambda rows, vocab: B.lib().adpsgd_distillation_workspace_bytes(rows, vocab, k))
+    teacher = B.Teacher(_TYPES[tz.dtype], 0, k, tt.data_ptr(), ld_tokens, tz.data_ptr(), ld)
+    new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)  # noqa: E731
+    loss, kl, logp = new(), new(rows), new(rows) if hard_weight else None
+    dz = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    _call(dev, B.lib().adpsgd_distillation_loss, C.byref(args), C.byref(teacher), temperature, hard_weight, loss_scale, loss.data_ptr(), dz.data_ptr(),
+          kl.data_ptr(), _ptr(logp))
+    del keep
+    return DistillationLoss(loss, dz, kl, logp)
 
 
 # ---- AdamW ------------------------------------------------------------------------------------------------------

@@ -147,3 +147,83 @@ def test_gated_shapes_and_types():
             (lambda: P.gated_gradients(dh, x, w, slopes[:, :3]), ValueError, "slopes"), (lambda: P.gated_gradients(dh, x, w, slopes.half()), ValueError, "slopes")]:
         with pytest.raises(kind, match=word):
             call()
+
+
+def logits_args(**kw):
+    o = dict(type=B.TYPE_BF16, rows=4, vocab=100, z=NOWHERE, ld=100, tokens=NOWHERE, workspace=NOWHERE, workspace_bytes=1 << 20)
+    o.update(kw)
+    return B.Logits(**o)
+
+
+def teacher_args(**kw):
+    o = dict(type=B.TYPE_F32, k=8, tokens=NOWHERE, ld_tokens=8, z=NOWHERE, ld=8)
+    o.update(kw)
+    return B.Teacher(**o)
+
+
+def distill(o=None, t=None, T=1.0, a=0.0, scale=1.0, loss=NOWHERE, dz=NOWHERE, kl=NOWHERE, logp=None):
+    return B.lib().adpsgd_distillation_loss(C.byref(o or logits_args()), C.byref(t or teacher_args()), T, a, scale, loss, dz, kl, logp, None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(type=3), "type"), (dict(rows=-1), "rows"), (dict(vocab=0), "rows"), (dict(ld=99), "leading"), (dict(z=None), "NULL"), (dict(tokens=None), "NULL"),
+    (dict(tokens=NOWHERE + 4), "aligned"), (dict(workspace=None), "workspace"), (dict(workspace=NOWHERE + 8), "workspace"), (dict(workspace_bytes=4 * 9 * 8), "workspace")])
+def test_distillation_logits(change, word):
+    refused(distill(logits_args(**change)), word)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(type=3), "type"), (dict(k=0), "1024"), (dict(k=1025), "1024"), (dict(ld=7), "leading"), (dict(ld_tokens=7), "leading"), (dict(ld=1 << 41), "leading"), (dict(z=None), "NULL"),
+    (dict(tokens=None), "NULL"), (dict(tokens=NOWHERE + 4), "aligned"), (dict(z=NOWHERE + 2), "aligned")])
+def test_distillation_teacher(change, word):
+    refused(distill(t=teacher_args(**change)), word)
+
+
+def test_distillation_calls():
+    L, at = B.lib(), NOWHERE
+    refused(L.adpsgd_distillation_loss(None, C.byref(teacher_args()), 1.0, 0.0, 1.0, at, at, at, None, None), "no arguments")
+    refused(L.adpsgd_distillation_loss(C.byref(logits_args()), None, 1.0, 0.0, 1.0, at, at, at, None, None), "no teacher")
+    for T in (0.0, -1.0, 1e-7, 1e7, float("nan"), float("inf")):
+        refused(distill(T=T), "temperature")
+    for a in (-0.1, 1.0, float("nan")):
+        refused(distill(a=a, logp=at), "hard_weight")
+    for scale in (float("inf"), float("nan"), 1e30):
+        refused(distill(scale=scale), "loss_scale")
+    refused(distill(a=0.1), "log_probs")
+    refused(distill(logp=at), "log_probs")
+    for kw in (dict(loss=None), dict(dz=None), dict(kl=None)):
+        refused(distill(**kw), "NULL")
+    for kw in (dict(loss=at + 2), dict(dz=at + 1), dict(kl=at + 2), dict(a=0.1, logp=at + 2)):
+        refused(distill(**kw), "aligned")
+    W = L.adpsgd_distillation_workspace_bytes
+    assert W(-1, 10, 1) == W(1, 0, 1) == W(1, 10, 0) == W(1, 10, 1025) == -1 and W(100, 10, 16) >= 100 * 17 * 8 and W(0, 10, 1) > 0
+
+
+def test_distillation_tensors_that_are_not_on_a_gpu():
+    import torch
+    z, tokens = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU"):
+        P.distillation_loss_and_gradient(z, tokens, tokens[:, None], z[:, :1])
+    with pytest.raises(TypeError, match="tensor"):
+        P.distillation_loss_and_gradient([1.0], tokens, tokens[:, None], z[:, :1])
+    from torch.autograd import forward_ad
+    with forward_ad.dual_level():
+        with pytest.raises(NotImplementedError, match="forward mode"):
+            P.distillation_loss_and_gradient(forward_ad.make_dual(z, z), tokens, tokens[:, None], z[:, :1])
+
+
+@pytest.mark.gpu
+def test_distillation_shapes_and_types():
+    import torch
+    new = lambda *s, dtype=torch.int64: torch.zeros(*s, dtype=dtype, device="cuda:0")  # noqa: E731
+    z, tokens, e, t = new(4, 8, dtype=torch.float32), new(4), new(4, 2), new(4, 2, dtype=torch.float32)
+    call = P.distillation_loss_and_gradient
+    for run, kind, word in [
+            (lambda: call(z.double(), tokens, e, t), TypeError, "logits"), (lambda: call(z[0], tokens, e, t), ValueError, "rows"), (lambda: call(z, tokens[:3], e, t), ValueError, "tokens"),
+            (lambda: call(z, tokens, e[:3], t), ValueError, "teacher_tokens"), (lambda: call(z, tokens, e, t[:3]), ValueError, "teacher_logits"),
+            (lambda: call(z, tokens, e[:, :0], t), ValueError, "teacher_tokens"), (lambda: call(z, tokens, e, t[:, :1]), TypeError, "same shape"),
+            (lambda: call(z, tokens, e.int(), t), TypeError, "int64"), (lambda: call(z, tokens, e, t.double()), TypeError, "float32"), (lambda: call(z, tokens, e.cpu(), t), ValueError, "GPU"),
+            (lambda: call(z, tokens, new(4, 1025), new(4, 1025, dtype=torch.float32)), P.AdpsgdError, "1024"), (lambda: call(z, tokens, e, t, temperature=0.0), P.AdpsgdError, "temperature"),
+            (lambda: call(z, tokens, e, t, hard_weight=1.5), P.AdpsgdError, "hard_weight"), (lambda: call(z, tokens, e, t, loss_scale=float("nan")), P.AdpsgdError, "loss_scale")]:
+        with pytest.raises(kind, match=word):
+            run()
