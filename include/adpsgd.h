@@ -505,8 +505,12 @@ int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, int64_t lddy,
 /* Host only: the workspace of a forward (backward = 0) or backward call of these sizes; -1 where an argument is refused. */
 int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward);
 
-/* h: M x N, contiguous.  slopes (or NULL): M x 2 N 16-bit words, contiguous, receives dh/dg and dh/du for the backward call (fp16: as
- * they are; bf16: the fp16 roots of their magnitudes with their signs). */
+/* Host only: the bytes of the slopes that a forward call keeps for its backward call; -1 where an argument is refused. */
+int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N);
+
+/* h: M x N, contiguous.  slopes (or NULL): adpsgd_gated_slopes_bytes, receives dh/dg and dh/du for the backward call.  BF16: M x 2 N words of 16
+ * bits, the fp16 roots of their magnitudes with their signs; F16: the same number of the first 24 bits of fp32, 16 bits of each and behind all of
+ * them the other 8. */
 int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream);
 
 /* Gradients for dh (M x N, row m at dh + m lddh): dx (M x K, contiguous), dw (as w is stored, contiguous) and db (2 N); each may be NULL.

@@ -28,7 +28,7 @@ EXPORTS = [
     "adpsgd_synth_gradient", "adpsgd_run_sync_steps", "adpsgd_run_sync_steps_with", "adpsgd_metropolis_weights",
     "adpsgd_get_event_count", "adpsgd_set_event_count", "adpsgd_verify_plan", "adpsgd_objective", "adpsgd_objective_weighted", "adpsgd_count_nonfinite",
     "adpsgd_dense_workspace_bytes", "adpsgd_dense_forward", "adpsgd_dense_backward", "adpsgd_loss_workspace_bytes", "adpsgd_token_log_probs",
-    "adpsgd_distillation_workspace_bytes", "adpsgd_distillation_loss", "adpsgd_gated_workspace_bytes", "adpsgd_gated_forward", "adpsgd_gated_backward",
+    "adpsgd_distillation_workspace_bytes", "adpsgd_distillation_loss", "adpsgd_gated_workspace_bytes", "adpsgd_gated_slopes_bytes", "adpsgd_gated_forward", "adpsgd_gated_backward",
     "adpsgd_layer_norm_workspace_bytes", "adpsgd_layer_norm_forward", "adpsgd_layer_norm_backward",
     "adpsgd_policy_loss", "adpsgd_preference_loss", "adpsgd_adamw_state_length", "adpsgd_adamw_create", "adpsgd_adamw_destroy", "adpsgd_adamw_step",
     "adpsgd_adamw_get_steps", "adpsgd_adamw_set_steps", "adpsgd_adamw_get_moments", "adpsgd_adamw_set_moments",
@@ -184,6 +184,7 @@ def lib():
         L.adpsgd_dense_forward.argtypes = [P(Dense), vp, vp, vp]
         L.adpsgd_dense_backward.argtypes = [P(Dense), vp, i64, vp, vp, vp, vp, vp]
         L.adpsgd_gated_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        L.adpsgd_gated_slopes_bytes.argtypes = [i32, i64, i64]
         L.adpsgd_gated_forward.argtypes = [P(Dense), vp, vp, vp]
         L.adpsgd_gated_backward.argtypes = [P(Dense), vp, i64, vp, vp, vp, vp, vp]
         L.adpsgd_layer_norm_workspace_bytes.argtypes = [i32, i64, i64]
@@ -205,7 +206,7 @@ def lib():
         L.adpsgd_adamw_get_moments.argtypes = [vp, vp, vp, vp]
         L.adpsgd_adamw_set_moments.argtypes = [vp, vp, vp, vp]
         for name in ("adpsgd_dense_workspace_bytes", "adpsgd_loss_workspace_bytes", "adpsgd_adamw_state_length",
-                     "adpsgd_distillation_workspace_bytes", "adpsgd_gated_workspace_bytes", "adpsgd_layer_norm_workspace_bytes"):
+                     "adpsgd_distillation_workspace_bytes", "adpsgd_gated_workspace_bytes", "adpsgd_gated_slopes_bytes", "adpsgd_layer_norm_workspace_bytes"):
             getattr(L, name).restype = i64
         _lib = L
     return _lib

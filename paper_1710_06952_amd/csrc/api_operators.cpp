@@ -204,6 +204,11 @@ extern "C" int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K,
     return backward ? backward_space(M, 2 * N, K).bytes : up256(gated_partial_bytes(M, N, K));
 }
 
+extern "C" int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N) {
+    if ((type != ADPSGD_TYPE_BF16 && type != ADPSGD_TYPE_F16) || N < 1 || N >= kMostSide || !dense_sizes(M, 2 * N, 1)) return -1;
+    return M * 2 * N * (type == ADPSGD_TYPE_BF16 ? 2 : 3);
+}
+
 extern "C" int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream) {
     return guarded([&]() -> int {
         if (const char* why = gated_fault(o)) return refuse(why);

@@ -99,19 +99,29 @@ __device__ __forceinline__ float slope_of(uint32_t w) {
     return w == 0u ? NAN : r * fabsf(r);
 }
 
-// Slopes of gated projections.  What the backward pass needs of a result h = act(g) u is dh/dg = u act'(g) and dh/du = act(g), kept in 16 bits each.  fp16: as they are.  bf16: their roots with
-// their signs, in fp16: a slope is within 2^-10 of itself, where bf16 would add 2^-8 to what dz is rounded by, from 4e-9 to 2^32 (down to 4e-15 in
-// larger steps, infinite above).
+// Slopes of gated projections.  What the backward pass needs of a result h = act(g) u is dh/dg = u act'(g) and dh/du = act(g).
+// bf16: 16 bits each, the fp16 roots of their magnitudes with their signs: a slope is within 2^-10 of itself from 4e-9 to 2^32 (in larger steps down to
+// 4e-15, infinite above), where bf16 would add 2^-8 to what dz is rounded by.
+// fp16: the first 24 bits of fp32, within 2^-16; 16 bits of them in one plane, eight in another behind it.  Slopes in fp16 as they are
+// would add as much as dz is rounded by: dx and dw sqrt 3 as far from 64 bits as their own rounding, with these sqrt 2.
 template <class T>
-__device__ __forceinline__ uint16_t gated_slope_word(float s) {
-    if constexpr (std::is_same<T, Bf16>::value) s = copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s);
-    return F16::down(s);
-}
-template <class T>
-__device__ __forceinline__ float gated_slope(uint16_t w) {
-    const float r = F16::up(w);
-    return std::is_same<T, Bf16>::value ? r * fabsf(r) : r;
-}
+struct GatedSlopes {
+    static constexpr bool kLow = std::is_same<T, F16>::value;
+    uint16_t* high;             // M x 2 N
+    uint8_t* low;               // M x 2 N, kLow only
+    __device__ __forceinline__ GatedSlopes(uint16_t* p, int64_t M, int64_t N) : high(p), low(reinterpret_cast<uint8_t*>(p + M * 2 * N)) {}
+    // 24 bits, the last eight of them `low`
+    __device__ static __forceinline__ uint32_t word(float s) {
+        if (!kLow) return static_cast<uint32_t>(F16::down(copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s))) << 8;
+        const uint32_t bits = __float_as_uint(s);
+        return s != s ? bits >> 8 | 0x4000u : (bits + 0x80u) >> 8;       // the largest round to infinity
+    }
+    __device__ static __forceinline__ float slope(uint32_t high, uint32_t low) {
+        if (kLow) return __uint_as_float(high << 16 | low << 8);
+        const float r = F16::up(static_cast<uint16_t>(high));
+        return r * fabsf(r);
+    }
+};
 
 // How a product is cut: tiles of side x side (0: columns, dense_narrow.hpp), `splits` parts of k whose sums are joined afterwards.
 struct DensePlan {

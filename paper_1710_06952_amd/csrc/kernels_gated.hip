@@ -2,7 +2,7 @@
 //
 // Both products are one pass over x: a tile holds eight gates, their eight partners, eight gates ... (gated_row in dense_tiles.hpp), so that a gate
 // and its partner end in the same lane, and activation and product are the epilogue of the matrix product of dense layers.  Neither g nor u goes to memory; a
-// backward pass gets dh/dg = u act'(g) and dh/du = act(g) in 16 bits each.  Then
+// backward pass gets dh/dg = u act'(g) and dh/du = act(g) in 16 or 24 bits each.  Then
 //   dz = [dh u act'(g) | dh act(g)],  db = sum over rows of dz      (this file)
 //   dx = dz w,  dw = dz^T x                                         the products of dense layers, over 2 N
 //
@@ -65,7 +65,7 @@ hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s
 namespace {
 
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
-// Memory: 2 + 4 + 4 bytes a result.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
+// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more).  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
 template <class T, int kAcross>
 __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
@@ -75,6 +75,7 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
     const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumns + 8 * cx;
     const int64_t m0 = M * blockIdx.y / gridDim.y, m1 = M * (blockIdx.y + 1) / gridDim.y;
     double sum[2][8] = {};
+    const GatedSlopes<T> kept(const_cast<uint16_t*>(slopes), M, N);
     auto rows = [&](auto whole_columns) {
         constexpr bool kWhole = decltype(whole_columns)::value;
         auto load = [&](const uint16_t* p) {
@@ -84,15 +85,30 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                 if (j + i < N) h[i] = p[i];
             return __builtin_bit_cast(v4u, h);
         };
+        auto load_low = [&](const uint8_t* p) {
+            uint64_t x = 0;
+            if (kWhole) {
+                __builtin_memcpy(&x, p, 8);
+            } else {
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < N) x |= static_cast<uint64_t>(p[i]) << (8 * i);
+            }
+            return v2u{static_cast<uint32_t>(x), static_cast<uint32_t>(x >> 32)};
+        };
         for (int64_t first = m0 + ry; first < m1; first += 4 * kRowsAtOnce) {
             float part[2][8] = {};
             v4u d[4], w[4][2];
+            v2u low[4][2];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {                // rows beyond the strip: its last one again, which counts nothing
                 const int64_t m = first + u * kRowsAtOnce < m1 ? first + u * kRowsAtOnce : m1 - 1;
                 d[u] = load(dh + m * lddh + j);
 #pragma unroll
-                for (int kind = 0; kind < 2; ++kind) w[u][kind] = load(slopes + (2 * m + kind) * N + j);
+                for (int kind = 0; kind < 2; ++kind) {
+                    const int64_t from = (2 * m + kind) * N + j;
+                    w[u][kind] = load(kept.high + from);
+                    if (GatedSlopes<T>::kLow) low[u][kind] = load_low(kept.low + from);
+                }
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -106,7 +122,7 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                     float f[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        f[i] = dy[i] * gated_slope<T>(s[i]);
+                        f[i] = dy[i] * GatedSlopes<T>::slope(s[i], GatedSlopes<T>::kLow ? low[u][kind][i / 4] >> (8 * (i % 4)) & 255u : 0u);
                         part[kind][i] += f[i];
                     }
                     if (!dz) continue;

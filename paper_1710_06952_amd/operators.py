@@ -215,6 +215,9 @@ def dense_gradients(dy, x, w, slope, *, activation="none", need=(True, True, Tru
 
 # ---- gated projections ------------------------------------------------------------------------------------------
 
+_SLOPE_BYTES = {torch.bfloat16: 2, torch.float16: 3}      # of adpsgd_gated_slopes_bytes
+
+
 def _check_gated(x, w, b, activation):
     _on_gpu("x", x)
     for name, t in (("w", w), ("bias", b)):
@@ -249,7 +252,7 @@ def _gated_args(x, w, activation, backward):
 def _gated_forward(x, w, b, activation, want_slopes):
     args, keep = _gated_args(x, w, activation, 0)
     h = torch.empty(*x.shape[:-1], args.N, dtype=x.dtype, device=x.device)
-    slopes = torch.empty(args.M, 2 * args.N, dtype=torch.int16, device=x.device) if want_slopes else None
+    slopes = torch.empty(_SLOPE_BYTES[x.dtype] * 2 * args.N * args.M, dtype=torch.uint8, device=x.device) if want_slopes else None
     if b is not None:
         b = b.contiguous()
         args.b = b.data_ptr()
@@ -291,7 +294,7 @@ def gated(x, w, bias=None, *, activation="silu"):
 
     x (..., in), w (2 out, in) the rows of wg and then those of wu, as it is or as the transpose of an (in, 2 out) tensor, bias (2 out)
     likewise, all bfloat16 or all float16; the result is (..., out).  Activations as dense's.  Both products and theirs are in 32 bits and
-    the result is rounded once.  With gradients, 4 bytes an output are kept for the backward pass.  Under capture of a HIP graph the
+    the result is rounded once.  With gradients, 4 bytes an output (float16: 6) are kept for the backward pass.  Under capture of a HIP graph the
     differentiable form is refused, as dense's is: gated_forward and gated_gradients can be captured."""
     _check_gated(x, w, bias, activation)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias)):
@@ -315,7 +318,7 @@ def gated_gradients(dh, x, w, slopes, *, need=(True, True, True)):
     _on_gpu("slopes", slopes, x.device)
     if dh.dtype != x.dtype or dh.shape != (*x.shape[:-1], w.shape[0] // 2):
         raise ValueError("dh is %s %s, must be as the result" % (tuple(dh.shape), dh.dtype))
-    if slopes.dtype != torch.int16 or slopes.shape != (x.numel() // x.shape[-1], w.shape[0]) or not slopes.is_contiguous():
+    if slopes.dtype != torch.uint8 or slopes.shape != (_SLOPE_BYTES[x.dtype] * dh.numel() * 2,) or not slopes.is_contiguous():
         raise ValueError("slopes must be what gated_forward returned")
     if not any(need):
         return None, None, None

@@ -2,8 +2,9 @@
 
 Tolerances, for products of `n` terms whose magnitudes sum to S: n + 8 roundings to 32 bits, (n + 8) 2^-24 S, and one rounding to the type,
 half a step of it.  Activations and slopes are within 5e-6 (the tail of gelu is fitted to 2.6e-6, the reciprocal and exponential of
-the instruction set add a few 2^-23); |act'| <= 1.13, |act''| <= 1.2.  A slope is kept in 16 bits: in fp16 half a step of that, 2^-11 of itself (2^-25 at
-least); in bf16 as the fp16 root, twice that, 2^-10 (and 1e-14 where the root is subnormal: (2^-25 + sqrt s)^2 - s for s < 2^-28)."""
+the instruction set add a few 2^-23); |act'| <= 1.13, |act''| <= 1.2.  A slope is kept beside fp16 in 24 bits
+of fp32, 2^-16 of itself; beside bf16 in 16 bits, as its root in fp16, twice half a step of that, 2^-10 (and 1e-14 where the root is subnormal: (2^-25 + sqrt s)^2 - s for
+s < 2^-28)."""
 import math
 
 import pytest
@@ -77,7 +78,7 @@ def reference(x, w, b, dh, act):
     out = {"y": (y, 1.01 * h * y.abs() + 1.01 * (aerr * (p.abs() + perr) + a.abs() * perr + 2 * u * y.abs()) + tiny)}
     slope = torch.cat([p * s, a], 1)
     off = torch.cat([serr * (p.abs() + perr) + s.abs() * perr + 2 * u * (p * s).abs(), aerr], 1)
-    kept = 1.01 * (off + (2.0 ** -11 if f16 else 2.0 ** -10) * (slope.abs() + off) + (2.0 ** -25 if f16 else 1e-14))
+    kept = 1.01 * (off + (2.0 ** -16 if f16 else 2.0 ** -10) * (slope.abs() + off) + (1e-38 if f16 else 1e-14))
     d2 = torch.cat([dh, dh], 1)
     dz = d2 * slope
     dzerr = d2.abs() * kept + 2 * u * dz.abs()
@@ -194,6 +195,11 @@ def test_slopes_of_all_sizes():
     db = P.gated_gradients(dh, x, w, slopes, need=(False, True, False))[1][0]      # dw row 0: dh u act'(1) of each row
     want = scale.bfloat16().double() * activation(torch.ones((), dtype=torch.float64), "silu")[1].item()
     assert ((db.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -10 + 1e-5)).all()
+    x, w, dh = x[:48, :48].half(), w[:, :48].half(), dh[:48].half()        # up to 10^3 only, which fp16 holds beside its gradient
+    _, slopes = P.gated_forward(x, w, activation="silu")
+    db = P.gated_gradients(dh, x, w, slopes, need=(False, True, False))[1][0]
+    want = w[8].double() * activation(torch.ones((), dtype=torch.float64), "silu")[1].item()
+    assert ((db.double() - want).abs() <= want * (2.0 ** -11 + 2.0 ** -11 + 2.0 ** -16 + 1e-5) + 2.0 ** -24).all()
 
 
 def test_no_rows():

@@ -118,12 +118,14 @@ def test_gated_calls():
     for sizes in ((-1, 1, 1), (1, 0, 1), (1, 1, 0), (1 << 31, 1, 1), (1 << 20, 1 << 20, 1), (1, 1 << 62, 1)):
         assert L.adpsgd_gated_workspace_bytes(*sizes, 0) == -1 and L.adpsgd_gated_workspace_bytes(*sizes, 1) == -1
     assert L.adpsgd_gated_workspace_bytes(64, 1024, 784, 1) >= 4 * 64 * 1024
+    assert L.adpsgd_gated_slopes_bytes(B.TYPE_BF16, 3, 5) == 60 and L.adpsgd_gated_slopes_bytes(B.TYPE_F16, 3, 5) == 90
+    assert L.adpsgd_gated_slopes_bytes(B.TYPE_F32, 3, 5) == L.adpsgd_gated_slopes_bytes(B.TYPE_F16, -1, 5) == L.adpsgd_gated_slopes_bytes(B.TYPE_F16, 1, 0) == -1
 
 
 def test_gated_tensors_that_are_not_on_a_gpu():
     import torch
     x, w = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(6, 8, dtype=torch.bfloat16)
-    for call in (lambda: P.gated(x, w), lambda: P.gated_forward(x, w), lambda: P.gated_gradients(x[:, :3], x, w, torch.zeros(4, 6, dtype=torch.int16))):
+    for call in (lambda: P.gated(x, w), lambda: P.gated_forward(x, w), lambda: P.gated_gradients(x[:, :3], x, w, torch.zeros(48, dtype=torch.uint8))):
         with pytest.raises(ValueError, match="GPU"):
             call()
     with pytest.raises(TypeError, match="tensor"):
@@ -138,13 +140,13 @@ def test_gated_tensors_that_are_not_on_a_gpu():
 def test_gated_shapes_and_types():
     import torch
     new = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda:0")  # noqa: E731
-    x, w, dh, slopes = new(4, 8), new(6, 8), new(4, 3), new(4, 6, dtype=torch.int16)
+    x, w, dh, slopes = new(4, 8), new(6, 8), new(4, 3), new(48, dtype=torch.uint8)
     for call, kind, word in [
             (lambda: P.gated(x, new(6, 9)), ValueError, "2 out x in"), (lambda: P.gated(x, new(5, 8)), ValueError, "2 out x in"), (lambda: P.gated(x, new(0, 8)), ValueError, "2 out x in"),
             (lambda: P.gated(x.float(), w.float()), TypeError, "float32"), (lambda: P.gated(x, w.half()), TypeError, "float16"), (lambda: P.gated(x, w, new(3)), ValueError, "bias"),
             (lambda: P.gated(x, w, activation="tanh"), ValueError, "activation"), (lambda: P.gated(x, w.cpu()), ValueError, "GPU"),
             (lambda: P.gated_gradients(new(4, 6), x, w, slopes), ValueError, "dh is"), (lambda: P.gated_gradients(dh.half(), x, w, slopes), ValueError, "dh is"),
-            (lambda: P.gated_gradients(dh, x, w, slopes[:, :3]), ValueError, "slopes"), (lambda: P.gated_gradients(dh, x, w, slopes.half()), ValueError, "slopes")]:
+            (lambda: P.gated_gradients(dh, x, w, slopes[:47]), ValueError, "slopes"), (lambda: P.gated_gradients(dh, x, w, slopes.half()), ValueError, "slopes")]:
         with pytest.raises(kind, match=word):
             call()
 
