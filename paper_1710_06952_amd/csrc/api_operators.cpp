@@ -46,11 +46,11 @@ int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 struct BackwardSpace {
     int64_t dz, sums, partial, bytes;       // where they begin
 };
-BackwardSpace backward_space(int64_t M, int64_t N, int64_t K) {
+BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes) {
     BackwardSpace b{};
     b.dz = 0;
     b.sums = up256(2 * M * N);
-    b.partial = b.sums + up256(dense_sums_bytes(M, N));
+    b.partial = b.sums + up256(sums_bytes);
     b.bytes = b.partial + up256(std::max(dense_partial_bytes(M, K, N), dense_partial_bytes(N, K, M)));
     return b;
 }
@@ -149,7 +149,7 @@ LossRows rows_of(const adpsgd_logits_t* o) { return LossRows{o->type, o->rows, o
 
 extern "C" int64_t adpsgd_dense_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward) {
     if (!dense_sizes(M, N, K)) return -1;
-    return backward ? backward_space(M, N, K).bytes : up256(dense_partial_bytes(M, N, K));
+    return backward ? backward_space(M, N, K, dense_sums_bytes(M, N)).bytes : up256(dense_partial_bytes(M, N, K));
 }
 
 extern "C" int adpsgd_dense_forward(const adpsgd_dense_t* o, void* y, uint16_t* slope, void* stream) {
@@ -179,7 +179,7 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
         if (lddy < o->N || lddy > kMostStride) return refuse("dense: the leading dimension of dy is not N .. 2^22");
         if (!slope && o->M > 0 && o->activation != ADPSGD_ACT_NONE) return refuse("dense: the backward call of an activation needs the slopes of the forward call");
         if (!aligned_to(dy, 2) || !aligned_to(slope, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(db, 2)) return refuse("dense: a tensor is not aligned to its type");
-        const BackwardSpace at = backward_space(o->M, o->N, o->K);
+        const BackwardSpace at = backward_space(o->M, o->N, o->K, dense_sums_bytes(o->M, o->N));
         if (o->workspace_bytes < at.bytes || (at.bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("dense: workspace missing, not 16-byte aligned or too small");
         hipStream_t s = static_cast<hipStream_t>(stream);
         char* ws = static_cast<char*>(o->workspace);
@@ -201,7 +201,7 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
 
 extern "C" int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward) {
     if (N < 1 || N >= kMostSide || !dense_sizes(M, 2 * N, K)) return -1;
-    return backward ? backward_space(M, 2 * N, K).bytes : up256(gated_partial_bytes(M, N, K));
+    return backward ? backward_space(M, 2 * N, K, gated_sums_bytes(M, N)).bytes : up256(gated_partial_bytes(M, N, K));
 }
 
 extern "C" int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N) {
@@ -234,7 +234,7 @@ extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, in
         if (o->M > 0 && (!dh || !slopes)) return refuse("gated: dh or slopes is NULL");
         if (lddh < o->N || lddh > kMostStride) return refuse("gated: the leading dimension of dh is not N .. 2^22");
         if (!aligned_to(dh, 2) || !aligned_to(slopes, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(db, 2)) return refuse("gated: a tensor is not aligned to its type");
-        const BackwardSpace at = backward_space(o->M, 2 * o->N, o->K);
+        const BackwardSpace at = backward_space(o->M, 2 * o->N, o->K, gated_sums_bytes(o->M, o->N));
         if (o->workspace_bytes < at.bytes || (at.bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("gated: workspace missing, not 16-byte aligned or too small");
         if (!dx && !dw && !db) return ADPSGD_OK;
         hipStream_t s = static_cast<hipStream_t>(stream);

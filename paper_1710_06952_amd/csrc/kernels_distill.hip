@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) 
     }
     wave_lds_sync();
     bool twice = false;
-    for (int j = lane; j <= k; j += 64) twice = twice || (place_of_entry[j] >= 0 && owner[place_of_entry[j]] != j);
+    for (int j = lane; j < k; j += 64) twice = twice || (place_of_entry[j] >= 0 && owner[place_of_entry[j]] != j);      // the token adds nothing
     twice = __any(twice);
     const double scale = 1.0 / Z;
     const bool bad = beyond || (some && !(Z > 0.0 && Z < INFINITY));

@@ -15,7 +15,6 @@
 //
 // Bound: memory, 2 to 4 bytes an element and tensor: x in, y out;  x and dy in, dx out.
 #include <algorithm>
-#include <type_traits>
 
 #include "elements.hpp"
 
@@ -115,7 +114,7 @@ constexpr int block_of(int lanes, int least) { return lanes > least ? lanes : le
 // stay in registers; blocks of 1024 threads have none left for them and read them for every row, from the caches.
 template <class E, class W, int kLanes, int kHeld>
 __global__ __launch_bounds__(block_of(kLanes, 256)) void norm_kernel(const NormArgs a) {
-    constexpr bool kKeep = kLanes < 1024;
+    constexpr bool kKeep = kLanes < 1024, kLate = kLanes * kHeld == 4096;
     constexpr int kTeams = block_of(kLanes, 256) / kLanes;
     __shared__ float2 at[2][Team<kLanes>::kWaves ? Team<kLanes>::kWaves : 1];
     Team<kLanes> team{at};
@@ -141,24 +140,26 @@ __global__ __launch_bounds__(block_of(kLanes, 256)) void norm_kernel(const NormA
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
     v4u x[kHeld];
     float x1 = 0.0f;
-    auto load = [&](int64_t row) {
-        const typename E::Raw* p = static_cast<const typename E::Raw*>(a.x) + (row < a.rows ? row : a.rows - 1) * a.ldx;
+    auto load = [&](int64_t first) {
+        if (first >= a.rows) return;                     // uniform over the block, as `first` is
+        const int64_t row = first + threadIdx.x / kLanes;
+        const typename E::Raw* from = static_cast<const typename E::Raw*>(a.x) + (row < a.rows ? row : a.rows - 1) * a.ldx;
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const int v = u * kLanes + lane;
-            if (vectors > 0) x[u] = load_row<E>(p, (v < vectors ? v : vectors - 1) * E::kN);
+            if (vectors > 0) x[u] = load_row<E>(from, (v < vectors ? v : vectors - 1) * E::kN);
         }
-        if (single) x1 = E::get(p + last);
+        if (single) x1 = E::get(from + last);
     };
     int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams;
-    load(first + threadIdx.x / kLanes);
-    for (; first < a.rows; first += stride) {            // uniform over the block
+    load(first);
+    for (; first < a.rows; first += stride) {
         const int64_t row = first + threadIdx.x / kLanes;
         float f[kHeld][E::kN];
         const float f1 = x1;
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) E::unpack(x[u], f[u]);
-        if (first + stride < a.rows) load(row + stride);
+        if (!kLate) load(first + stride);
         const RowStat st = row_stat(team, static_cast<float>(a.n), a.eps, [&](const auto& add) {
 #pragma unroll
             for (int u = 0; u < kHeld; ++u)
@@ -168,20 +169,20 @@ __global__ __launch_bounds__(block_of(kLanes, 256)) void norm_kernel(const NormA
                 }
             if (single) add(f1);
         });
-        if (row < a.rows) {
-            typename E::Raw* y = static_cast<typename E::Raw*>(a.y) + row * a.n;
+        if (kLate) load(first + stride);
+        if (row >= a.rows) continue;
+        typename E::Raw* y = static_cast<typename E::Raw*>(a.y) + row * a.n;
 #pragma unroll
-            for (int u = 0; u < kHeld; ++u) {
-                const int v = u * kLanes + lane;
-                float o[E::kN];
-                if (!kKeep) params(u);
+        for (int u = 0; u < kHeld; ++u) {
+            const int v = u * kLanes + lane;
+            float o[E::kN];
+            if (!kKeep) params(u);
 #pragma unroll
-                for (int i = 0; i < E::kN; ++i) o[i] = fmaf(normed(f[u][i], st), w[u][i], b[u][i]);
-                if (v < vectors) store_row<E>(y, v * E::kN, o);
-            }
-            if (single) E::put(y + last, fmaf(normed(f1, st), w1, b1));
-            if (a.stats && lane == 0) keep_stat(a, row, st);
+            for (int i = 0; i < E::kN; ++i) o[i] = fmaf(normed(f[u][i], st), w[u][i], b[u][i]);
+            if (v < vectors) store_row<E>(y, v * E::kN, o);
         }
+        if (single) E::put(y + last, fmaf(normed(f1, st), w1, b1));
+        if (a.stats && lane == 0) keep_stat(a, row, st);
     }
 }
 
@@ -230,7 +231,8 @@ struct NormGradArgs {
     int n;
     const float* stats;
     void* dx;                   // or nullptr
-    float* sums;                // [parts][2][n] columns' sums of dy h and dy, or nullptr
+    float* sums;                // [parts][2][n] columns' sums of dy h and dy; nullptr: dw and db are written as they are
+    void *dw, *db;              // either may be nullptr
 };
 __device__ __forceinline__ RowStat kept_stat(const NormGradArgs& a, int64_t row) {
     return RowStat{a.stats[row], a.stats[a.rows + row], a.stats[2 * a.rows + row], 1.0f};
@@ -239,7 +241,7 @@ __device__ __forceinline__ RowStat kept_stat(const NormGradArgs& a, int64_t row)
 // As norm_kernel; a thread's columns are the same in every row.
 template <class E, class W, int kLanes, int kHeld, int kBlock>
 __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArgs a) {
-    constexpr bool kKeep = kHeld < 4;
+    constexpr bool kAgain = kHeld == 4, kKeep = !kAgain;
     constexpr int kTeams = kBlock / kLanes, kWide = kLanes * kHeld * E::kN + E::kN;
     __shared__ float2 at[2][Team<kLanes>::kWaves ? Team<kLanes>::kWaves : 1];
     __shared__ float joined[kTeams > 1 ? 2 : 1][kTeams > 1 ? kWide : 1];
@@ -264,28 +266,29 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
     v4u x[kHeld], d[kHeld];
     float x1 = 0.0f, d1 = 0.0f;
     RowStat next{};
-    auto load = [&](int64_t row) {
-        const int64_t from = row < a.rows ? row : a.rows - 1;
-        const typename E::Raw* p = static_cast<const typename E::Raw*>(a.x) + from * a.ldx;
-        const typename E::Raw* q = static_cast<const typename E::Raw*>(a.dy) + from * a.lddy;
+    auto load = [&](int64_t first) {
+        if (first >= a.rows) return;                     // uniform over the block, as `first` is
+        const int64_t row = first + threadIdx.x / kLanes, from = row < a.rows ? row : a.rows - 1;
+        const typename E::Raw* of_x = static_cast<const typename E::Raw*>(a.x) + from * a.ldx;
+        const typename E::Raw* of_d = static_cast<const typename E::Raw*>(a.dy) + from * a.lddy;
         next = kept_stat(a, from);
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const int v = u * kLanes + lane, e = (v < vectors ? v : vectors - 1) * E::kN;
             if (vectors > 0) {
-                x[u] = load_row<E>(p, e);
-                d[u] = load_row<E>(q, e);
+                x[u] = load_row<E>(of_x, e);
+                d[u] = load_row<E>(of_d, e);
             }
         }
         if (single) {
-            x1 = E::get(p + last);
-            d1 = E::get(q + last);
+            x1 = E::get(of_x + last);
+            d1 = E::get(of_d + last);
         }
     };
     float sw[kHeld][E::kN] = {}, sb[kHeld][E::kN] = {}, sw1 = 0.0f, sb1 = 0.0f;
     int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams;
-    load(first + threadIdx.x / kLanes);
-    for (; first < a.rows; first += stride) {            // uniform over the block
+    load(first);
+    for (; first < a.rows; first += stride) {
         const int64_t row = first + threadIdx.x / kLanes;
         const bool there = row < a.rows;
         const RowStat st = next;
@@ -293,6 +296,7 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const bool mine = there && u * kLanes + lane < vectors;
+            if (kAgain) __builtin_amdgcn_sched_barrier(0);           // one vector after the other: unpacked, they would not all fit
             if (!kKeep) params(u);
             E::unpack(x[u], h[u]);
             E::unpack(d[u], g[u]);
@@ -315,7 +319,7 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
             p += g1;
             q = fmaf(g1, h1, q);
         }
-        if (first + stride < a.rows) load(row + stride);
+        if (!kAgain) load(first + stride);
         const float2 t = team.sum(p, q);
         const float mp = t.x * inv, mq = t.y * inv;
         if (there && a.dx) {
@@ -324,54 +328,60 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
             for (int u = 0; u < kHeld; ++u) {
                 const int v = u * kLanes + lane;
                 float o[E::kN];
+                if (kAgain) {                            // unpacked and computed anew, not kept since the sum
+                    __builtin_amdgcn_sched_barrier(0);
+                    asm volatile("" : "+v"(x[u]), "+v"(d[u]));
+                    params(u);
+                    E::unpack(x[u], h[u]);
+                    E::unpack(d[u], g[u]);
+#pragma unroll
+                    for (int i = 0; i < E::kN; ++i) {
+                        h[u][i] = normed(h[u][i], st);
+                        g[u][i] *= w[u][i];
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < E::kN; ++i) o[i] = st.r * (g[u][i] - mp - h[u][i] * mq);
                 if (v < vectors) store_row<E>(dx, v * E::kN, o);
             }
             if (single) E::put(dx + last, st.r * (g1 - mp - h1 * mq));
         }
+        if (kAgain) load(first + stride);
     }
-    if (!a.sums) return;
-    float* out = a.sums + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
-    if constexpr (kTeams == 1) {
+    if (!a.dw && !a.db) return;
+    auto finish = [&](int e, float s, float c) {
+        if (a.sums) {
+            float* out = a.sums + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
+            out[e] = s;
+            out[a.n + e] = c;
+        } else {                                         // the only block
+            if (a.dw) W::put(static_cast<typename W::Raw*>(a.dw) + e, s);
+            if (a.db) W::put(static_cast<typename W::Raw*>(a.db) + e, c);
+        }
+    };
+    auto columns = [&](const auto& f) {                  // a thread's own
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const int v = u * kLanes + lane;
             if (v < vectors) {
 #pragma unroll
-                for (int i = 0; i < E::kN; ++i) {
-                    out[v * E::kN + i] = sw[u][i];
-                    out[a.n + v * E::kN + i] = sb[u][i];
-                }
+                for (int i = 0; i < E::kN; ++i) f(v * E::kN + i, sw[u][i], sb[u][i]);
             }
         }
-        if (single) {
-            out[last] = sw1;
-            out[a.n + last] = sb1;
-        }
+        if (single) f(last, sw1, sb1);
+    };
+    if constexpr (kTeams == 1) {
+        columns(finish);
     } else {                                             // one team after the other, in their order
         for (int t = 0; t < kTeams; ++t) {
-            if (static_cast<int>(threadIdx.x) / kLanes == t) {
-                auto add = [&](int e, float s, float c) {
+            if (static_cast<int>(threadIdx.x) / kLanes == t)
+                columns([&](int e, float s, float c) {
                     joined[0][e] = t == 0 ? s : joined[0][e] + s;
                     joined[1][e] = t == 0 ? c : joined[1][e] + c;
-                };
-#pragma unroll
-                for (int u = 0; u < kHeld; ++u) {
-                    const int v = u * kLanes + lane;
-                    if (v < vectors) {
-#pragma unroll
-                        for (int i = 0; i < E::kN; ++i) add(v * E::kN + i, sw[u][i], sb[u][i]);
-                    }
-                }
-                if (single) add(last, sw1, sb1);
-            }
+                });
             __syncthreads();
         }
-        for (int e = threadIdx.x; e < a.n; e += kBlock) {
-            out[e] = joined[0][e];
-            out[a.n + e] = joined[1][e];
-        }
+        for (int e = threadIdx.x; e < a.n; e += kBlock) finish(e, joined[0][e], joined[1][e]);
     }
 }
 
@@ -467,81 +477,92 @@ __global__ __launch_bounds__(64 * kJoin) void norm_join_kernel(const float* sums
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
-// The team for rows of so many vectors: lanes, vectors of a lane.
+// The team for rows of so many vectors (lanes, vectors of a lane; lanes 0: `long`), threads of a block, and blocks at most.  Microseconds for 2^27
+// elements in bf16 (537 MB forward, 805 backward, 6.1 TB/s at most), forward:
+//   1024 vectors  256 lanes of 4 in 2048 blocks 94 (8192 blocks 98, all rows at once 114), 512 of 2 96, 1024 of 1 134
+//    512          256 of 2 in 8192 blocks 90 (1024 blocks 93, all 111), 512 of 1 106, 64 of 8 104
+//    256          64 of 4 in 8192 blocks 89, 256 of 1 97;    128: 64 of 2 91;    64: 64 of 1 98;    16: 98 to 103
+// backward, where every block costs its columns' sums:
+//   1024 vectors  1024 lanes of 1 in 256 blocks 139 (512 blocks 147), 512 of 2 152
+//    512          512 of 1 in 512 blocks 138, 256 of 2 143;    256: 256 of 1 in 1024 blocks 140 (512: 154);    128: 64 of 2 in 512 blocks 138
+//     64          64 of 1, blocks of 512 threads, 512 of them 135 (256 threads, 1024 blocks 139)
+// A second row under way: 92 for 94 and 135 for 139 at 1024 vectors, and slower at most others.
 struct Shape {
-    int lanes, held;            // lanes 0: `long`
+    int lanes, held, block;
+    int64_t blocks;
 };
 Shape forward_shape(int64_t vectors) {
     for (int lanes : {8, 16, 32, 64})
-        if (vectors <= lanes) return Shape{lanes, 1};
-    if (vectors <= 128) return Shape{64, 2};
-    if (vectors <= 256) return Shape{64, 4};
-    if (vectors <= 1024) return Shape{256, 4};
-    if (vectors <= 2048) return Shape{1024, 2};
-    if (vectors <= 4096) return Shape{1024, 4};
-    return Shape{0, 0};
+        if (vectors <= lanes) return Shape{lanes, 1, 256, 8192};
+    if (vectors <= 128) return Shape{64, 2, 256, 8192};
+    if (vectors <= 256) return Shape{64, 4, 256, 8192};
+    if (vectors <= 512) return Shape{256, 2, 256, 8192};
+    if (vectors <= 1024) return Shape{256, 4, 256, 2048};
+    if (vectors <= 2048) return Shape{1024, 2, 1024, 512};
+    if (vectors <= 4096) return Shape{1024, 4, 1024, 512};
+    return Shape{0, 0, kLongThreads, 512};
 }
 Shape gradient_shape(int64_t vectors) {
     for (int lanes : {8, 16, 32, 64})
-        if (vectors <= lanes) return Shape{lanes, 1};
-    if (vectors <= 128) return Shape{64, 2};
-    if (vectors <= 256) return Shape{256, 1};
-    if (vectors <= 512) return Shape{256, 2};
-    if (vectors <= 1024) return Shape{512, 2};
-    if (vectors <= 2048) return Shape{512, 4};
-    return Shape{0, 0};
+        if (vectors <= lanes) return Shape{lanes, 1, 512, 512};
+    if (vectors <= 128) return Shape{64, 2, 256, 512};
+    if (vectors <= 256) return Shape{256, 1, 256, 1024};
+    if (vectors <= 512) return Shape{512, 1, 512, 512};
+    if (vectors <= 1024) return Shape{1024, 1, 1024, 256};
+    if (vectors <= 2048) return Shape{512, 4, 512, 256};
+    return Shape{0, 0, kLongThreads, 512};
 }
-constexpr int kGradientBlock = 256;
-constexpr int64_t kMostParts = 512;
 int64_t vectors_of(int32_t type, int64_t n) { return n / (type == ADPSGD_TYPE_F32 ? F32::kN : Bf16::kN); }
-// Blocks of the gradient's pass, and parts of the columns' sums.
+// Blocks of the gradient's pass, and parts of the columns' sums.  Up to eight rows of a team are left to one block, which writes dw and db itself: a
+// launch and a workspace less (128 x 128 in fp32: 5 us of host time, and on the GPU eight turns take no longer than one and the join).
 int64_t parts_of(int32_t type, int64_t rows, int64_t n) {
     const Shape s = gradient_shape(vectors_of(type, n));
-    const int64_t teams = s.lanes == 0 ? 1 : std::max(1, kGradientBlock / s.lanes), turns = (rows + teams - 1) / teams;
-    return std::max<int64_t>(std::min(turns, kMostParts), (turns + kChain - 1) / kChain);
+    const int64_t teams = s.lanes == 0 ? 1 : s.block / s.lanes, turns = (rows + teams - 1) / teams;
+    if (s.lanes > 0 && turns <= 8) return 1;
+    return std::max<int64_t>(std::min(turns, s.blocks), (turns + kChain - 1) / kChain);
 }
 
 template <class E, class W>
 void launch_norm_of(const NormArgs& a, hipStream_t s) {
     const Shape shape = forward_shape(a.n / E::kN);
-    auto go = [&](auto kernel, int lanes, int block) {
-        const int64_t teams = block / lanes, blocks = std::min<int64_t>((a.rows + teams - 1) / teams, 256 * 2048 / block);
-        hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(block), 0, s, a);
-    };
-    if (shape.lanes == 8) go(norm_kernel<E, W, 8, 1>, 8, 256);
-    else if (shape.lanes == 16) go(norm_kernel<E, W, 16, 1>, 16, 256);
-    else if (shape.lanes == 32) go(norm_kernel<E, W, 32, 1>, 32, 256);
-    else if (shape.lanes == 64 && shape.held == 1) go(norm_kernel<E, W, 64, 1>, 64, 256);
-    else if (shape.lanes == 64 && shape.held == 2) go(norm_kernel<E, W, 64, 2>, 64, 256);
-    else if (shape.lanes == 64) go(norm_kernel<E, W, 64, 4>, 64, 256);
-    else if (shape.lanes == 256) go(norm_kernel<E, W, 256, 4>, 256, 256);
-    else if (shape.held == 2) go(norm_kernel<E, W, 1024, 2>, 1024, 1024);
-    else if (shape.held == 4) go(norm_kernel<E, W, 1024, 4>, 1024, 1024);
-    else go(norm_long_kernel<E, W>, kLongThreads, kLongThreads);
+    const int64_t teams = shape.lanes ? shape.block / shape.lanes : 1, blocks = std::min<int64_t>((a.rows + teams - 1) / teams, shape.blocks);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(shape.block), 0, s, a); };
+    switch (shape.lanes * 8 + shape.held) {
+        case 8 * 8 + 1: return go(norm_kernel<E, W, 8, 1>);
+        case 16 * 8 + 1: return go(norm_kernel<E, W, 16, 1>);
+        case 32 * 8 + 1: return go(norm_kernel<E, W, 32, 1>);
+        case 64 * 8 + 1: return go(norm_kernel<E, W, 64, 1>);
+        case 64 * 8 + 2: return go(norm_kernel<E, W, 64, 2>);
+        case 64 * 8 + 4: return go(norm_kernel<E, W, 64, 4>);
+        case 256 * 8 + 2: return go(norm_kernel<E, W, 256, 2>);
+        case 256 * 8 + 4: return go(norm_kernel<E, W, 256, 4>);
+        case 1024 * 8 + 2: return go(norm_kernel<E, W, 1024, 2>);
+        case 1024 * 8 + 4: return go(norm_kernel<E, W, 1024, 4>);
+        default: return go(norm_long_kernel<E, W>);
+    }
 }
 
 template <class E, class W>
-void launch_norm_gradient_of(int32_t type, const NormGradArgs& a, void* dw, void* db, hipStream_t s) {
+void launch_norm_gradient_of(int32_t type, const NormGradArgs& a, hipStream_t s) {
     const Shape shape = gradient_shape(a.n / E::kN);
     const int64_t parts = parts_of(type, a.rows, a.n);
-    auto go = [&](auto kernel, int block) { hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(parts)), dim3(block), 0, s, a); };
-    if (a.rows > 0) {
-        if (shape.lanes == 8) go(norm_gradient_kernel<E, W, 8, 1, 256>, 256);
-        else if (shape.lanes == 16) go(norm_gradient_kernel<E, W, 16, 1, 256>, 256);
-        else if (shape.lanes == 32) go(norm_gradient_kernel<E, W, 32, 1, 256>, 256);
-        else if (shape.lanes == 64 && shape.held == 1) go(norm_gradient_kernel<E, W, 64, 1, 256>, 256);
-        else if (shape.lanes == 64) go(norm_gradient_kernel<E, W, 64, 2, 256>, 256);
-        else if (shape.lanes == 256 && shape.held == 1) go(norm_gradient_kernel<E, W, 256, 1, 256>, 256);
-        else if (shape.lanes == 256) go(norm_gradient_kernel<E, W, 256, 2, 256>, 256);
-        else if (shape.lanes == 512 && shape.held == 2) go(norm_gradient_kernel<E, W, 512, 2, 512>, 512);
-        else if (shape.lanes == 512) go(norm_gradient_kernel<E, W, 512, 4, 512>, 512);
-        else {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(parts)), dim3(shape.block), 0, s, a); };
+    if (a.rows > 0) switch (shape.lanes * 8 + shape.held) {
+        case 8 * 8 + 1: go(norm_gradient_kernel<E, W, 8, 1, 512>); break;
+        case 16 * 8 + 1: go(norm_gradient_kernel<E, W, 16, 1, 512>); break;
+        case 32 * 8 + 1: go(norm_gradient_kernel<E, W, 32, 1, 512>); break;
+        case 64 * 8 + 1: go(norm_gradient_kernel<E, W, 64, 1, 512>); break;
+        case 64 * 8 + 2: go(norm_gradient_kernel<E, W, 64, 2, 256>); break;
+        case 256 * 8 + 1: go(norm_gradient_kernel<E, W, 256, 1, 256>); break;
+        case 512 * 8 + 1: go(norm_gradient_kernel<E, W, 512, 1, 512>); break;
+        case 1024 * 8 + 1: go(norm_gradient_kernel<E, W, 1024, 1, 1024>); break;
+        case 512 * 8 + 4: go(norm_gradient_kernel<E, W, 512, 4, 512>); break;
+        default:
             if (a.dx) hipLaunchKernelGGL((norm_gradient_long_kernel<E, W>), dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 512))), dim3(kLongThreads), 0, s, a);
             if (a.sums) hipLaunchKernelGGL(norm_columns_kernel<E>, dim3(static_cast<uint32_t>((a.n + 255) / 256), static_cast<uint32_t>(parts)), dim3(256), 0, s, a);
-        }
     }
-    if (dw || db)
-        hipLaunchKernelGGL(norm_join_kernel<W>, dim3(static_cast<uint32_t>((a.n + 63) / 64), 2), dim3(64 * kJoin), 0, s, a.sums, a.rows > 0 ? parts : 0, a.n, dw, db);
+    if ((a.dw || a.db) && (a.sums || a.rows == 0))
+        hipLaunchKernelGGL(norm_join_kernel<W>, dim3(static_cast<uint32_t>((a.n + 63) / 64), 2), dim3(64 * kJoin), 0, s, a.sums, a.rows > 0 ? parts : 0, a.n, a.dw, a.db);
 }
 
 // f(E, W) for the two types
@@ -555,7 +576,8 @@ void with_types(int32_t type, int32_t params, const F& f) {
 }  // namespace
 
 int64_t norm_workspace_bytes(int32_t type, int64_t rows, int64_t n) {
-    return rows > 0 ? parts_of(type, rows, n) * 2 * n * static_cast<int64_t>(sizeof(float)) : 0;
+    const int64_t parts = rows > 0 ? parts_of(type, rows, n) : 0;
+    return parts > 1 || gradient_shape(vectors_of(type, n)).lanes == 0 ? parts * 2 * n * static_cast<int64_t>(sizeof(float)) : 0;
 }
 
 hipError_t launch_norm(const NormRows& r, const void* b, double eps, void* y, float* stats, hipStream_t s) {
@@ -574,8 +596,9 @@ hipError_t launch_norm_gradient(const NormRows& r, const void* dy, int64_t lddy,
     a.lddy = lddy; a.ldx = r.ldx; a.rows = r.rows; a.n = static_cast<int>(r.n);
     a.stats = stats;
     a.dx = dx;
-    a.sums = dw || db ? static_cast<float*>(ws) : nullptr;
-    with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_gradient_of<decltype(e), decltype(w)>(r.type, a, dw, db, s); });
+    a.dw = dw; a.db = db;
+    a.sums = (dw || db) && norm_workspace_bytes(r.type, r.rows, r.n) > 0 ? static_cast<float*>(ws) : nullptr;
+    with_types(r.type, r.param_type, [&](auto e, auto w) { launch_norm_gradient_of<decltype(e), decltype(w)>(r.type, a, s); });
     return hipGetLastError();
 }
 

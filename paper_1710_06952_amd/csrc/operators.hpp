@@ -31,6 +31,7 @@ int64_t dense_sums_bytes(int64_t M, int64_t N);
 // ---- gated projections (kernels_gated.hip): g of J gates with their partners, act(gate) partner ----
 hipError_t launch_gated_gemm(int32_t type, const DenseGemm& g, hipStream_t s);      // b_up is set here
 int64_t gated_partial_bytes(int64_t I, int64_t J, int64_t K);
+int64_t gated_sums_bytes(int64_t M, int64_t N);
 // dz = [dh slope | dh slope'] (dz may be nullptr: only db), db = column sums of the unrounded dz (db may be nullptr)
 hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* db, double* sums, int64_t M, int64_t N,
                            hipStream_t s);

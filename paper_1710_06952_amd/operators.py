@@ -267,7 +267,7 @@ def _gated_backward(dh, x, w, slopes, need_dx, need_dw, need_db):
     dhm, lddh = _as_rows(dh)
     M, N, K = args.M, args.N, args.K
     new = lambda *shape: torch.empty(*shape, dtype=x.dtype, device=x.device)  # noqa: E731
-    dx = new(*x.shape) if need_dx else None
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
     dw = (new(K, 2 * N).t() if args.w_transposed else new(2 * N, K)) if need_dw else None
     db = new(2 * N) if need_db else None
     _call(x.device, B.lib().adpsgd_gated_backward, C.byref(args), dhm.data_ptr(), lddh, slopes.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db))
@@ -363,7 +363,7 @@ def _norm_args(x, w, b, eps):
 
 def _norm_forward(x, w, b, eps, want_stats):
     args, keep = _norm_args(x, w, b, eps)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
     stats = torch.empty(3, args.rows, dtype=torch.float32, device=x.device) if want_stats else None
     _call(x.device, B.lib().adpsgd_layer_norm_forward, C.byref(args), y.data_ptr(), _ptr(stats))
     del keep
@@ -373,7 +373,7 @@ def _norm_forward(x, w, b, eps, want_stats):
 def _norm_backward(dy, x, w, stats, need_dx, need_dw, need_db):
     args, keep = _norm_args(x, w, None, 1.0)
     dym, lddy = _as_rows(dy, _FAR)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_dx else None
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
     dw, db = (torch.empty_like(w, memory_format=torch.contiguous_format) if needed and w is not None else None for needed in (need_dw, need_db))
     space = None
     if dw is not None or db is not None:
@@ -525,7 +525,7 @@ def distillation_loss_and_gradient(logits, tokens, teacher_tokens, teacher_logit
     teacher = B.Teacher(_TYPES[tz.dtype], 0, k, tt.data_ptr(), ld_tokens, tz.data_ptr(), ld)
     new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)  # noqa: E731
     loss, kl, logp = new(), new(rows), new(rows) if hard_weight else None
-    dz = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    dz = torch.empty_like(logits, memory_format=torch.contiguous_format)
     _call(dev, B.lib().adpsgd_distillation_loss, C.byref(args), C.byref(teacher), temperature, hard_weight, loss_scale, loss.data_ptr(), dz.data_ptr(),
           kl.data_ptr(), _ptr(logp))
     del keep

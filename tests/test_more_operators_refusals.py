@@ -46,11 +46,11 @@ def test_layer_norm_calls():
     refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(w=None, b=None)), at, 16, at, at, at, None, None), "dw without w")
     refused(L.adpsgd_layer_norm_backward(C.byref(o), at, 16, at, at, at + 1, at, None), "aligned")
     for short in (dict(workspace_bytes=8), dict(workspace=None), dict(workspace=at + 8)):
-        refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(**short)), at, 16, at, None, at, None, None), "workspace")
+        refused(L.adpsgd_layer_norm_backward(C.byref(norm_args(rows=4000, **short)), at, 16, at, None, at, None, None), "workspace")
     assert L.adpsgd_layer_norm_forward(C.byref(norm_args(rows=0, x=None)), None, None, None) == B.OK       # no rows: nothing to do
     assert L.adpsgd_layer_norm_backward(C.byref(norm_args(rows=0, x=None)), None, 16, None, None, None, None, None) == B.OK
     assert L.adpsgd_layer_norm_workspace_bytes(9, 4, 16) == L.adpsgd_layer_norm_workspace_bytes(0, -1, 16) == L.adpsgd_layer_norm_workspace_bytes(0, 4, 0) == -1
-    assert L.adpsgd_layer_norm_workspace_bytes(0, 0, 16) == 0 and L.adpsgd_layer_norm_workspace_bytes(1, 4, 16) >= 128
+    assert L.adpsgd_layer_norm_workspace_bytes(0, 0, 16) == 0 and L.adpsgd_layer_norm_workspace_bytes(1, 4000, 16) >= 256
 
 
 def test_layer_norm_tensors_that_are_not_on_a_gpu():
