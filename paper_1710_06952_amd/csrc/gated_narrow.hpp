@@ -12,13 +12,18 @@ namespace {
 
 // kTI: tiles of 16 rows; kV: gates of a lane's operands, 16 kV of a block
 template <class T, bool kBOuter, int kTI, int kV>
-__global__ __launch_bounds__(kNarrowWaves * 64) void gated_narrow_kernel(const DenseGemm g, const int splits) {
+__global__ __launch_bounds__(kNarrowWaves * 64, kTI == 1 && !kBOuter ? 4 : 2) void gated_narrow_kernel(const DenseGemm g, const int splits) {
     constexpr int kColumns = 16 * kV, kStep = kBOuter ? 32 : 64, kPitch = 2 * kColumns + 4;
     static_assert(kBOuter || kV == 1, "");
     extern __shared__ __attribute__((aligned(16))) float sums[];         // [wave][16 kTI][kPitch]: gates, partners
     const int wave = threadIdx.x >> 6, l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
     int64_t none, tile, split;
-    place_of(blockIdx.x, gridDim.x, 1, gridDim.x / splits, none, tile, split);
+    if (kBOuter) {
+        place_of(blockIdx.x, gridDim.x, 1, gridDim.x / splits, none, tile, split);      // neighbouring columns on one XCD: they share lines
+    } else {                                             // rows of their own; in their order over the XCDs 25.8 us for 27.3
+        tile = blockIdx.x / splits;
+        split = blockIdx.x % splits;
+    }
     const int64_t j0 = tile * kColumns;
     const uint16_t* a[kTI];
 #pragma unroll
@@ -33,45 +38,72 @@ __global__ __launch_bounds__(kNarrowWaves * 64) void gated_narrow_kernel(const D
         for (int m = 0; m < kTI; ++m)
 #pragma unroll
             for (int n = 0; n < kV; ++n) acc[kind][m][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kTogether = kTI == 1 ? 2 : 1;
-    const int64_t whole = g.K / kStep, until = whole * (split + 1) / splits;
-    auto walk = [&](auto go) {
-        int64_t s = whole * split / splits + wave;
-        if (kTogether > 1)
-            for (; s + (kTogether - 1) * kNarrowWaves < until; s += kTogether * kNarrowWaves) go(s, std::integral_constant<int, kTogether>(), std::false_type());
-#pragma unroll 1
-        for (; s < until; s += kNarrowWaves) go(s, std::integral_constant<int, 1>(), std::false_type());
-        if (whole * kStep < g.K && split + 1 == splits && wave == 0) go(whole, std::integral_constant<int, 1>(), std::true_type());
-    };
-
+    const int64_t whole = g.K / kStep, until = whole * (split + 1) / splits;          // this block's steps, wavefronts in turn
     if constexpr (!kBOuter) {
         const int64_t j = j0 + l < g.J ? j0 + l : g.J - 1;
         const uint16_t* b[2] = {static_cast<const uint16_t*>(g.b) + j * g.ldb, static_cast<const uint16_t*>(g.b) + j * g.ldb + g.b_up};
-        auto go = [&](int64_t s, auto some, auto last) {
-            constexpr int kSome = decltype(some)::value;
+        // kDeep steps are on their way while one is multiplied, so that the loads of a wavefront never run dry.  1 x 4096 x (2 x 8192): three steps
+        // 25.8 us, two 27, four (of which registers spill) 32; two steps that are waited for together 31.
+        constexpr int kDeep = kTI == 1 ? 3 : 2;
+        v4u fb[kDeep][2][2], fa[kDeep][2][kTI];
+        auto load = [&](int64_t s, auto place, auto last) {
+            constexpr int u = decltype(place)::value;
             constexpr bool kLast = decltype(last)::value;
-            v4u fb[kSome][2][2], fa[kSome][2][kTI];
 #pragma unroll
-            for (int u = 0; u < kSome; ++u)
+            for (int h = 0; h < 2; ++h) {
+                const int64_t k = s * kStep + 16 * q + 8 * h;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t k = (s + u * kNarrowWaves) * kStep + 16 * q + 8 * h;
+                for (int kind = 0; kind < 2; ++kind) fb[u][h][kind] = kLast ? load_cut(b[kind], k, g.K) : *reinterpret_cast<const v4u_any*>(b[kind] + k);
 #pragma unroll
-                    for (int kind = 0; kind < 2; ++kind) fb[u][h][kind] = kLast ? load_cut(b[kind], k, g.K) : *reinterpret_cast<const v4u_any*>(b[kind] + k);
-#pragma unroll
-                    for (int m = 0; m < kTI; ++m) fa[u][h][m] = kLast ? load_cut(a[m], k, g.K) : *reinterpret_cast<const v4u_any*>(a[m] + k);
-                }
-#pragma unroll
-            for (int u = 0; u < kSome; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int m = 0; m < kTI; ++m)
-#pragma unroll
-                        for (int kind = 0; kind < 2; ++kind) acc[kind][m][0] = T::mfma(fb[u][h][kind], fa[u][h][m], acc[kind][m][0]);
+                for (int m = 0; m < kTI; ++m) fa[u][h][m] = kLast ? load_cut(a[m], k, g.K) : *reinterpret_cast<const v4u_any*>(a[m] + k);
+            }
         };
-        walk(go);
+        auto multiply = [&](auto place) {
+            constexpr int u = decltype(place)::value;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int m = 0; m < kTI; ++m)
+#pragma unroll
+                    for (int kind = 0; kind < 2; ++kind) acc[kind][m][0] = T::mfma(fb[u][h][kind], fa[u][h][m], acc[kind][m][0]);
+        };
+        auto each = [&](const auto& f) {                 // of the kDeep places
+            f(std::integral_constant<int, 0>());
+            f(std::integral_constant<int, 1>());
+            if constexpr (kDeep == 3) f(std::integral_constant<int, 2>());
+        };
+        const std::false_type inside;
+        const int64_t first = whole * split / splits + wave;
+        int64_t groups = first < until ? ((until - first + kNarrowWaves - 1) / kNarrowWaves) / kDeep : 0, s = first;
+        if (groups > 0) {
+            each([&](auto place) { load(s + place * kNarrowWaves, place, inside); });
+            for (s += kDeep * kNarrowWaves; groups > 1; --groups, s += kDeep * kNarrowWaves)
+                each([&](auto place) {
+                    multiply(place);
+                    load(s + place * kNarrowWaves, place, inside);
+                });
+            each([&](auto place) { multiply(place); });
+        }
+        const std::integral_constant<int, 0> one;
+#pragma unroll 1
+        for (; s < until; s += kNarrowWaves) {
+            load(s, one, inside);
+            multiply(one);
+        }
+        if (whole * kStep < g.K && split + 1 == splits && wave == 0) {
+            load(whole, one, std::true_type());
+            multiply(one);
+        }
     } else {
+        constexpr int kTogether = kTI == 1 ? 2 : 1;
+        auto walk = [&](auto go) {
+            int64_t s = whole * split / splits + wave;
+            if (kTogether > 1)
+                for (; s + (kTogether - 1) * kNarrowWaves < until; s += kTogether * kNarrowWaves) go(s, std::integral_constant<int, kTogether>(), std::false_type());
+#pragma unroll 1
+            for (; s < until; s += kNarrowWaves) go(s, std::integral_constant<int, 1>(), std::false_type());
+            if (whole * kStep < g.K && split + 1 == splits && wave == 0) go(whole, std::integral_constant<int, 1>(), std::true_type());
+        };
         const int64_t j = j0 + l * kV;
         const bool cut = j + kV > g.J;
         auto go = [&](int64_t s, auto some, auto last) {

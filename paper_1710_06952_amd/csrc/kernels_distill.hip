@@ -5,9 +5,9 @@
 //      = [sum_j p_j t_j / T - log Z] - sum_j p_j z[v_j] / T + m / T + log s        Z of the entries, m and s of the row: the first part needs no pass over z
 //   dL/dz = cs (q_T - sum_j p_j onehot(v_j)) + ch (q - onehot(token)),   cs = (1 - a) T / counted,  ch = a / counted
 //
-//   teacher_rows     p and the first part of KL, one wavefront a row; entries of the same token become one, and the token itself is the last
-//   distill_rows     statistics, KL and gradient with the row held in registers: the logits are read once
-//   stats, finish, gradient, entries: the same in passes, for rows that registers do not hold, and for few rows, which are split over the chip
+//   teacher_row      p and the first part of KL by one wavefront; entries of the same token become one, and the token itself is the last
+//   distill_rows     all of a row with its logits held in registers: they are read once
+//   teacher, stats, finish, gradient, entries: the same in passes, for rows that registers do not hold, and for few rows, which are split over the chip
 //
 // The gradient of all elements is stored without the entries first; behind a barrier the few that have an entry are stored again.  (The pass
 // would have to look for its own elements among the entries.)
@@ -31,9 +31,9 @@ struct Entry {
     int v;                      // of the vocabulary, or -1: nothing
     float p;
 };
-// log2 e / T in two parts, the second positive: a difference of -infinity is e^-infinity by both.
+// log2 e / T as it rounds, and in two parts, the second positive: a difference of -infinity is e^-infinity by both.
 struct Heat {
-    float hi, lo;
+    float near, hi, lo;
 };
 struct Stat2 {
     float m, s, s1;             // the largest value, sum exp((z - m) / T), sum exp(z - m)
@@ -62,7 +62,10 @@ struct DistillArgs {
 };
 
 template <bool kFine>
-__device__ __forceinline__ float warm(float d, const Heat& h) { return __builtin_amdgcn_exp2f(kFine ? fmaf(d, h.hi, d * h.lo) : d * h.hi); }
+__device__ __forceinline__ float warm(float d, const Heat& h) { return __builtin_amdgcn_exp2f(kFine ? fmaf(d, h.hi, d * h.lo) : d * h.near); }
+// In the sums of a row: 32-bit logits take the second part as well.  Beside 16 bits its 3e-8 of z / T is left out: 2e-7 of log s, which is 5 to 15.
+template <class E>
+__device__ __forceinline__ float warm_in_sum(float d, const Heat& h) { return warm<E::kN == 4>(d, h); }
 template <bool kTwo>
 __device__ __forceinline__ Stat2 joined2(Stat2 a, Stat2 b, const Heat& h) {
     const float m = fmaxf(a.m, b.m), base = base_of(m);
@@ -117,19 +120,15 @@ __host__ __device__ constexpr int teacher_places(int k) {
     while (n < 2 * (k + 1)) n *= 2;
     return n;
 }
-static_assert(64 * 1024 > 4 * (3 * 1025 + 2 * 4096), "the words of 1024 entries");
+static_assert(60 * 1024 > 4 * (3 * 1025 + 2 * 4096) + 8 * 1025, "the words of 1024 entries, and the entries, beside what a block has of its own");
 __host__ __device__ constexpr int teacher_words(int k) { return 3 * (k + 1) + 2 * teacher_places(k); }
 
-// One wavefront a row; as many in a block, up to four, as have their words in 64 KB.
+// One wavefront, a row: leaves its entries in `out` (k + 1 of them), with `words` of LDS, and gives the first part of KL: NaN where there is none, -infinity where
+// there is no entry.
 template <class E>
-__global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) {
-    extern __shared__ int words[];
+__device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row, int64_t token, int* words, Entry* out) {
     const int lane = threadIdx.x & 63, k = static_cast<int>(a.k), places = teacher_places(k);
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (row >= a.rows) return;
-    const int64_t token = a.tokens[row];
-    if (token < 0) return;                               // nothing of the row is read
-    int* token_of = words + (threadIdx.x >> 6) * teacher_words(k);
+    int* token_of = words;
     float* value = reinterpret_cast<float*>(token_of + (k + 1));
     int *place_of_entry = token_of + 2 * (k + 1), *key = token_of + 3 * (k + 1), *owner = key + places;
     for (int i = lane; i < places; i += 64) {
@@ -191,8 +190,6 @@ __global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) 
     for (int j = lane; j < k; j += 64) twice = twice || (place_of_entry[j] >= 0 && owner[place_of_entry[j]] != j);      // the token adds nothing
     twice = __any(twice);
     const double scale = 1.0 / Z;
-    const bool bad = beyond || (some && !(Z > 0.0 && Z < INFINITY));
-    Entry* out = a.entries + row * (k + 1);
     for (int j = lane; j <= k; j += 64) {
         const int at = place_of_entry[j];
         Entry e{at >= 0 && owner[at] == j ? token_of[j] : -1, 0.0f};
@@ -204,12 +201,21 @@ __global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) 
         }
         out[j] = e;
     }
-    if (lane == 0) {
-        const float near = static_cast<float>(Z);
-        const double log_Z = log_of(near) + (Z - static_cast<double>(near)) * scale;
-        // infinity tells that there is no entry; NaN is one
-        a.first[row] = bad ? static_cast<double>(NAN) : some ? with_t * scale - log_Z - with_z * scale * a.inv_T : static_cast<double>(-INFINITY);
-    }
+    if (beyond || (some && !(Z > 0.0 && Z < INFINITY))) return NAN;
+    if (!some) return -INFINITY;
+    const float near = static_cast<float>(Z);
+    return with_t * scale - (log_of(near) + (Z - static_cast<double>(near)) * scale) - with_z * scale * a.inv_T;
+}
+// For rows in passes.  One wavefront a row; as many in a block, up to four, as have their words in 64 KB.
+template <class E>
+__global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) {
+    extern __shared__ int words[];
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 6) + (threadIdx.x >> 6);
+    if (row >= a.rows) return;
+    const int64_t token = a.tokens[row];
+    if (token < 0) return;                               // nothing of the row is read
+    const double first = teacher_row<E>(a, row, token, words + (threadIdx.x >> 6) * teacher_words(static_cast<int>(a.k)), a.entries + row * (a.k + 1));
+    if ((threadIdx.x & 63) == 0) a.first[row] = first;
 }
 
 // ---- what one thread does once for a row --------------------------------------------------------------------
@@ -218,8 +224,7 @@ struct RowEnd {
     float cp, ct;               // of an entry's p, of the token
 };
 template <bool kTwo>
-__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, float at, const Stat2& st, float share, bool writes) {
-    const double first = a.first[row];
+__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2& st, float share, bool writes) {
     const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0.0f && st.s < INFINITY;
     double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of(st.s) : 0.0, logp = 0.0;
     if (!good || first != first) kl = NAN;
@@ -258,8 +263,7 @@ __device__ __forceinline__ void slopes_of(v4u x, float m, const RowEnd& e, const
 }
 // The elements that have an entry, by threads threadIdx.x, + threads, ...
 template <class E, bool kTwo>
-__device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row, int64_t token, float m, const RowEnd& e, int from, int threads) {
-    const Entry* list = a.entries + row * (a.k + 1);
+__device__ __forceinline__ void store_entries(const DistillArgs& a, const Entry* list, int64_t row, int64_t token, float m, const RowEnd& e, int from, int threads) {
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
     typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
     for (int j = from; j <= a.k; j += threads) {
@@ -269,10 +273,34 @@ __device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row,
 }
 
 // ---- rows held in registers -----------------------------------------------------------------------------------
-// kWaves wavefronts a row, up to kHeld vectors a thread; as policy_rows_kernel of the policy loss.
+// What lanes behind the end of a row read: 16 bytes of -infinity.
+__device__ const uint32_t kNone[3][4] = {{kNothing<F32>, kNothing<F32>, kNothing<F32>, kNothing<F32>},
+                                         {kNothing<Bf16>, kNothing<Bf16>, kNothing<Bf16>, kNothing<Bf16>},
+                                         {kNothing<F16>, kNothing<F16>, kNothing<F16>, kNothing<F16>}};
+template <class E>
+constexpr int kTypeOf = E::kN == 4 ? 0 : 1;
+template <>
+constexpr int kTypeOf<F16> = 2;
+
+// The gradient beside 16 bits: cs exp((z - m) / T) = 2^(z log2 e / T + c), c = log2 cs - m log2 e / T, is one FMA and one exponential.  c is rounded, which makes
+// all of a row's q too large or small by 2^-24 |c|: under 1e-5 for |m log2 e / T| < 128.  Other rows, and signs, take the long way.
+struct RowLine {
+    float c, c1;
+    bool short_way;
+};
+template <class E, bool kTwo>
+__device__ __forceinline__ RowLine line_of(const RowEnd& e, float m, const Heat& h) {
+    const float at = m * h.near, at1 = m * kLog2e;
+    const bool good = E::kN == 8 && fabsf(at) < 128.0f && (!kTwo || fabsf(at1) < 128.0f) && e.cs >= 0.0f && e.ch >= 0.0f;
+    return RowLine{__builtin_amdgcn_logf(e.cs) - at, __builtin_amdgcn_logf(e.ch) - at1, good};
+}
+
+// kWaves wavefronts a row, up to kHeld vectors a thread; as policy_rows_kernel of the policy loss.  The first wavefront does the teacher's row in front of
+// its own loads, while those of the others are on their way.
 template <class E, bool kTwo, int kWaves, int kHeld, int kPerSimd>
 __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(const DistillArgs a) {
     constexpr int kThreads = kWaves * 64;
+    extern __shared__ int words[];                       // the entries, and the teacher's words
     __shared__ Stat2 at[kWaves];
     __shared__ float counts[kWaves];
     __shared__ RowEnd of_row;
@@ -284,8 +312,11 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
     const int single = cut.single();
     RowEnd end{0.0f, 0.0f, 0.0f, 0.0f};
     float m = 0.0f, alone = -INFINITY;
+    Entry* list = reinterpret_cast<Entry*>(words);
     v4u x[kHeld];
     if (token >= 0) {                   // uniform over the block
+        double first = 0.0;
+        if (threadIdx.x < 64) first = teacher_row<E>(a, row, token, words + 2 * (a.k + 1), list);
         const float value = token < a.vocab ? E::get(z + token) : NAN;
         float share = a.rows <= kCountHere ? 0.0f : *a.share;
         if (single >= 0) alone = E::get(z + single);
@@ -294,17 +325,19 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             const int v = u * kThreads + static_cast<int>(threadIdx.x);
-            x[u] = load_vector<E, false>(z, cut.at(v < cut.vectors ? v : cut.vectors - 1));
+            const typename E::Raw* from = v < cut.vectors ? z + cut.at(v) : reinterpret_cast<const typename E::Raw*>(kNone[kTypeOf<E>]);
+            x[u] = load_vector<E, false>(from, 0);
         }
         if (a.rows <= kCountHere) share = 1.0f / fmaxf(counted_rows<kWaves>(a.tokens, a.rows, counts), 1.0f);
         __builtin_amdgcn_sched_barrier(0);
         Stat2 st{-INFINITY, 0.0f, 0.0f};
+        const float e1 = in_vector(kLog2e);              // in vector registers: an operand in a scalar one costs most of an instruction more
+        Heat h = a.heat;
+        h.near = in_vector(h.near);
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
             float f[E::kN], top = -INFINITY;
-            if ((u + 1) * kThreads > cut.vectors)        // uniform
-                x[u] = u * kThreads + static_cast<int>(threadIdx.x) < cut.vectors ? x[u] : v4u{kNothing<E>, kNothing<E>, kNothing<E>, kNothing<E>};
-            asm volatile("" : "+v"(x[u]));               // held packed, however it was come by
+            asm volatile("" : "+v"(x[u]));               // held packed
             E::unpack(x[u], f);
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[i]);
@@ -312,8 +345,8 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
             float part = 0.0f, part1 = 0.0f;
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) {
-                part += warm<true>(f[i] - base, a.heat);
-                if (kTwo) part1 += exp_in_sum<false>(f[i] - base);
+                part += warm_in_sum<E>(f[i] - base, h);
+                if (kTwo) part1 += __builtin_amdgcn_exp2f((f[i] - base) * e1);
             }
             st.s = fmaf(st.s, warm<true>(st.m - base, a.heat), part);
             if (kTwo) st.s1 = fmaf(st.s1, exp_in_sum<true>(st.m - base), part1);
@@ -323,7 +356,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
         if (single >= 0) st = joined2<kTwo>(st, of_one2(alone, a.heat), a.heat);
         st = block_joined2<kTwo, kWaves>(st, a.heat, at);
         if (threadIdx.x < 64) {
-            const RowEnd e = end_of_row<kTwo>(a, row, value, st, share, threadIdx.x == 0);
+            const RowEnd e = end_of_row<kTwo>(a, row, first, value, st, share, threadIdx.x == 0);
             if (threadIdx.x == 0) of_row = e;
         }
         __syncthreads();
@@ -336,25 +369,45 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
     }
     const bool zero = end.cs == 0.0f && end.ch == 0.0f;  // NaN is not
     if (single >= 0) E::put(dz + single, zero ? 0.0f : slope_at<E, kTwo>(alone, m, end, a.heat));
+    auto store = [&](const auto& of) {
 #pragma unroll
-    for (int u = 0; u < kHeld; ++u) {
-        const int v = u * kThreads + static_cast<int>(threadIdx.x);
-        if (v < cut.vectors) {
-            float d[E::kN];
-            if (zero) {
-#pragma unroll
-                for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
-            } else {
-                asm volatile("" : "+v"(x[u]));           // unpacked anew, not kept unpacked since the sum
-                slopes_of<E, kTwo>(x[u], m, end, a.heat, d);
+        for (int u = 0; u < kHeld; ++u) {
+            const int v = u * kThreads + static_cast<int>(threadIdx.x);
+            if (v < cut.vectors) {
+                float d[E::kN];
+                of(u, d);
+                store_vector<E>(dz, cut.at(v), d);
             }
-            store_vector<E>(dz, cut.at(v), d);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    const RowLine line = line_of<E, kTwo>(end, m, a.heat);
+    if (zero) {
+        store([&](int, float* d) {
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) d[i] = 0.0f;
+        });
+    } else if (line.short_way) {
+        const float near = in_vector(a.heat.near), e1 = in_vector(kLog2e);
+        store([&](int u, float* d) {
+            asm volatile("" : "+v"(x[u]));               // unpacked anew, not kept unpacked since the sum
+            E::unpack(x[u], d);
+#pragma unroll
+            for (int i = 0; i < E::kN; ++i) {
+                const float z = d[i];
+                d[i] = __builtin_amdgcn_exp2f(fmaf(z, near, line.c));
+                if (kTwo) d[i] += __builtin_amdgcn_exp2f(fmaf(z, e1, line.c1));
+            }
+        });
+    } else {
+        store([&](int u, float* d) {
+            asm volatile("" : "+v"(x[u]));
+            slopes_of<E, kTwo>(x[u], m, end, a.heat, d);
+        });
     }
     if (token < 0) return;
     __syncthreads();
-    store_entries<E, kTwo>(a, row, token, m, end, static_cast<int>(threadIdx.x), kThreads);
+    store_entries<E, kTwo>(a, list, row, token, m, end, static_cast<int>(threadIdx.x), kThreads);
 }
 
 // ---- in passes ------------------------------------------------------------------------------------------------
@@ -391,7 +444,7 @@ __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a) 
             part[u] = part1[u] = 0.0f;
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) {
-                part[u] += warm<true>(f[u][i] - base, a.heat);
+                part[u] += warm_in_sum<E>(f[u][i] - base, a.heat);
                 if (kTwo) part1[u] += exp_in_sum<true>(f[u][i] - base);
             }
         }
@@ -427,7 +480,7 @@ __global__ __launch_bounds__(kT) void distill_finish_kernel(const DistillArgs a)
     for (int q = lane; q < a.splits; q += 64) st = joined2<kTwo>(st, a.parts[row * a.splits + q], a.heat);
     st = lanes_joined2<kTwo, 64>(st, a.heat);
     const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
-    const RowEnd e = end_of_row<kTwo>(a, row, at, st, share, lane == 0);
+    const RowEnd e = end_of_row<kTwo>(a, row, a.first[row], at, st, share, lane == 0);
     if (lane == 0) {
         a.stat[row] = Stat2{st.m, e.cp, e.ct};
         a.coef[row] = make_float2(e.cs, e.ch);
@@ -482,7 +535,7 @@ __global__ __launch_bounds__(kT) void distill_entries_kernel(const DistillArgs a
     if (token < 0) return;
     float m;
     const RowEnd e = kept_end(a, row, m);
-    store_entries<E, kTwo>(a, row, token, m, e, threadIdx.x & 63, 64);
+    store_entries<E, kTwo>(a, a.entries + row * (a.k + 1), row, token, m, e, threadIdx.x & 63, 64);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------
@@ -522,25 +575,25 @@ void launch_rows(DistillArgs a, hipStream_t s) {
     const int64_t rows = a.rows, vectors = a.vocab / E::kN;
     const dim3 grid(static_cast<uint32_t>(rows)), waves(static_cast<uint32_t>((rows + kT / 64 - 1) / (kT / 64)));
     const bool apart = vectors < 2 || vectors > 16384 || (rows <= 32 && vectors >= 2048);
+    const int bytes = teacher_words(static_cast<int>(a.k)) * static_cast<int>(sizeof(int)), held = bytes + static_cast<int>((a.k + 1) * sizeof(Entry));
     if (apart) {                         // perhaps none behind the first 16-byte address, or more than a block's registers hold, or few rows
+        int together = 4;
+        while (together > 1 && together * bytes > 64 * 1024) together /= 2;
+        hipLaunchKernelGGL(teacher_rows_kernel<E>, dim3(static_cast<uint32_t>((rows + together - 1) / together)), dim3(together * 64), together * bytes, s, a);
         a.splits = split_of(rows, vectors);
         a.blocks = std::max<int64_t>(1, (vectors + kT * kUnroll - 1) / (kT * kUnroll));
         hipLaunchKernelGGL((distill_stats_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.splits)), dim3(kT), 0, s, a);
         hipLaunchKernelGGL((distill_finish_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
         hipLaunchKernelGGL((distill_gradient_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.blocks)), dim3(kT), 0, s, a);
         hipLaunchKernelGGL((distill_entries_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
-    } else if (vectors <= 256) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 1, 4, 4>), grid, dim3(64), 0, s, a);
-    else if (vectors <= 1024) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 4, 4, 8>), grid, dim3(256), 0, s, a);
-    else if (vectors <= 4096) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 8, 8, 8>), grid, dim3(512), 0, s, a);
-    else if (vectors <= 8192) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 8, 8>), grid, dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 16, 4>), grid, dim3(1024), 0, s, a);
+    } else if (vectors <= 256) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 1, 4, 4>), grid, dim3(64), held, s, a);
+    else if (vectors <= 1024) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 4, 4, 8>), grid, dim3(256), held, s, a);
+    else if (vectors <= 4096) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 8, 8, 8>), grid, dim3(512), held, s, a);
+    else if (vectors <= 8192) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 8, 8>), grid, dim3(1024), held, s, a);
+    else hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 16, 4>), grid, dim3(1024), held, s, a);
 }
 template <class E>
 void launch_of(const DistillArgs& a, hipStream_t s) {
-    const int bytes = teacher_words(static_cast<int>(a.k)) * static_cast<int>(sizeof(int));
-    int waves = 4;
-    while (waves > 1 && waves * bytes > 64 * 1024) waves /= 2;
-    hipLaunchKernelGGL(teacher_rows_kernel<E>, dim3(static_cast<uint32_t>((a.rows + waves - 1) / waves)), dim3(waves * 64), waves * bytes, s, a);
     if (a.hard > 0.0 && a.T != 1.0) launch_rows<E, true>(a, s);
     else launch_rows<E, false>(a, s);
 }
@@ -559,7 +612,7 @@ hipError_t launch_distill(const LossRows& r, const TeacherRows& t, double temper
     a.cs = static_cast<float>((1.0 - hard_weight) * temperature * loss_scale);
     a.ch = static_cast<float>(hard_weight * loss_scale);
     const double heat = 1.4426950408889634 / temperature;
-    a.heat.hi = static_cast<float>(heat);
+    a.heat.near = a.heat.hi = static_cast<float>(heat);
     if (static_cast<double>(a.heat.hi) >= heat) a.heat.hi = std::nextafterf(a.heat.hi, 0.0f);
     a.heat.lo = static_cast<float>(heat - static_cast<double>(a.heat.hi));
     a.share = w.share;
