@@ -44,12 +44,13 @@ bool dense_sizes(int64_t M, int64_t N, int64_t K) {
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
 struct BackwardSpace {
-    int64_t dz, sums, partial, bytes;       // where they begin
+    int64_t dz, low, sums, partial, bytes;  // where they begin
 };
-BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes) {
+BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes, bool with_low = false) {
     BackwardSpace b{};
     b.dz = 0;
-    b.sums = up256(2 * M * N);
+    b.low = up256(2 * M * N);
+    b.sums = b.low + (with_low ? up256(2 * M * N) : 0);
     b.partial = b.sums + up256(sums_bytes);
     b.bytes = b.partial + up256(std::max(dense_partial_bytes(M, K, N), dense_partial_bytes(N, K, M)));
     return b;
@@ -69,6 +70,9 @@ const char* dense_fault(const adpsgd_dense_t* o) {
 }
 
 // ---- gated projections ----
+BackwardSpace gated_space(int64_t M, int64_t N, int64_t K) {
+    return backward_space(M, 2 * N, K, gated_sums_bytes(M, N), gated_low(M * K) || gated_low(2 * N * K));
+}
 const char* gated_fault(const adpsgd_dense_t* o) {
     if (!o) return "gated: no arguments";
     if (o->type != ADPSGD_TYPE_BF16 && o->type != ADPSGD_TYPE_F16) return "gated: type must be BF16 or F16";
@@ -81,8 +85,9 @@ const char* gated_fault(const adpsgd_dense_t* o) {
     if (!aligned_to(o->x, 2) || !aligned_to(o->w, 2) || !aligned_to(o->b, 2)) return "gated: a tensor is not aligned to its type";
     return nullptr;
 }
-// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.
-hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, void* dx, void* dw, void* partial, int64_t partial_bytes, hipStream_t s) {
+// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.  low_dx, low_dw: what dz's rounding has left, for the one and the other, or nullptr.
+hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, const void* low_dx, const void* low_dw, void* dx, void* dw, void* partial,
+                             int64_t partial_bytes, hipStream_t s) {
     DenseGemm g{};
     g.act = ADPSGD_ACT_NONE;
     g.partial = static_cast<float*>(partial);
@@ -91,11 +96,13 @@ hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz,
         g.a = dz; g.lda = lddz; g.a_outer = false;
         g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed == 0;
         g.I = o->M; g.J = o->K; g.K = N;
+        g.a_low = low_dx;
         g.out = dx;
         hipError_t e = launch_dense_gemm(o->type, g, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
+        g.a_low = nullptr;
         g.a_outer = g.b_outer = true;
         g.K = o->M;
         g.out = dw;
@@ -106,6 +113,7 @@ hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz,
             g.a = dz; g.lda = lddz; g.I = N;
             g.b = o->x; g.ldb = o->ldx; g.J = o->K;
         }
+        (o->w_transposed ? g.b_low : g.a_low) = low_dw;
         return launch_dense_gemm(o->type, g, s);
     }
     return hipSuccess;
@@ -195,13 +203,13 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
             hipError_t e = launch_dense_dz(o->type, dy, lddy, of, own ? ws + at.dz : nullptr, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
             if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
         }
-        return ended(backward_products(o, o->N, dz, lddz, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
+        return ended(backward_products(o, o->N, dz, lddz, nullptr, nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
     });
 }
 
 extern "C" int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t backward) {
     if (N < 1 || N >= kMostSide || !dense_sizes(M, 2 * N, K)) return -1;
-    return backward ? backward_space(M, 2 * N, K, gated_sums_bytes(M, N)).bytes : up256(gated_partial_bytes(M, N, K));
+    return backward ? gated_space(M, N, K).bytes : up256(gated_partial_bytes(M, N, K));
 }
 
 extern "C" int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N) {
@@ -234,14 +242,17 @@ extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, in
         if (o->M > 0 && (!dh || !slopes)) return refuse("gated: dh or slopes is NULL");
         if (lddh < o->N || lddh > kMostStride) return refuse("gated: the leading dimension of dh is not N .. 2^22");
         if (!aligned_to(dh, 2) || !aligned_to(slopes, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(db, 2)) return refuse("gated: a tensor is not aligned to its type");
-        const BackwardSpace at = backward_space(o->M, 2 * o->N, o->K, gated_sums_bytes(o->M, o->N));
+        const BackwardSpace at = gated_space(o->M, o->N, o->K);
         if (o->workspace_bytes < at.bytes || (at.bytes > 0 && (!o->workspace || !aligned16(o->workspace)))) return refuse("gated: workspace missing, not 16-byte aligned or too small");
         if (!dx && !dw && !db) return ADPSGD_OK;
         hipStream_t s = static_cast<hipStream_t>(stream);
         char* ws = static_cast<char*>(o->workspace);
         void* dz = dx || dw ? ws + at.dz : nullptr;
-        hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
-        if (e == hipSuccess) e = backward_products(o, 2 * o->N, dz, 2 * o->N, dx, dw, ws + at.partial, at.bytes - at.partial, s);
+        const bool low_dx = dx && gated_low(o->M * o->K), low_dw = dw && gated_low(2 * o->N * o->K);
+        void* low = low_dx || low_dw ? ws + at.low : nullptr;
+        hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, low, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
+        if (e == hipSuccess)
+            e = backward_products(o, 2 * o->N, dz, 2 * o->N, low_dx ? low : nullptr, low_dw ? low : nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s);
         return ended(e, "gated backward");
     });
 }

@@ -158,6 +158,8 @@ template <class T>
 hipError_t launch_dense_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 
 template <class T>
+hipError_t launch_low_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
+template <class T>
 hipError_t launch_gated_tiles(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 
 }  // namespace adpsgd_impl

@@ -354,22 +354,27 @@ __device__ __forceinline__ void place_of(int64_t b, int64_t blocks, int64_t tile
     ti = in / size;
 }
 
-// kSide x kSide tiles, kWI x kWJ wavefronts.  kGated: of kSide / 2 results and their partners.
-template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false>
+// kSide x kSide tiles, kWI x kWJ wavefronts.  kGated: of kSide / 2 results and their partners.  kLow: A (1) or B (2) is in two
+// parts, whose products are added.
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false, int kLow = 0>
 __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseGemm g, const int splits) {
     constexpr int kThreads = kWI * kWJ * 64, kTI = kSide / kWI / 16, kTJ = kSide / kWJ / 16;
     typedef Operand<kAOuter, kSide, kThreads, 0> OpA;
     typedef Operand<kBOuter, kSide, kThreads, 4 * kTJ, kGated> OpB;
     constexpr int kSideJ = kGated ? kSide / 2 : kSide;
-    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B]
-    constexpr int kHalf = kSide * kBK;                                   // elements of one operand's step
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // [2][A | B | the low part]
+    constexpr int kHalf = kSide * kBK, kAll = (kLow ? 3 : 2) * kHalf;    // elements of one operand's step, of all operands'
+
     const int64_t tiles_i = (g.I + kSide - 1) / kSide, tiles_j = (g.J + kSideJ - 1) / kSideJ;
     int64_t ti, tj, split;
     place_of(blockIdx.x, gridDim.x, tiles_i, tiles_j, ti, tj, split);
     const int64_t steps = (g.K + kBK - 1) / kBK, s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
     OpA a;
     OpB b;
+    typename std::conditional<kLow == 2, OpB, OpA>::type low;
     a.start(g.a, g.lda, ti * kSide, g.I, g.K);
+    if (kLow == 1) low.start(g.a_low, g.lda, ti * kSide, g.I, g.K);
+    if (kLow == 2) low.start(g.b_low, g.ldb, tj * kSideJ, g.J, g.K);
     b.start(g.b, g.ldb, tj * kSideJ, g.J, g.K, g.b_up);
     const int wave = threadIdx.x >> 6, wi = wave / kWJ * (kTI * 16), wj = wave % kWJ * (kTJ * 16);
     v4f acc[kTI][kTJ];
@@ -383,19 +388,25 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
         if (last) {
             a.load(step, true);
             b.load(step, true);
+            if (kLow) low.load(step, true);
         } else {
             a.load(step, false);
             b.load(step, false);
+            if (kLow) low.load(step, false);
         }
+    };
+    auto put = [&](uint16_t* to) {
+        a.store(to);
+        b.store(to + kHalf);
+        if (kLow) low.store(to + 2 * kHalf);
     };
     if (s0 < s1) {
         fetch(s0);
-        a.store(lds);
-        b.store(lds + kHalf);
+        put(lds);
         __syncthreads();
     }
     for (int64_t step = s0; step < s1; ++step) {
-        const uint16_t* now = lds + ((step - s0) & 1) * (2 * kHalf);
+        const uint16_t* now = lds + ((step - s0) & 1) * kAll;
         if (step + 1 < s1) fetch(step + 1);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -408,12 +419,21 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
             for (int m = 0; m < kTI; ++m)
 #pragma unroll
                 for (int n = 0; n < kTJ; ++n) acc[m][n] = T::mfma(fb[n], fa[m], acc[m][n]);
+            if constexpr (kLow != 0) {
+                if constexpr (kLow == 1) {
+#pragma unroll
+                    for (int m = 0; m < kTI; ++m) fa[m] = OpA::fragment(now + 2 * kHalf, wi, m, h);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < kTJ; ++n) fb[n] = OpB::fragment(now + 2 * kHalf, wj, n, h);
+                }
+#pragma unroll
+                for (int m = 0; m < kTI; ++m)
+#pragma unroll
+                    for (int n = 0; n < kTJ; ++n) acc[m][n] = T::mfma(fb[n], fa[m], acc[m][n]);
+            }
         }
-        if (step + 1 < s1) {
-            uint16_t* next = lds + ((step + 1 - s0) & 1) * (2 * kHalf);
-            a.store(next);
-            b.store(next + kHalf);
-        }
+        if (step + 1 < s1) put(lds + ((step + 1 - s0) & 1) * kAll);
         __syncthreads();
     }
 
@@ -496,12 +516,12 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const DenseGemm g, cons
     end.finish(i, f[0], f[1]);
 }
 
-template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false>
+template <class T, bool kAOuter, bool kBOuter, int kSide, int kWI, int kWJ, bool kGated = false, int kLow = 0>
 hipError_t launch_tile(const DenseGemm& g, int splits, hipStream_t s) {
     constexpr int kSideJ = kGated ? kSide / 2 : kSide;
     const int64_t tiles = (g.I + kSide - 1) / kSide * ((g.J + kSideJ - 1) / kSideJ);
-    constexpr int kBytes = 4 * kSide * kBK * 2;
-    auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ, kGated>;
+    constexpr int kBytes = (kLow ? 6 : 4) * kSide * kBK * 2;
+    auto kernel = dense_tile_kernel<T, kAOuter, kBOuter, kSide, kWI, kWJ, kGated, kLow>;
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
     if (e != hipSuccess) return e;

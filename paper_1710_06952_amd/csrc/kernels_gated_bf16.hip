@@ -3,6 +3,7 @@
 
 namespace adpsgd_impl {
 
+template hipError_t launch_low_tiles<Bf16>(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 template hipError_t launch_gated_tiles<Bf16>(const DenseGemm& g, const DensePlan& p, hipStream_t s);
 
 }  // namespace adpsgd_impl

@@ -4,7 +4,8 @@ Tolerances, for products of `n` terms whose magnitudes sum to S: n + 8 roundings
 half a step of it.  Activations and slopes are within 5e-6 (the tail of gelu is fitted to 2.6e-6, the reciprocal and exponential of
 the instruction set add a few 2^-23); |act'| <= 1.13, |act''| <= 1.2.  A slope is kept beside fp16 in 24 bits
 of fp32, 2^-16 of itself; beside bf16 in 16 bits, as its root in fp16, twice half a step of that, 2^-10 (and 1e-14 where the root is subnormal: (2^-25 + sqrt s)^2 - s for
-s < 2^-28)."""
+s < 2^-28).  dz is rounded to the type for the two products, and kept in two parts, 2^-16 (bf16) or 2^-21 (fp16: its rest has 2^-25 at least) of
+itself, for results of up to 8192 elements."""
 import math
 
 import pytest
@@ -83,10 +84,12 @@ def reference(x, w, b, dh, act):
     dz = d2 * slope
     dzerr = d2.abs() * kept + 2 * u * dz.abs()
     rounded = dzerr + 1.01 * h * (dz.abs() + dzerr) + (2.0 ** -25 if f16 else 0.0)
+    twice = dzerr + 1.01 * h * h * (dz.abs() + dzerr) + (2.0 ** -25 if f16 else 0.0)
+    of_dx, of_dw = (twice if size <= 8192 else rounded for size in (M * K, 2 * N * K))
     mm = lambda p, q: torch.mm(p, q.contiguous())  # noqa: E731
     dx, dw, db = mm(dz, w), mm(dz.t().contiguous(), x), dz.sum(0)
-    out["dx"] = (dx, 1.01 * h * dx.abs() + 1.01 * (mm(rounded, w.abs()) + (2 * N + 8) * u * mm(dz.abs(), w.abs())) + tiny)
-    out["dw"] = (dw, 1.01 * h * dw.abs() + 1.01 * (mm(rounded.t().contiguous(), x.abs()) + (M + 8) * u * mm(dz.abs().t().contiguous(), x.abs())) + tiny)
+    out["dx"] = (dx, 1.01 * h * dx.abs() + 1.01 * (mm(of_dx, w.abs()) + (4 * N + 8) * u * mm(dz.abs(), w.abs())) + tiny)
+    out["dw"] = (dw, 1.01 * h * dw.abs() + 1.01 * (mm(of_dw.t().contiguous(), x.abs()) + (2 * M + 8) * u * mm(dz.abs().t().contiguous(), x.abs())) + tiny)
     out["db"] = (db, 1.01 * h * db.abs() + 1.01 * (dzerr.sum(0) + 16 * u * dz.abs().sum(0)) + tiny)
     return out
 
