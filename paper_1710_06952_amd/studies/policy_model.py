@@ -1,5 +1,6 @@
 """A small language policy trained by AD-PSGD workers with the library's operators of a training step: dense layers
-with their epilogues, a policy or preference loss over the vocabulary, and AdamW with 8-bit moments.
+with their epilogues or a normalised gated block, a policy, preference or distillation loss over the vocabulary, and AdamW with
+8-bit moments.
 
 Every worker has prompts of its own, each with one right answer token.  For an event the library hands the gradient
 function the worker's stale row and the slot that receives a gradient (model "external", adpsgd_run_events_with).  The
@@ -7,15 +8,21 @@ function rounds the row to bfloat16 weights, runs
 
     h = dense(e, W1, b1, residual=e, activation="gelu"),   logits = dense(h, W2, b2)
 
-on a minibatch of prompts, takes the loss with its gradient for the logits, lets autograd run the dense layers'
+or, with --block gated,
+
+    h = dense(gated(layer_norm(e, s, t), Wg, activation="silu"), Wd, residual=e),   logits = dense(h, W2, b2)
+
+on a minibatch of prompts, takes the loss with its gradient for the logits, lets autograd run the layers'
 backward pass, and hands the event the worker's AdamW direction (clipped by the global norm) in the place of a gradient:
 the event averages with a neighbour and steps along it.  Moments are the worker's own, as momentum buffers are.
 
   --loss policy       answers are sampled; reward 1 for the right one, less the batch's mean, and a KL term to the
                       initial model, whose log-probabilities come from token_log_probs
   --loss preference   pairs of answers of one token: the right one is chosen, a random one rejected
+  --loss distill      the stored eight largest logits of a teacher that prefers the right answer, at temperature 2, with a
+                      little of the right answer itself
 
-    python -m paper_1710_06952_amd.studies.policy_model [--loss policy] [--n 4] [--events 400] [--json]
+    python -m paper_1710_06952_amd.studies.policy_model [--loss policy] [--block dense] [--n 4] [--events 400] [--json]
 """
 from __future__ import annotations
 
@@ -28,12 +35,16 @@ from .convergence import ring
 
 
 class Policy:
-    """The network at a flat parameter vector [W1 | b1 | W2 | b2], W1 width x width, W2 vocab x width."""
+    """The network at a flat parameter vector [W1 | b1 | W2 | b2], W1 width x width, W2 vocab x width; with block "gated"
+    [s | t | Wg | Wd | W2 | b2], s and t the normalisation's, Wg 4 width x width, Wd width x 2 width."""
 
-    def __init__(self, vocab, width, prompts, seed, device):
+    def __init__(self, vocab, width, prompts, seed, device, block="dense"):
         import torch
-        self.vocab, self.width = vocab, width
-        self.shapes = [(width, width), (width,), (vocab, width), (vocab,)]
+        if block not in ("dense", "gated"):
+            raise ValueError("block must be dense or gated")
+        self.vocab, self.width, self.block = vocab, width, block
+        first = [(width, width), (width,)] if block == "dense" else [(width,), (width,), (4 * width, width), (width, 2 * width)]
+        self.shapes = first + [(vocab, width), (vocab,)]
         self.sizes = [int(np.prod(s)) for s in self.shapes]
         self.d = sum(self.sizes)
         rng = np.random.default_rng(seed)
@@ -41,7 +52,9 @@ class Policy:
 
     def initial(self, seed):
         rng = np.random.default_rng(seed + 1)
-        parts = [rng.standard_normal(s) / np.sqrt(self.width) if len(s) == 2 else np.zeros(s) for s in self.shapes]
+        parts = [rng.standard_normal(s) / np.sqrt(s[1]) if len(s) == 2 else np.zeros(s) for s in self.shapes]
+        if self.block == "gated":
+            parts[0] = np.ones(self.shapes[0])
         return np.concatenate([p.reshape(-1) for p in parts]).astype(np.float32)
 
     def views(self, flat):
@@ -53,9 +66,13 @@ class Policy:
 
     def logits(self, weights, prompts):
         import paper_1710_06952_amd as P
-        w1, b1, w2, b2 = weights
         e = self.embeddings[prompts]
-        h = P.dense(e, w1, b1, residual=e, activation="gelu")
+        if self.block == "gated":
+            scale, shift, wg, wd, w2, b2 = weights
+            h = P.dense(P.gated(P.layer_norm(e, scale, shift), wg, activation="silu"), wd, residual=e)
+        else:
+            w1, b1, w2, b2 = weights
+            h = P.dense(e, w1, b1, residual=e, activation="gelu")
         return P.dense(h, w2, b2)
 
 
@@ -82,11 +99,11 @@ class Worker:
 
 
 def run_study(loss="policy", n=4, vocab=512, width=128, prompts_each=64, M=128, events=400, T_max=2, gamma=2e-3, weight_decay=0.01, kl=0.01, seed=0,
-              device="cuda:0"):
+              device="cuda:0", block="dense"):
     import torch
     import paper_1710_06952_amd as P
     prompts = n * prompts_each
-    policy = Policy(vocab, width, prompts, seed, device)
+    policy = Policy(vocab, width, prompts, seed, device, block)
     right = torch.from_numpy(np.random.default_rng(seed + 2).integers(0, vocab, prompts)).to(device)
     eng = P.Engine(ring(n), policy.d, "external", gamma=gamma, T_max=T_max, device=device)
     x0 = policy.initial(seed)
@@ -94,6 +111,10 @@ def run_study(loss="policy", n=4, vocab=512, width=128, prompts_each=64, M=128, 
     frozen = policy.views(torch.from_numpy(x0).to(device).bfloat16())
     workers = [Worker(policy, device, weight_decay, seed + 10 + i) for i in range(n)]
     offsets = torch.arange(2 * M + 1, device=device)      # answers of one token
+    if loss == "distill":
+        told = torch.from_numpy(np.random.default_rng(seed + 3).standard_normal((prompts, vocab)).astype(np.float32)).to(device)
+        told[torch.arange(prompts, device=device), right] += 8.0
+        teacher = torch.topk(told, min(8, vocab), 1)
     losses = torch.zeros(events, device=device)
 
     def gradient(worker, event, xhat, out):
@@ -109,6 +130,9 @@ def run_study(loss="policy", n=4, vocab=512, width=128, prompts_each=64, M=128, 
             reward = (answers == right[asked]).float()
             old, ref = P.token_log_probs(logits, answers), P.token_log_probs(policy.logits(frozen, asked), answers)
             r = P.policy_loss_and_gradient(logits, answers, old, reward - reward.mean(), ref, clip=(0.2, 0.2), kl_coef=kl)
+        elif loss == "distill":
+            logits = policy.logits(weights, asked)
+            r = P.distillation_loss_and_gradient(logits, right[asked], teacher.indices[asked], teacher.values[asked], temperature=2.0, hard_weight=0.1)
         else:
             twice = torch.cat([asked, asked])
             logits = policy.logits(weights, twice)
@@ -129,7 +153,7 @@ def run_study(loss="policy", n=4, vocab=512, width=128, prompts_each=64, M=128, 
     sched = P.adpsgd_make_schedule(ring(n), events, seed=seed, T_max=T_max)
     eng.run_events_in_pieces(sched, max(1, events // 4), gradient_fn=gradient, between=lambda _events: curve.append(chance()))
     per = max(1, events // 4)
-    res = {"loss": loss, "n": n, "d": policy.d, "vocab": vocab, "events": eng.get_stats()["events"], "gamma": gamma, "chance": curve,
+    res = {"loss": loss, "block": block, "n": n, "d": policy.d, "vocab": vocab, "events": eng.get_stats()["events"], "gamma": gamma, "chance": curve,
            "losses": [float(losses[a:a + per].mean()) for a in range(0, events, per)], "consensus_distance": eng.consensus_distance(),
            "steps": [w.optimizer.steps for w in workers]}
     eng.close()
@@ -146,14 +170,15 @@ def format_table(res):
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
-    ap.add_argument("--loss", choices=("policy", "preference"), default="policy")
+    ap.add_argument("--loss", choices=("policy", "preference", "distill"), default="policy")
+    ap.add_argument("--block", choices=("dense", "gated"), default="dense")
     ap.add_argument("--n", type=int, default=4)
     ap.add_argument("--events", type=int, default=400)
     ap.add_argument("--gamma", type=float, default=2e-3)
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--json", action="store_true")
     a = ap.parse_args(argv)
-    res = run_study(a.loss, a.n, events=a.events, gamma=a.gamma, seed=a.seed)
+    res = run_study(a.loss, a.n, events=a.events, gamma=a.gamma, seed=a.seed, block=a.block)
     print(json.dumps(res) if a.json else format_table(res))
 
 
