@@ -7,7 +7,7 @@
 //
 //   teacher_row      p and the first part of KL by one wavefront; entries of the same token become one, and the token itself is the last
 //   distill_rows     all of a row with its logits held in registers: they are read once
-//   teacher, stats, finish, gradient, entries: the same in passes, for rows that registers do not hold, and for few rows, which are split over the chip
+//   stats, gradient  the same in two passes, for rows that registers do not hold, and for few rows, which are split over the chip
 //
 // The gradient of all elements is stored without the entries first; behind a barrier the few that have an entry are stored again.  (The pass
 // would have to look for its own elements among the entries.)
@@ -53,9 +53,9 @@ struct DistillArgs {
     Entry* entries;             // [row][k + 1]
     double* first;              // of KL: its first part
     double* term;
-    Stat2 *stat, *parts;        // in passes: of rows, of parts of rows
-    float2* coef;               // in passes: cs / s, ch / s1 of a row
-    int splits;
+    Stat2* parts;               // in passes: of parts of rows
+    int splits, together;       // ... of a row; teacher's rows of a block
+    float* loss;
     int64_t blocks;             // of a row, in the gradient's pass
     void* dz;
     float *kl, *logp;           // logp may be nullptr
@@ -206,25 +206,19 @@ __device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row,
     const float near = static_cast<float>(Z);
     return with_t * scale - (log_of(near) + (Z - static_cast<double>(near)) * scale) - with_z * scale * a.inv_T;
 }
-// For rows in passes.  One wavefront a row; as many in a block, up to four, as have their words in 64 KB.
-template <class E>
-__global__ __launch_bounds__(256) void teacher_rows_kernel(const DistillArgs a) {
-    extern __shared__ int words[];
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    if (row >= a.rows) return;
-    const int64_t token = a.tokens[row];
-    if (token < 0) return;                               // nothing of the row is read
-    const double first = teacher_row<E>(a, row, token, words + (threadIdx.x >> 6) * teacher_words(static_cast<int>(a.k)), a.entries + row * (a.k + 1));
-    if ((threadIdx.x & 63) == 0) a.first[row] = first;
-}
 
 // ---- what one thread does once for a row --------------------------------------------------------------------
 struct RowEnd {
     float cs, ch;               // of exp((z - m) / T) and exp(z - m): cs / s, ch / s1
     float cp, ct;               // of an entry's p, of the token
 };
+__device__ __forceinline__ void empty_row(const DistillArgs& a, int64_t row) {
+    a.kl[row] = 0.0f;
+    if (a.logp) a.logp[row] = 0.0f;
+    a.term[row] = 0.0;
+}
 template <bool kTwo>
-__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2& st, float share, bool writes) {
+__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2& st, float share, bool writes, double& term) {
     const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0.0f && st.s < INFINITY;
     double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of(st.s) : 0.0, logp = 0.0;
     if (!good || first != first) kl = NAN;
@@ -235,10 +229,11 @@ __device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, 
     } else if (at != at) {
         kl = NAN;                                        // the token is beyond the vocabulary
     }
+    term = a.soft * a.T * a.T * kl - (a.hard > 0.0 ? a.hard * logp : 0.0);
     if (writes) {
         a.kl[row] = static_cast<float>(kl);
         if (a.logp) a.logp[row] = static_cast<float>(logp);
-        a.term[row] = a.soft * a.T * a.T * kl - (a.hard > 0.0 ? a.hard * logp : 0.0);
+        a.term[row] = term;
     }
     RowEnd e;
     e.cp = there ? a.cs * share : 0.0f;
@@ -261,15 +256,11 @@ __device__ __forceinline__ void slopes_of(v4u x, float m, const RowEnd& e, const
 #pragma unroll
     for (int i = 0; i < E::kN; ++i) d[i] = slope_at<E, kTwo>(d[i], m, e, h);
 }
-// The elements that have an entry, by threads threadIdx.x, + threads, ...
+// An element that has an entry.
 template <class E, bool kTwo>
-__device__ __forceinline__ void store_entries(const DistillArgs& a, const Entry* list, int64_t row, int64_t token, float m, const RowEnd& e, int from, int threads) {
-    const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
-    typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
-    for (int j = from; j <= a.k; j += threads) {
-        const Entry n = list[j];
-        if (n.v >= 0) E::put(dz + n.v, slope_at<E, kTwo>(E::get(z + n.v), m, e, a.heat) - e.cp * n.p - (n.v == token ? e.ct : 0.0f));
-    }
+__device__ __forceinline__ void store_entry(const DistillArgs& a, const Entry& n, int64_t row, int64_t token, float m, const RowEnd& e) {
+    const float z = E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + n.v);
+    E::put(static_cast<typename E::Raw*>(a.dz) + row * a.vocab + n.v, slope_at<E, kTwo>(z, m, e, a.heat) - e.cp * n.p - (n.v == token ? e.ct : 0.0f));
 }
 
 // ---- rows held in registers -----------------------------------------------------------------------------------
@@ -356,16 +347,15 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
         if (single >= 0) st = joined2<kTwo>(st, of_one2(alone, a.heat), a.heat);
         st = block_joined2<kTwo, kWaves>(st, a.heat, at);
         if (threadIdx.x < 64) {
-            const RowEnd e = end_of_row<kTwo>(a, row, first, value, st, share, threadIdx.x == 0);
+            double term;
+            const RowEnd e = end_of_row<kTwo>(a, row, first, value, st, share, threadIdx.x == 0, term);
             if (threadIdx.x == 0) of_row = e;
         }
         __syncthreads();
         end = of_row;
         m = st.m;
     } else if (threadIdx.x == 0) {
-        a.kl[row] = 0.0f;
-        if (a.logp) a.logp[row] = 0.0f;
-        a.term[row] = 0.0;
+        empty_row(a, row);
     }
     const bool zero = end.cs == 0.0f && end.ch == 0.0f;  // NaN is not
     if (single >= 0) E::put(dz + single, zero ? 0.0f : slope_at<E, kTwo>(alone, m, end, a.heat));
@@ -407,16 +397,28 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
     }
     if (token < 0) return;
     __syncthreads();
-    store_entries<E, kTwo>(a, list, row, token, m, end, static_cast<int>(threadIdx.x), kThreads);
+    for (int j = threadIdx.x; j <= a.k; j += kThreads)
+        if (list[j].v >= 0) store_entry<E, kTwo>(a, list[j], row, token, m, end);
 }
 
 // ---- in passes ------------------------------------------------------------------------------------------------
-// grid: rows * splits.
+// grid: the teacher's rows, one wavefront each, a.together in a block; then rows * splits.
 template <class E, bool kTwo>
-__global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a, const int64_t teachers) {
+    extern __shared__ int words[];
     __shared__ Stat2 at[kT / 64];
-    const int64_t row = blockIdx.x / a.splits;
-    const int part = blockIdx.x % a.splits;
+    if (blockIdx.x < teachers) {
+        const int wave = threadIdx.x >> 6;
+        const int64_t row = static_cast<int64_t>(blockIdx.x) * a.together + wave;
+        if (wave >= a.together || row >= a.rows) return;
+        const int64_t token = a.tokens[row];
+        if (token < 0) return;                           // nothing of the row is read
+        const double first = teacher_row<E>(a, row, token, words + wave * teacher_words(static_cast<int>(a.k)), a.entries + row * (a.k + 1));
+        if ((threadIdx.x & 63) == 0) a.first[row] = first;
+        return;
+    }
+    const int64_t id = blockIdx.x - teachers, row = id / a.splits;
+    const int part = static_cast<int>(id % a.splits);
     if (a.tokens[row] < 0) return;
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
     const Cut<E> cut(static_cast<const typename E::Raw*>(a.dz) + row * a.vocab, static_cast<int>(a.vocab));    // as the gradient's pass
@@ -459,52 +461,54 @@ __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a) 
     if (threadIdx.x == 0) a.parts[row * a.splits + part] = st;
 }
 
-// The parts of a row joined and what there is one of: one wavefront a row.
+// A row's parts joined, by every wavefront for itself, and what follows from them.
 template <class E, bool kTwo>
-__global__ __launch_bounds__(kT) void distill_finish_kernel(const DistillArgs a) {
-    __shared__ float counts[kT / 64];
-    const float share = a.rows <= kCountHere ? 1.0f / fmaxf(counted_rows<kT / 64>(a.tokens, a.rows, counts), 1.0f) : *a.share;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kT / 64) + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= a.rows) return;
-    const int64_t token = a.tokens[row];
-    if (token < 0) {
-        if (lane == 0) {
-            a.kl[row] = 0.0f;
-            if (a.logp) a.logp[row] = 0.0f;
-            a.term[row] = 0.0;
-        }
-        return;
-    }
+__device__ __forceinline__ RowEnd joined_row(const DistillArgs& a, int64_t row, int64_t token, float share, bool writes, float& m, double& term) {
     Stat2 st{-INFINITY, 0.0f, 0.0f};
-    for (int q = lane; q < a.splits; q += 64) st = joined2<kTwo>(st, a.parts[row * a.splits + q], a.heat);
+    for (int q = threadIdx.x & 63; q < a.splits; q += 64) st = joined2<kTwo>(st, a.parts[row * a.splits + q], a.heat);
     st = lanes_joined2<kTwo, 64>(st, a.heat);
-    const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
-    const RowEnd e = end_of_row<kTwo>(a, row, a.first[row], at, st, share, lane == 0);
-    if (lane == 0) {
-        a.stat[row] = Stat2{st.m, e.cp, e.ct};
-        a.coef[row] = make_float2(e.cs, e.ch);
-    }
-}
-__device__ __forceinline__ RowEnd kept_end(const DistillArgs& a, int64_t row, float& m) {
-    const Stat2 st = a.stat[row];
-    const float2 c = a.coef[row];
     m = st.m;
-    return RowEnd{c.x, c.y, st.s, st.s1};
+    const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
+    return end_of_row<kTwo>(a, row, a.first[row], at, st, share, writes, term);
 }
 
-// grid: rows * blocks.  The last rows first: they are the ones that the pass before has left in the last-level cache.
+constexpr int64_t kLossHere = 64;       // rows whose loss terms one more block of the gradient's pass adds up: a launch less
+
+// grid: rows * blocks, and the block for the loss.  The last rows first: they are the ones that the pass before has left in the last-level cache.
 template <class E, bool kTwo>
 __global__ __launch_bounds__(kT) void distill_gradient_kernel(const DistillArgs a) {
+    __shared__ float counts[kT / 64];
+    __shared__ double terms[kT / 64];
+    const float counted = a.rows <= kCountHere ? fmaxf(counted_rows<kT / 64>(a.tokens, a.rows, counts), 1.0f) : 0.0f;
+    const float share = a.rows <= kCountHere ? 1.0f / counted : *a.share;
     const int64_t row = a.rows - 1 - blockIdx.x / a.blocks;
+    float m = 0.0f;
+    double term = 0.0;
+    if (row < 0) {                                       // the block for the loss
+        double sum = 0.0;
+        for (int64_t i = threadIdx.x >> 6; i < a.rows; i += kT / 64)
+            if (a.tokens[i] >= 0) {
+                joined_row<E, kTwo>(a, i, a.tokens[i], share, false, m, term);
+                sum += term;
+            }
+        if ((threadIdx.x & 63) == 0) terms[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) *a.loss = static_cast<float>((((terms[0] + terms[1]) + terms[2]) + terms[3]) / static_cast<double>(counted));
+        static_assert(kT / 64 == 4, "");
+        return;
+    }
+    const int part = static_cast<int>(blockIdx.x % a.blocks);
+    const int64_t token = a.tokens[row];
+    const bool writes = part == 0 && threadIdx.x == 0;
+    RowEnd e{0.0f, 0.0f, 0.0f, 0.0f};
+    if (token >= 0) e = joined_row<E, kTwo>(a, row, token, share, writes, m, term);
+    else if (writes) empty_row(a, row);
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
     typename E::Raw* dz = static_cast<typename E::Raw*>(a.dz) + row * a.vocab;
     const Cut<E> cut(dz, static_cast<int>(a.vocab));
-    float m = 0.0f;
-    const RowEnd e = a.tokens[row] < 0 ? RowEnd{0.0f, 0.0f, 0.0f, 0.0f} : kept_end(a, row, m);
     const bool zero = e.cs == 0.0f && e.ch == 0.0f;
-    const int v0 = static_cast<int>(blockIdx.x % a.blocks) * (kT * kUnroll) + static_cast<int>(threadIdx.x);
-    const int single = blockIdx.x % a.blocks == 0 ? cut.single() : -1;
+    const int v0 = part * (kT * kUnroll) + static_cast<int>(threadIdx.x);
+    const int single = part == 0 ? cut.single() : -1;
     if (single >= 0) E::put(dz + single, zero ? 0.0f : slope_at<E, kTwo>(E::get(z + single), m, e, a.heat));
     v4u x[kUnroll];
     float d[E::kN];
@@ -514,28 +518,26 @@ __global__ __launch_bounds__(kT) void distill_gradient_kernel(const DistillArgs 
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (v0 + u * kT < cut.vectors) store_vector<E>(dz, cut.at(v0 + u * kT), d);
-        return;
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (v0 + u * kT < cut.vectors) x[u] = load_vector<E, true>(z, cut.at(v0 + u * kT));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (v0 + u * kT < cut.vectors) {
+                slopes_of<E, kTwo>(x[u], m, e, a.heat, d);
+                store_vector<E>(dz, cut.at(v0 + u * kT), d);
+            }
     }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-        if (v0 + u * kT < cut.vectors) x[u] = load_vector<E, true>(z, cut.at(v0 + u * kT));
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-        if (v0 + u * kT < cut.vectors) {
-            slopes_of<E, kTwo>(x[u], m, e, a.heat, d);
-            store_vector<E>(dz, cut.at(v0 + u * kT), d);
-        }
-}
-// One wavefront a row.
-template <class E, bool kTwo>
-__global__ __launch_bounds__(kT) void distill_entries_kernel(const DistillArgs a) {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (kT / 64) + (threadIdx.x >> 6);
-    if (row >= a.rows) return;
-    const int64_t token = a.tokens[row];
     if (token < 0) return;
-    float m;
-    const RowEnd e = kept_end(a, row, m);
-    store_entries<E, kTwo>(a, a.entries + row * (a.k + 1), row, token, m, e, threadIdx.x & 63, 64);
+    __syncthreads();
+    const Entry* list = a.entries + row * (a.k + 1);
+    for (int j = threadIdx.x; j <= a.k; j += kT) {       // those of this part
+        const Entry n = list[j];
+        if (n.v < 0) continue;
+        const int v = cut.vector_of(n.v);
+        if ((v < 0 ? 0 : v / (kT * kUnroll)) == part) store_entry<E, kTwo>(a, n, row, token, m, e);
+    }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------
@@ -547,8 +549,7 @@ int split_of(int64_t rows, int64_t vectors) {
 struct Workspace {
     Entry* entries;
     double *first, *term;
-    Stat2 *stat, *parts;
-    float2* coef;
+    Stat2* parts;
     float* share;
     int64_t bytes;
 };
@@ -563,40 +564,37 @@ Workspace laid_out(void* at, int64_t rows, int64_t k) {
     w.entries = reinterpret_cast<Entry*>(take(rows * (k + 1) * sizeof(Entry)));
     w.first = reinterpret_cast<double*>(take(rows * sizeof(double)));
     w.term = reinterpret_cast<double*>(take(rows * sizeof(double)));
-    w.stat = reinterpret_cast<Stat2*>(take(rows * sizeof(Stat2)));
     w.parts = reinterpret_cast<Stat2*>(take(std::max(rows, kSplitBlocks) * sizeof(Stat2)));    // rows * split_of(rows, .) at most
-    w.coef = reinterpret_cast<float2*>(take(rows * sizeof(float2)));
     w.share = reinterpret_cast<float*>(take(sizeof(float)));
     return w;
 }
 
+// Whether the loss is there as well.
 template <class E, bool kTwo>
-void launch_rows(DistillArgs a, hipStream_t s) {
+bool launch_rows(DistillArgs a, hipStream_t s) {
     const int64_t rows = a.rows, vectors = a.vocab / E::kN;
-    const dim3 grid(static_cast<uint32_t>(rows)), waves(static_cast<uint32_t>((rows + kT / 64 - 1) / (kT / 64)));
+    const dim3 grid(static_cast<uint32_t>(rows));
     const bool apart = vectors < 2 || vectors > 16384 || (rows <= 32 && vectors >= 2048);
     const int bytes = teacher_words(static_cast<int>(a.k)) * static_cast<int>(sizeof(int)), held = bytes + static_cast<int>((a.k + 1) * sizeof(Entry));
     if (apart) {                         // perhaps none behind the first 16-byte address, or more than a block's registers hold, or few rows
-        int together = 4;
-        while (together > 1 && together * bytes > 64 * 1024) together /= 2;
-        hipLaunchKernelGGL(teacher_rows_kernel<E>, dim3(static_cast<uint32_t>((rows + together - 1) / together)), dim3(together * 64), together * bytes, s, a);
+        a.together = 4;
+        while (a.together > 1 && a.together * bytes > 16 * 1024) a.together /= 2;      // of LDS, which all blocks of the pass get
+        const int64_t teachers = (rows + a.together - 1) / a.together;
         a.splits = split_of(rows, vectors);
         a.blocks = std::max<int64_t>(1, (vectors + kT * kUnroll - 1) / (kT * kUnroll));
-        hipLaunchKernelGGL((distill_stats_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.splits)), dim3(kT), 0, s, a);
-        hipLaunchKernelGGL((distill_finish_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
-        hipLaunchKernelGGL((distill_gradient_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.blocks)), dim3(kT), 0, s, a);
-        hipLaunchKernelGGL((distill_entries_kernel<E, kTwo>), waves, dim3(kT), 0, s, a);
+        const bool loss = rows <= kLossHere;
+        hipLaunchKernelGGL((distill_stats_kernel<E, kTwo>), dim3(static_cast<uint32_t>(teachers + rows * a.splits)), dim3(kT), a.together * bytes, s, a, teachers);
+        hipLaunchKernelGGL((distill_gradient_kernel<E, kTwo>), dim3(static_cast<uint32_t>(rows * a.blocks + (loss ? 1 : 0))), dim3(kT), 0, s, a);
+        return loss;
     } else if (vectors <= 256) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 1, 4, 4>), grid, dim3(64), held, s, a);
     else if (vectors <= 1024) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 4, 4, 8>), grid, dim3(256), held, s, a);
     else if (vectors <= 4096) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 8, 8, 8>), grid, dim3(512), held, s, a);
     else if (vectors <= 8192) hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 8, 8>), grid, dim3(1024), held, s, a);
     else hipLaunchKernelGGL((distill_rows_kernel<E, kTwo, 16, 16, 4>), grid, dim3(1024), held, s, a);
+    return false;
 }
 template <class E>
-void launch_of(const DistillArgs& a, hipStream_t s) {
-    if (a.hard > 0.0 && a.T != 1.0) launch_rows<E, true>(a, s);
-    else launch_rows<E, false>(a, s);
-}
+bool launch_of(const DistillArgs& a, hipStream_t s) { return a.hard > 0.0 && a.T != 1.0 ? launch_rows<E, true>(a, s) : launch_rows<E, false>(a, s); }
 
 }  // namespace
 
@@ -616,15 +614,11 @@ hipError_t launch_distill(const LossRows& r, const TeacherRows& t, double temper
     if (static_cast<double>(a.heat.hi) >= heat) a.heat.hi = std::nextafterf(a.heat.hi, 0.0f);
     a.heat.lo = static_cast<float>(heat - static_cast<double>(a.heat.hi));
     a.share = w.share;
-    a.entries = w.entries; a.first = w.first; a.term = w.term; a.stat = w.stat; a.parts = w.parts; a.coef = w.coef;
-    a.dz = dz; a.kl = kl; a.logp = logp;
+    a.entries = w.entries; a.first = w.first; a.term = w.term; a.parts = w.parts;
+    a.dz = dz; a.kl = kl; a.logp = logp; a.loss = loss;
     if (r.rows > kCountHere) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, r.tokens, r.rows, w.share);
-    if (r.rows > 0) {
-        if (r.type == ADPSGD_TYPE_F32) launch_of<F32>(a, s);
-        else if (r.type == ADPSGD_TYPE_BF16) launch_of<Bf16>(a, s);
-        else launch_of<F16>(a, s);
-    }
-    hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(1024), 0, s, w.term, r.tokens, r.rows, loss);
+    const bool done = r.rows > 0 && (r.type == ADPSGD_TYPE_F32 ? launch_of<F32>(a, s) : r.type == ADPSGD_TYPE_BF16 ? launch_of<Bf16>(a, s) : launch_of<F16>(a, s));
+    if (!done) hipLaunchKernelGGL(mean_terms_kernel, dim3(1), dim3(1024), 0, s, w.term, r.tokens, r.rows, loss);
     return hipGetLastError();
 }
 
