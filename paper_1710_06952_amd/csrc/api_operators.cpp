@@ -49,8 +49,8 @@ struct BackwardSpace {
 BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes, bool with_low = false) {
     BackwardSpace b{};
     b.dz = 0;
-    b.low = up256(2 * M * N);
-    b.sums = b.low + (with_low ? up256(2 * M * N) : 0);
+    b.low = up256(2 * M * ((N + 7) / 8 * 8));
+    b.sums = b.low + (with_low ? b.low : 0);
     b.partial = b.sums + up256(sums_bytes);
     b.bytes = b.partial + up256(std::max(dense_partial_bytes(M, K, N), dense_partial_bytes(N, K, M)));
     return b;
@@ -85,8 +85,8 @@ const char* gated_fault(const adpsgd_dense_t* o) {
     if (!aligned_to(o->x, 2) || !aligned_to(o->w, 2) || !aligned_to(o->b, 2)) return "gated: a tensor is not aligned to its type";
     return nullptr;
 }
-// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.  low_dx, low_dw: what dz's rounding has left, for the one and the other, or nullptr.
-hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, const void* low_dx, const void* low_dw, void* dx, void* dw, void* partial,
+// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.  padded: dz's rows have zeros up to whole pieces.  low_dx, low_dw: what dz's rounding has left, for the one and the other, or nullptr.
+hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, bool padded, const void* low_dx, const void* low_dw, void* dx, void* dw, void* partial,
                              int64_t partial_bytes, hipStream_t s) {
     DenseGemm g{};
     g.act = ADPSGD_ACT_NONE;
@@ -97,12 +97,15 @@ hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz,
         g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed == 0;
         g.I = o->M; g.J = o->K; g.K = N;
         g.a_low = low_dx;
+        g.a_padded = padded;
         g.out = dx;
         hipError_t e = launch_dense_gemm(o->type, g, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
         g.a_low = nullptr;
+        g.a_padded = !o->w_transposed && padded;
+        g.b_padded = o->w_transposed && padded;
         g.a_outer = g.b_outer = true;
         g.K = o->M;
         g.out = dw;
@@ -203,7 +206,7 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
             hipError_t e = launch_dense_dz(o->type, dy, lddy, of, own ? ws + at.dz : nullptr, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
             if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
         }
-        return ended(backward_products(o, o->N, dz, lddz, nullptr, nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
+        return ended(backward_products(o, o->N, dz, lddz, false, nullptr, nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
     });
 }
 
@@ -250,9 +253,11 @@ extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, in
         void* dz = dx || dw ? ws + at.dz : nullptr;
         const bool low_dx = dx && gated_low(o->M * o->K), low_dw = dw && gated_low(2 * o->N * o->K);
         void* low = low_dx || low_dw ? ws + at.low : nullptr;
-        hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, low, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
+        const bool padded = gated_padded(o->M, o->N, o->K);      // else the products would copy dz to rows of whole pieces
+        const int64_t lddz = padded ? (2 * o->N + 7) / 8 * 8 : 2 * o->N;
+        hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, low, lddz, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
         if (e == hipSuccess)
-            e = backward_products(o, 2 * o->N, dz, 2 * o->N, low_dx ? low : nullptr, low_dw ? low : nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s);
+            e = backward_products(o, 2 * o->N, dz, lddz, padded, low_dx ? low : nullptr, low_dw ? low : nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s);
         return ended(e, "gated backward");
     });
 }

@@ -237,7 +237,7 @@ hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s
         return type == ADPSGD_TYPE_BF16 ? launch_low_tiles<Bf16>(g, p, s) : launch_low_tiles<F16>(g, p, s);
     }
     const int64_t a_inner = g.a_outer ? g.I : g.K, a_rows = g.a_outer ? g.K : g.I, b_inner = g.b_outer ? g.J : g.K, b_rows = g.b_outer ? g.K : g.J;
-    const bool a_whole = whole_pieces(g.a, g.lda, a_inner), b_whole = whole_pieces(g.b, g.ldb, b_inner);
+    const bool a_whole = g.a_padded || whole_pieces(g.a, g.lda, a_inner), b_whole = g.b_padded || whole_pieces(g.b, g.ldb, b_inner);
     const bool pack = !(a_whole && b_whole) && (g.I % 8 || g.J % 8 || g.K % 8) && worth_packing(g.I, g.J, g.K);
     const bool direct = g.K >= 1 && ((a_whole && b_whole) || pack);
     const DensePlan p = plan_of(g.I, g.J, g.K, !g.a_outer && few_rows(g.I, g.J, g.K, g.b_outer, b_whole), direct);

@@ -472,7 +472,7 @@ __device__ __forceinline__ RowEnd joined_row(const DistillArgs& a, int64_t row, 
     return end_of_row<kTwo>(a, row, a.first[row], at, st, share, writes, term);
 }
 
-constexpr int64_t kLossHere = 64;       // rows whose loss terms one more block of the gradient's pass adds up: a launch less
+constexpr int64_t kLossHere = 8;        // rows whose loss terms one more block of the gradient's pass adds up: a launch less, but a quarter of a microsecond a row
 
 // grid: rows * blocks, and the block for the loss.  The last rows first: they are the ones that the pass before has left in the last-level cache.
 template <class E, bool kTwo>
@@ -574,7 +574,11 @@ template <class E, bool kTwo>
 bool launch_rows(DistillArgs a, hipStream_t s) {
     const int64_t rows = a.rows, vectors = a.vocab / E::kN;
     const dim3 grid(static_cast<uint32_t>(rows));
-    const bool apart = vectors < 2 || vectors > 16384 || (rows <= 32 && vectors >= 2048);
+    // Microseconds held and in passes, bf16, 64 entries:  1 row of 8192 9.9 and 9.5, 16 384 11.8 and 9.7, 65 536 15 and 10, 131 072 20 and 10;  8 rows of 8192
+    // 10.3 and 10.8, 16 384 12.2 and 10.8;  16 rows (the loss is a launch more) of 32 768 12.8 and 13.0, 65 536 16.8 and 13.0;  64 rows of 65 536 17.5 and
+    // 14.3, 131 072 24 and 16;  96 rows 17.8 and 16.2, 24.2 and 22.5;  128 rows 17.8 and 16.0, 24.1 and 25.8;  256 rows 20 and 26, 34 and 42.
+    const bool few = rows <= 8 ? vectors >= 2048 : rows <= 96 && vectors >= 8192;
+    const bool apart = vectors < 2 || vectors > 16384 || few;
     const int bytes = teacher_words(static_cast<int>(a.k)) * static_cast<int>(sizeof(int)), held = bytes + static_cast<int>((a.k + 1) * sizeof(Entry));
     if (apart) {                         // perhaps none behind the first 16-byte address, or more than a block's registers hold, or few rows
         a.together = 4;

@@ -32,6 +32,7 @@ int gated_strips(int64_t M, int64_t N) {
 
 }  // namespace
 
+bool gated_padded(int64_t M, int64_t N, int64_t K) { return 2 * N % 8 != 0 && worth_packing(M, 2 * N, K); }
 bool gated_low(int64_t elements) { return elements <= 8192; }
 int64_t gated_sums_bytes(int64_t M, int64_t N) { return gated_strips(M, N) * 2 * N * static_cast<int64_t>(sizeof(double)); }
 
@@ -81,7 +82,7 @@ namespace {
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
 // Memory: 2 + 4 + 4 bytes a result (fp16: 2 more).  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
 template <class T, int kAcross>
-__global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, uint16_t* rest, double* sums, uint16_t* db, int64_t M,
+__global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, uint16_t* rest, int64_t lddz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
     constexpr int kColumns = 8 * kAcross, kRowsAtOnce = kT / kAcross;
     __shared__ double at[kRowsAtOnce][kColumns];
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                     }
                     if (!dz) continue;
                     auto write = [&](uint16_t* to, v4u p) {
-                        to += (2 * m + kind) * N + j;
+                        to += m * lddz + kind * N + j;
                         if (kWhole) {
                             *reinterpret_cast<v4u_any*>(to) = p;
                         } else {
@@ -147,6 +148,8 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                             for (int i = 0; i < 8; ++i)
                                 if (j + i < N) to[i] = h[i];
                         }
+                        if (kind == 1 && j < N && j + 8 >= N)
+                            for (int64_t i = 2 * N; i < lddz; ++i) to[i - N - j] = 0;
                     };
                     const v4u p = pack8<T>(f);
                     write(dz, p);
@@ -184,11 +187,11 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
 }
 
 template <class T>
-void launch_dz_of(const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, void* db, double* sums, int64_t M, int64_t N, hipStream_t s) {
+void launch_dz_of(const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, int64_t lddz, void* db, double* sums, int64_t M, int64_t N, hipStream_t s) {
     const int strips = gated_strips(M, N);
     auto go = [&](auto kernel, int64_t columns) {
         hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((N + columns - 1) / columns), strips), dim3(kT), 0, s, static_cast<const uint16_t*>(dh), lddh, slopes,
-                           static_cast<uint16_t*>(dz), static_cast<uint16_t*>(low), db ? sums : nullptr, strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
+                           static_cast<uint16_t*>(dz), static_cast<uint16_t*>(low), lddz, db ? sums : nullptr, strips == 1 ? static_cast<uint16_t*>(db) : nullptr, M, N);
     };
     if (strips == 1) go(gated_dz_kernel<T, 8>, 64);
     else if (strips > 1) go(gated_dz_kernel<T, 32>, 256);
@@ -197,10 +200,10 @@ void launch_dz_of(const void* dh, int64_t lddh, const uint16_t* slopes, void* dz
 
 }  // namespace
 
-hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, void* db, double* sums, int64_t M, int64_t N,
-                           hipStream_t s) {
-    if (type == ADPSGD_TYPE_BF16) launch_dz_of<Bf16>(dh, lddh, slopes, dz, low, db, sums, M, N, s);
-    else launch_dz_of<F16>(dh, lddh, slopes, dz, low, db, sums, M, N, s);
+hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, int64_t lddz, void* db, double* sums, int64_t M,
+                           int64_t N, hipStream_t s) {
+    if (type == ADPSGD_TYPE_BF16) launch_dz_of<Bf16>(dh, lddh, slopes, dz, low, lddz, db, sums, M, N, s);
+    else launch_dz_of<F16>(dh, lddh, slopes, dz, low, lddz, db, sums, M, N, s);
     return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@ struct DenseGemm {                  // D[i][j] = sum_k A(i, k) B(j, k), i < I, j
     int64_t lda, ldb;
     bool a_outer, b_outer;          // false: (i, k) at a + i lda + k;  true: at a + k lda + i.  b likewise
     const void *a_low, *b_low;      // what a's or b's rounding has left, laid out as a or b; nullptr but for small results of a gated projection's backward pass
+    bool a_padded, b_padded;        // rows begin at whole pieces and have zeros up to one behind them
     int64_t b_up;                   // gated products (kernels_gated.hip) only: elements from a gate's weight to its partner's
     int64_t I, J, K;
     int32_t act;
@@ -33,9 +34,10 @@ int64_t dense_sums_bytes(int64_t M, int64_t N);
 hipError_t launch_gated_gemm(int32_t type, const DenseGemm& g, hipStream_t s);      // b_up is set here
 int64_t gated_partial_bytes(int64_t I, int64_t J, int64_t K);
 int64_t gated_sums_bytes(int64_t M, int64_t N);
-// dz = [dh slope | dh slope'] (dz may be nullptr: only db), low (or nullptr) what its rounding has left, db = column sums of the unrounded dz (db may be nullptr)
-hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, void* db, double* sums, int64_t M, int64_t N,
-                           hipStream_t s);
+// dz = [dh slope | dh slope'], rows of lddz >= 2 N with zeros at their ends (dz may be nullptr: only db), low (or nullptr) what its rounding has left, db = column sums of the unrounded dz (db may be nullptr)
+hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, int64_t lddz, void* db, double* sums, int64_t M,
+                           int64_t N, hipStream_t s);
+bool gated_padded(int64_t M, int64_t N, int64_t K);        // whether dz is written in rows of whole pieces
 bool gated_low(int64_t elements);   // whether a result of so many is computed from dz in two parts
 
 // ---- layer norm (kernels_norm.hip) ----
