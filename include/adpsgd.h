@@ -456,7 +456,7 @@ int adpsgd_synth_gradient(uint64_t seed, uint64_t k, float std, int64_t d, float
                           void* stream);
 
 /* ---- Operators of a worker's own training step -----------------------------------------------------------
- * Products with their epilogue, log-probabilities and losses over a vocabulary, and AdamW, for gradient functions of
+ * Products with their epilogue, layer norm, log-probabilities and losses over a vocabulary, and AdamW, for gradient functions of
  * ADPSGD_MODEL_EXTERNAL and programs around them.  No handle is needed (AdamW has one of its own).  All pointers are device
  * memory unless "host" is stated; nothing is allocated, work is enqueued on `stream` and the calls return at once.  Elements are
  * addressed with 64-bit offsets, and tensors need the alignment of their type only.  adpsgd_last_error(NULL) has the message of

@@ -1,11 +1,13 @@
-"""Operators of a worker's own training step on torch tensors: dense layers, log-probabilities and losses over a
-vocabulary, AdamW over many tensors.  The same entry points as include/adpsgd.h; every computation runs in the HIP
+"""Operators of a worker's own training step on torch tensors: dense layers, gated projections and layer norm,
+log-probabilities and losses over a vocabulary, AdamW over many tensors.  The same entry points as include/adpsgd.h; every computation runs in the HIP
 library, on the current stream of the tensors' device.
 
     y = dense(x, w, bias, residual=r, activation="gelu")           # differentiable
+    h = gated(layer_norm(x, scale, shift), w2, activation="silu")  # differentiable
     lp = token_log_probs(logits, tokens)                           # of a frozen model, or to sample with
     r = policy_loss_and_gradient(logits, tokens, old, advantages, ref, clip=(0.2, 0.2), kl_coef=0.05)
     r = preference_loss_and_gradient(logits, tokens, offsets, ref, beta=0.1)
+    r = distillation_loss_and_gradient(logits, tokens, teacher_tokens, teacher_logits, temperature=2.0)
     logits.backward(r.dlogits)                                     # or torch.autograd.grad
     opt = AdamW(params, grads, lr=1e-3, state_bits=8);  opt.step(max_norm=1.0)
 
@@ -220,19 +222,21 @@ _SLOPE_BYTES = {torch.bfloat16: 2, torch.float16: 3}      # of adpsgd_gated_slop
 
 def _check_gated(x, w, b, activation):
     _on_gpu("x", x)
+    T, device = x.dtype, x.device
     for name, t in (("w", w), ("bias", b)):
         if t is None and name != "w":
             continue
-        _on_gpu(name, t, x.device)
-        if t.dtype != x.dtype:
-            raise TypeError("x is %s, %s is %s" % (x.dtype, name, t.dtype))
-    if x.dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError("gated takes bfloat16 or float16, not %s" % x.dtype)
+        _on_gpu(name, t, device)
+        if t.dtype != T:
+            raise TypeError("x is %s, %s is %s" % (T, name, t.dtype))
+    if T not in _SLOPE_BYTES:
+        raise TypeError("gated takes bfloat16 or float16, not %s" % T)
     if activation not in _ACTIVATIONS:
         raise ValueError("activation must be one of %s" % ", ".join(_ACTIVATIONS))
-    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1] or w.shape[0] < 2 or w.shape[0] % 2 or w.shape[1] < 1:
+    rows, inner = w.shape if w.dim() == 2 else (0, 0)
+    if x.dim() < 1 or x.shape[-1] != inner or rows < 2 or rows % 2 or inner < 1:
         raise ValueError("x is %s, w %s: w must be 2 out x in, the gates' rows and then their partners'" % (tuple(x.shape), tuple(w.shape)))
-    if b is not None and b.shape != (w.shape[0],):
+    if b is not None and (b.dim() != 1 or b.numel() != rows):
         raise ValueError("bias is %s, w %s" % (tuple(b.shape), tuple(w.shape)))
 
 
@@ -268,7 +272,7 @@ def _gated_backward(dh, x, w, slopes, need_dx, need_dw, need_db):
     M, N, K = args.M, args.N, args.K
     new = lambda *shape: torch.empty(*shape, dtype=x.dtype, device=x.device)  # noqa: E731
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if need_dx else None
-    dw = (new(K, 2 * N).t() if args.w_transposed else new(2 * N, K)) if need_dw else None
+    dw = torch.empty_strided((2 * N, K), (1, 2 * N) if args.w_transposed else (K, 1), dtype=x.dtype, device=x.device) if need_dw else None
     db = new(2 * N) if need_db else None
     _call(x.device, B.lib().adpsgd_gated_backward, C.byref(args), dhm.data_ptr(), lddh, slopes.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db))
     del keep
@@ -307,8 +311,7 @@ def gated(x, w, bias=None, *, activation="silu"):
 def gated_forward(x, w, bias=None, *, activation="silu"):
     """(h, slopes): the forward pass without autograd, and what gated_gradients needs."""
     _check_gated(x, w, bias, activation)
-    with torch.no_grad():
-        return _gated_forward(x, w, bias, activation, True)
+    return _gated_forward(x, w, bias, activation, True)
 
 
 def gated_gradients(dh, x, w, slopes, *, need=(True, True, True)):
@@ -322,8 +325,7 @@ def gated_gradients(dh, x, w, slopes, *, need=(True, True, True)):
         raise ValueError("slopes must be what gated_forward returned")
     if not any(need):
         return None, None, None
-    with torch.no_grad():
-        return _gated_backward(dh, x, w, slopes, *need)
+    return _gated_backward(dh, x, w, slopes, *need)
 
 
 # ---- layer norm -------------------------------------------------------------------------------------------------
@@ -333,24 +335,26 @@ _FAR = 1 << 40          # elements from one row to the next, at most, where rows
 
 def _check_norm(x, w, b, dy=None):
     _on_gpu("x", x)
-    if x.dtype not in _TYPES:
-        raise TypeError("layer_norm takes float32, bfloat16 or float16, not %s" % x.dtype)
-    if x.dim() < 1 or x.shape[-1] < 1:
+    T, device = x.dtype, x.device
+    if T not in _TYPES:
+        raise TypeError("layer_norm takes float32, bfloat16 or float16, not %s" % T)
+    n = x.shape[-1] if x.dim() else 0
+    if n < 1:
         raise ValueError("x is %s: the last dimension is what is normalised" % (tuple(x.shape),))
     if b is not None and w is None:
         raise ValueError("a bias without a weight")
     for name, t in (("weight", w), ("bias", b)):
         if t is None:
             continue
-        _on_gpu(name, t, x.device)
-        if t.dtype not in (x.dtype, torch.float32) or t.dtype != w.dtype:
-            raise TypeError("x is %s, %s is %s: weight and bias are both of that type or both float32" % (x.dtype, name, t.dtype))
-        if t.shape != x.shape[-1:]:
+        _on_gpu(name, t, device)
+        if (t.dtype != T and t.dtype != torch.float32) or t.dtype != w.dtype:
+            raise TypeError("x is %s, %s is %s: weight and bias are both of that type or both float32" % (T, name, t.dtype))
+        if t.dim() != 1 or t.numel() != n:
             raise ValueError("%s is %s, x %s" % (name, tuple(t.shape), tuple(x.shape)))
     if dy is not None:
-        _on_gpu("dy", dy, x.device)
-        if dy.dtype != x.dtype or dy.shape != x.shape:
-            raise ValueError("dy is %s %s, must be as x, %s %s" % (tuple(dy.shape), dy.dtype, tuple(x.shape), x.dtype))
+        _on_gpu("dy", dy, device)
+        if dy.dtype != T or dy.shape != x.shape:
+            raise ValueError("dy is %s %s, must be as x, %s %s" % (tuple(dy.shape), dy.dtype, tuple(x.shape), T))
 
 
 def _norm_args(x, w, b, eps):
@@ -418,8 +422,7 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5):
 def layer_norm_forward(x, weight=None, bias=None, *, eps=1e-5):
     """(y, stats): the forward pass without autograd, and what layer_norm_gradients needs."""
     _check_norm(x, weight, bias)
-    with torch.no_grad():
-        return _norm_forward(x, weight, bias, eps, True)
+    return _norm_forward(x, weight, bias, eps, True)
 
 
 def layer_norm_gradients(dy, x, weight, stats, *, need=(True, True, True)):
@@ -431,8 +434,7 @@ def layer_norm_gradients(dy, x, weight, stats, *, need=(True, True, True)):
     need = (need[0], need[1] and weight is not None, need[2] and weight is not None)
     if not any(need):
         return None, None, None
-    with torch.no_grad():
-        return _norm_backward(dy, x, weight, stats, *need)
+    return _norm_backward(dy, x, weight, stats, *need)
 
 
 # ---- losses over a vocabulary -----------------------------------------------------------------------------------
