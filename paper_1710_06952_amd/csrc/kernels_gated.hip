@@ -10,7 +10,8 @@
 // up to 2^13 elements are computed from dz in two parts (its rounding, and the rounding of what that has left): their products take little time, and few
 // elements are up to 1.6 times as far in the one form, which is 1.0 in the other.
 //
-// Bound: the matrix cores, with few rows the bytes of the weights.
+// Bound: the matrix cores, with few rows the bytes of the weights.  8192 x 2048 x (2 x 8192) in bf16 with slopes: 470 us by itself, 557 between the products of the
+// backward pass (a library product of that size without an end 417); silu is 22 us of it and the slopes 25.  1 x 4096 x (2 x 8192): 26 us.
 #include <algorithm>
 
 #include "dense_tiles.hpp"
@@ -80,7 +81,7 @@ hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s
 namespace {
 
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
-// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more).  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
+// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 106 us, 6.3 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
 template <class T, int kAcross>
 __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, uint16_t* rest, int64_t lddz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
