@@ -146,8 +146,15 @@ DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct);
 bool whole_pieces(const void* p, int64_t ld, int64_t inner);
 bool worth_packing(int64_t I, int64_t J, int64_t K);
 int64_t packed_bytes(int64_t rows, int64_t inner);
-// rows x inner at `from` to rows of ldto elements at `to`, whole pieces with zeros at their ends
-void launch_pack(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t inner, hipStream_t s);
+// rows x inner at `from` to rows of ldto elements at `to`, whole pieces with zeros at their ends; up to kMostPacks of them in a launch
+struct PackJob {
+    const void* from;
+    int64_t ld;
+    void* to;
+    int64_t ldto, rows, inner;
+};
+constexpr int kMostPacks = 3;
+void launch_pack(const PackJob* job, int jobs, hipStream_t s);
 
 // Strips that a pass over dy sums by itself (256 rows each, as many as 64: with N = 8192 four blocks for a compute unit), and their sums.
 int strips_of(int64_t M);

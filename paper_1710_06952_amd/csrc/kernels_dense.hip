@@ -191,21 +191,29 @@ DensePlan plan_of(int64_t I, int64_t J, int64_t K, bool few, bool direct) {
 }
 
 namespace {
-// Rows of `inner` elements as whole 16-byte pieces with zeros at their ends.  grid: ceil(rows ceil(inner / 8) / 256).
-__global__ __launch_bounds__(kT) void dense_pack_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t ldto, int64_t rows, int64_t inner) {
-    const int64_t pieces = (inner + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * kT + threadIdx.x;
+// Rows of `inner` elements as whole 16-byte pieces with zeros at their ends, of several matrices in one launch.  grid: the sum of ceil(rows ceil(inner / 8) / 256).
+struct PackJobs {
+    PackJob job[kMostPacks];
+    uint32_t blocks[kMostPacks];
+};
+__global__ __launch_bounds__(kT) void dense_pack_kernel(const PackJobs jobs) {
+    uint32_t block = blockIdx.x;
+    int n = 0;
+    while (n + 1 < kMostPacks && block >= jobs.blocks[n]) block -= jobs.blocks[n++];
+    const PackJob& j = jobs.job[n];
+    const int64_t pieces = (j.inner + 7) / 8, id = static_cast<int64_t>(block) * kT + threadIdx.x;
     const int64_t row = id / pieces, c = id % pieces * 8;
-    if (row >= rows) return;
-    const uint16_t* p = from + row * ld + c;
+    if (row >= j.rows) return;
+    const uint16_t* p = static_cast<const uint16_t*>(j.from) + row * j.ld + c;
     v8h h = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (c + 8 <= inner) {
+    if (c + 8 <= j.inner) {
         h = __builtin_bit_cast(v8h, *reinterpret_cast<const v4u_any*>(p));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i < inner) h[i] = p[i];
+            if (c + i < j.inner) h[i] = p[i];
     }
-    *reinterpret_cast<v4u*>(to + (row * ldto + c)) = __builtin_bit_cast(v4u, h);
+    *reinterpret_cast<v4u*>(static_cast<uint16_t*>(j.to) + (row * j.ldto + c)) = __builtin_bit_cast(v4u, h);
 }
 }  // namespace
 
@@ -214,9 +222,15 @@ bool whole_pieces(const void* p, int64_t ld, int64_t inner) { return reinterpret
 // dx 60 us with the copies, 257 with tiles of 64 from the operands as they are).
 bool worth_packing(int64_t I, int64_t J, int64_t K) { return static_cast<double>(I) * static_cast<double>(J) * static_cast<double>(K) >= 4294967296.0; }
 int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(inner)); }
-void launch_pack(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t inner, hipStream_t s) {
-    const uint32_t blocks = static_cast<uint32_t>((rows * (up8(inner) / 8) + kT - 1) / kT);
-    hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, static_cast<const uint16_t*>(from), ld, static_cast<uint16_t*>(to), ldto, rows, inner);
+void launch_pack(const PackJob* job, int jobs, hipStream_t s) {
+    PackJobs all{};
+    uint32_t blocks = 0;
+    for (int i = 0; i < jobs; ++i) {
+        all.job[i] = job[i];
+        all.blocks[i] = static_cast<uint32_t>((job[i].rows * (up8(job[i].inner) / 8) + kT - 1) / kT);
+        blocks += all.blocks[i];
+    }
+    if (blocks > 0) hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, all);
 }
 
 // Both ways of storing an operand, and operands that begin anywhere: what any of them may ask for.
@@ -243,14 +257,17 @@ hipError_t launch_dense_gemm(int32_t type, const DenseGemm& given, hipStream_t s
     const DensePlan p = plan_of(g.I, g.J, g.K, !g.a_outer && few_rows(g.I, g.J, g.K, g.b_outer, b_whole), direct);
     if (p.side >= 128 && pack) {
         char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * g.J * static_cast<int64_t>(sizeof(float))) : 0);
+        PackJob jobs[2];
+        int n = 0;
         auto copy = [&](const void*& from, int64_t& ld, int64_t rows, int64_t inner) {
-            launch_pack(from, ld, at, up8(inner), rows, inner, s);
+            jobs[n++] = PackJob{from, ld, at, up8(inner), rows, inner};
             from = at;
             ld = up8(inner);
             at += packed_bytes(rows, inner);
         };
         if (!a_whole) copy(g.a, g.lda, a_rows, a_inner);
         if (!b_whole) copy(g.b, g.ldb, b_rows, b_inner);
+        launch_pack(jobs, n, s);
     }
     return type == ADPSGD_TYPE_BF16 ? launch_dense_tiles<Bf16>(g, p, s) : launch_dense_tiles<F16>(g, p, s);
 }

@@ -55,8 +55,10 @@ hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s
     const DensePlan p = plan_of(g.I, 2 * g.J, g.K, few_rows(g.I, 2 * g.J, g.K, g.b_outer, b_whole), (a_whole && b_whole) || pack);
     if (p.side >= 128 && pack) {
         char* at = reinterpret_cast<char*>(g.partial) + (p.splits > 1 ? up256(p.splits * g.I * 2 * g.J * static_cast<int64_t>(sizeof(float))) : 0);
+        PackJob jobs[kMostPacks];
+        int n = 0;
         if (!a_whole) {
-            launch_pack(g.a, g.lda, at, up8(g.K), g.I, g.K, s);
+            jobs[n++] = PackJob{g.a, g.lda, at, up8(g.K), g.I, g.K};
             g.a = at;
             g.lda = up8(g.K);
             at += packed_bytes(g.I, g.K);
@@ -64,21 +66,41 @@ hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s
         if (!b_whole && g.b_outer) {                     // gates and partners each in whole pieces
             const int64_t half = up8(g.J);
             for (int kind = 0; kind < 2; ++kind)
-                launch_pack(static_cast<const uint16_t*>(g.b) + kind * g.J, g.ldb, at + kind * 2 * half, 2 * half, g.K, g.J, s);
+                jobs[n++] = PackJob{static_cast<const uint16_t*>(g.b) + kind * g.J, g.ldb, at + kind * 2 * half, 2 * half, g.K, g.J};
             g.b = at;
             g.ldb = 2 * half;
             g.b_up = half;
         } else if (!b_whole) {
-            launch_pack(g.b, g.ldb, at, up8(g.K), 2 * g.J, g.K, s);
+            jobs[n++] = PackJob{g.b, g.ldb, at, up8(g.K), 2 * g.J, g.K};
             g.b = at;
             g.ldb = up8(g.K);
             g.b_up = g.J * g.ldb;
         }
+        launch_pack(jobs, n, s);
     }
     return type == ADPSGD_TYPE_BF16 ? launch_gated_tiles<Bf16>(g, p, s) : launch_gated_tiles<F16>(g, p, s);
 }
 
 namespace {
+
+// The elements skip .. 7 of a vector, to + 8 the end of their row: pieces of four, two and one from behind.
+__device__ __forceinline__ void store_end(uint16_t* to, v4u p, int skip) {
+    const int n = 8 - skip;
+    int at = 8;
+    if (n & 4) {
+        at = 4;
+        __builtin_memcpy(to + 4, reinterpret_cast<const char*>(&p) + 8, 8);
+    }
+    if (n & 2) {
+        at -= 2;
+        const uint32_t w = at == 6 ? p.w : p.y;
+        __builtin_memcpy(to + at, &w, 4);
+    }
+    if (n & 1) {
+        at -= 1;                         // odd: the upper half of its word
+        to[at] = static_cast<uint16_t>((at == 7 ? p.w : at == 5 ? p.z : at == 3 ? p.y : p.x) >> 16);
+    }
+}
 
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
 // Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 106 us, 6.3 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
@@ -92,20 +114,20 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
     const int64_t m0 = M * blockIdx.y / gridDim.y, m1 = M * (blockIdx.y + 1) / gridDim.y;
     double sum[2][8] = {};
     const GatedSlopes<T> kept(const_cast<uint16_t*>(slopes), M, N);
-    auto rows = [&](auto whole_columns) {
-        constexpr bool kWhole = decltype(whole_columns)::value;
-        // A cut vector is read ending at the row's end and shifted: eight loads of an element each took 151 us for 2003 x 2731.
-        auto load = [&](const uint16_t* p) { return kWhole ? static_cast<v4u>(__builtin_nontemporal_load(reinterpret_cast<const v4u_any*>(p))) : load_cut(p - j, j, N); };
+    // A vector that the end of the row cuts is the last whole one, of which the first `skip` columns are its neighbour's: it stores the others and counts
+    // them only.  (A way of its own for it, element by element, doubled the time of its block: 151 us for 2003 x 2731 in fp16, 30 with shifted loads, 20 so.)
+    const int skip = N >= 8 && j < N && j + 8 > N ? static_cast<int>(j + 8 - N) : 0;
+    const int64_t from_j = j - skip;
+    auto rows = [&](auto vectors) {
+        constexpr bool kVectors = decltype(vectors)::value;      // else there are less than eight columns in all
+        auto load = [&](const uint16_t* p) { return kVectors ? static_cast<v4u>(__builtin_nontemporal_load(reinterpret_cast<const v4u_any*>(p))) : load_cut(p, 0, N); };
         auto load_low = [&](const uint8_t* p) {
             uint64_t x = 0;
-            if (kWhole) {
+            if (kVectors) {
                 __builtin_memcpy(&x, p, 8);
-            } else if (N >= 8) {
-                __builtin_memcpy(&x, p - (j + 8 - N), 8);
-                x >>= 8 * (j + 8 - N);
             } else {
                 for (int i = 0; i < 8; ++i)
-                    if (j + i < N) x |= static_cast<uint64_t>(p[i]) << (8 * i);
+                    if (i < N) x |= static_cast<uint64_t>(p[i]) << (8 * i);
             }
             return v2u{static_cast<uint32_t>(x), static_cast<uint32_t>(x >> 32)};
         };
@@ -116,10 +138,10 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
 #pragma unroll
             for (int u = 0; u < 4; ++u) {                // rows beyond the strip: its last one again, which counts nothing
                 const int64_t m = first + u * kRowsAtOnce < m1 ? first + u * kRowsAtOnce : m1 - 1;
-                d[u] = load(dh + m * lddh + j);
+                d[u] = load(dh + m * lddh + from_j);
 #pragma unroll
                 for (int kind = 0; kind < 2; ++kind) {
-                    const int64_t from = (2 * m + kind) * N + j;
+                    const int64_t from = (2 * m + kind) * N + from_j;
                     w[u][kind] = load(kept.high + from);
                     if (GatedSlopes<T>::kLow) low[u][kind] = load_low(kept.low + from);
                 }
@@ -141,16 +163,18 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                     }
                     if (!dz) continue;
                     auto write = [&](uint16_t* to, v4u p) {
-                        to += m * lddz + kind * N + j;
-                        if (kWhole) {
-                            *reinterpret_cast<v4u_any*>(to) = p;
-                        } else {
+                        to += m * lddz + kind * N + from_j;
+                        if (!kVectors) {
                             const v8h h = __builtin_bit_cast(v8h, p);
                             for (int i = 0; i < 8; ++i)
-                                if (j + i < N) to[i] = h[i];
+                                if (i < N) to[i] = h[i];
+                        } else if (skip == 0) {
+                            *reinterpret_cast<v4u_any*>(to) = p;
+                        } else {
+                            store_end(to, p, skip);
                         }
-                        if (kind == 1 && j < N && j + 8 >= N)
-                            for (int64_t i = 2 * N; i < lddz; ++i) to[i - N - j] = 0;
+                        if (kind == 1 && j + 8 >= N)
+                            for (int64_t i = 2 * N; i < lddz; ++i) to[i - N - from_j] = 0;
                     };
                     const v4u p = pack8<T>(f);
                     write(dz, p);
@@ -169,13 +193,17 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                 for (int i = 0; i < 8; ++i) sum[kind][i] += static_cast<double>(part[kind][i]);
         }
     };
-    if (j + 8 <= N) rows(std::true_type());
-    else if (j < N) rows(std::false_type());
+    if (N < 8) {
+        if (j == 0) rows(std::false_type());
+    } else if (j < N) {
+        rows(std::true_type());
+    }
     if (!sums && !db) return;
     for (int kind = 0; kind < 2; ++kind) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at[ry][8 * cx + i] = sum[kind][i];
+        for (int i = 0; i < 8; ++i)
+            if (i >= skip) at[ry][8 * cx + i - skip] = sum[kind][i];
         __syncthreads();
         const int64_t column = static_cast<int64_t>(blockIdx.x) * kColumns + threadIdx.x;
         if (static_cast<int>(threadIdx.x) < kColumns && column < N) {
