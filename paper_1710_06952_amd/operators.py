@@ -45,6 +45,12 @@ def _call(device, fn, *args):
         raise B.AdpsgdError(rc, (B.lib().adpsgd_last_error(None) or b"").decode())
 
 
+def _refuse_capture(name):
+    """Of a differentiable form and of its backward pass: what autograd does around them depends on graphs of the same leaves that live outside."""
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("%s with gradients cannot be captured: capture %s_forward and %s_gradients" % (name, name, name))
+
+
 def _on_gpu(name, t, device=None):
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a tensor" % name)
@@ -289,6 +295,7 @@ class _Gated(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dh):
+        _refuse_capture("gated")
         return (*_gated_backward(dh, *ctx.saved_tensors, *ctx.needs_input_grad[:3]), None)
 
 
@@ -302,8 +309,7 @@ def gated(x, w, bias=None, *, activation="silu"):
     differentiable form is refused, as dense's is: gated_forward and gated_gradients can be captured."""
     _check_gated(x, w, bias, activation)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias)):
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("gated with gradients cannot be captured: capture gated_forward and gated_gradients")
+        _refuse_capture("gated")
         return _Gated.apply(x, w, bias, activation)
     return _gated_forward(x, w, bias, activation, False)[0]
 
@@ -400,6 +406,7 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
+        _refuse_capture("layer_norm")
         x, w, stats = ctx.saved_tensors
         return (*_norm_backward(dy, x, w, stats, *ctx.needs_input_grad[:3]), None)
 
@@ -413,8 +420,7 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5):
     layer_norm_gradients can be captured."""
     _check_norm(x, weight, bias)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("layer_norm with gradients cannot be captured: capture layer_norm_forward and layer_norm_gradients")
+        _refuse_capture("layer_norm")
         return _LayerNorm.apply(x, weight, bias, eps)
     return _norm_forward(x, weight, bias, eps, False)[0]
 

@@ -229,3 +229,34 @@ def test_distillation_shapes_and_types():
             (lambda: call(z, tokens, e, t, hard_weight=1.5), P.AdpsgdError, "hard_weight"), (lambda: call(z, tokens, e, t, loss_scale=float("nan")), P.AdpsgdError, "loss_scale")]:
         with pytest.raises(kind, match=word):
             run()
+
+
+@pytest.mark.parametrize("name", ["_LayerNorm", "_Gated"])
+def test_a_captured_backward_pass(name, monkeypatch):
+    """Refused before it looks at anything, on the CPU with the capture made up."""
+    import torch
+    from paper_1710_06952_amd import operators
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="captured"):
+        getattr(operators, name).backward(object(), torch.zeros(1))
+
+
+@pytest.mark.gpu
+def test_a_captured_backward_pass_of_eager_graphs():
+    """... and in a capture on the stream of the forward pass, behind which the same graphs give their gradients."""
+    import torch
+    new = lambda *s: torch.randn(*s, device="cuda:0").bfloat16()  # noqa: E731
+    side = torch.cuda.Stream()
+    x, w, b, wg, dy = new(24, 64).requires_grad_(), new(64), new(64), new(80, 64), new(24, 64)
+    dh = new(24, 40)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y, h = P.layer_norm(x, w, b), P.gated(x, wg)
+    for out, d, word in ((y, dy, "layer_norm"), (h, dh, "gated")):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=side), pytest.raises(RuntimeError, match=word):
+            torch.autograd.grad(out, x, d, retain_graph=True)
+    torch.cuda.synchronize()
+    _, stats = P.layer_norm_forward(x.detach(), w, b)
+    _, slopes = P.gated_forward(x.detach(), wg)
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], P.layer_norm_gradients(dy, x.detach(), w, stats)[0])
+    assert torch.equal(torch.autograd.grad(h, x, dh)[0], P.gated_gradients(dh, x.detach(), wg, slopes)[0])
