@@ -459,8 +459,8 @@ int adpsgd_synth_gradient(uint64_t seed, uint64_t k, float std, int64_t d, float
  * Products with their epilogue, layer norm, log-probabilities and losses over a vocabulary, and AdamW, for gradient functions of
  * ADPSGD_MODEL_EXTERNAL and programs around them.  No handle is needed (AdamW has one of its own).  All pointers are device
  * memory unless "host" is stated; nothing is allocated, work is enqueued on `stream` and the calls return at once.  Elements are
- * addressed with 64-bit offsets, and tensors need the alignment of their type only.  adpsgd_last_error(NULL) has the message of
- * the calling thread's last failure. */
+ * addressed with 64-bit offsets, and tensors need the alignment of their type only.  What layer norm, gated projections and
+ * distillation write must not overlap what they read, nor their other results.  adpsgd_last_error(NULL) has the message of the calling thread's last failure. */
 enum { ADPSGD_TYPE_F32 = 0, ADPSGD_TYPE_BF16 = 1, ADPSGD_TYPE_F16 = 2 };
 enum { ADPSGD_ACT_NONE = 0, ADPSGD_ACT_RELU = 1, ADPSGD_ACT_GELU = 2, ADPSGD_ACT_SILU = 3 };
 
@@ -514,8 +514,9 @@ int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N);
 int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream);
 
 /* Gradients for dh (M x N, row m at dh + m lddh): dx (M x K, contiguous), dw (as w is stored, contiguous) and db (2 N); each may be NULL.
- * slopes: as the forward call wrote them.  dz = [dh dh/dg | dh dh/du] is rounded to the type once for the two products; db adds it before
- * that rounding. */
+ * slopes: as the forward call wrote them.  dz = [dh dh/dg | dh dh/du] is rounded to the type once for the two products (a result of up to 8192
+ * elements is computed from what that rounding leaves as well); db adds it before that rounding.  A gate within the rounding of its 32-bit sum of 0 is on
+ * either side of relu's corner. */
 int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, int64_t lddh, const uint16_t* slopes, void* dx, void* dw, void* db,
                           void* stream);
 
@@ -542,8 +543,8 @@ int64_t adpsgd_layer_norm_workspace_bytes(int32_t type, int64_t rows, int64_t n)
 int adpsgd_layer_norm_forward(const adpsgd_layer_norm_t* o, void* y, float* stats, void* stream);
 
 /* Gradients for dy (rows x n, row i at dy + i lddy): dx (rows x n, contiguous, the type of x), dw and db (n, param_type); each may be
- * NULL.  stats: as the forward call wrote them.  b and eps are not read.  dw and db are added in 32 bits over up to 128 rows and in 64 from there
- * on, in an order that the sizes give. */
+ * NULL.  stats: as the forward call wrote them.  b and eps are not read.  dw and db are added in 32 bits over up to 128 rows of a team of
+ * lanes and the teams of a block (64 at most), and in 64 over the blocks, in an order that the sizes give. */
 int adpsgd_layer_norm_backward(const adpsgd_layer_norm_t* o, const void* dy, int64_t lddy, const float* stats, void* dx, void* dw, void* db,
                                void* stream);
 

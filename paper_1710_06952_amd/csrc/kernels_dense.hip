@@ -223,14 +223,24 @@ bool whole_pieces(const void* p, int64_t ld, int64_t inner) { return reinterpret
 bool worth_packing(int64_t I, int64_t J, int64_t K) { return static_cast<double>(I) * static_cast<double>(J) * static_cast<double>(K) >= 4294967296.0; }
 int64_t packed_bytes(int64_t rows, int64_t inner) { return up256(2 * rows * up8(inner)); }
 void launch_pack(const PackJob* job, int jobs, hipStream_t s) {
+    constexpr uint32_t kMostBlocks = (uint32_t(1) << 24) - 1;        // under 2^32 threads; one matrix has up to 2^23 blocks
     PackJobs all{};
     uint32_t blocks = 0;
+    int n = 0;
+    auto go = [&]() {
+        if (blocks > 0) hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, all);
+        all = PackJobs{};
+        blocks = 0;
+        n = 0;
+    };
     for (int i = 0; i < jobs; ++i) {
-        all.job[i] = job[i];
-        all.blocks[i] = static_cast<uint32_t>((job[i].rows * (up8(job[i].inner) / 8) + kT - 1) / kT);
-        blocks += all.blocks[i];
+        const uint32_t more = static_cast<uint32_t>((job[i].rows * (up8(job[i].inner) / 8) + kT - 1) / kT);
+        if (blocks + more > kMostBlocks) go();
+        all.job[n] = job[i];
+        all.blocks[n++] = more;
+        blocks += more;
     }
-    if (blocks > 0) hipLaunchKernelGGL(dense_pack_kernel, dim3(blocks), dim3(kT), 0, s, all);
+    go();
 }
 
 // Both ways of storing an operand, and operands that begin anywhere: what any of them may ask for.
