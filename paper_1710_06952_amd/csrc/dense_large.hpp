@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
                         f[4 * v + 3] = part.w;
                     }
                     if (splits > 1) store_gated_part(g, split, gi0 + m * 16 + turn * kAtOnce, gj, f, f + 8);
-                    else end.finish(gi0 + m * 16 + turn * kAtOnce, f, f + 8);
+                    else end.finish(gi0 + m * 16 + turn * kAtOnce, f, f + 8, [&](const float* gate, float* scale) { end.template of_columns<kPairs, kAtOnce>(gate, scale); });
                 }
                 wave_lds_sync();
             }

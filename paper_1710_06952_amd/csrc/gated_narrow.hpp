@@ -10,8 +10,9 @@
 namespace adpsgd_impl {
 namespace {
 
-// kTI: tiles of 16 rows; kV: gates of a lane's operands, 16 kV of a block
-template <class T, bool kBOuter, int kTI, int kV>
+// kTI: tiles of 16 rows; kV: gates of a lane's operands, 16 kV of a block; kCorner: relu with slopes (its end in the other calls' code as well: 27.4 us
+// for 26.5 of 1 x 4096 x (2 x 8192))
+template <class T, bool kBOuter, int kTI, int kV, bool kCorner>
 __global__ __launch_bounds__(kNarrowWaves * 64, kTI == 1 && !kBOuter ? 4 : 2) void gated_narrow_kernel(const DenseGemm g, const int splits) {
     constexpr int kColumns = 16 * kV, kStep = kBOuter ? 32 : 64, kPitch = 2 * kColumns + 4;
     static_assert(kBOuter || kV == 1, "");
@@ -169,25 +170,32 @@ __global__ __launch_bounds__(kNarrowWaves * 64, kTI == 1 && !kBOuter ? 4 : 2) vo
 #pragma unroll
                 for (int v = 0; v < 8; ++v) f[kind][v] += sums[(w * 16 * kTI + i) * kPitch + kind * kColumns + c + v];
         if (splits > 1) store_gated_part(g, split, i, j0 + c, f[0], f[1]);
-        else end.finish(i, f[0], f[1]);
+        else
+            end.template finish<kCorner>(i, f[0], f[1], [&](const float*, float* scale) {
+                if constexpr (kCorner) end.of_parts(kNarrowWaves, [&](int w, int v) { return sums[(w * 16 * kTI + i) * kPitch + c + v]; }, scale);
+            });
     }
 }
 
-template <class T, bool kBOuter, int kTI, int kV>
+template <class T, bool kBOuter, int kTI, int kV, bool kCorner>
 hipError_t launch_gated_narrow_of(const DenseGemm& g, int splits, hipStream_t s) {
     constexpr int kBytes = kNarrowWaves * 16 * kTI * (2 * 16 * kV + 4) * 4;
     const dim3 grid(static_cast<uint32_t>((g.J + 16 * kV - 1) / (16 * kV) * splits));
-    auto kernel = gated_narrow_kernel<T, kBOuter, kTI, kV>;
+    auto kernel = gated_narrow_kernel<T, kBOuter, kTI, kV, kCorner>;
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_lds(allowed, reinterpret_cast<const void*>(kernel), kBytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, grid, dim3(kNarrowWaves * 64), kBytes, s, g, splits);
     return hipSuccess;
 }
+template <class T, bool kCorner>
+hipError_t launch_gated_narrow_as(const DenseGemm& g, int splits, hipStream_t s) {
+    if (g.b_outer) return g.I <= 16 ? launch_gated_narrow_of<T, true, 1, 2, kCorner>(g, splits, s) : launch_gated_narrow_of<T, true, 4, 2, kCorner>(g, splits, s);
+    return g.I <= 16 ? launch_gated_narrow_of<T, false, 1, 1, kCorner>(g, splits, s) : launch_gated_narrow_of<T, false, 4, 1, kCorner>(g, splits, s);
+}
 template <class T>
 hipError_t launch_gated_narrow(const DenseGemm& g, int splits, hipStream_t s) {
-    if (g.b_outer) return g.I <= 16 ? launch_gated_narrow_of<T, true, 1, 2>(g, splits, s) : launch_gated_narrow_of<T, true, 4, 2>(g, splits, s);
-    return g.I <= 16 ? launch_gated_narrow_of<T, false, 1, 1>(g, splits, s) : launch_gated_narrow_of<T, false, 4, 1>(g, splits, s);
+    return g.act == ADPSGD_ACT_RELU && g.slope && splits == 1 ? launch_gated_narrow_as<T, true>(g, splits, s) : launch_gated_narrow_as<T, false>(g, splits, s);
 }
 
 }  // namespace

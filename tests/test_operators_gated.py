@@ -268,3 +268,44 @@ def test_another_stream_and_a_graph(size):
         assert torch.equal(hg, h)
         for got, want in zip(gg, P.gated_gradients(dnew, new, w, slopes)):
             assert torch.equal(got, want)
+
+
+# One row, few rows and many, both layouts, split sums, tiles of 64, 128 and 256, copies of whole pieces
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("M,K,N", [(1, 1024, 72), (5, 4100, 72), (40, 1000, 520), (300, 1000, 100), (1100, 200, 1000), (2049, 72, 2050), (2952, 1416, 1548), (256, 8192, 128), (520, 4096, 196)])
+def test_gates_next_to_the_corner_of_relu(M, K, N, dtype, layout):
+    """A gate in one row of every fourth column is brought to within about 2^-24 of its terms' sum of 0: its last weights take away what the sum of the others
+    comes to, two roundings deep in fp16 (2^-11 each) and three in bf16 (2^-8 each).  A sum in 32 bits has either sign there; the slope is the one of the sum in
+    64 bits.  dh is 1 at these gates and 0 elsewhere, so db has the partner (within half a step of its type, the step of a slope and the 32 bits of the sum: 2^-6 is more) where
+    the gate is over 0, and 0 where it is not."""
+    import torch
+    import paper_1710_06952_amd as P
+    t = getattr(torch, dtype)
+    gen = torch.Generator()
+    gen.manual_seed(M + 3 * K + N)
+    new = lambda *s: torch.randn(*s, generator=gen).to(t)  # noqa: E731
+    depth = 2 if t is torch.float16 else 3
+    x, w, b = new(M, K), new(2 * N, K), new(2 * N)
+    for d in range(depth):
+        x[:, K - depth + d] = 2.0 ** (-8 * d)
+    at = torch.arange(1, N, 4)
+    rows = at * 7 % M
+    w[at, K - depth:] = 0
+    rest = (x[rows].double() * w[at].double()).sum(1) + b[at].double()
+    for d in range(depth):
+        scale = 2.0 ** (-8 * d)
+        w[at, K - depth + d] = (-rest / scale).to(t)
+        rest = rest + w[at, K - depth + d].double() * scale
+    assert torch.isfinite(w).all()
+    partner = (x[rows].double() * w[N + at].double()).sum(1) + b[N + at].double()
+    want = torch.where(rest > 0, partner, 0.0)
+    dh = torch.zeros(M, N, dtype=t)
+    dh[rows, at] = 1
+    wd = w.cuda() if layout == "nk" else w.t().contiguous().cuda().t()
+    _, slopes = P.gated_forward(x.cuda(), wd, b.cuda(), activation="relu")
+    db = P.gated_gradients(dh.cuda(), x.cuda(), wd, slopes, need=(False, False, True))[2][:N].cpu().double()
+    assert not db[dh.sum(0) == 0].any()
+    wrong = ((db[at] != 0) != (want != 0)) & (partner.abs() > 1e-2)
+    assert not wrong.any(), "%d of %d on the other side" % (int(wrong.sum()), len(at))
+    assert ((db[at] - want).abs() <= 2.0 ** -6 * partner.abs() + 1e-3).all()
