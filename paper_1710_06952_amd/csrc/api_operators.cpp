@@ -44,14 +44,15 @@ bool dense_sizes(int64_t M, int64_t N, int64_t K) {
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
 struct BackwardSpace {
-    int64_t dz, low, sums, partial, bytes;  // where they begin
+    int64_t dz, low, sums, copies, partial, bytes;  // where they begin
 };
-BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes, bool with_low = false) {
+BackwardSpace backward_space(int64_t M, int64_t N, int64_t K, int64_t sums_bytes, bool with_low = false, int64_t copies_bytes = 0) {
     BackwardSpace b{};
     b.dz = 0;
     b.low = up256(2 * M * ((N + 7) / 8 * 8));
     b.sums = b.low + (with_low ? b.low : 0);
-    b.partial = b.sums + up256(sums_bytes);
+    b.copies = b.sums + up256(sums_bytes);
+    b.partial = b.copies + copies_bytes;
     b.bytes = b.partial + up256(std::max(dense_partial_bytes(M, K, N), dense_partial_bytes(N, K, M)));
     return b;
 }
@@ -71,7 +72,7 @@ const char* dense_fault(const adpsgd_dense_t* o) {
 
 // ---- gated projections ----
 BackwardSpace gated_space(int64_t M, int64_t N, int64_t K) {
-    return backward_space(M, 2 * N, K, gated_sums_bytes(M, N), gated_low(M * K) || gated_low(2 * N * K));
+    return backward_space(M, 2 * N, K, gated_sums_bytes(M, N), gated_low(M * K) || gated_low(2 * N * K), gated_copies_bytes(M, N, K));
 }
 const char* gated_fault(const adpsgd_dense_t* o) {
     if (!o) return "gated: no arguments";
@@ -85,8 +86,8 @@ const char* gated_fault(const adpsgd_dense_t* o) {
     if (!aligned_to(o->x, 2) || !aligned_to(o->w, 2) || !aligned_to(o->b, 2)) return "gated: a tensor is not aligned to its type";
     return nullptr;
 }
-// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.  padded: dz's rows have zeros up to whole pieces.  low_dx, low_dw: what dz's rounding has left, for the one and the other, or nullptr.
-hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, bool padded, const void* low_dx, const void* low_dw, void* dx, void* dw, void* partial,
+// dx = dz w and dw = dz^T x, N columns of dz; either may be nullptr.  padded: dz's rows have zeros up to whole pieces.  copies: w and x in such rows, or nullptr.  low_dx, low_dw: what dz's rounding has left, for the one and the other, or nullptr.
+hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz, int64_t lddz, bool padded, const GatedCopies* copies, const void* low_dx, const void* low_dw, void* dx, void* dw, void* partial,
                              int64_t partial_bytes, hipStream_t s) {
     DenseGemm g{};
     g.act = ADPSGD_ACT_NONE;
@@ -94,27 +95,30 @@ hipError_t backward_products(const adpsgd_dense_t* o, int64_t N, const void* dz,
     g.partial_bytes = partial_bytes;
     if (dx && o->M > 0) {
         g.a = dz; g.lda = lddz; g.a_outer = false;
-        g.b = o->w; g.ldb = o->ldw; g.b_outer = o->w_transposed == 0;
+        g.b = copies ? copies->w : o->w; g.ldb = copies ? copies->ldw : o->ldw; g.b_outer = o->w_transposed == 0;
         g.I = o->M; g.J = o->K; g.K = N;
         g.a_low = low_dx;
         g.a_padded = padded;
+        g.b_padded = copies != nullptr;
         g.out = dx;
         hipError_t e = launch_dense_gemm(o->type, g, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
+        const void* x = copies ? copies->x : o->x;
+        const int64_t ldx = copies ? copies->ldx : o->ldx;
         g.a_low = nullptr;
-        g.a_padded = !o->w_transposed && padded;
-        g.b_padded = o->w_transposed && padded;
+        g.a_padded = o->w_transposed ? copies != nullptr : padded;
+        g.b_padded = o->w_transposed ? padded : copies != nullptr;
         g.a_outer = g.b_outer = true;
         g.K = o->M;
         g.out = dw;
         if (o->w_transposed) {
-            g.a = o->x; g.lda = o->ldx; g.I = o->K;
+            g.a = x; g.lda = ldx; g.I = o->K;
             g.b = dz; g.ldb = lddz; g.J = N;
         } else {
             g.a = dz; g.lda = lddz; g.I = N;
-            g.b = o->x; g.ldb = o->ldx; g.J = o->K;
+            g.b = x; g.ldb = ldx; g.J = o->K;
         }
         (o->w_transposed ? g.b_low : g.a_low) = low_dw;
         return launch_dense_gemm(o->type, g, s);
@@ -206,7 +210,7 @@ extern "C" int adpsgd_dense_backward(const adpsgd_dense_t* o, const void* dy, in
             hipError_t e = launch_dense_dz(o->type, dy, lddy, of, own ? ws + at.dz : nullptr, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
             if (e != hipSuccess) return hip_fail(nullptr, e, "dense backward");
         }
-        return ended(backward_products(o, o->N, dz, lddz, false, nullptr, nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
+        return ended(backward_products(o, o->N, dz, lddz, false, nullptr, nullptr, nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s), "dense backward");
     });
 }
 
@@ -256,8 +260,11 @@ extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, in
         const bool padded = gated_padded(o->M, o->N, o->K);      // else the products would copy dz to rows of whole pieces
         const int64_t lddz = padded ? (2 * o->N + 7) / 8 * 8 : 2 * o->N;
         hipError_t e = launch_gated_dz(o->type, dh, lddh, slopes, dz, low, lddz, db, reinterpret_cast<double*>(ws + at.sums), o->M, o->N, s);
+        GatedCopies copies{};
+        const bool copied = dx && dw && gated_copies(o->M, o->N, o->K, o->w_transposed != 0);
+        if (copied) launch_gated_copies(o->w, o->ldw, o->w_transposed != 0, o->x, o->ldx, o->M, o->N, o->K, ws + at.copies, &copies, s);
         if (e == hipSuccess)
-            e = backward_products(o, 2 * o->N, dz, lddz, padded, low_dx ? low : nullptr, low_dw ? low : nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s);
+            e = backward_products(o, 2 * o->N, dz, lddz, padded, copied ? &copies : nullptr, low_dx ? low : nullptr, low_dw ? low : nullptr, dx, dw, ws + at.partial, at.bytes - at.partial, s);
         return ended(e, "gated backward");
     });
 }

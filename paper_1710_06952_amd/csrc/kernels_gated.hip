@@ -46,6 +46,26 @@ int64_t gated_partial_bytes(int64_t I, int64_t J, int64_t K) {
     return (parts > 1 ? up256(parts * I * 2 * J * static_cast<int64_t>(sizeof(float))) : 0) + copies;
 }
 
+// Copies of w and x for the two products of a backward pass in one launch, where launch_dense_gemm would make one in front of each.  Sizes decide, so that
+// the products are cut alike.
+bool gated_copies(int64_t M, int64_t N, int64_t K, bool w_transposed) {
+    if (K % 8 == 0 || (w_transposed && 2 * N % 8 == 0) || M <= 64 || !worth_packing(M, 2 * N, K)) return false;
+    const DensePlan of_dw = w_transposed ? plan_of(K, 2 * N, M, false, true) : plan_of(2 * N, K, M, false, true);
+    return of_dw.side >= 128 && plan_of(M, K, 2 * N, false, true).side >= 128;
+}
+int64_t gated_copies_bytes(int64_t M, int64_t N, int64_t K) {
+    int64_t bytes = 0;
+    if (gated_copies(M, N, K, false)) bytes = packed_bytes(2 * N, K);
+    if (gated_copies(M, N, K, true)) bytes = std::max(bytes, packed_bytes(K, 2 * N));
+    return bytes > 0 ? bytes + packed_bytes(M, K) : 0;
+}
+void launch_gated_copies(const void* w, int64_t ldw, bool w_transposed, const void* x, int64_t ldx, int64_t M, int64_t N, int64_t K, void* to, GatedCopies* copies, hipStream_t s) {
+    const int64_t rows = w_transposed ? K : 2 * N, inner = w_transposed ? 2 * N : K;
+    *copies = GatedCopies{to, up8(inner), static_cast<char*>(to) + packed_bytes(rows, inner), up8(K)};
+    const PackJob jobs[2] = {{w, ldw, to, up8(inner), rows, inner}, {x, ldx, static_cast<char*>(to) + packed_bytes(rows, inner), up8(K), M, K}};
+    launch_pack(jobs, 2, s);
+}
+
 // As launch_dense_gemm, for 2 J columns.
 hipError_t launch_gated_gemm(int32_t type, const DenseGemm& given, hipStream_t s) {
     DenseGemm g = given;

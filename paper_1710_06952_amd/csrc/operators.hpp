@@ -37,6 +37,16 @@ int64_t gated_sums_bytes(int64_t M, int64_t N);
 // dz = [dh slope | dh slope'], rows of lddz >= 2 N with zeros at their ends (dz may be nullptr: only db), low (or nullptr) what its rounding has left, db = column sums of the unrounded dz (db may be nullptr)
 hipError_t launch_gated_dz(int32_t type, const void* dh, int64_t lddh, const uint16_t* slopes, void* dz, void* low, int64_t lddz, void* db, double* sums, int64_t M,
                            int64_t N, hipStream_t s);
+// w and x as the products of the backward pass want them, in rows of whole pieces
+struct GatedCopies {
+    const void* w;
+    int64_t ldw;
+    const void* x;
+    int64_t ldx;
+};
+bool gated_copies(int64_t M, int64_t N, int64_t K, bool w_transposed);      // whether both products want them
+int64_t gated_copies_bytes(int64_t M, int64_t N, int64_t K);
+void launch_gated_copies(const void* w, int64_t ldw, bool w_transposed, const void* x, int64_t ldx, int64_t M, int64_t N, int64_t K, void* to, GatedCopies* copies, hipStream_t s);
 bool gated_padded(int64_t M, int64_t N, int64_t K);        // whether dz is written in rows of whole pieces
 bool gated_low(int64_t elements);   // whether a result of so many is computed from dz in two parts
 
