@@ -12,8 +12,9 @@
 // The gradient of all elements is stored without the entries first; behind a barrier the few that have an entry are stored again.  (The pass
 // would have to look for its own elements among the entries.)
 //
-// Exponentials, sums of a row and the gradient are in 32 bits, what there is one of in a row or an entry in 64.  Orders depend on the sizes and the
-// alignment of the gradient alone.
+// Exponentials, sums of a row and the gradient are in 32 bits, what there is one of in a row or an entry in 64.  Where a teacher and a row are sure of the same token,
+// q - p there is what is left of two numbers next to 1: in fp32 it is computed in 64 bits, and the sums of a row are in 64 bits too (2^-25 of a sum of
+// 1 + 10^-3 would be 3e-5 of that; 1 to 5 % of the time).  Orders depend on the sizes and the alignment of the gradient alone.
 //
 // Bound: memory, 2 or 4 bytes an element in and out: 4096 x 65 536 in bf16, a fifth of the rows not counted, 172 us (5.6 TB/s).  With labels at another
 // temperature the instructions: two softmaxes of 2001 x 50 001 in fp16 84 us (4.5 TB/s).
@@ -30,14 +31,18 @@ constexpr int64_t kSplitBlocks = 1024;  // blocks that fill the chip: rows are s
 
 struct Entry {
     int v;                      // of the vocabulary, or -1: nothing
-    float p;
+    float p, rest;              // p in two parts
 };
 // log2 e / T as it rounds, and in two parts, the second positive: a difference of -infinity is e^-infinity by both.
 struct Heat {
     float near, hi, lo;
 };
+template <class E>
+using Sum = std::conditional_t<E::kN == 4, double, float>;
+template <class S>
 struct Stat2 {
-    float m, s, s1;             // the largest value, sum exp((z - m) / T), sum exp(z - m)
+    float m;
+    S s, s1;                    // the largest value, sum exp((z - m) / T), sum exp(z - m)
 };
 struct DistillArgs {
     const void* z;
@@ -54,7 +59,7 @@ struct DistillArgs {
     Entry* entries;             // [row][k + 1]
     double* first;              // of KL: its first part
     double* term;
-    Stat2* parts;               // in passes: of parts of rows
+    void* parts;                // in passes: Stat2 of parts of rows
     int splits, together;       // ... of a row; teacher's rows of a block
     float* loss;
     int64_t blocks;             // of a row, in the gradient's pass
@@ -67,29 +72,30 @@ __device__ __forceinline__ float warm(float d, const Heat& h) { return __builtin
 // In the sums of a row: 32-bit logits take the second part as well.  Beside 16 bits its 3e-8 of z / T is left out: 2e-7 of log s, which is 5 to 15.
 template <class E>
 __device__ __forceinline__ float warm_in_sum(float d, const Heat& h) { return warm<E::kN == 4>(d, h); }
-template <bool kTwo>
-__device__ __forceinline__ Stat2 joined2(Stat2 a, Stat2 b, const Heat& h) {
+template <bool kTwo, class S>
+__device__ __forceinline__ Stat2<S> joined2(Stat2<S> a, Stat2<S> b, const Heat& h) {
     const float m = fmaxf(a.m, b.m), base = base_of(m);
-    Stat2 r{m, a.s * warm<true>(a.m - base, h) + b.s * warm<true>(b.m - base, h), 0.0f};
+    Stat2<S> r{m, a.s * warm<true>(a.m - base, h) + b.s * warm<true>(b.m - base, h), 0};
     if (kTwo) r.s1 = a.s1 * exp_in_sum<true>(a.m - base) + b.s1 * exp_in_sum<true>(b.m - base);
     return r;
 }
-__device__ __forceinline__ Stat2 of_one2(float z, const Heat& h) { return Stat2{z, warm<true>(z - base_of(z), h), exp_in_sum<true>(z - base_of(z))}; }
-template <bool kTwo, int kLanes>
-__device__ __forceinline__ Stat2 lanes_joined2(Stat2 a, const Heat& h) {
+template <class S>
+__device__ __forceinline__ Stat2<S> of_one2(float z, const Heat& h) { return Stat2<S>{z, warm<true>(z - base_of(z), h), exp_in_sum<true>(z - base_of(z))}; }
+template <bool kTwo, int kLanes, class S>
+__device__ __forceinline__ Stat2<S> lanes_joined2(Stat2<S> a, const Heat& h) {
     float m = a.m;
 #pragma unroll
     for (int off = kLanes / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    float s = a.s * warm<true>(a.m - base_of(m), h), s1 = kTwo ? a.s1 * exp_in_sum<true>(a.m - base_of(m)) : 0.0f;
+    S s = a.s * warm<true>(a.m - base_of(m), h), s1 = kTwo ? a.s1 * exp_in_sum<true>(a.m - base_of(m)) : 0;
 #pragma unroll
     for (int off = kLanes / 2; off > 0; off >>= 1) {
         s += __shfl_xor(s, off, 64);
         if (kTwo) s1 += __shfl_xor(s1, off, 64);
     }
-    return Stat2{m, s, s1};
+    return Stat2<S>{m, s, s1};
 }
-template <bool kTwo, int kWaves>
-__device__ __forceinline__ Stat2 block_joined2(Stat2 a, const Heat& h, Stat2* at) {
+template <bool kTwo, int kWaves, class S>
+__device__ __forceinline__ Stat2<S> block_joined2(Stat2<S> a, const Heat& h, Stat2<S>* at) {
     a = lanes_joined2<kTwo, 64>(a, h);
     if (kWaves == 1) return a;
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = a;
@@ -103,6 +109,23 @@ __device__ __forceinline__ float exp_of_entry(double x) {
     const float hi = static_cast<float>(x), t = hi * kLog2e;
     const float rest = fmaf(hi, kLog2e, -t) + hi * kLog2eRest + static_cast<float>(x - static_cast<double>(hi)) * kLog2e, e = __builtin_amdgcn_exp2f(t);
     return fabsf(t) < 126.0f ? fmaf(e, rest * 0.6931471805599453f, e) : e;
+}
+// ... in 64 bits, x <= 0 or NaN: 2^n e^r with |r| <= ln 2 / 2, the series up to r^11 (the next term is 6e-15).
+__device__ __forceinline__ double exp64(double x) {
+    if (x < -745.0) return 0.0;
+    const double n = rint(x * 1.4426950408889634), r = fma(-n, 0x1.ef35793c7673p-45, fma(-n, 0x1.62e42fefa38p-1, x));
+    double p = 1.0 / 39916800.0;
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    return x == x ? ldexp(fma(p, r, 1.0), static_cast<int>(n)) : x;
 }
 __device__ __forceinline__ float teacher_logit(const void* t, int32_t type, int64_t at) {
     if (type == ADPSGD_TYPE_F32) return F32::get(static_cast<const float*>(t) + at);
@@ -121,7 +144,7 @@ __host__ __device__ constexpr int teacher_places(int k) {
     while (n < 2 * (k + 1)) n *= 2;
     return n;
 }
-static_assert(60 * 1024 > 4 * (3 * 1025 + 2 * 4096) + 8 * 1025, "the words of 1024 entries, and the entries, beside what a block has of its own");
+static_assert(60 * 1024 > 4 * (3 * 1025 + 2 * 4096) + 12 * 1025, "the words of 1024 entries, and the entries, beside what a block has of its own");
 __host__ __device__ constexpr int teacher_words(int k) { return 3 * (k + 1) + 2 * teacher_places(k); }
 
 // One wavefront, a row: leaves its entries in `out` (k + 1 of them), with `words` of LDS, and gives the first part of KL: NaN where there is none, -infinity where
@@ -193,12 +216,15 @@ __device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row,
     const double scale = 1.0 / Z;
     for (int j = lane; j <= k; j += 64) {
         const int at = place_of_entry[j];
-        Entry e{at >= 0 && owner[at] == j ? token_of[j] : -1, 0.0f};
+        Entry e{at >= 0 && owner[at] == j ? token_of[j] : -1, 0.0f, 0.0f};
         if (e.v >= 0) {
             double w = value[j];
             if (twice)
                 for (int i = j + 1; i <= k; ++i) w += place_of_entry[i] == at ? static_cast<double>(value[i]) : 0.0;
-            e.p = some ? static_cast<float>(w * scale) : 0.0f;
+            if (some) {
+                e.p = static_cast<float>(w * scale);
+                e.rest = static_cast<float>(w * scale - static_cast<double>(e.p));
+            }
         }
         out[j] = e;
     }
@@ -212,21 +238,28 @@ __device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row,
 struct RowEnd {
     float cs, ch;               // of exp((z - m) / T) and exp(z - m): cs / s, ch / s1
     float cp, ct;               // of an entry's p, of the token
+    double q, q1;               // 1 / s and 1 / s1, for entries
 };
+// log s.
+__device__ __forceinline__ double log_of_sum(float s) { return log_of(s); }
+__device__ __forceinline__ double log_of_sum(double s) {
+    const float near = static_cast<float>(s);
+    return log_of(near) + (s - static_cast<double>(near)) / s;
+}
 __device__ __forceinline__ void empty_row(const DistillArgs& a, int64_t row) {
     a.kl[row] = 0.0f;
     if (a.logp) a.logp[row] = 0.0f;
     a.term[row] = 0.0;
 }
-template <bool kTwo>
-__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2& st, float share, bool writes, double& term) {
-    const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0.0f && st.s < INFINITY;
-    double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of(st.s) : 0.0, logp = 0.0;
+template <bool kTwo, class S>
+__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2<S>& st, float share, bool writes, double& term) {
+    const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0 && st.s < static_cast<S>(INFINITY);
+    double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of_sum(st.s) : 0.0, logp = 0.0;
     if (!good || first != first) kl = NAN;
     if (a.hard > 0.0) {
-        const float s1 = kTwo ? st.s1 : st.s;
-        logp = static_cast<double>(at) - static_cast<double>(st.m) - log_of(s1);
-        if (!(s1 > 0.0f && s1 < INFINITY)) logp = NAN;
+        const S s1 = kTwo ? st.s1 : st.s;
+        logp = static_cast<double>(at) - static_cast<double>(st.m) - log_of_sum(s1);
+        if (!(s1 > 0 && s1 < static_cast<S>(INFINITY))) logp = NAN;
     } else if (at != at) {
         kl = NAN;                                        // the token is beyond the vocabulary
     }
@@ -240,9 +273,11 @@ __device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, 
     e.cp = there ? a.cs * share : 0.0f;
     e.ct = a.ch * share;
     if (kl != kl || logp != logp) e.cp = NAN;
-    e.cs = e.cp / st.s;
-    e.ch = kTwo ? e.ct / st.s1 : 0.0f;
-    if (!kTwo) e.cs += e.ct / st.s;                      // one softmax for both
+    e.cs = e.cp / static_cast<float>(st.s);
+    e.ch = kTwo ? e.ct / static_cast<float>(st.s1) : 0.0f;
+    if (!kTwo) e.cs += e.ct / static_cast<float>(st.s);  // one softmax for both
+    e.q = 1.0 / static_cast<double>(st.s);
+    e.q1 = kTwo ? 1.0 / static_cast<double>(st.s1) : 0.0;
     return e;
 }
 template <class E, bool kTwo>
@@ -261,7 +296,15 @@ __device__ __forceinline__ void slopes_of(v4u x, float m, const RowEnd& e, const
 template <class E, bool kTwo>
 __device__ __forceinline__ void store_entry(const DistillArgs& a, const Entry& n, int64_t row, int64_t token, float m, const RowEnd& e) {
     const float z = E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + n.v);
-    E::put(static_cast<typename E::Raw*>(a.dz) + row * a.vocab + n.v, slope_at<E, kTwo>(z, m, e, a.heat) - e.cp * n.p - (n.v == token ? e.ct : 0.0f));
+    typename E::Raw* to = static_cast<typename E::Raw*>(a.dz) + row * a.vocab + n.v;
+    if (E::kN == 8) {                                    // 16 bits hold no more than this
+        E::put(to, slope_at<E, kTwo>(z, m, e, a.heat) - e.cp * n.p - (n.v == token ? e.ct : 0.0f));
+        return;
+    }
+    const double x = static_cast<double>(z) - static_cast<double>(m), q = exp64(x * a.inv_T) * e.q;
+    double d = static_cast<double>(e.cp) * ((q - static_cast<double>(n.p)) - static_cast<double>(n.rest));
+    if (e.ct != 0.0f) d += static_cast<double>(e.ct) * ((kTwo ? exp64(x) * e.q1 : q) - (n.v == token ? 1.0 : 0.0));
+    E::put(to, static_cast<float>(d));
 }
 
 // ---- rows held in registers -----------------------------------------------------------------------------------
@@ -293,7 +336,7 @@ template <class E, bool kTwo, int kWaves, int kHeld, int kPerSimd>
 __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(const DistillArgs a) {
     constexpr int kThreads = kWaves * 64;
     extern __shared__ int words[];                       // the entries, and the teacher's words
-    __shared__ Stat2 at[kWaves];
+    __shared__ Stat2<Sum<E>> at[kWaves];
     __shared__ float counts[kWaves];
     __shared__ RowEnd of_row;
     const int64_t row = blockIdx.x;
@@ -302,13 +345,13 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
     const Cut<E> cut(dz, static_cast<int>(a.vocab));
     const int64_t token = a.tokens[row];
     const int single = cut.single();
-    RowEnd end{0.0f, 0.0f, 0.0f, 0.0f};
+    RowEnd end{};
     float m = 0.0f, alone = -INFINITY;
     Entry* list = reinterpret_cast<Entry*>(words);
     v4u x[kHeld];
     if (token >= 0) {                   // uniform over the block
         double first = 0.0;
-        if (threadIdx.x < 64) first = teacher_row<E>(a, row, token, words + 2 * (a.k + 1), list);
+        if (threadIdx.x < 64) first = teacher_row<E>(a, row, token, words + sizeof(Entry) / sizeof(int) * (a.k + 1), list);
         const float value = token < a.vocab ? E::get(z + token) : NAN;
         float share = a.rows <= kCountHere ? 0.0f : *a.share;
         if (single >= 0) alone = E::get(z + single);
@@ -322,7 +365,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
         }
         if (a.rows <= kCountHere) share = 1.0f / fmaxf(counted_rows<kWaves>(a.tokens, a.rows, counts), 1.0f);
         __builtin_amdgcn_sched_barrier(0);
-        Stat2 st{-INFINITY, 0.0f, 0.0f};
+        Stat2<Sum<E>> st{-INFINITY, 0, 0};
         const float e1 = in_vector(kLog2e);              // in vector registers: an operand in a scalar one costs most of an instruction more
         Heat h = a.heat;
         h.near = in_vector(h.near);
@@ -334,18 +377,18 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[i]);
             const float most = fmaxf(st.m, top), base = base_of(most);
-            float part = 0.0f, part1 = 0.0f;
+            Sum<E> part = 0, part1 = 0;
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) {
                 part += warm_in_sum<E>(f[i] - base, h);
                 if (kTwo) part1 += __builtin_amdgcn_exp2f((f[i] - base) * e1);
             }
-            st.s = fmaf(st.s, warm<true>(st.m - base, a.heat), part);
-            if (kTwo) st.s1 = fmaf(st.s1, exp_in_sum<true>(st.m - base), part1);
+            st.s = fma(st.s, static_cast<Sum<E>>(warm<true>(st.m - base, a.heat)), part);
+            if (kTwo) st.s1 = fma(st.s1, static_cast<Sum<E>>(exp_in_sum<true>(st.m - base)), part1);
             st.m = most;
             __builtin_amdgcn_sched_barrier(0);           // one vector after the other: unpacked, they would not all fit
         }
-        if (single >= 0) st = joined2<kTwo>(st, of_one2(alone, a.heat), a.heat);
+        if (single >= 0) st = joined2<kTwo>(st, of_one2<Sum<E>>(alone, a.heat), a.heat);
         st = block_joined2<kTwo, kWaves>(st, a.heat, at);
         if (threadIdx.x < 64) {
             double term;
@@ -407,7 +450,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
 template <class E, bool kTwo>
 __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a, const int64_t teachers) {
     extern __shared__ int words[];
-    __shared__ Stat2 at[kT / 64];
+    __shared__ Stat2<Sum<E>> at[kT / 64];
     if (blockIdx.x < teachers) {
         const int wave = threadIdx.x >> 6;
         const int64_t row = static_cast<int64_t>(blockIdx.x) * a.together + wave;
@@ -441,10 +484,10 @@ __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a, 
             for (int i = 0; i < E::kN; ++i) top = fmaxf(top, f[u][i]);
         }
         const float m = fmaxf(most, top), base = base_of(m);
-        float part[kUnroll], part1[kUnroll];
+        Sum<E> part[kUnroll], part1[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            part[u] = part1[u] = 0.0f;
+            part[u] = part1[u] = 0;
 #pragma unroll
             for (int i = 0; i < E::kN; ++i) {
                 part[u] += warm_in_sum<E>(f[u][i] - base, a.heat);
@@ -456,17 +499,17 @@ __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a, 
         if (kTwo) sum1 = sum1 * static_cast<double>(exp_in_sum<true>(most - base)) + static_cast<double>((part1[0] + part1[1]) + (part1[2] + part1[3]));
         most = m;
     }
-    Stat2 st{most, static_cast<float>(sum), static_cast<float>(sum1)};
-    if (part == 0 && cut.single() >= 0) st = joined2<kTwo>(st, of_one2(E::get(z + cut.single()), a.heat), a.heat);
+    Stat2<Sum<E>> st{most, static_cast<Sum<E>>(sum), static_cast<Sum<E>>(sum1)};
+    if (part == 0 && cut.single() >= 0) st = joined2<kTwo>(st, of_one2<Sum<E>>(E::get(z + cut.single()), a.heat), a.heat);
     st = block_joined2<kTwo, kT / 64>(st, a.heat, at);
-    if (threadIdx.x == 0) a.parts[row * a.splits + part] = st;
+    if (threadIdx.x == 0) static_cast<Stat2<Sum<E>>*>(a.parts)[row * a.splits + part] = st;
 }
 
 // A row's parts joined, by every wavefront for itself, and what follows from them.
 template <class E, bool kTwo>
 __device__ __forceinline__ RowEnd joined_row(const DistillArgs& a, int64_t row, int64_t token, float share, bool writes, float& m, double& term) {
-    Stat2 st{-INFINITY, 0.0f, 0.0f};
-    for (int q = threadIdx.x & 63; q < a.splits; q += 64) st = joined2<kTwo>(st, a.parts[row * a.splits + q], a.heat);
+    Stat2<Sum<E>> st{-INFINITY, 0, 0};
+    for (int q = threadIdx.x & 63; q < a.splits; q += 64) st = joined2<kTwo>(st, static_cast<const Stat2<Sum<E>>*>(a.parts)[row * a.splits + q], a.heat);
     st = lanes_joined2<kTwo, 64>(st, a.heat);
     m = st.m;
     const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
@@ -501,7 +544,7 @@ __global__ __launch_bounds__(kT) void distill_gradient_kernel(const DistillArgs 
     const int part = static_cast<int>(blockIdx.x % a.blocks);
     const int64_t token = a.tokens[row];
     const bool writes = part == 0 && threadIdx.x == 0;
-    RowEnd e{0.0f, 0.0f, 0.0f, 0.0f};
+    RowEnd e{};
     if (token >= 0) e = joined_row<E, kTwo>(a, row, token, share, writes, m, term);
     else if (writes) empty_row(a, row);
     const typename E::Raw* z = static_cast<const typename E::Raw*>(a.z) + row * a.ld;
@@ -550,7 +593,7 @@ int split_of(int64_t rows, int64_t vectors) {
 struct Workspace {
     Entry* entries;
     double *first, *term;
-    Stat2* parts;
+    void* parts;
     float* share;
     int64_t bytes;
 };
@@ -565,7 +608,7 @@ Workspace laid_out(void* at, int64_t rows, int64_t k) {
     w.entries = reinterpret_cast<Entry*>(take(rows * (k + 1) * sizeof(Entry)));
     w.first = reinterpret_cast<double*>(take(rows * sizeof(double)));
     w.term = reinterpret_cast<double*>(take(rows * sizeof(double)));
-    w.parts = reinterpret_cast<Stat2*>(take(std::max(rows, kSplitBlocks) * sizeof(Stat2)));    // rows * split_of(rows, .) at most
+    w.parts = take(std::max(rows, kSplitBlocks) * sizeof(Stat2<double>));    // rows * split_of(rows, .) at most
     w.share = reinterpret_cast<float*>(take(sizeof(float)));
     return w;
 }

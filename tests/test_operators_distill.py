@@ -256,3 +256,33 @@ def test_another_stream_and_a_graph(size):
         graph.replay()
         torch.cuda.synchronize()
         assert same(captured, call(*new))
+
+
+@pytest.mark.parametrize("T,a", [(1.0, 0.0), (2.0, 0.0), (1.0, 0.25), (1.5, 0.25)])
+@pytest.mark.parametrize("rows,vocab,k", [(64, 1000, 4), (1, 872, 2), (4, 5, 3), (3, 33333, 16), (1, 131072, 64), (100, 50001, 8), (17, 9001, 1), (2, 2049, 1024)])
+def test_rows_that_are_sure_of_the_teachers_token(rows, vocab, k, T, a):
+    """fp32 rows and teachers with nearly all weight on the same token: q - p is what two numbers next to 1 leave, 1 - q down to 10^-7.  An entry's q is e / (e + rest)
+    with e to 10^-15 and the rest of the row off by E of itself, so q by E q (1 - q); its p by 3 u p (1 - p), each exponential rounded once.  What multiplies
+    them and the rounding of the result are 6 u of it."""
+    import torch
+    import paper_1710_06952_amd as P
+    z, _, _, _ = make(rows, vocab, 1, "float32", "float32", 31 + rows + k, masked=0.0)
+    z = z.contiguous()
+    tokens = torch.arange(rows, device="cuda:0") * 37 % vocab
+    z[torch.arange(rows), tokens] += T * torch.linspace(9.0, 25.0, rows, device="cuda:0")
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(5)
+    top = torch.topk(z + torch.randn(rows, vocab, generator=g, device="cuda:0"), k, 1)
+    entries, t = top.indices.contiguous(), top.values.contiguous()
+    got = P.distillation_loss_and_gradient(z, tokens, entries, t, temperature=T, hard_weight=a).dlogits.double()
+    u = 2.0 ** -24
+    E = (160 + 3 * 45) * u
+    q, q1, p = torch.softmax(z.double() / T, 1), torch.softmax(z.double(), 1), torch.zeros(rows, vocab, dtype=torch.float64, device="cuda:0")
+    p.scatter_(1, entries, torch.softmax(t.double() / T, 1))
+    hot = torch.zeros_like(p).scatter_(1, tokens[:, None], 1.0)
+    cs, ch = (1 - a) * T / rows, a / rows
+    d = cs * (q - p) + ch * (q1 - hot)
+    bound = cs * (E * q * (1 - q) + 3 * u * p * (1 - p)) + ch * E * q1 * (1 - q1) + 6 * u * (cs * (q - p).abs() + ch * (q1 - hot).abs()) + 1e-37
+    apart = (p == 0) & (hot == 0)                            # an element of the pass: q by E as it is, and what it is multiplied with
+    bound = torch.where(apart, (E + 60 * u) * (cs * q + ch * q1) + 1e-37, bound)
+    assert ((got - d).abs() <= bound).all(), float(((got - d).abs() / bound).max())
