@@ -72,7 +72,7 @@ const char* dense_fault(const adpsgd_dense_t* o) {
 
 // ---- gated projections ----
 BackwardSpace gated_space(int64_t M, int64_t N, int64_t K) {
-    return backward_space(M, 2 * N, K, gated_sums_bytes(M, N), gated_low(M * K) || gated_low(2 * N * K), gated_copies_bytes(M, N, K));
+    return backward_space(M, 2 * N, K, gated_sums_bytes(M, N), gated_low(std::min(M * K, 2 * N * K), M * 2 * N), gated_copies_bytes(M, N, K));
 }
 const char* gated_fault(const adpsgd_dense_t* o) {
     if (!o) return "gated: no arguments";
@@ -255,7 +255,7 @@ extern "C" int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, in
         hipStream_t s = static_cast<hipStream_t>(stream);
         char* ws = static_cast<char*>(o->workspace);
         void* dz = dx || dw ? ws + at.dz : nullptr;
-        const bool low_dx = dx && gated_low(o->M * o->K), low_dw = dw && gated_low(2 * o->N * o->K);
+        const bool low_dx = dx && gated_low(o->M * o->K, o->M * 2 * o->N), low_dw = dw && gated_low(2 * o->N * o->K, o->M * 2 * o->N);
         void* low = low_dx || low_dw ? ws + at.low : nullptr;
         const bool padded = gated_padded(o->M, o->N, o->K);      // else the products would copy dz to rows of whole pieces
         const int64_t lddz = padded ? (2 * o->N + 7) / 8 * 8 : 2 * o->N;

@@ -7,8 +7,8 @@
 //   dx = dz w,  dw = dz^T x                                         the products of dense layers, over 2 N
 //
 // dz is rounded to 16 bits once for these products, which puts dx and dw sqrt 2 as far from 64 bits as their own rounding: 2.4e-3 for 1.7e-3 in bf16.  Results of
-// up to 2^13 elements are computed from dz in two parts (its rounding, and the rounding of what that has left): their products take little time, and few
-// elements are up to 1.6 times as far in the one form, which is 1.0 in the other.
+// up to 2^13 elements, and those of up to 2^12 elements of dz, are computed from dz in two parts (its rounding, and the rounding of what that has left): their products
+// take little time, and few elements, or those that few roundings go into, are up to 1.6 times as far in the one form, which is 1.0 in the other.
 //
 // Bound: the matrix cores, with few rows the bytes of the weights.  8192 x 2048 x (2 x 8192) in bf16 with slopes: 470 us by itself, 557 between the products of the
 // backward pass (a library product of that size without an end 417); silu is 22 us of it and the slopes 25.  1 x 4096 x (2 x 8192): 26 us.
@@ -34,7 +34,7 @@ int gated_strips(int64_t M, int64_t N) {
 }  // namespace
 
 bool gated_padded(int64_t M, int64_t N, int64_t K) { return 2 * N % 8 != 0 && worth_packing(M, 2 * N, K); }
-bool gated_low(int64_t elements) { return elements <= 8192; }
+bool gated_low(int64_t of_result, int64_t of_dz) { return of_result <= 8192 || of_dz <= 4096; }
 int64_t gated_sums_bytes(int64_t M, int64_t N) { return gated_strips(M, N) * 2 * N * static_cast<int64_t>(sizeof(double)); }
 
 int64_t gated_partial_bytes(int64_t I, int64_t J, int64_t K) {

@@ -48,7 +48,7 @@ bool gated_copies(int64_t M, int64_t N, int64_t K, bool w_transposed);      // w
 int64_t gated_copies_bytes(int64_t M, int64_t N, int64_t K);
 void launch_gated_copies(const void* w, int64_t ldw, bool w_transposed, const void* x, int64_t ldx, int64_t M, int64_t N, int64_t K, void* to, GatedCopies* copies, hipStream_t s);
 bool gated_padded(int64_t M, int64_t N, int64_t K);        // whether dz is written in rows of whole pieces
-bool gated_low(int64_t elements);   // whether a result of so many is computed from dz in two parts
+bool gated_low(int64_t of_result, int64_t of_dz);   // whether a result of so many elements is computed from dz in two parts
 
 // ---- layer norm (kernels_norm.hip) ----
 struct NormRows {
