@@ -8,14 +8,17 @@
 // Rows too long for that are read again for every pass (`long`); sums of columns are then a kernel of their own.
 //
 // The mean is taken in two parts: m1 = sum x / n as it rounds, then c = x - m1, which is exact where it matters, and m2 = mean c.  The
-// variance is mean c^2 - m2^2, with nothing to cancel, and (c - m2) r has the accuracy of 32 bits where the mean is 10^4 standard deviations away too
-// (with m1 alone: 10^-3 of them).  The backward pass gets m1, m2 and r.  Where squares overflow 32 bits the row is taken times 2^-90.
+// variance is mean c^2 - m2^2, and (c - m2) r has the accuracy of 32 bits where the mean is 10^4 standard deviations away too
+// (with m1 alone: 10^-3 of them).  The backward pass gets m1, m2 and r.  Two kinds of rows are summed again, with mean (c - m2)^2 for the variance: those whose
+// spread is a few roundings of their mean, for which the difference of the squares is another rounding (the largest gradients: 1 / sqrt(eps)), and those whose
+// squares or sum overflow 32 bits, which are taken times 2^-90.
 //
 // Columns' sums are in 32 bits over kChain rows of a team and over the teams of a block, and in 64 over the blocks; their order depends on the sizes alone.
 //
 // Bound: memory, 2 to 4 bytes an element and tensor: x in, y out;  x and dy in, dx out.  16 384 x 8192 in bf16: 95 us forward (5.7 TB/s), 140 and 5 for the
 // join of the columns' sums backward (5.8); the sizes of the teams are at `Shape`.
 #include <algorithm>
+#include <limits>
 
 #include "elements.hpp"
 
@@ -75,22 +78,35 @@ struct RowStat {
 // each(f, s): s += f(element) over a thread's elements of the row, absent ones passed over
 template <class Sums, class Each>
 __device__ __forceinline__ RowStat row_stat(Sums& team, float n, float eps, const Each& each) {
-    auto with = [&](float scale) {
-        float s = 0.0f, c1 = 0.0f, c2 = 0.0f;
-        each([&](float x) { s = fmaf(x, scale, s); });
-        const float m1 = team.sum(s, 0.0f).x / n;
-        each([&](float x) {
-            const float c = fmaf(x, scale, -m1);
-            c1 += c;
-            c2 = fmaf(c, c, c2);
-        });
-        const float2 t = team.sum(c1, c2);
-        const float m2 = t.x / n, v = fmaxf(t.y / n - m2 * m2, 0.0f);
-        return RowStat{m1, m2, t.y < INFINITY ? __builtin_amdgcn_rsqf(v + eps * scale * scale) : NAN, scale};
-    };
-    RowStat st = with(1.0f);
-    if (st.r != st.r) st = with(kSmall);
-    return st;
+    float s = 0.0f, c1 = 0.0f, c2 = 0.0f;
+    each([&](float x) { s += x; });
+    float m1 = team.sum(s, 0.0f).x / n;
+    each([&](float x) {
+        const float c = x - m1;
+        c1 += c;
+        c2 = fmaf(c, c, c2);
+    });
+    const float2 t = team.sum(c1, c2);
+    float m2 = t.x / n;
+    const float v = t.y / n - m2 * m2;
+    if (v >= m2 * m2 && t.y < INFINITY) return RowStat{m1, m2, __builtin_amdgcn_rsqf(v + eps), 1.0f};
+    // Nearly one value, of which the difference is what the sums were rounded by or little more; or squares or a sum that 32 bits do not hold.
+    constexpr float kMost = std::numeric_limits<float>::max() * kSmall;
+    const float scale = t.y < INFINITY ? 1.0f : kSmall;
+    s = c1 = c2 = 0.0f;
+    each([&](float x) { s = fmaf(x, scale, s); });
+    m1 = team.sum(s, 0.0f).x / n;
+    if (scale != 1.0f) m1 = fminf(fmaxf(m1, -kMost), kMost);         // the mean of the largest numbers may round to more than they are
+    each([&](float x) { c1 += fmaf(x, scale, -m1); });
+    m2 = team.sum(c1, 0.0f).x / n;
+    asm volatile("" : "+v"(m1));        // x - m1 computed anew, not kept since the sum
+    each([&](float x) {
+        const float c = fmaf(x, scale, -m1) - m2;
+        c2 = fmaf(c, c, c2);
+    });
+    const float rest = team.sum(c2, 0.0f).x / n, up = scale == 1.0f ? 1.0f : 1.0f / kSmall;
+    if (rest == 0.0f) return RowStat{m1 * up, m2 * up, __builtin_amdgcn_rsqf(eps), 1.0f};        // one value only: eps times 2^-180 would be 0, and r infinite
+    return RowStat{m1, m2, rest < INFINITY ? __builtin_amdgcn_rsqf(rest + eps * scale * scale) : NAN, scale};
 }
 __device__ __forceinline__ float normed(float x, const RowStat& st) { return (fmaf(x, st.scale, -st.m1) - st.m2) * st.r; }
 
@@ -110,11 +126,14 @@ __device__ __forceinline__ void keep_stat(const NormArgs& a, int64_t row, const 
 }
 
 constexpr int block_of(int lanes, int least) { return lanes > least ? lanes : least; }
+// Wavefronts of a SIMD that the registers have to leave room for, where row_stat's second way would just take it (a wavefront less: 65 536 x 1024 in
+// bf16 57 us for 52).
+constexpr int waves_of(int lanes, int held, int elements) { return held == 1 ? 8 : lanes == 256 && held * elements == 8 ? 6 : 1; }
 
 // Vectors v = u kLanes + lane, u < kHeld, and the elements behind the last whole vector one for each of the first lanes.  kKeep: w and b
 // stay in registers; blocks of 1024 threads have none left for them and read them for every row, from the caches.
 template <class E, class W, int kLanes, int kHeld>
-__global__ __launch_bounds__(block_of(kLanes, 256)) void norm_kernel(const NormArgs a) {
+__global__ __launch_bounds__(block_of(kLanes, 256), waves_of(kLanes, kHeld, E::kN)) void norm_kernel(const NormArgs a) {
     constexpr bool kKeep = kLanes < 1024, kLate = kLanes * kHeld == 4096;
     constexpr int kTeams = block_of(kLanes, 256) / kLanes;
     __shared__ float2 at[2][Team<kLanes>::kWaves ? Team<kLanes>::kWaves : 1];
