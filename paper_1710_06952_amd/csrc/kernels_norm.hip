@@ -257,6 +257,14 @@ struct NormGradArgs {
 __device__ __forceinline__ RowStat kept_stat(const NormGradArgs& a, int64_t row) {
     return RowStat{a.stats[row], a.stats[a.rows + row], a.stats[2 * a.rows + row], 1.0f};
 }
+// Where 1 / r is so large that a value may be further from the mean than the largest number (no further than sqrt n / r, n <= 2^28), the row is taken times
+// 1/4.  Not a part of kept_stat: what is loaded is not waited for there.
+__device__ __forceinline__ RowStat within_reach(const RowStat& st) {
+    const bool far = st.r < 0x1p-100f;
+    const float scale = far ? 0.25f : 1.0f;
+    return RowStat{st.m1 * scale, st.m2 * scale, far ? 4.0f * st.r : st.r, scale};
+}
+__device__ __forceinline__ float unscaled(const RowStat& st) { return st.r * st.scale; }
 
 // As norm_kernel; a thread's columns are the same in every row.
 template <class E, class W, int kLanes, int kHeld, int kBlock>
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
     for (; first < a.rows; first += stride) {
         const int64_t row = first + threadIdx.x / kLanes;
         const bool there = row < a.rows;
-        const RowStat st = next;
+        const RowStat st = within_reach(next);
         float h[kHeld][E::kN], g[kHeld][E::kN], h1 = 0.0f, g1 = 0.0f, p = 0.0f, q = 0.0f;
 #pragma unroll
         for (int u = 0; u < kHeld; ++u) {
@@ -341,7 +349,7 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
         }
         if (!kAgain) load(first + stride);
         const float2 t = team.sum(p, q);
-        const float mp = t.x * inv, mq = t.y * inv;
+        const float mp = t.x * inv, mq = t.y * inv, r = unscaled(st);
         if (there && a.dx) {
             typename E::Raw* dx = static_cast<typename E::Raw*>(a.dx) + row * a.n;
 #pragma unroll
@@ -361,10 +369,10 @@ __global__ __launch_bounds__(kBlock) void norm_gradient_kernel(const NormGradArg
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < E::kN; ++i) o[i] = st.r * (g[u][i] - mp - h[u][i] * mq);
+                for (int i = 0; i < E::kN; ++i) o[i] = r * (g[u][i] - mp - h[u][i] * mq);
                 if (v < vectors) store_row<E>(dx, v * E::kN, o);
             }
-            if (single) E::put(dx + last, st.r * (g1 - mp - h1 * mq));
+            if (single) E::put(dx + last, r * (g1 - mp - h1 * mq));
         }
         if (kAgain) load(first + stride);
     }
@@ -416,7 +424,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_gradient_long_kernel(const 
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const typename E::Raw* x = static_cast<const typename E::Raw*>(a.x) + row * a.ldx;
         const typename E::Raw* dy = static_cast<const typename E::Raw*>(a.dy) + row * a.lddy;
-        const RowStat st = kept_stat(a, row);
+        const RowStat st = within_reach(kept_stat(a, row));
         auto both = [&](int v, float* g, float* h) {
             float w[E::kN];
             E::unpack(*reinterpret_cast<const v4u_any*>(x + v * E::kN), h);
@@ -445,16 +453,16 @@ __global__ __launch_bounds__(kLongThreads) void norm_gradient_long_kernel(const 
             q = fmaf(g1, h1, q);
         }
         const float2 t = team.sum(p, q);
-        const float mp = t.x * inv, mq = t.y * inv;
+        const float mp = t.x * inv, mq = t.y * inv, r = unscaled(st);
         typename E::Raw* dx = static_cast<typename E::Raw*>(a.dx) + row * a.n;
         for (int v = threadIdx.x; v < vectors; v += kLongThreads) {
             float g[E::kN], h[E::kN];
             both(v, g, h);
 #pragma unroll
-            for (int i = 0; i < E::kN; ++i) g[i] = st.r * (g[i] - mp - h[i] * mq);
+            for (int i = 0; i < E::kN; ++i) g[i] = r * (g[i] - mp - h[i] * mq);
             store_row<E>(dx, v * E::kN, g);
         }
-        if (single) E::put(dx + last, st.r * (g1 - mp - h1 * mq));
+        if (single) E::put(dx + last, r * (g1 - mp - h1 * mq));
     }
 }
 // ... and the columns' sums of a strip of rows, a column a thread.  grid: (ceil(n / 256), parts).
@@ -465,7 +473,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormGradArgs a)
     double sw = 0.0, sb = 0.0;
     for (int64_t row = a.rows * blockIdx.y / gridDim.y, end = a.rows * (blockIdx.y + 1) / gridDim.y; row < end; ++row) {
         const float dy = E::get(static_cast<const typename E::Raw*>(a.dy) + row * a.lddy + e);
-        sw += static_cast<double>(dy) * normed(E::get(static_cast<const typename E::Raw*>(a.x) + row * a.ldx + e), kept_stat(a, row));
+        sw += static_cast<double>(dy) * normed(E::get(static_cast<const typename E::Raw*>(a.x) + row * a.ldx + e), within_reach(kept_stat(a, row)));
         sb += dy;
     }
     float* out = a.sums + static_cast<int64_t>(blockIdx.y) * 2 * a.n;
