@@ -531,7 +531,7 @@ typedef struct {
     int64_t ldx;
     const void* w;           /* n, or NULL: 1                                                                */
     const void* b;           /* n, or NULL: 0; not without w                                                 */
-    double eps;              /* >= 2^-126                                                                    */
+    double eps;              /* 2^-126 <= eps < 2^128                                                     */
     void* workspace;         /* of the backward call: adpsgd_layer_norm_workspace_bytes, 16-byte aligned; may be used again in stream order */
     int64_t workspace_bytes;
 } adpsgd_layer_norm_t;

@@ -276,7 +276,7 @@ extern "C" int64_t adpsgd_layer_norm_workspace_bytes(int32_t type, int64_t rows,
 extern "C" int adpsgd_layer_norm_forward(const adpsgd_layer_norm_t* o, void* y, float* stats, void* stream) {
     return guarded([&]() -> int {
         if (const char* why = norm_fault(o)) return refuse(why);
-        if (!(o->eps < INFINITY) || !(static_cast<float>(o->eps) >= std::numeric_limits<float>::min())) return refuse("layer_norm: eps must be finite and 2^-126 or more");
+        if (!(o->eps <= std::numeric_limits<float>::max()) || !(static_cast<float>(o->eps) >= std::numeric_limits<float>::min())) return refuse("layer_norm: eps must be 2^-126 or more, and finite in 32 bits");
         if (o->rows > 0 && !y) return refuse("layer_norm: y is NULL");
         if (!aligned_to(y, size_of(o->type)) || !aligned_to(stats, 4)) return refuse("layer_norm: a tensor is not aligned to its type");
         if (o->rows == 0) return ADPSGD_OK;
