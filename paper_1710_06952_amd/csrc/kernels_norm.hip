@@ -465,10 +465,13 @@ __global__ __launch_bounds__(kLongThreads) void norm_gradient_long_kernel(const 
         if (single) E::put(dx + last, r * (g1 - mp - h1 * mq));
     }
 }
-// ... and the columns' sums of a strip of rows, a column a thread.  grid: (ceil(n / 256), parts).
+// ... and the columns' sums of a strip of rows, a column a thread.  grid: (ceil(n / kColumns), parts), as many strips as fill the chip: with min(rows, 512) of
+// them, whatever n is, the sums of 512 x 2^20 in bf16 took 4.3 GB beside 1.07 GB of x, and the backward pass 3880 us for 1710 (2000 x 32 768: 236 us for 148).
+constexpr int kColumns = 256;
+constexpr int64_t kColumnBlocks = 2048;
 template <class E>
-__global__ __launch_bounds__(256) void norm_columns_kernel(const NormGradArgs a) {
-    const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+__global__ __launch_bounds__(kColumns) void norm_columns_kernel(const NormGradArgs a) {
+    const int64_t e = static_cast<int64_t>(blockIdx.x) * kColumns + threadIdx.x;
     if (e >= a.n) return;
     double sw = 0.0, sb = 0.0;
     for (int64_t row = a.rows * blockIdx.y / gridDim.y, end = a.rows * (blockIdx.y + 1) / gridDim.y; row < end; ++row) {
@@ -545,8 +548,9 @@ int64_t vectors_of(int32_t type, int64_t n) { return n / (type == ADPSGD_TYPE_F3
 // launch and a workspace less (128 x 128 in fp32: 5 us of host time, and on the GPU eight turns take no longer than one and the join).
 int64_t parts_of(int32_t type, int64_t rows, int64_t n) {
     const Shape s = gradient_shape(vectors_of(type, n));
-    const int64_t teams = s.lanes == 0 ? 1 : s.block / s.lanes, turns = (rows + teams - 1) / teams;
-    if (s.lanes > 0 && turns <= 8) return 1;
+    if (s.lanes == 0) return std::max<int64_t>(1, std::min(rows, kColumnBlocks / ((n + kColumns - 1) / kColumns)));
+    const int64_t teams = s.block / s.lanes, turns = (rows + teams - 1) / teams;
+    if (turns <= 8) return 1;
     return std::max<int64_t>(std::min(turns, s.blocks), (turns + kChain - 1) / kChain);
 }
 
@@ -587,7 +591,7 @@ void launch_norm_gradient_of(int32_t type, const NormGradArgs& a, hipStream_t s)
         case 512 * 8 + 4: go(norm_gradient_kernel<E, W, 512, 4, 512>); break;
         default:
             if (a.dx) hipLaunchKernelGGL((norm_gradient_long_kernel<E, W>), dim3(static_cast<uint32_t>(std::min<int64_t>(a.rows, 512))), dim3(kLongThreads), 0, s, a);
-            if (a.sums) hipLaunchKernelGGL(norm_columns_kernel<E>, dim3(static_cast<uint32_t>((a.n + 255) / 256), static_cast<uint32_t>(parts)), dim3(256), 0, s, a);
+            if (a.sums) hipLaunchKernelGGL(norm_columns_kernel<E>, dim3(static_cast<uint32_t>((a.n + kColumns - 1) / kColumns), static_cast<uint32_t>(parts)), dim3(kColumns), 0, s, a);
     }
     if ((a.dw || a.db) && (a.sums || a.rows == 0))
         hipLaunchKernelGGL(norm_join_kernel<W>, dim3(static_cast<uint32_t>((a.n + 63) / 64), 2), dim3(64 * kJoin), 0, s, a.sums, a.rows > 0 ? parts : 0, a.n, a.dw, a.db);
