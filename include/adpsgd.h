@@ -509,8 +509,9 @@ int64_t adpsgd_gated_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t ba
 int64_t adpsgd_gated_slopes_bytes(int32_t type, int64_t M, int64_t N);
 
 /* h: M x N, contiguous.  slopes (or NULL): adpsgd_gated_slopes_bytes, receives dh/dg and dh/du for the backward call.  BF16: M x 2 N words of 16
- * bits, the fp16 roots of their magnitudes with their signs; F16: the same number of the first 24 bits of fp32, 16 bits of each and behind all of
- * them the other 8. */
+ * bits, the fp16 roots of their magnitudes with their signs: a slope is within 2^-10 of itself from 2^-28 to 65504^2, in larger steps down to 2^-50 and 0
+ * below; above 65504^2 it is one of 1022 numbers up to 2^128, within 3.4 %, or infinite or NaN where it is.  F16: the same number of the first 24
+ * bits of fp32, 16 bits of each and behind all of them the other 8. */
 int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, void* stream);
 
 /* Gradients for dh (M x N, row m at dh + m lddh): dx (M x K, contiguous), dw (as w is stored, contiguous) and db (2 N); each may be NULL.

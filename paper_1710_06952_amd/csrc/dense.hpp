@@ -100,8 +100,9 @@ __device__ __forceinline__ float slope_of(uint32_t w) {
 }
 
 // Slopes of gated projections.  What the backward pass needs of a result h = act(g) u is dh/dg = u act'(g) and dh/du = act(g).
-// bf16: 16 bits each, the fp16 roots of their magnitudes with their signs: a slope is within 2^-10 of itself from 4e-9 to 2^32 (in larger steps down to
-// 4e-15, infinite above), where bf16 would add 2^-8 to what dz is rounded by.
+// bf16: 16 bits each, the fp16 roots of their magnitudes with their signs: a slope is within 2^-10 of itself from 4e-9 to 65504^2 (in larger steps down to
+// 2^-50, 0 below), where bf16 would add 2^-8 to what dz is rounded by.  Above, where the root is over what fp16 holds, fp16's 1024 words for infinity and NaN are 1022
+// numbers in equal ratios up to 2^128, within 3.4 %, and those two: so that a slope is infinite where it is, and not the whole gradient with it.
 // fp16: the first 24 bits of fp32, within 2^-16; 16 bits of them in one plane, eight in another behind it.  Slopes in fp16 as they are
 // would add as much as dz is rounded by: dx and dw sqrt 3 as far from 64 bits as their own rounding, with these sqrt 2.
 template <class T>
@@ -110,16 +111,61 @@ struct GatedSlopes {
     uint16_t* high;             // M x 2 N
     uint8_t* low;               // M x 2 N, kLow only
     __device__ __forceinline__ GatedSlopes(uint16_t* p, int64_t M, int64_t N) : high(p), low(reinterpret_cast<uint8_t*>(p + M * 2 * N)) {}
-    // 24 bits, the last eight of them `low`
-    __device__ static __forceinline__ uint32_t word(float s) {
-        if (!kLow) return static_cast<uint32_t>(F16::down(copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s))) << 8;
-        const uint32_t bits = __float_as_uint(s);
-        return s != s ? bits >> 8 | 0x4000u : (bits + 0x80u) >> 8;       // the largest round to infinity
+
+    static constexpr float kMostRoot = 65504.0f * 65504.0f;
+    static constexpr uint32_t kLarge = 0x7C00u, kInfinite = 0x7FFEu, kNaN = 0x7FFFu;
+    static constexpr float kRatio = 96.0f / 1022.0f;         // of an octave from 2^32 on
+    __device__ static __forceinline__ uint32_t large_word(float s) {
+        const float f = fabsf(s), at = (__builtin_amdgcn_logf(f) - 32.0f) * (1.0f / kRatio);
+        const uint32_t finite = kLarge + static_cast<uint32_t>(fminf(fmaxf(at, 0.0f), 1021.0f));
+        return (__float_as_uint(s) >> 16 & 0x8000u) | (s != s ? kNaN : f == INFINITY ? kInfinite : finite);
     }
-    __device__ static __forceinline__ float slope(uint32_t high, uint32_t low) {
-        if (kLow) return __uint_as_float(high << 16 | low << 8);
-        const float r = F16::up(static_cast<uint16_t>(high));
-        return r * fabsf(r);
+    __device__ static __forceinline__ float large_slope(uint32_t w) {
+        const uint32_t word = w & 0x7FFFu;
+        const float f = __builtin_amdgcn_exp2f(fmaf(static_cast<float>(word - kLarge) + 0.5f, kRatio, 32.0f));
+        return word == kNaN ? NAN : copysignf(word == kInfinite ? INFINITY : f, __uint_as_float(w << 16));
+    }
+    // Whether all of the roots are there in fp16, of eight slopes of each kind.
+    __device__ static __forceinline__ bool ordinary(const float* s, const float* t) {
+        if (kLow) return true;
+        float all[2] = {0.0f, 0.0f};                     // NaN where one is
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            all[0] += fabsf(s[v]);
+            all[1] += fabsf(t[v]);
+        }
+        return all[0] + all[1] < kMostRoot;
+    }
+    // A slope's word of 24 bits, the last eight of them `low`.
+    template <bool kOrdinary>
+    __device__ static __forceinline__ uint32_t word(float s) {
+        if (kLow) {
+            const uint32_t bits = __float_as_uint(s);
+            return s != s ? bits >> 8 | 0x4000u : (bits + 0x80u) >> 8;           // the largest round to infinity
+        }
+        const uint32_t root = F16::down(copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s));
+        return (kOrdinary || fabsf(s) < kMostRoot ? root : large_word(s)) << 8;
+    }
+    // ... and back: the high parts of eight, and the low parts.
+    __device__ static __forceinline__ void slopes(v4u high, v2u low, float* s) {
+        uint32_t large = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t h = high[i / 2] >> (16 * (i % 2)) & 0xFFFFu;
+            if (kLow) {
+                s[i] = __uint_as_float(h << 16 | (low[i / 4] >> (8 * (i % 4)) & 255u) << 8);
+            } else {
+                const float r = F16::up(static_cast<uint16_t>(h));
+                s[i] = r * fabsf(r);
+                if (i % 2 == 0) large |= (high[i / 2] & 0x7C007C00u) + 0x04000400u;      // one of the upper bits of the two halves
+            }
+        }
+        if (kLow || (large & 0x80008000u) == 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t h = high[i / 2] >> (16 * (i % 2)) & 0xFFFFu;
+            s[i] = (h & kLarge) == kLarge ? large_slope(h) : s[i];
+        }
     }
 };
 

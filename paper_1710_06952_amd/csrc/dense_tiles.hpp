@@ -398,25 +398,31 @@ struct GatedEnding {
             if (g.act != ADPSGD_ACT_NONE) activate8<true>(gate, slope, g.act);
             const GatedSlopes<T> kept(g.slope, g.I, g.J);
 #pragma unroll
-            for (int kind = 0; kind < 2; ++kind) {
-                const int64_t at = (2 * i + kind) * g.J + j;
-                uint32_t w[8];
+            for (int v = 0; v < 8; ++v) slope[v] *= up[v];
+            auto keep = [&](auto ordinary) {
 #pragma unroll
-                for (int v = 0; v < 8; ++v) w[v] = GatedSlopes<T>::word(kind ? gate[v] : up[v] * slope[v]);
+                for (int kind = 0; kind < 2; ++kind) {
+                    const int64_t at = (2 * i + kind) * g.J + j;
+                    uint32_t w[8];
 #pragma unroll
-                for (int v = 0; v < 8; ++v) h[v] = static_cast<uint16_t>(w[v] >> 8);
-                store(kept.high + at, h);
-                if (!GatedSlopes<T>::kLow) continue;
-                if (kWhole || n == 8) {
-                    const uint32_t low[2] = {(w[0] & 255u) | (w[1] & 255u) << 8 | (w[2] & 255u) << 16 | w[3] << 24,
-                                             (w[4] & 255u) | (w[5] & 255u) << 8 | (w[6] & 255u) << 16 | w[7] << 24};
-                    __builtin_memcpy(kept.low + at, low, 8);
-                } else {
+                    for (int v = 0; v < 8; ++v) w[v] = GatedSlopes<T>::template word<decltype(ordinary)::value>(kind ? gate[v] : slope[v]);
 #pragma unroll
-                    for (int v = 0; v < 8; ++v)
-                        if (v < n) kept.low[at + v] = static_cast<uint8_t>(w[v]);
+                    for (int v = 0; v < 8; ++v) h[v] = static_cast<uint16_t>(w[v] >> 8);
+                    store(kept.high + at, h);
+                    if (!GatedSlopes<T>::kLow) continue;
+                    if (kWhole || n == 8) {
+                        const uint32_t low[2] = {(w[0] & 255u) | (w[1] & 255u) << 8 | (w[2] & 255u) << 16 | w[3] << 24,
+                                                 (w[4] & 255u) | (w[5] & 255u) << 8 | (w[6] & 255u) << 16 | w[7] << 24};
+                        __builtin_memcpy(kept.low + at, low, 8);
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < 8; ++v)
+                            if (v < n) kept.low[at + v] = static_cast<uint8_t>(w[v]);
+                    }
                 }
-            }
+            };
+            if (__builtin_expect(__ballot(!GatedSlopes<T>::ordinary(gate, slope)) == 0, 1)) keep(std::true_type());      // of all lanes: one way for all
+            else keep(std::false_type());
         } else if (g.act != ADPSGD_ACT_NONE) {
             activate8<false>(gate, slope, g.act);
         }

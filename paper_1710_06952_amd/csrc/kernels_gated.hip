@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
         for (int64_t first = m0 + ry; first < m1; first += 4 * kRowsAtOnce) {
             float part[2][8] = {};
             v4u d[4], w[4][2];
-            v2u low[4][2];
+            v2u low[4][2] = {};
 #pragma unroll
             for (int u = 0; u < 4; ++u) {                // rows beyond the strip: its last one again, which counts nothing
                 const int64_t m = first + u * kRowsAtOnce < m1 ? first + u * kRowsAtOnce : m1 - 1;
@@ -174,11 +174,11 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                 unpack8<T>(d[u], dy);
 #pragma unroll
                 for (int kind = 0; kind < 2; ++kind) {
-                    const v8h s = __builtin_bit_cast(v8h, w[u][kind]);
                     float f[8];
+                    GatedSlopes<T>::slopes(w[u][kind], low[u][kind], f);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        f[i] = dy[i] * GatedSlopes<T>::slope(s[i], GatedSlopes<T>::kLow ? low[u][kind][i / 4] >> (8 * (i % 4)) & 255u : 0u);
+                        f[i] *= dy[i];
                         part[kind][i] += f[i];
                     }
                     if (!dz) continue;

@@ -305,7 +305,8 @@ def gated(x, w, bias=None, *, activation="silu"):
 
     x (..., in), w (2 out, in) the rows of wg and then those of wu, as it is or as the transpose of an (in, 2 out) tensor, bias (2 out)
     likewise, all bfloat16 or all float16; the result is (..., out).  Activations as dense's.  Both products and theirs are in 32 bits and
-    the result is rounded once.  With gradients, 4 bytes an output (float16: 6) are kept for the backward pass.  Under capture of a HIP graph the
+    the result is rounded once.  With gradients, 4 bytes an output (float16: 6) are kept for the backward pass: its slopes for the two projections, in
+    bfloat16 within 2^-10 from 2^-28 to 65504^2, 0 below 2^-50 and within 3.4 % above 65504^2 (float16: within 2^-16).  Under capture of a HIP graph the
     differentiable form is refused, as dense's is: gated_forward and gated_gradients can be captured."""
     _check_gated(x, w, bias, activation)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias)):
