@@ -296,7 +296,7 @@ struct GatedEnding {
     }
     // The slope of relu jumps at 0, and a gate that is 0 but for the rounding of its sum has either sign: one such gate in a million puts the gradients
     // of a layer twice as far from 64 bits as their other roundings do.  Gates under sqrt(K + 64) 2^-25 of the largest of their eight neighbours and of their
-    // column's scale (about ten times what sums are off by; six of 2003 x 2731) are added again in 64 bits by all lanes that are here.
+    // column's scale (about ten times what sums are off by; six of 2003 x 2731), a column alone in its eight of the latter, are added again in 64 bits by all lanes that are here.
     // The column's scale keeps out the gates whose weights are all 0 or tiny, each of which would be one of them: a tenth of the columns of 8192 x 2048 x 8192 so took
     // 51 ms without it.  That call takes 524 us (silu 494), with such columns 615;  2003 x 1021 x 2731: 56 (55), 62.  scales(gate, s): s[v],
     // infinite where there is nothing to tell it by.
@@ -309,13 +309,14 @@ struct GatedEnding {
             least = kWhole || v < n ? fminf(least, fabsf(gate[v])) : least;
             top = kWhole || v < n ? fmaxf(top, fabsf(gate[v])) : top;
         }
-        const bool some = least < top * corner && top < INFINITY;
+        const bool alone = !kWhole && n == 1;            // no neighbours: its column tells
+        const bool some = (alone || least < top * corner) && top < INFINITY;
         if (__ballot(some) == 0) return;
         float scale[8];
         scales(gate, scale);
         uint32_t open = 0;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) open |= some && v < n && fabsf(gate[v]) < corner * fminf(top, scale[v]) ? 1u << v : 0u;
+        for (int v = 0; v < 8; ++v) open |= some && v < n && fabsf(gate[v]) < corner * (alone ? scale[v] : fminf(top, scale[v])) ? 1u << v : 0u;
         const int me = threadIdx.x & 63;
         const uint64_t here = __ballot(1);
         while (const uint64_t left = __ballot(open != 0)) {
