@@ -517,7 +517,9 @@ int adpsgd_gated_forward(const adpsgd_dense_t* o, void* h, uint16_t* slopes, voi
 /* Gradients for dh (M x N, row m at dh + m lddh): dx (M x K, contiguous), dw (as w is stored, contiguous) and db (2 N); each may be NULL.
  * slopes: as the forward call wrote them.  dz = [dh dh/dg | dh dh/du] is rounded to the type once for the two products (a result of up to 8192
  * elements, and one of up to 4096 of dz, is computed from what that rounding leaves as well); db adds it before that rounding.  With relu the
- * forward call that keeps slopes adds gates next to 0 again in 64 bits, so that they are on the right side of its corner. */
+ * forward call that keeps slopes adds gates far below their neighbours in row and column again in 64 bits, so that they are on the right side of its
+ * corner (as many as a wavefront's bound allows, which sums that cancel in a large share of the gates reach: the others keep the side of their 32 bits);
+ * h of such a gate may differ from that of a call without slopes in what its sum was rounded by. */
 int adpsgd_gated_backward(const adpsgd_dense_t* o, const void* dh, int64_t lddh, const uint16_t* slopes, void* dx, void* dw, void* db,
                           void* stream);
 

@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256, kSide == 256 ? 1 : 2) void dense_large_kernel(
         const int pair = lane % kPairs, first = lane / kPairs;
         const int64_t gi0 = ti * kSide + wi + first, gj = tj * kSideJ + wj / 2 + 8 * pair;
         auto finish_gated = [&](auto whole) {
-            const GatedEnding<T, decltype(whole)::value> end(g, gj);
+            const GatedEnding<T, decltype(whole)::value> end(g, gj, kSide == 256 ? 32 : 8);        // of 8192 gates, or 2048
 #pragma unroll 1
             for (int m = 0; m < kTI; ++m) {
 #pragma unroll

@@ -279,8 +279,10 @@ struct GatedEnding {
     int64_t j;
     int n;                      // columns that are there, up to 8
     float bias[2][8];
+    mutable int walks, idle;    // gates that this wavefront may still add again, and those of 0 that may come out as 0
 
-    __device__ __forceinline__ GatedEnding(const DenseGemm& gemm, int64_t column) : g(gemm), j(column) {
+    // most: of `walks`
+    __device__ __forceinline__ GatedEnding(const DenseGemm& gemm, int64_t column, int most) : g(gemm), j(column), walks(most), idle(4) {
         n = g.J - j < 0 ? 0 : g.J - j < 8 ? static_cast<int>(g.J - j) : 8;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
@@ -297,9 +299,12 @@ struct GatedEnding {
     // The slope of relu jumps at 0, and a gate that is 0 but for the rounding of its sum has either sign: one such gate in a million puts the gradients
     // of a layer twice as far from 64 bits as their other roundings do.  Gates under sqrt(K + 64) 2^-25 of the largest of their eight neighbours and of their
     // column's scale (about ten times what sums are off by; six of 2003 x 2731), a column alone in its eight of the latter, are added again in 64 bits by all lanes that are here.
-    // The column's scale keeps out the gates whose weights are all 0 or tiny, each of which would be one of them: a tenth of the columns of 8192 x 2048 x 8192 so took
-    // 51 ms without it.  That call takes 524 us (silu 494), with such columns 615;  2003 x 1021 x 2731: 56 (55), 62.  scales(gate, s): s[v],
-    // infinite where there is nothing to tell it by.
+    // The column's scale keeps out the gates whose weights are all 0 or tiny, each of which would be one of them.  Sums that are 0 because no product is anything (one-hot
+    // rows of x beside pruned weights) are among their row's and column's ordinary gates: a wavefront adds those that are 0 again only until four of them were 0 after
+    // all, and no more than `walks` gates in all, those that are not 0 first; the others keep the side that 32 bits give them.
+    // 8192 x 2048 x 8192 in bf16, forward with slopes: 560 us (silu 540);  with a tenth of the columns tiny 660;  half of the gates sums of zeros 740 (95 ms if all of them
+    // are added again);  half of them sums that cancel to what they are rounded by 1470 (99 ms).  2003 x 1021 x 2731 in fp16: 58, 62, 84.
+    // scales(gate, s): s[v], infinite where there is nothing to tell it by.
     template <class Scales>
     __device__ __forceinline__ void settle(int64_t i, float* gate, const Scales& scales) const {
         const float corner = 0x1p-25f * __builtin_amdgcn_sqrtf(static_cast<float>(g.K + 64));
@@ -314,13 +319,22 @@ struct GatedEnding {
         if (__ballot(some) == 0) return;
         float scale[8];
         scales(gate, scale);
-        uint32_t open = 0;
+        uint32_t open = 0, zero = 0;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) open |= some && v < n && fabsf(gate[v]) < corner * (alone ? scale[v] : fminf(top, scale[v])) ? 1u << v : 0u;
+        for (int v = 0; v < 8; ++v) {
+            const bool near = some && v < n && fabsf(gate[v]) < corner * (alone ? scale[v] : fminf(top, scale[v]));
+            open |= near && gate[v] != 0.0f ? 1u << v : 0u;
+            zero |= near && gate[v] == 0.0f ? 1u << v : 0u;
+        }
         const int me = threadIdx.x & 63;
         const uint64_t here = __ballot(1);
-        while (const uint64_t left = __ballot(open != 0)) {
-            const int lane = __builtin_ctzll(left), v = __builtin_ctz(read_lane(open, lane));
+        int may = __builtin_amdgcn_readfirstlane(walks), vain = __builtin_amdgcn_readfirstlane(idle);       // rows ascend: who is here now was here before
+        for (; may > 0; --may) {
+            uint64_t left = __ballot(open != 0);
+            const bool zeros = left == 0;
+            if (zeros) left = vain > 0 ? __ballot(zero != 0) : 0;
+            if (left == 0) break;
+            const int lane = __builtin_ctzll(left), v = __builtin_ctz(read_lane(zeros ? zero : open, lane));
             const int64_t row = read_lane(i, lane), column = read_lane(j, lane) + v;
             const uint16_t* a = static_cast<const uint16_t*>(g.a) + row * g.lda;
             const uint16_t* b = static_cast<const uint16_t*>(g.b) + (g.b_outer ? column : column * g.ldb);
@@ -341,12 +355,20 @@ struct GatedEnding {
             if (lanes == 64) sum = wave_sum(part);
             else
                 for (uint64_t l = here; l; l &= l - 1) sum += read_lane(part, __builtin_ctzll(l));
+            bool still = false;
             if (me == lane) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) gate[u] = u == v ? static_cast<float>(sum + static_cast<double>(bias[0][u])) : gate[u];
-                open &= open - 1;
+                for (int u = 0; u < 8; ++u) {
+                    gate[u] = u == v ? static_cast<float>(sum + static_cast<double>(bias[0][u])) : gate[u];
+                    still = still || (u == v && gate[u] == 0.0f);
+                }
+                if (zeros) zero &= zero - 1;
+                else open &= open - 1;
             }
+            vain -= zeros && __ballot(still) != 0;
         }
+        walks = may;
+        idle = vain;
     }
     // Scales of a tile: the largest of the wavefront's other rows, kLanes lanes kApart apart.
     template <int kApart, int kLanes>
@@ -549,7 +571,7 @@ __global__ __launch_bounds__(kWI * kWJ * 64) void dense_tile_kernel(const DenseG
     const int l = threadIdx.x & 15, q = threadIdx.x >> 4 & 3;
     if constexpr (kGated) {                              // a lane has eight neighbouring gates and their partners
         static_assert(kTJ == 4 && kWJ == 1, "");
-        const GatedEnding<T, false> end(g, tj * kSideJ + q * 8);
+        const GatedEnding<T, false> end(g, tj * kSideJ + q * 8, 8);
 #pragma unroll
         for (int m = 0; m < kTI; ++m) {
             const int64_t i = ti * kSide + wi + l + m * 16;
@@ -611,7 +633,7 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const DenseGemm g, cons
     const int64_t eights = (g.J + 7) / 8, id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int64_t i = id / eights, j = id % eights * 8;
     if (i >= g.I) return;
-    const GatedEnding<T, false> end(g, j);
+    const GatedEnding<T, false> end(g, j, 32);
     float f[2][8] = {};
     for (int s = 0; s < splits; ++s) {
 #pragma unroll

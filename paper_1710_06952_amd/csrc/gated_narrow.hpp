@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kNarrowWaves * 64, kTI == 1 && !kBOuter ? 4 : 2) vo
     for (int id = threadIdx.x; id < 16 * kTI * kEights; id += kNarrowWaves * 64) {
         const int i = id / kEights, c = id % kEights * 8;
         if (i >= g.I || j0 + c >= g.J) continue;
-        const GatedEnding<T, false> end(g, j0 + c);
+        const GatedEnding<T, false> end(g, j0 + c, 32);
         float f[2][8] = {};
 #pragma unroll
         for (int w = 0; w < kNarrowWaves; ++w)

@@ -316,7 +316,8 @@ def gated(x, w, bias=None, *, activation="silu"):
 
 
 def gated_forward(x, w, bias=None, *, activation="silu"):
-    """(h, slopes): the forward pass without autograd, and what gated_gradients needs."""
+    """(h, slopes): the forward pass without autograd, and what gated_gradients needs.  With relu h is gated's but for gates next to 0, whose sums are added again in
+    64 bits for their slopes: there it may differ by what a sum in 32 bits is rounded by.  (gated with gradients keeps slopes too.)"""
     _check_gated(x, w, bias, activation)
     return _gated_forward(x, w, bias, activation, True)
 
