@@ -125,30 +125,47 @@ struct GatedSlopes {
         const float f = __builtin_amdgcn_exp2f(fmaf(static_cast<float>(word - kLarge) + 0.5f, kRatio, 32.0f));
         return word == kNaN ? NAN : copysignf(word == kInfinite ? INFINITY : f, __uint_as_float(w << 16));
     }
-    // Whether all of the roots are there in fp16, of eight slopes of each kind.
-    __device__ static __forceinline__ bool ordinary(const float* s, const float* t) {
-        if (kLow) return true;
+    // Whether one of eight slopes of each kind may have no root in fp16.
+    __device__ static __forceinline__ bool some_large(const float* s, const float* t) {
+        if (kLow) return false;
         float all[2] = {0.0f, 0.0f};                     // NaN where one is
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
             all[0] += fabsf(s[v]);
             all[1] += fabsf(t[v]);
         }
-        return all[0] + all[1] < kMostRoot;
+        return !(all[0] + all[1] < kMostRoot);
     }
-    // A slope's word of 24 bits, the last eight of them `low`.
-    template <bool kOrdinary>
+    // A slope's word of 24 bits, the last eight of them `low`; large ones' are put in its place afterwards.
     __device__ static __forceinline__ uint32_t word(float s) {
-        if (kLow) {
-            const uint32_t bits = __float_as_uint(s);
-            return s != s ? bits >> 8 | 0x4000u : (bits + 0x80u) >> 8;           // the largest round to infinity
-        }
-        const uint32_t root = F16::down(copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s));
-        return (kOrdinary || fabsf(s) < kMostRoot ? root : large_word(s)) << 8;
+        if (!kLow) return static_cast<uint32_t>(F16::down(copysignf(__builtin_amdgcn_sqrtf(fabsf(s)), s))) << 8;
+        const uint32_t bits = __float_as_uint(s);
+        return s != s ? bits >> 8 | 0x4000u : (bits + 0x80u) >> 8;       // the largest round to infinity
     }
-    // ... and back: the high parts of eight, and the low parts.
-    __device__ static __forceinline__ void slopes(v4u high, v2u low, float* s) {
+    // ... one after the other: this is code that few calls come to, and must not be long beside what all of them run.
+    __device__ __forceinline__ void put_large(const float* s, const float* t, int64_t i, int64_t j, int64_t N, int n) const {
         uint32_t large = 0;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) large |= (fabsf(s[v]) < kMostRoot ? 0u : 1u << v) | (fabsf(t[v]) < kMostRoot ? 0u : 256u << v);
+        large &= 257u * ((1u << n) - 1u);
+#pragma unroll 1
+        for (; large; large &= large - 1) {
+            const int which = __builtin_ctz(large);
+            float f = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 8; ++v) f = which == v ? s[v] : which == v + 8 ? t[v] : f;
+            high[(2 * i + (which >> 3)) * N + j + (which & 7)] = static_cast<uint16_t>(large_word(f));
+        }
+    }
+    // Words of large slopes: bit 15 or 31.
+    __device__ static __forceinline__ uint32_t large_in(v4u high) {
+        uint32_t of = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) of |= (high[i] & 0x7C007C00u) + 0x04000400u;
+        return of;
+    }
+    // Eight slopes from their high and low parts.  large: of all lanes, whether there may be a large one.
+    __device__ static __forceinline__ void slopes(v4u high, v2u low, bool large, float* s) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t h = high[i / 2] >> (16 * (i % 2)) & 0xFFFFu;
@@ -157,14 +174,19 @@ struct GatedSlopes {
             } else {
                 const float r = F16::up(static_cast<uint16_t>(h));
                 s[i] = r * fabsf(r);
-                if (i % 2 == 0) large |= (high[i / 2] & 0x7C007C00u) + 0x04000400u;      // one of the upper bits of the two halves
             }
         }
-        if (kLow || (large & 0x80008000u) == 0) return;
+        if (kLow || !large) return;
+        uint32_t at = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t h = high[i / 2] >> (16 * (i % 2)) & 0xFFFFu;
-            s[i] = (h & kLarge) == kLarge ? large_slope(h) : s[i];
+        for (int i = 0; i < 8; ++i) at |= (high[i / 2] >> (16 * (i % 2)) & kLarge) == kLarge ? 1u << i : 0u;
+#pragma unroll 1
+        for (; at; at &= at - 1) {
+            const int which = __builtin_ctz(at);
+            const uint32_t pair = which < 4 ? (which < 2 ? high.x : high.y) : (which < 6 ? high.z : high.w);
+            const float f = large_slope(pair >> (16 * (which & 1)));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = which == i ? f : s[i];
         }
     }
 };

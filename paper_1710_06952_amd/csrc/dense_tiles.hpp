@@ -302,8 +302,8 @@ struct GatedEnding {
     // The column's scale keeps out the gates whose weights are all 0 or tiny, each of which would be one of them.  Sums that are 0 because no product is anything (one-hot
     // rows of x beside pruned weights) are among their row's and column's ordinary gates: a wavefront adds those that are 0 again only until four of them were 0 after
     // all, and no more than `walks` gates in all, those that are not 0 first; the others keep the side that 32 bits give them.
-    // 8192 x 2048 x 8192 in bf16, forward with slopes: 560 us (silu 540);  with a tenth of the columns tiny 660;  half of the gates sums of zeros 740 (95 ms if all of them
-    // are added again);  half of them sums that cancel to what they are rounded by 1470 (99 ms).  2003 x 1021 x 2731 in fp16: 58, 62, 84.
+    // 8192 x 2048 x 8192 in bf16, forward with slopes, one call after the other: 527 us (silu 520 to 530);  a tenth of the columns tiny 690;  half of the gates sums of zeros
+    // 700 (95 ms if all of them are added again);  half of them sums that cancel to what they are rounded by 1465 (99 ms).  2003 x 1021 x 2731 in fp16: 57 (silu 56), 62, 82.
     // scales(gate, s): s[v], infinite where there is nothing to tell it by.
     template <class Scales>
     __device__ __forceinline__ void settle(int64_t i, float* gate, const Scales& scales) const {
@@ -319,13 +319,15 @@ struct GatedEnding {
         if (__ballot(some) == 0) return;
         float scale[8];
         scales(gate, scale);
-        uint32_t open = 0, zero = 0;
+        uint32_t near = 0, zero = 0;
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
-            const bool near = some && v < n && fabsf(gate[v]) < corner * (alone ? scale[v] : fminf(top, scale[v]));
-            open |= near && gate[v] != 0.0f ? 1u << v : 0u;
-            zero |= near && gate[v] == 0.0f ? 1u << v : 0u;
+            near |= fabsf(gate[v]) < corner * (alone ? scale[v] : fminf(top, scale[v])) ? 1u << v : 0u;
+            zero |= gate[v] == 0.0f ? 1u << v : 0u;
         }
+        near &= some ? (1u << n) - 1u : 0u;
+        uint32_t open = near & ~zero;
+        zero &= near;
         const int me = threadIdx.x & 63;
         const uint64_t here = __ballot(1);
         int may = __builtin_amdgcn_readfirstlane(walks), vain = __builtin_amdgcn_readfirstlane(idle);       // rows ascend: who is here now was here before
@@ -422,30 +424,27 @@ struct GatedEnding {
             const GatedSlopes<T> kept(g.slope, g.I, g.J);
 #pragma unroll
             for (int v = 0; v < 8; ++v) slope[v] *= up[v];
-            auto keep = [&](auto ordinary) {
 #pragma unroll
-                for (int kind = 0; kind < 2; ++kind) {
-                    const int64_t at = (2 * i + kind) * g.J + j;
-                    uint32_t w[8];
+            for (int kind = 0; kind < 2; ++kind) {
+                const int64_t at = (2 * i + kind) * g.J + j;
+                uint32_t w[8];
 #pragma unroll
-                    for (int v = 0; v < 8; ++v) w[v] = GatedSlopes<T>::template word<decltype(ordinary)::value>(kind ? gate[v] : slope[v]);
+                for (int v = 0; v < 8; ++v) w[v] = GatedSlopes<T>::word(kind ? gate[v] : slope[v]);
 #pragma unroll
-                    for (int v = 0; v < 8; ++v) h[v] = static_cast<uint16_t>(w[v] >> 8);
-                    store(kept.high + at, h);
-                    if (!GatedSlopes<T>::kLow) continue;
-                    if (kWhole || n == 8) {
-                        const uint32_t low[2] = {(w[0] & 255u) | (w[1] & 255u) << 8 | (w[2] & 255u) << 16 | w[3] << 24,
-                                                 (w[4] & 255u) | (w[5] & 255u) << 8 | (w[6] & 255u) << 16 | w[7] << 24};
-                        __builtin_memcpy(kept.low + at, low, 8);
-                    } else {
+                for (int v = 0; v < 8; ++v) h[v] = static_cast<uint16_t>(w[v] >> 8);
+                store(kept.high + at, h);
+                if (!GatedSlopes<T>::kLow) continue;
+                if (kWhole || n == 8) {
+                    const uint32_t low[2] = {(w[0] & 255u) | (w[1] & 255u) << 8 | (w[2] & 255u) << 16 | w[3] << 24,
+                                             (w[4] & 255u) | (w[5] & 255u) << 8 | (w[6] & 255u) << 16 | w[7] << 24};
+                    __builtin_memcpy(kept.low + at, low, 8);
+                } else {
 #pragma unroll
-                        for (int v = 0; v < 8; ++v)
-                            if (v < n) kept.low[at + v] = static_cast<uint8_t>(w[v]);
-                    }
+                    for (int v = 0; v < 8; ++v)
+                        if (v < n) kept.low[at + v] = static_cast<uint8_t>(w[v]);
                 }
-            };
-            if (__builtin_expect(__ballot(!GatedSlopes<T>::ordinary(gate, slope)) == 0, 1)) keep(std::true_type());      // of all lanes: one way for all
-            else keep(std::false_type());
+            }
+            if (__builtin_expect(GatedSlopes<T>::some_large(slope, gate), 0)) kept.put_large(slope, gate, i, j, g.J, n);
         } else if (g.act != ADPSGD_ACT_NONE) {
             activate8<false>(gate, slope, g.act);
         }

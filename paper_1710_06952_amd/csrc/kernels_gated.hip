@@ -10,8 +10,9 @@
 // up to 2^13 elements, and those of up to 2^12 elements of dz, are computed from dz in two parts (its rounding, and the rounding of what that has left): their products
 // take little time, and few elements, or those that few roundings go into, are up to 1.6 times as far in the one form, which is 1.0 in the other.
 //
-// Bound: the matrix cores, with few rows the bytes of the weights.  8192 x 2048 x (2 x 8192) in bf16 with slopes: 470 us by itself, 557 between the products of the
-// backward pass (a library product of that size without an end 417); silu is 22 us of it and the slopes 25.  1 x 4096 x (2 x 8192): 26 us.
+// Bound: the matrix cores, with few rows the bytes of the weights.  8192 x 2048 x (2 x 8192) in bf16, one call after the other: 452 us without an activation, 490 with
+// silu, and 38 more where slopes are kept (520 to 530);  between the products of the backward pass 570, where a library product of that size without an end takes 417 by
+// itself.  1 x 4096 x (2 x 8192): 26 us.
 #include <algorithm>
 
 #include "dense_tiles.hpp"
@@ -123,7 +124,7 @@ __device__ __forceinline__ void store_end(uint16_t* to, v4u p, int skip) {
 }
 
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
-// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 106 us, 6.3 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
+// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 108 us, 6.2 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
 template <class T, int kAcross>
 __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, uint16_t* rest, int64_t lddz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
@@ -166,6 +167,12 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
                     if (GatedSlopes<T>::kLow) low[u][kind] = load_low(kept.low + from);
                 }
             }
+            uint32_t words = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int kind = 0; kind < 2; ++kind) words |= GatedSlopes<T>::large_in(w[u][kind]);
+            const bool large = !GatedSlopes<T>::kLow && __ballot(words & 0x80008000u) != 0;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t m = first + u * kRowsAtOnce;
@@ -175,7 +182,7 @@ __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_
 #pragma unroll
                 for (int kind = 0; kind < 2; ++kind) {
                     float f[8];
-                    GatedSlopes<T>::slopes(w[u][kind], low[u][kind], f);
+                    GatedSlopes<T>::slopes(w[u][kind], low[u][kind], large, f);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         f[i] *= dy[i];
