@@ -124,7 +124,7 @@ __device__ __forceinline__ void store_end(uint16_t* to, v4u p, int skip) {
 }
 
 // dz = [dh slope | dh slope'], rounded once, and sums of the unrounded dz over a strip of rows (32 bits for up to 4 rows of a thread, then 64).
-// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 108 us, 6.2 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
+// Memory: 2 + 4 + 4 bytes a result (fp16: 2 more); 8192 x 8192 in bf16 109 us, 6.1 TB/s.  kAcross threads of eight columns in a block.  grid: (ceil(N / (8 kAcross)), strips).
 template <class T, int kAcross>
 __global__ __launch_bounds__(kT) void gated_dz_kernel(const uint16_t* dh, int64_t lddh, const uint16_t* slopes, uint16_t* dz, uint16_t* rest, int64_t lddz, double* sums, uint16_t* db, int64_t M,
                                                      int64_t N) {
