@@ -171,8 +171,15 @@ __global__ __launch_bounds__(kNarrowWaves * 64, kTI == 1 && !kBOuter ? 4 : 2) vo
                 for (int v = 0; v < 8; ++v) f[kind][v] += sums[(w * 16 * kTI + i) * kPitch + kind * kColumns + c + v];
         if (splits > 1) store_gated_part(g, split, i, j0 + c, f[0], f[1]);
         else
-            end.template finish<kCorner>(i, f[0], f[1], [&](const float*, float* scale) {
-                if constexpr (kCorner) end.of_parts(kNarrowWaves, [&](int w, int v) { return sums[(w * 16 * kTI + i) * kPitch + c + v]; }, scale);
+            end.template finish<kCorner>(i, f[0], f[1], [&](const float* gate, float* scale) {
+                if constexpr (kCorner) {
+                    end.of_parts(kNarrowWaves, [&](int w, int v) { return sums[(w * 16 * kTI + i) * kPitch + c + v]; }, scale);
+                    if (end.n == 1) {                    // alone: where one part is all there is, its other rows tell (else all of them are added again: 67 us for 6 of 64 x 64 x 1)
+                        float rows[8];
+                        end.template of_columns<kEights, 64 / kEights>(gate, rows);
+                        scale[0] = scale[0] < INFINITY ? scale[0] : rows[0];
+                    }
+                }
             });
     }
 }
