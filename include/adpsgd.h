@@ -591,7 +591,7 @@ int adpsgd_preference_loss(const adpsgd_logits_t* o, const int64_t* offsets, int
  * row's entries, q_T = softmax(z / T) and q = softmax(z) over the vocabulary, and c the counted rows (tokens as for the losses above):
  *   KL_i = sum_j p_j (log p_j - log q_T[v_j])            0 where no entry is used, NaN where all that are have no weight
  *   loss = 1/max(1, c) sum_i [ (1 - hard_weight) T^2 KL_i - hard_weight log q[tokens[i]] ]
- * An entry with weight whose logit is -infinity makes the loss infinite, and its gradient is finite. */
+ * An entry with weight whose logit is -infinity makes the loss infinite, and its gradient is finite; a weight under 2^-126 of the row's largest is none. */
 typedef struct {
     int32_t type;            /* of the teacher's logits: ADPSGD_TYPE_*                                       */
     int32_t reserved;

@@ -2,7 +2,9 @@
 //
 // A row has logits z and up to k entries (v_j, t_j) of the teacher.  With p = softmax(t / T) over its entries, q_T = softmax(z / T), q = softmax(z):
 //   KL = sum_j p_j (log p_j - log q_T[v_j])
-//      = [sum_j p_j t_j / T - log Z] - sum_j p_j z[v_j] / T + m / T + log s        Z of the entries, m and s of the row: the first part needs no pass over z
+//      = [sum_j p_j t_j / T - log Z + sum_j p_j (b - z[v_j]) / T] + (m - b) / T + log s        Z and b = max z[v_j] of the entries, m and s of the row
+//   The first part needs no pass over z.  b is what z[v_j] and m are taken from: neither sum of differences has another sign in it, while p_j z[v_j] / T and m / T of
+//   their own would leave 2^-53 |m| / T of each other.
 //   dL/dz = cs (q_T - sum_j p_j onehot(v_j)) + ch (q - onehot(token)),   cs = (1 - a) T / counted,  ch = a / counted
 //
 //   teacher_row      p and the first part of KL by one wavefront; entries of the same token become one, and the token itself is the last
@@ -57,7 +59,8 @@ struct DistillArgs {
     Heat heat;
     const float* share;         // 1 / counted, where rows > kCountHere
     Entry* entries;             // [row][k + 1]
-    double* first;              // of KL: its first part
+    double* first;              // of KL: its first part ...
+    float* best;                // ... and the largest of a row's logits that have an entry
     double* term;
     void* parts;                // in passes: Stat2 of parts of rows
     int splits, together;       // ... of a row; teacher's rows of a block
@@ -148,9 +151,9 @@ static_assert(60 * 1024 > 4 * (3 * 1025 + 2 * 4096) + 12 * 1025, "the words of 1
 __host__ __device__ constexpr int teacher_words(int k) { return 3 * (k + 1) + 2 * teacher_places(k); }
 
 // One wavefront, a row: leaves its entries in `out` (k + 1 of them), with `words` of LDS, and gives the first part of KL: NaN where there is none, -infinity where
-// there is no entry.
+// there is no entry.  best: the largest logit that has an entry, 0 where there is none but -infinity.
 template <class E>
-__device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row, int64_t token, int* words, Entry* out) {
+__device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row, int64_t token, int* words, Entry* out, float& best) {
     const int lane = threadIdx.x & 63, k = static_cast<int>(a.k), places = teacher_places(k);
     int* token_of = words;
     float* value = reinterpret_cast<float*>(token_of + (k + 1));
@@ -179,18 +182,24 @@ __device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row,
     some = __any(some);
     top = wave_max(top);
     wave_lds_sync();
-    double Z = 0.0, with_t = 0.0, with_z = 0.0;
+    double Z = 0.0, with_t = 0.0, with_z = 0.0;          // with_z: from a lane's largest logit so far
+    float most = -INFINITY;
     for (int j = lane; j < k; j += 64) {
         const int v = token_of[j];
         const double x = (static_cast<double>(value[j]) - static_cast<double>(top)) * a.inv_T;
         const float e = v < 0 ? 0.0f : exp_of_entry(x);
         value[j] = e;
         if (e != 0.0f) {
+            const float own = E::get(z + v), was = most == -INFINITY ? own : most;
+            most = fmaxf(was, own);
+            const double from = base_of(most);
+            with_z += Z * (from - static_cast<double>(base_of(was))) + static_cast<double>(e) * (from - static_cast<double>(own));
             Z += static_cast<double>(e);
             with_t += static_cast<double>(e) * x;
-            with_z += static_cast<double>(e) * static_cast<double>(E::get(z + v));
         }
     }
+    best = base_of(wave_max(most));
+    if (most > -INFINITY) with_z += Z * (static_cast<double>(best) - static_cast<double>(most));
     Z = wave_sum(Z);
     with_t = wave_sum(with_t);
     with_z = wave_sum(with_z);
@@ -231,7 +240,7 @@ __device__ __forceinline__ double teacher_row(const DistillArgs& a, int64_t row,
     if (beyond || (some && !(Z > 0.0 && Z < INFINITY))) return NAN;
     if (!some) return -INFINITY;
     const float near = static_cast<float>(Z);
-    return with_t * scale - (log_of(near) + (Z - static_cast<double>(near)) * scale) - with_z * scale * a.inv_T;
+    return with_t * scale - (log_of(near) + (Z - static_cast<double>(near)) * scale) + with_z * scale * a.inv_T;
 }
 
 // ---- what one thread does once for a row --------------------------------------------------------------------
@@ -252,9 +261,9 @@ __device__ __forceinline__ void empty_row(const DistillArgs& a, int64_t row) {
     a.term[row] = 0.0;
 }
 template <bool kTwo, class S>
-__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float at, const Stat2<S>& st, float share, bool writes, double& term) {
+__device__ __forceinline__ RowEnd end_of_row(const DistillArgs& a, int64_t row, double first, float best, float at, const Stat2<S>& st, float share, bool writes, double& term) {
     const bool there = first != static_cast<double>(-INFINITY), good = st.s > 0 && st.s < static_cast<S>(INFINITY);
-    double kl = there ? first + static_cast<double>(st.m) * a.inv_T + log_of_sum(st.s) : 0.0, logp = 0.0;
+    double kl = there ? first + (static_cast<double>(st.m) - static_cast<double>(best)) * a.inv_T + log_of_sum(st.s) : 0.0, logp = 0.0;
     if (!good || first != first) kl = NAN;
     if (a.hard > 0.0) {
         const S s1 = kTwo ? st.s1 : st.s;
@@ -351,7 +360,8 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
     v4u x[kHeld];
     if (token >= 0) {                   // uniform over the block
         double first = 0.0;
-        if (threadIdx.x < 64) first = teacher_row<E>(a, row, token, words + sizeof(Entry) / sizeof(int) * (a.k + 1), list);
+        float best = 0.0f;
+        if (threadIdx.x < 64) first = teacher_row<E>(a, row, token, words + sizeof(Entry) / sizeof(int) * (a.k + 1), list, best);
         const float value = token < a.vocab ? E::get(z + token) : NAN;
         float share = a.rows <= kCountHere ? 0.0f : *a.share;
         if (single >= 0) alone = E::get(z + single);
@@ -392,7 +402,7 @@ __global__ __launch_bounds__(kWaves * 64, kPerSimd) void distill_rows_kernel(con
         st = block_joined2<kTwo, kWaves>(st, a.heat, at);
         if (threadIdx.x < 64) {
             double term;
-            const RowEnd e = end_of_row<kTwo>(a, row, first, value, st, share, threadIdx.x == 0, term);
+            const RowEnd e = end_of_row<kTwo>(a, row, first, best, value, st, share, threadIdx.x == 0, term);
             if (threadIdx.x == 0) of_row = e;
         }
         __syncthreads();
@@ -457,8 +467,12 @@ __global__ __launch_bounds__(kT) void distill_stats_kernel(const DistillArgs a, 
         if (wave >= a.together || row >= a.rows) return;
         const int64_t token = a.tokens[row];
         if (token < 0) return;                           // nothing of the row is read
-        const double first = teacher_row<E>(a, row, token, words + wave * teacher_words(static_cast<int>(a.k)), a.entries + row * (a.k + 1));
-        if ((threadIdx.x & 63) == 0) a.first[row] = first;
+        float best;
+        const double first = teacher_row<E>(a, row, token, words + wave * teacher_words(static_cast<int>(a.k)), a.entries + row * (a.k + 1), best);
+        if ((threadIdx.x & 63) == 0) {
+            a.first[row] = first;
+            a.best[row] = best;
+        }
         return;
     }
     const int64_t id = blockIdx.x - teachers, row = id / a.splits;
@@ -513,7 +527,7 @@ __device__ __forceinline__ RowEnd joined_row(const DistillArgs& a, int64_t row, 
     st = lanes_joined2<kTwo, 64>(st, a.heat);
     m = st.m;
     const float at = token < a.vocab ? E::get(static_cast<const typename E::Raw*>(a.z) + row * a.ld + token) : NAN;
-    return end_of_row<kTwo>(a, row, a.first[row], at, st, share, writes, term);
+    return end_of_row<kTwo>(a, row, a.first[row], a.best[row], at, st, share, writes, term);
 }
 
 constexpr int64_t kLossHere = 8;        // rows whose loss terms one more block of the gradient's pass adds up: a launch less, but a quarter of a microsecond a row
@@ -594,7 +608,7 @@ struct Workspace {
     Entry* entries;
     double *first, *term;
     void* parts;
-    float* share;
+    float *share, *best;
     int64_t bytes;
 };
 Workspace laid_out(void* at, int64_t rows, int64_t k) {
@@ -610,6 +624,7 @@ Workspace laid_out(void* at, int64_t rows, int64_t k) {
     w.term = reinterpret_cast<double*>(take(rows * sizeof(double)));
     w.parts = take(std::max(rows, kSplitBlocks) * sizeof(Stat2<double>));    // rows * split_of(rows, .) at most
     w.share = reinterpret_cast<float*>(take(sizeof(float)));
+    w.best = reinterpret_cast<float*>(take(rows * sizeof(float)));
     return w;
 }
 
@@ -662,7 +677,7 @@ hipError_t launch_distill(const LossRows& r, const TeacherRows& t, double temper
     if (static_cast<double>(a.heat.hi) >= heat) a.heat.hi = std::nextafterf(a.heat.hi, 0.0f);
     a.heat.lo = static_cast<float>(heat - static_cast<double>(a.heat.hi));
     a.share = w.share;
-    a.entries = w.entries; a.first = w.first; a.term = w.term; a.parts = w.parts;
+    a.entries = w.entries; a.first = w.first; a.best = w.best; a.term = w.term; a.parts = w.parts;
     a.dz = dz; a.kl = kl; a.logp = logp; a.loss = loss;
     if (r.rows > kCountHere) hipLaunchKernelGGL(count_rows_kernel, dim3(1), dim3(1024), 0, s, r.tokens, r.rows, w.share);
     const bool done = r.rows > 0 && (r.type == ADPSGD_TYPE_F32 ? launch_of<F32>(a, s) : r.type == ADPSGD_TYPE_BF16 ? launch_of<Bf16>(a, s) : launch_of<F16>(a, s));
