@@ -11,7 +11,7 @@
 // take little time, and few elements, or those that few roundings go into, are up to 1.6 times as far in the one form, which is 1.0 in the other.
 //
 // Bound: the matrix cores, with few rows the bytes of the weights.  8192 x 2048 x (2 x 8192) in bf16, one call after the other: 452 us without an activation, 490 with
-// silu, and 38 more where slopes are kept (520 to 530);  between the products of the backward pass 570, where a library product of that size without an end takes 417 by
+// silu, and 38 more where slopes are kept (520 to 530);  between the products of the backward pass 570 to 580, where a library product of that size without an end takes 417 by
 // itself.  1 x 4096 x (2 x 8192): 26 us.
 #include <algorithm>
 
